@@ -314,6 +314,95 @@ wdc_status wdc_attention_plan(const wdc_ctx *ctx, int64_t n, int32_t *qb_main, i
 wdc_status wdc_linear(wdc_ctx *ctx, const void *d_a, int64_t lda, const void *d_w, const void *d_bias, void *d_c,
                       int64_t ldc, int64_t m, int64_t n, int64_t k);
 
+/* ---------------------------------------------------------------- paged key/value cache
+ * Operators of a rollout that continues a clip chunk by chunk: attention from a
+ * chunk's new rows over the keys and values of everything before, kept in pages.
+ * Per layer and chunk: wdc_cache_append, wdc_cache_attention, and where the cache is
+ * bounded wdc_cache_mass and, when it is full, wdc_cache_evict. heads, head_dim
+ * (64 or 128, else WDC_E_UNSUPPORTED), dtype, qk_norm and rope_* are the context's;
+ * neither weights nor a workspace need be bound. All four are asynchronous on the
+ * context's stream, allocate nothing and can be captured into a graph; they are not part of the
+ * timing classes. d_scratch memory (16-byte aligned) is in use until the call's work is done. */
+
+/* Pages of one layer: slot p of page g and kv head h is row (g * kv_heads + h) *
+ * page + p of d_k and d_v, [pages, kv_heads, page, head_dim] in the model dtype.
+ * page is 16, 32, 64, 128 or 256 (else WDC_E_UNSUPPORTED); kv_heads divides heads:
+ * query head i uses kv head i / (heads / kv_heads). */
+typedef struct {
+  void *d_k, *d_v;
+  int32_t pages, page, kv_heads;
+  int32_t pad_;
+} wdc_paged_cache;
+
+/* The chunks of one call. Sequence b < batch: its rows are [d_q_start[b],
+ * d_q_start[b + 1]) of the packed tensors (d_q_start [batch + 1] rises from 0; chunks may be empty),
+ * its cache holds d_kv_len[b] keys, the chunk's own included, and its slot j lies on page
+ * d_table[b * table_ld + j / page]. Row i of a chunk of q rows has slot d_kv_len[b] - q + i.
+ * The host gives bounds: rows of the packed tensors, the longest chunk and the longest cache. Device
+ * values beyond them (or beyond the table's pages) are cut to them: rows past max_q of a chunk are
+ * left out, keys past max_kv are not there. A slot whose table entry is not a page of the cache is read
+ * as one of its pages and never written. Rows of no chunk are not written. batch * max_q * heads <= 2^26,
+ * batch * kv_heads * (keys) <= 2^29 and batch * kv_heads <= 65535, else WDC_E_SHAPE. */
+typedef struct {
+  const int32_t *d_q_start, *d_kv_len, *d_table;
+  int32_t batch, table_ld;
+  int32_t rows, max_q, max_kv;
+  int32_t pad_;
+} wdc_chunks;
+
+/* Store a chunk: d_qkv [rows, ld] holds q (heads * head_dim columns), k and v
+ * (kv_heads * head_dim each) of every row. q and k are normalised per head, x / sqrt(mean(x^2) +
+ * 1e-6) (descriptor qk_norm), multiplied by d_q_weight / d_k_weight ([head_dim] float32, or NULL), and
+ * their pairs (2p, 2p + 1) turned by the row's coordinates d_pos [rows, 3] (frame, row, column; as the
+ * blocks turn theirs, angles in float64): a row with a negative first coordinate (a text token), and
+ * every row when d_pos is NULL or the descriptor has no rotary dims, is not turned. One rounding.
+ * q goes to d_q [rows, ldq] (which may be d_qkv with ldq = ld), k and v to the rows' slots; a row
+ * whose slot is negative or on no page is not stored. Pointers and row strides: multiples of 16 bytes. */
+wdc_status wdc_cache_append(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_qkv,
+                            int64_t ld, const int32_t *d_pos, const float *d_q_weight, const float *d_k_weight,
+                            void *d_q, int64_t ldq);
+
+/* o = softmax(q k^T / sqrt(head_dim)) v over the cached keys that a row sees.
+ * Row i of a chunk of q rows over n keys sees slot j if j < n and, with frame > 0,
+ * j < n - q + (i / frame + 1) * frame: all of the past, and of the chunk's own
+ * frames of `frame` rows those up to its own (frame = 1: up to itself; 0: all).
+ * What a row does not see has no influence on it, whatever its value; a row that sees nothing gets
+ * zeros. d_q [rows, ldq], d_o [rows, ldo], head h at columns [h * head_dim, ..), multiples of 16
+ * bytes; d_lse [rows, heads] float32 (or NULL): ln sum exp of the scores, -inf for a row that sees
+ * nothing. float32 accumulation and statistics; bf16: attention weights rounded to bf16 before the product
+ * with v. d_scratch: memory for splitting the keys of few rows over the device,
+ * wdc_cache_attention_scratch() bytes; with less (or NULL) the call runs with fewer parts. */
+size_t wdc_cache_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks);
+wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_q,
+                               int64_t ldq, int32_t frame, void *d_o, int64_t ldo, float *d_lse, void *d_scratch,
+                               size_t scratch_bytes);
+
+/* Attention weight received by every cached key, per kv head: for slot j,
+ * mass_out[j] = decay * mass[j] + sum of exp(score - lse) over the rows and query heads that see it,
+ * with the chunk, frame and d_lse of wdc_cache_attention. The chunk's own keys have no past: their
+ * mass[j] is not read. d_mass and d_mass_out: [pages, kv_heads, page] float32 (they may be the same);
+ * slots of no cached key are not touched. decay is finite. d_scratch as above, wdc_cache_mass_scratch() bytes. d_v of the
+ * cache is not used. Sums in float32 in a fixed order. */
+size_t wdc_cache_mass_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks);
+wdc_status wdc_cache_mass(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_q,
+                          int64_t ldq, int32_t frame, const float *d_lse, float decay, const float *d_mass,
+                          float *d_mass_out, void *d_scratch, size_t scratch_bytes);
+
+/* Trim every sequence to `keep` keys. Per sequence of n > keep keys and per kv
+ * head stay the first `sink` slots, the last `recent` slots and of the others the keep - sink - recent of
+ * largest mass (equal ones: the lower slot; NaN counts as -inf). Kept keys in slots below keep stay where they are; the j-th
+ * of the other slots below keep takes the j-th kept key from above (k, v and mass), so the order of
+ * the keys changes (attention does not depend on it) and `recent` means what was appended last only
+ * while it is at most the rows appended since the last eviction. d_kv_len_out [batch] = min(n, keep)
+ * (may be d_kv_len). d_index [batch, kv_heads, keep] int32 or NULL: the former slot of every slot, -1 past n.
+ * d_mass_out as in wdc_cache_mass: the kept keys' masses. sink + recent <= keep, keep >= 1.
+ * d_scratch: wdc_cache_evict_scratch() bytes, required (else WDC_E_WORKSPACE). Of d_chunks only batch,
+ * d_kv_len, d_table, table_ld and max_kv are used. */
+size_t wdc_cache_evict_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, int32_t keep);
+wdc_status wdc_cache_evict(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const float *d_mass,
+                           float *d_mass_out, int32_t keep, int32_t sink, int32_t recent, int32_t *d_kv_len_out,
+                           int32_t *d_index, void *d_scratch, size_t scratch_bytes);
+
 /* Kernel timing for benchmarks. While timing is on (wdc_set_timing(ctx, 1),
  * which also clears the totals), every launch of the classes below on the
  * context's stream is bracketed by HIP events; wdc_timing synchronises the

@@ -81,6 +81,17 @@ assert _STEP_LOG.size == C.sizeof(StepLog)
 _STEP_LOG_NAMES = tuple(n for n, _ in StepLog._fields_)
 
 
+class CacheDesc(C.Structure):
+    """wdc_paged_cache"""
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p)] + [(n, C.c_int32) for n in ("pages", "page", "kv_heads", "pad_")]
+
+
+class ChunksDesc(C.Structure):
+    """wdc_chunks"""
+    _fields_ = [(n, C.c_void_p) for n in ("d_q_start", "d_kv_len", "d_table")] + [(n, C.c_int32) for n in (
+        "batch", "table_ld", "rows", "max_q", "max_kv", "pad_")]
+
+
 _lib = None
 
 
@@ -93,6 +104,7 @@ def load() -> C.CDLL:
         raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2608_01845_amd.build`")
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64, sz, dbl, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_double, C.c_float
+    pc, pq = C.POINTER(CacheDesc), C.POINTER(ChunksDesc)
     sig = {
         "wdc_params_default": (None, [C.POINTER(Params)]),
         "wdc_create": (i32, [C.POINTER(ModelDesc), C.POINTER(Params), vp, C.POINTER(vp)]),
@@ -126,6 +138,13 @@ def load() -> C.CDLL:
         "wdc_attention": (i32, [vp, vp, vp, vp, i64, vp, i64]),
         "wdc_attention_plan": (i32, [vp, i64, C.POINTER(i32), C.POINTER(i32)]),
         "wdc_linear": (i32, [vp, vp, i64, vp, vp, vp, i64, i64, i64, i64]),
+        "wdc_cache_append": (i32, [vp, pc, pq, vp, i64, vp, vp, vp, vp, i64]),
+        "wdc_cache_attention_scratch": (sz, [vp, pc, pq]),
+        "wdc_cache_attention": (i32, [vp, pc, pq, vp, i64, i32, vp, i64, vp, vp, sz]),
+        "wdc_cache_mass_scratch": (sz, [vp, pc, pq]),
+        "wdc_cache_mass": (i32, [vp, pc, pq, vp, i64, i32, vp, f32, vp, vp, vp, sz]),
+        "wdc_cache_evict_scratch": (sz, [vp, pc, pq, i32]),
+        "wdc_cache_evict": (i32, [vp, pc, pq, vp, vp, i32, i32, i32, vp, vp, vp, sz]),
         "wdc_set_timing": (i32, [vp, i32]),
         "wdc_timing": (i32, [vp, C.POINTER(dbl), C.POINTER(i64), C.POINTER(dbl)]),
     }
@@ -144,6 +163,8 @@ def exported_symbols() -> List[str]:
         "wdc_state_bytes", "wdc_state_create", "wdc_state_reset", "wdc_state_destroy", "wdc_state_bank_slot",
         "wdc_cond_embed", "wdc_dit_block_forward", "wdc_dit_forward", "wdc_dit_forward_batch", "wdc_scheduler_step",
         "wdc_surrogate_step", "wdc_surrogate_step_noalloc", "wdc_risk_update", "wdc_rollout", "wdc_rollout_batch", "wdc_attn_pad", "wdc_attention", "wdc_attention_plan", "wdc_linear",
+        "wdc_cache_append", "wdc_cache_attention_scratch", "wdc_cache_attention", "wdc_cache_mass_scratch",
+        "wdc_cache_mass", "wdc_cache_evict_scratch", "wdc_cache_evict",
         "wdc_set_timing", "wdc_timing"]
 
 
@@ -165,6 +186,11 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+def _ld(t) -> int:
+    """Row stride of a [rows, cols] tensor (one of at most one row: its columns)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
 def _ptrs(ts):
     """Host array of device pointers of a list of tensors (None entries -> NULL), or None."""
     if ts is None:
@@ -175,6 +201,39 @@ def _ptrs(ts):
 def _torch():
     import torch
     return torch
+
+
+class PagedCache:
+    """Pages of one layer's keys and values: k, v [pages, kv_heads, page, head_dim]
+    contiguous device tensors (wdc_paged_cache)."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
+            raise ValueError(f"k {tuple(k.shape)} {k.dtype} and v {tuple(v.shape)} {v.dtype} must be alike, "
+                             "[pages, kv_heads, page, head_dim]")
+        if not (k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("k and v must be contiguous")
+        self.k, self.v = k, v
+        self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], 0)
+        self.ref = C.byref(self.desc)
+
+
+class Chunks:
+    """The chunks of one call (wdc_chunks): q_start [batch + 1], kv_len [batch] and table
+    [batch, pages] int32 device tensors, read when the work runs; rows, max_q and max_kv
+    bound them (max_q: all rows, max_kv: all pages of the table, if not given)."""
+
+    def __init__(self, q_start, kv_len, table, rows: int, max_q: Optional[int] = None, max_kv: Optional[int] = None):
+        torch = _torch()
+        for name, t, dim in (("q_start", q_start, 1), ("kv_len", kv_len, 1), ("table", table, 2)):
+            if t.dtype != torch.int32 or t.dim() != dim or not t.is_contiguous() or t.device != kv_len.device:
+                raise ValueError(f"{name}: a contiguous int32 tensor of {dim} dimension(s) on one device is needed")
+        if q_start.numel() != kv_len.numel() + 1 or table.shape[0] != kv_len.numel():
+            raise ValueError("q_start [batch + 1], kv_len [batch] and table [batch, pages] disagree on the batch")
+        self.q_start, self.kv_len, self.table = q_start, kv_len, table
+        self.desc = ChunksDesc(q_start.data_ptr(), kv_len.data_ptr(), table.data_ptr(), kv_len.numel(), table.shape[1],
+                               rows, rows if max_q is None else max_q, 0x7fffffff if max_kv is None else max_kv, 0)
+        self.ref = C.byref(self.desc)
 
 
 class Context:
@@ -325,6 +384,102 @@ class Context:
     def linear(self, a, w, bias, out, m: int, n: int, k: int, lda: int = None, ldc: int = None):
         self._check(self.lib.wdc_linear(self.h, _ptr(a), lda or k, _ptr(w), _ptr(bias), _ptr(out), ldc or n, m, n, k))
         return out
+
+    # ---------------------------------------------------------------- paged key/value cache
+    def _cache_check(self, cache, chunks, **tensors):
+        """Devices, types and shapes of a cache call: name=(tensor, dtype, shape); None in a shape: any length."""
+        if cache.k.dtype != self.tdtype or cache.k.shape[3] != self.cfg.head_dim:
+            raise ValueError(f"cache of {cache.k.dtype}, head size {cache.k.shape[3]}: the context has {self.tdtype}, "
+                             f"{self.cfg.head_dim}")
+        dev = cache.k.device
+        if dev != self.device and (self.device.index is not None or dev.type != self.device.type) or (
+                chunks.kv_len.device != dev):
+            raise ValueError(f"cache or chunks not on {self.device}")
+        for name, (t, dtype, shape) in tensors.items():
+            if t is None:
+                continue
+            if t.dtype != dtype or t.device != dev or t.dim() != len(shape) or any(
+                    n is not None and n != m for n, m in zip(shape, t.shape)):
+                raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, expected {shape} {dtype} on {dev}")
+            if t.stride(-1) != 1 if name in ("qkv", "q", "out") and t.dim() == 2 else not t.is_contiguous():
+                raise ValueError(f"{name}: unsupported strides {t.stride()}")
+
+    def _scratch(self, nbytes: int):
+        """Device memory that lives as long as the work just enqueued on this context's stream."""
+        torch = _torch()
+        if not nbytes:
+            return None
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    def _cache_call(self, fn, *args):
+        torch = _torch()
+        if torch.cuda.current_device() == self.device.index:
+            self._check(fn(self.h, *args))
+        else:
+            with torch.cuda.device(self.device):
+                self._check(fn(self.h, *args))
+
+    def cache_append(self, cache: PagedCache, chunks: Chunks, qkv, q, pos=None, q_weight=None, k_weight=None):
+        """Normalise and rotate q and k of qkv [rows, (heads + 2 kv_heads) head_dim], store k and v in the
+        cache and write q [rows, heads head_dim]. Rows may be strided."""
+        torch = _torch()
+        hd, kvh, rows = self.cfg.head_dim, cache.k.shape[1], chunks.desc.rows
+        self._cache_check(cache, chunks, qkv=(qkv, self.tdtype, (rows, (self.cfg.heads + 2 * kvh) * hd)),
+                          q=(q, self.tdtype, (rows, self.cfg.heads * hd)), pos=(pos, torch.int32, (rows, 3)),
+                          q_weight=(q_weight, torch.float32, (hd,)), k_weight=(k_weight, torch.float32, (hd,)))
+        self._cache_call(self.lib.wdc_cache_append, cache.ref, chunks.ref, _ptr(qkv), _ld(qkv), _ptr(pos),
+                         _ptr(q_weight), _ptr(k_weight), _ptr(q), _ld(q))
+        return q
+
+    def cache_attention(self, cache: PagedCache, chunks: Chunks, q, out, frame: int = 0, lse=None):
+        """Attention of the chunks' rows q [rows, heads head_dim] over the cache into out (same shape);
+        lse [rows, heads] float32 takes the rows' log-sum-exp. frame: rows per frame (0: all see all)."""
+        torch = _torch()
+        rows, cols = chunks.desc.rows, self.cfg.heads * self.cfg.head_dim
+        self._cache_check(cache, chunks, q=(q, self.tdtype, (rows, cols)), out=(out, self.tdtype, (rows, cols)),
+                          lse=(lse, torch.float32, (rows, self.cfg.heads)))
+        nbytes = self.lib.wdc_cache_attention_scratch(self.h, cache.ref, chunks.ref)
+        scratch = self._scratch(nbytes)
+        self._cache_call(self.lib.wdc_cache_attention, cache.ref, chunks.ref, _ptr(q), _ld(q), frame, _ptr(out),
+                         _ld(out), _ptr(lse), _ptr(scratch), nbytes)
+        return out
+
+    def cache_mass(self, cache: PagedCache, chunks: Chunks, q, lse, mass, frame: int = 0, decay: float = 1.0, out=None):
+        """out = decay * mass + the weight each cached key receives from the chunks' rows (out: mass itself
+        if not given); mass [pages, kv_heads, page] float32, lse from cache_attention with the same frame."""
+        torch = _torch()
+        rows, shape = chunks.desc.rows, tuple(cache.k.shape[:3])
+        out = mass if out is None else out
+        self._cache_check(cache, chunks, q=(q, self.tdtype, (rows, self.cfg.heads * self.cfg.head_dim)),
+                          lse=(lse, torch.float32, (rows, self.cfg.heads)), mass=(mass, torch.float32, shape),
+                          out=(out, torch.float32, shape))
+        nbytes = self.lib.wdc_cache_mass_scratch(self.h, cache.ref, chunks.ref)
+        scratch = self._scratch(nbytes)
+        self._cache_call(self.lib.wdc_cache_mass, cache.ref, chunks.ref, _ptr(q), _ld(q), frame, _ptr(lse), decay,
+                         _ptr(mass), _ptr(out), _ptr(scratch), nbytes)
+        return out
+
+    def cache_evict(self, cache: PagedCache, chunks: Chunks, mass, keep: int, sink: int = 0, recent: int = 0,
+                    kv_len_out=None, index=None, out=None):
+        """Trim every sequence to `keep` keys in place: the first `sink`, the last `recent` and the others of
+        largest mass. kv_len_out takes the new lengths (chunks.kv_len itself if not given), out the masses
+        (mass itself), index [batch, kv_heads, keep] int32 the former slots."""
+        torch = _torch()
+        shape = tuple(cache.k.shape[:3])
+        kv_len_out = chunks.kv_len if kv_len_out is None else kv_len_out
+        out = mass if out is None else out
+        batch = chunks.kv_len.numel()
+        self._cache_check(cache, chunks, mass=(mass, torch.float32, shape), out=(out, torch.float32, shape),
+                          kv_len_out=(kv_len_out, torch.int32, (batch,)),
+                          index=(index, torch.int32, (batch, shape[1], keep)))
+        nbytes = self.lib.wdc_cache_evict_scratch(self.h, cache.ref, chunks.ref, keep)
+        scratch = self._scratch(nbytes)
+        self._cache_call(self.lib.wdc_cache_evict, cache.ref, chunks.ref, _ptr(mass), _ptr(out), keep, sink, recent,
+                         _ptr(kv_len_out), _ptr(index), _ptr(scratch), nbytes)
+        return kv_len_out
 
     def set_timing(self, on: bool):
         self._check(self.lib.wdc_set_timing(self.h, int(on)))

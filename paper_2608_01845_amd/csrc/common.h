@@ -185,6 +185,102 @@ inline bool attn_len_ok(int64_t n, int hd) { return attn_pad(n) * hd * 2 <= (int
 void attn_split_plan(AttnArgs &a);
 hipError_t launch_attention(int dtype, const AttnArgs &a, hipStream_t s);
 
+// ------------------------------------------------------------------ paged key/value cache
+// A cache and the chunks of one call (wdc_paged_cache, wdc_chunks), lengths still
+// on the device. Every kernel reads them through cache_seq and cache_page, which
+// clamp them to the sizes given by the host, so that no device value leads
+// outside the buffers.
+struct CacheArgs {
+  void *k, *v;              // [pages, kvh, 1 << plog, hd]
+  const int32_t *q_start;   // [batch + 1]
+  const int32_t *kv_len;    // [batch]
+  const int32_t *table;     // [batch, table_ld]
+  int pages, plog, kvh;
+  int batch, rows, max_q, table_ld;
+  int cap;                  // most keys of a sequence: max_kv, or what the table's pages hold
+  int heads, hd, frame;
+  int xcd_order;            // 1: the blocks of one (sequence, kv head) run on one XCD
+};
+
+struct CacheSeq {
+  int q0, nq;  // first packed row, rows taken
+  int n;       // cached keys
+  int start;   // slot of the chunk's first row (negative if the chunk is longer than the cache)
+};
+__device__ __forceinline__ CacheSeq cache_seq(const CacheArgs &a, int b) {
+  CacheSeq s;
+  s.q0 = min(max(a.q_start[b], 0), a.rows);
+  const int q1 = min(max(a.q_start[b + 1], s.q0), a.rows);
+  s.nq = min(q1 - s.q0, a.max_q);
+  s.n = min(max(a.kv_len[b], 0), a.cap);
+  s.start = s.n - (q1 - s.q0);
+  return s;
+}
+// page index of a table entry
+__device__ __forceinline__ int cache_page(const CacheArgs &a, int entry) { return min(max(entry, 0), a.pages - 1); }
+// keys that row i of a chunk sees: slots [0, cache_limit)
+__device__ __forceinline__ int cache_limit(const CacheArgs &a, const CacheSeq &s, int i) {
+  if (a.frame <= 0) return s.n;
+  const int64_t e = s.start + ((int64_t)(i / a.frame) + 1) * a.frame;
+  return (int)(e < 0 ? 0 : e < s.n ? e : s.n);
+}
+
+struct CacheAppendArgs {
+  CacheArgs c;
+  const void *qkv;
+  int64_t ld;
+  const int32_t *pos;       // [rows, 3] or null
+  const float *qw, *kw;     // [hd] or null
+  void *q;
+  int64_t ldq;
+  int norm;
+  int axis_end[3];          // pairs [axis_end[a - 1], axis_end[a]) turn by coordinate a
+  double freq[64];          // turns per unit of the coordinate, per pair
+};
+hipError_t launch_cache_append(int dtype, const CacheAppendArgs &a, hipStream_t s);
+
+struct CacheAttnArgs {
+  CacheArgs c;
+  const void *q;
+  int64_t ldq;
+  void *o;
+  int64_t ldo;
+  float *lse;               // [rows, heads] or null
+  float *part;              // key-range parts of a split launch
+  int splits;
+};
+// Key ranges a launch over these bounds is split into, and the scratch bytes they need
+int cache_attn_splits(int dtype, const CacheArgs &c, size_t scratch);
+size_t cache_attn_scratch(int dtype, const CacheArgs &c);
+hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &a, hipStream_t s);
+
+struct CacheMassArgs {
+  CacheArgs c;
+  const void *q;
+  int64_t ldq;
+  const float *lse;         // [rows, heads]
+  const float *mass;        // [pages, kvh, page]
+  float *out;               // may be mass
+  float decay;
+  float *part;              // row-range parts of a split launch
+  int splits;
+};
+int cache_mass_splits(int dtype, const CacheArgs &c, size_t scratch);
+size_t cache_mass_scratch(int dtype, const CacheArgs &c);
+hipError_t launch_cache_mass(int dtype, const CacheMassArgs &a, hipStream_t s);
+
+struct CacheEvictArgs {
+  CacheArgs c;
+  const float *mass;
+  float *out;               // may be mass
+  int32_t *len_out, *index; // index may be null
+  int keep, sink, recent;
+  int32_t *list;            // scratch: per (sequence, kv head) a count, then moves (to, from)
+  int moves;                // most moves of a (sequence, kv head)
+};
+size_t cache_evict_scratch(const CacheArgs &c, int keep);
+hipError_t launch_cache_evict(int dtype, const CacheEvictArgs &a, hipStream_t s);
+
 // ------------------------------------------------------------------ elementwise and small kernels
 // h[r, :] = LN(x[r, :]) * (1 + scale) + shift; x float32, h model dtype.
 // Rows come in groups of rps (one sample each): logical row i is row

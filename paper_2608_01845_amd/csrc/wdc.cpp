@@ -1661,6 +1661,231 @@ wdc_status wdc_linear(wdc_ctx *ctx, const void *d_a, int64_t lda, const void *d_
   return gemm(ctx, d_a, lda, d_w, d_bias, d_c, ldc, m, n, k, EPI_STORE);
 }
 
+// ---------------------------------------------------------------- paged key/value cache
+}  // extern "C"
+
+namespace {
+constexpr int64_t kCacheRows = int64_t(1) << 26, kCacheKeys = int64_t(1) << 29;
+
+// Descriptor checks shared by the cache operators; fills *a. `rows`: the call takes chunk rows.
+wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q, bool rows, bool values, CacheArgs *a) {
+  if (!c) return WDC_E_ARG;
+  if (!p || !q || !p->d_k || (values && !p->d_v) || !q->d_kv_len || !q->d_table || (rows && !q->d_q_start) ||
+      p->pages < 1 || q->batch < 1 || q->table_ld < 1 || q->max_kv < 0 || (rows && (q->rows < 0 || q->max_q < 0))) {
+    set_err(c, "cache or chunk descriptor: null pointer or size out of range");
+    return WDC_E_ARG;
+  }
+  if (c->hd != 64 && c->hd != 128) {
+    set_err(c, "head_dim must be 64 or 128");
+    return WDC_E_UNSUPPORTED;
+  }
+  if (p->page < 16 || p->page > 256 || (p->page & (p->page - 1))) {
+    set_err(c, "page must be 16, 32, 64, 128 or 256, got %d", p->page);
+    return WDC_E_UNSUPPORTED;
+  }
+  if (c->H < 1 || p->kv_heads < 1 || c->H % p->kv_heads) {
+    set_err(c, "kv_heads (%d) must divide heads (%d)", p->kv_heads, c->H);
+    return WDC_E_SHAPE;
+  }
+  if (!aligned16(p->d_k) || (values && !aligned16(p->d_v))) {
+    set_err(c, "cache not 16-byte aligned");
+    return WDC_E_ALIGN;
+  }
+  if ((uintptr_t)q->d_kv_len % 4 || (uintptr_t)q->d_table % 4 || (rows && (uintptr_t)q->d_q_start % 4)) {
+    set_err(c, "chunk descriptor arrays not 4-byte aligned");
+    return WDC_E_ALIGN;
+  }
+  int plog = 4;
+  while ((1 << plog) < p->page) ++plog;
+  const int64_t cap = std::min<int64_t>(q->max_kv, (int64_t)q->table_ld << plog);
+  const int64_t nrows = rows ? q->rows : 0, max_q = rows ? std::min(q->max_q, q->rows) : 0, heads = (int64_t)q->batch * p->kv_heads;
+  if (heads > 65535 || nrows * c->H > kCacheRows || max_q * q->batch * c->H > kCacheRows || heads * cap > kCacheKeys) {
+    set_err(c, "cache call too large: %d sequences, %d kv heads, %lld rows, %lld keys", q->batch, p->kv_heads,
+            (long long)nrows, (long long)cap);
+    return WDC_E_SHAPE;
+  }
+  *a = CacheArgs{};
+  a->k = p->d_k;
+  a->v = p->d_v;
+  a->q_start = q->d_q_start;
+  a->kv_len = q->d_kv_len;
+  a->table = q->d_table;
+  a->pages = p->pages;
+  a->plog = plog;
+  a->kvh = p->kv_heads;
+  a->batch = q->batch;
+  a->rows = (int)nrows;
+  a->max_q = (int)max_q;
+  a->table_ld = q->table_ld;
+  a->cap = (int)cap;
+  a->heads = c->H;
+  a->hd = c->hd;
+  return WDC_OK;
+}
+
+// a row-major tensor of the model dtype read and written in 16-byte groups
+wdc_status cache_rows(wdc_ctx *c, const char *what, const void *p, int64_t ld, int64_t cols, int rows) {
+  if ((!p && rows > 0) || ld < cols) {
+    set_err(c, "%s: null, or row stride %lld below %lld", what, (long long)ld, (long long)cols);
+    return WDC_E_ARG;
+  }
+  if (!aligned16(p) || ld * c->esz % 16) {
+    set_err(c, "%s: pointer and row stride must be multiples of 16 bytes", what);
+    return WDC_E_ALIGN;
+  }
+  return WDC_OK;
+}
+
+wdc_status cache_f32(wdc_ctx *c, const char *what, const void *p, bool null_ok, size_t align) {
+  if (!p && !null_ok) {
+    set_err(c, "%s is null", what);
+    return WDC_E_ARG;
+  }
+  if ((uintptr_t)p % align) {
+    set_err(c, "%s not %zu-byte aligned", what, align);
+    return WDC_E_ALIGN;
+  }
+  return WDC_OK;
+}
+}  // namespace
+
+extern "C" {
+
+wdc_status wdc_cache_append(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_qkv,
+                            int64_t ld, const int32_t *d_pos, const float *d_q_weight, const float *d_k_weight,
+                            void *d_q, int64_t ldq) {
+  CacheAppendArgs a{};
+  CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
+  CHK(cache_rows(ctx, "qkv", d_qkv, ld, (int64_t)(a.c.heads + 2 * a.c.kvh) * a.c.hd, a.c.rows));
+  CHK(cache_rows(ctx, "q", d_q, ldq, (int64_t)a.c.heads * a.c.hd, a.c.rows));
+  CHK(cache_f32(ctx, "q_weight", d_q_weight, true, 16));
+  CHK(cache_f32(ctx, "k_weight", d_k_weight, true, 16));
+  CHK(cache_f32(ctx, "pos", d_pos, true, 4));
+  const int dims[3] = {ctx->d.rope_t, ctx->d.rope_h, ctx->d.rope_w};
+  const int rs = dims[0] + dims[1] + dims[2];
+  if (rs != 0 && (dims[0] < 0 || dims[1] < 0 || dims[2] < 0 || rs != a.c.hd || dims[0] % 2 || dims[1] % 2 || dims[2] % 2)) {
+    set_err(ctx, "rotary dims must be even and sum to head_dim");
+    return WDC_E_SHAPE;
+  }
+  a.qkv = d_qkv;
+  a.ld = ld;
+  a.pos = rs ? d_pos : nullptr;
+  a.qw = d_q_weight;
+  a.kw = d_k_weight;
+  a.q = d_q;
+  a.ldq = ldq;
+  a.norm = ctx->d.qk_norm;
+  int p = 0;
+  for (int ax = 0; ax < 3; ++ax) {
+    for (int j = 0; j < dims[ax] / 2 && rs; ++j)
+      a.freq[p++] = std::pow(10000.0, -2.0 * j / dims[ax]) / (2.0 * 3.14159265358979323846);
+    a.axis_end[ax] = p;
+  }
+  HIPCHK(ctx, launch_cache_append(ctx->d.dtype, a, ctx->stream));
+  return WDC_OK;
+}
+
+size_t wdc_cache_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks) {
+  CacheArgs a;
+  if (!ctx || cache_args(const_cast<wdc_ctx *>(ctx), cache, chunks, true, false, &a) != WDC_OK) return 0;
+  return cache_attn_scratch(ctx->d.dtype, a);
+}
+
+wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_q,
+                               int64_t ldq, int32_t frame, void *d_o, int64_t ldo, float *d_lse, void *d_scratch,
+                               size_t scratch_bytes) {
+  CacheAttnArgs a{};
+  CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
+  const int64_t cols = (int64_t)a.c.heads * a.c.hd;
+  CHK(cache_rows(ctx, "q", d_q, ldq, cols, a.c.rows));
+  CHK(cache_rows(ctx, "o", d_o, ldo, cols, a.c.rows));
+  CHK(cache_f32(ctx, "lse", d_lse, true, 4));
+  CHK(cache_f32(ctx, "scratch", d_scratch, true, 16));
+  if (frame < 0) {
+    set_err(ctx, "frame must not be negative");
+    return WDC_E_ARG;
+  }
+  a.c.frame = frame;
+  a.q = d_q;
+  a.ldq = ldq;
+  a.o = d_o;
+  a.ldo = ldo;
+  a.lse = d_lse;
+  a.part = (float *)d_scratch;
+  a.splits = cache_attn_splits(ctx->d.dtype, a.c, d_scratch ? scratch_bytes : 0);
+  HIPCHK(ctx, launch_cache_attention(ctx->d.dtype, a, ctx->stream));
+  return WDC_OK;
+}
+
+size_t wdc_cache_mass_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks) {
+  CacheArgs a;
+  if (!ctx || cache_args(const_cast<wdc_ctx *>(ctx), cache, chunks, true, false, &a) != WDC_OK) return 0;
+  return cache_mass_scratch(ctx->d.dtype, a);
+}
+
+wdc_status wdc_cache_mass(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_q,
+                          int64_t ldq, int32_t frame, const float *d_lse, float decay, const float *d_mass,
+                          float *d_mass_out, void *d_scratch, size_t scratch_bytes) {
+  CacheMassArgs a{};
+  CHK(cache_args(ctx, cache, chunks, true, false, &a.c));
+  CHK(cache_rows(ctx, "q", d_q, ldq, (int64_t)a.c.heads * a.c.hd, a.c.rows));
+  CHK(cache_f32(ctx, "lse", d_lse, a.c.rows == 0, 4));
+  CHK(cache_f32(ctx, "mass", d_mass, false, 4));
+  CHK(cache_f32(ctx, "mass_out", d_mass_out, false, 4));
+  CHK(cache_f32(ctx, "scratch", d_scratch, true, 16));
+  if (frame < 0 || !std::isfinite(decay)) {
+    set_err(ctx, "frame must not be negative and decay must be finite");
+    return WDC_E_ARG;
+  }
+  a.c.frame = frame;
+  a.q = d_q;
+  a.ldq = ldq;
+  a.lse = d_lse;
+  a.mass = d_mass;
+  a.out = d_mass_out;
+  a.decay = decay;
+  a.part = (float *)d_scratch;
+  a.splits = cache_mass_splits(ctx->d.dtype, a.c, d_scratch ? scratch_bytes : 0);
+  HIPCHK(ctx, launch_cache_mass(ctx->d.dtype, a, ctx->stream));
+  return WDC_OK;
+}
+
+size_t wdc_cache_evict_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, int32_t keep) {
+  CacheArgs a;
+  if (!ctx || keep < 1 || cache_args(const_cast<wdc_ctx *>(ctx), cache, chunks, false, false, &a) != WDC_OK) return 0;
+  return cache_evict_scratch(a, keep);
+}
+
+wdc_status wdc_cache_evict(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const float *d_mass,
+                           float *d_mass_out, int32_t keep, int32_t sink, int32_t recent, int32_t *d_kv_len_out,
+                           int32_t *d_index, void *d_scratch, size_t scratch_bytes) {
+  CacheEvictArgs a{};
+  CHK(cache_args(ctx, cache, chunks, false, true, &a.c));
+  CHK(cache_f32(ctx, "mass", d_mass, false, 4));
+  CHK(cache_f32(ctx, "mass_out", d_mass_out, false, 4));
+  CHK(cache_f32(ctx, "kv_len_out", d_kv_len_out, false, 4));
+  CHK(cache_f32(ctx, "index", d_index, true, 4));
+  if (keep < 1 || sink < 0 || recent < 0 || (int64_t)sink + recent > keep) {
+    set_err(ctx, "keep %d, sink %d, recent %d: need keep >= 1 and sink + recent <= keep", keep, sink, recent);
+    return WDC_E_ARG;
+  }
+  if (!d_scratch || scratch_bytes < cache_evict_scratch(a.c, keep)) {
+    set_err(ctx, "scratch too small: %zu < %zu", d_scratch ? scratch_bytes : (size_t)0, cache_evict_scratch(a.c, keep));
+    return WDC_E_WORKSPACE;
+  }
+  CHK(cache_f32(ctx, "scratch", d_scratch, false, 16));
+  a.mass = d_mass;
+  a.out = d_mass_out;
+  a.keep = keep;
+  a.sink = sink;
+  a.recent = recent;
+  a.len_out = d_kv_len_out;
+  a.index = d_index;
+  a.list = (int32_t *)d_scratch;
+  HIPCHK(ctx, launch_cache_evict(ctx->d.dtype, a, ctx->stream));
+  return WDC_OK;
+}
+
 wdc_status wdc_set_timing(wdc_ctx *ctx, int32_t on) {
   if (!ctx) return WDC_E_ARG;
   ctx->timing = on != 0;
