@@ -117,10 +117,19 @@ struct Few {
   static constexpr int TILE = 32 * ROWB;
   static constexpr int WAVE = 4 * TILE;          // two K and two V tiles
   // 16-byte chunk c of row r lies at c ^ key(r): the 16 rows of a K fragment, and
-  // the rows of a transposed V read in pairs of chunks, spread over the banks
+  // the 4 rows that 16 lanes of a transposed V read take (a pair of chunks each), spread over the banks
   static __device__ __forceinline__ int kkey(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
-  static __device__ __forceinline__ int vkey(int r) { return HD == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
+  static __device__ __forceinline__ int vkey(int r) { return HD == 128 ? 2 * (r & 3) : 2 * ((r >> 1) & 1); }
+  // transposed V reads of dims 16 i ..: lane offset i % VR, the rest a constant
+  static constexpr int VR = HD == 128 ? 4 : 2;
 };
+
+// V^T fragment (16 dims, 32 keys): keys 4 lg .. of the first and the second 16 rows
+template <int HD>
+__device__ __forceinline__ bf16x8 v_frag(const char *p) {
+  const s16x4 v0 = lds_read_tr(p), v1 = lds_read_tr(p + 16 * Few<HD>::ROWB);
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+}
 
 template <int HD, int RT>
 __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
@@ -169,11 +178,11 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   int kro[NC];                                   // K fragment of rows lr, dims 32 c + 8 lg
 #pragma unroll
   for (int j = 0; j < NC; ++j) kro[j] = lr * F::ROWB + ((4 * j + lg) ^ F::kkey(lr)) * 16;
-  int vro[NI];                                   // transposed V read of rows 4 lg .. + 3, dims 16 i ..
+  int vro[F::VR];                                // transposed V read of rows 4 lg .. + 3, dims 16 i ..
   {
-    const int r = 4 * lg + ((lane & 15) >> 2), j = lane & 3;
+    const int r = 4 * lg + (lr >> 2), j = lane & 3;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) vro[i] = r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
+    for (int i = 0; i < F::VR; ++i) vro[i] = r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
   PageWalk pw;
   pw.init(c, b, (32 * t0) >> c.plog);
@@ -304,11 +313,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const s16x4 v0 = lds_read_tr(vt + vro[i]), v1 = lds_read_tr(vt + 16 * F::ROWB + vro[i]);
-        bf16x8 vf;
-        s16x4 *vp = (s16x4 *)&vf;
-        vp[0] = v0;
-        vp[1] = v1;
+        const bf16x8 vf = v_frag<HD>(vt + vro[i % F::VR] + i / F::VR * F::VR * 32);
 #pragma unroll
         for (int r = 0; r < RT; ++r) o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][i], 0, 0, 0);
       }
@@ -366,6 +371,428 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     *(bf16x4 *)((bf16_t *)a.o + (int64_t)(s.q0 + i) * a.ldo + (int64_t)head * HD + 4 * e) = y;
     if (a.lse && e == 0)
       a.lse[(int64_t)(s.q0 + i) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
+  }
+}
+
+// ---------------------------------------------------------------- bf16, many rows
+// 256 query rows per block of eight waves, 32 each (two tiles of 16), two waves per
+// SIMD; key tiles of 64 reach four K and four V slots of LDS by direct buffer loads
+// of waves 0 to 3, up to four tiles ahead. Bound by the matrix cores, with the
+// exponentials close behind.
+//
+// Tiles that all rows see whole run through a software pipeline: step t holds the P V
+// products of tile t, the Q K products of tile t + 2 and, in the same instruction
+// stream, the vector work of tile t + 1 (P = exp2(sc S - m), its row sum in float32, its
+// rounding to bf16). m is a reference per row, not a running maximum: the first tile's
+// maximum, moved only when a lane's sum of weights over a tile passes 2^64 (then O and the
+// sum are rescaled and P is taken again); any reference gives the same result.
+// Tiles that some row sees in part, and the cache's last, partial one, follow one at a
+// time with their masks.
+constexpr int KV = 64, NB = 4;
+constexpr float SUM_LIMIT = 0x1p64f;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+
+// Loads of one wave (of four): stripe i of a tile is rows [(4 i + w) RPL, + RPL). SMALL:
+// pages of 16 or 32 slots, where every stripe has its own page; otherwise a tile lies on one page.
+template <int HD, bool SMALL>
+struct TileLoads {
+  using F = Few<HD>;
+  static constexpr int NS = KV / (4 * F::RPL);   // stripes of a wave per tile (4 or 2)
+  static constexpr int NP = SMALL ? NS : 1;
+  struct Where {
+    int64_t off[NP];                             // bytes from the pool to the tile (SMALL: the stripe's 16 rows)
+    int bytes[NP];                               // what lies before the end of the cache
+  };
+  PageWalk pw;
+  int kvo, vvo, w, h, n;
+  __device__ __forceinline__ void init(const CacheArgs &c, const CacheSeq &s, int b, int h_, int w_, int lane, int tile0) {
+    w = w_;
+    h = h_;
+    n = s.n;
+    const int r = w * F::RPL + lane / (HD / 8), ch = lane % (HD / 8);
+    const int at = SMALL ? r & 15 : r;
+    kvo = at * F::ROWB + (ch ^ F::kkey(r)) * 16;
+    vvo = at * F::ROWB + (ch ^ F::vkey(r)) * 16;
+    pw.init(c, b, (KV * tile0) >> c.plog);
+  }
+  __device__ __forceinline__ void find(const CacheArgs &c, int tile, Where &x) {
+    const int pmask = (1 << c.plog) - 1;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int key = KV * tile + (SMALL ? (4 * i + w) * F::RPL / 16 * 16 : 0);
+      const int pg = pw.get(key >> c.plog);
+      x.off[i] = ((((int64_t)pg * c.kvh + h) << c.plog) + (key & pmask)) * F::ROWB;
+      x.bytes[i] = min(max(n - key, 0), SMALL ? 16 : KV) * F::ROWB;
+    }
+  }
+  __device__ __forceinline__ void load(const void *pool, const Where &x, char *lds, int vo) const {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc((char *)pool + x.off[SMALL ? i : 0], (short)0,
+                                                                        x.bytes[SMALL ? i : 0], RSRC_WORD3);
+      lds_load16(d, lds + i * 4096 + w * 1024, SMALL ? vo : vo + i * 4096, 0);
+    }
+  }
+};
+
+template <int HD>
+__device__ __forceinline__ float rowmax(const f32x4 (&S)[4][2], int t) {
+  float mx = S[0][t][0];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, S[k][t][e]);
+  return quad_max(mx);
+}
+// P of one row tile, its lane sums
+__device__ __forceinline__ float weights(const f32x4 (&S)[4][2], bf16x8 (&pf)[2], int t, float sc, float m) {
+  float ls = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[k][t][e], sc, -m));
+      ls += p;
+      pf[k >> 1][4 * (k & 1) + e] = (__bf16)p;
+    }
+  return ls;
+}
+
+template <int HD, bool SMALL>
+__global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
+  using F = Few<HD>;
+  using TL = TileLoads<HD, SMALL>;
+  constexpr int NC = HD / 32, NI = HD / 16;
+  constexpr int TB = KV * F::ROWB;               // bytes of a K or V tile
+  constexpr int V_BASE = NB * TB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const CacheArgs &c = a.c;
+  const int group = c.heads / c.kvh;
+  const int nrb = (c.max_q * group + 255) / 256;
+  int bh, li;
+  cache_block(c, nrb * a.splits, bh, li);
+  const int sp = li % a.splits, rb = li / a.splits, b = bh / c.kvh, h = bh % c.kvh;
+  const CacheSeq s = uniform_seq(c, b);
+  const int m0 = rb * 256, count = s.nq * group;
+  if (m0 >= count) return;
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool grp_a = wid < 4;
+  const int mlast = min(m0 + 256, count) - 1;
+  const int lim_lo = cache_limit(c, s, m0 / group), lim_hi = cache_limit(c, s, mlast / group);
+  const int tiles = (lim_hi + KV - 1) / KV;
+  const int t_first = (int)((int64_t)sp * tiles / a.splits), t_end = (int)((int64_t)(sp + 1) * tiles / a.splits);
+  // tiles of the range, relative to t_first: `nf` that every row sees whole, then masked ones
+  const int tot = t_end - t_first, nf = min(max(lim_lo / KV - t_first, 0), tot);
+
+  const float sc = LOG2E / sqrtf((float)HD);
+  bf16x8 qf[2][NC];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int mm = min(m0 + 32 * wid + 16 * t + lr, mlast), i = mm / group;
+    const bf16_t *Q = (const bf16_t *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)(h * group + mm % group) * HD + 8 * lg;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) qf[t][j] = *(const bf16x8 *)(Q + 32 * j);
+  }
+  int kro[NC];                                   // K fragment of rows lr, dims 32 c + 8 lg
+#pragma unroll
+  for (int j = 0; j < NC; ++j) kro[j] = lr * F::ROWB + ((4 * j + lg) ^ F::kkey(lr)) * 16;
+  int vro[F::VR];                                // transposed V read of rows 4 lg .. + 3, dims 16 i ..
+  {
+    const int r = 4 * lg + (lr >> 2), j = lane & 3;
+#pragma unroll
+    for (int i = 0; i < F::VR; ++i) vro[i] = V_BASE + r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
+  }
+  TL tl;
+  typename TL::Where wk, wv;                     // of the latest K tile asked for, and of the one before
+  auto load_k = [&](int tile) {
+    wv = wk;
+    tl.find(c, t_first + tile, wk);
+    tl.load(c.k, wk, smem + (tile % NB) * TB, tl.kvo);
+  };
+  auto load_v = [&](int tile, const typename TL::Where &x) { tl.load(c.v, x, smem + V_BASE + (tile % NB) * TB, tl.vvo); };
+
+  if (grp_a) {                                   // K_0 .. K_3, V_0 .. V_2
+    tl.init(c, s, b, h, wid, lane, t_first);
+    wk = typename TL::Where{};
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (j < tot) {
+        load_k(j);
+        if (j < NB - 1) load_v(j, wk);
+      }
+    wait_vm<0>();
+  }
+  __syncthreads();
+
+  f32x4 o[NI][2];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+  auto qk = [&](f32x4 (&S)[4][2], const char *kb) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bf16x8 kf = *(const bf16x8 *)(kb + kro[j] + k * 16 * F::ROWB);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          S[k][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][j], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[k][t], 0, 0, 0);
+      }
+  };
+  auto vfrag = [&](const char *vb, int i, int p) {   // V^T fragment: dims 16 i .., keys of the 32-key group p
+    return v_frag<HD>(vb + vro[i % F::VR] + i / F::VR * F::VR * 32 + p * 32 * F::ROWB);
+  };
+
+  if (nf > 0) {
+    f32x4 S[2][4][2];                            // S of tiles t + 1 and t + 2 (index tile & 1)
+    bf16x8 pf[2][2][2];                          // P of tiles t and t + 1 (index tile & 1), [row tile][32-key group]
+    qk(S[0], smem);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      m[t] = fmaxf(rowmax<HD>(S[0], t) * sc, -1e30f);
+      l[t] = weights(S[0], pf[0][t], t, sc, m[t]);
+    }
+    if (nf > 1) qk(S[1], smem + TB);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // step 0 refills the slot of K_0
+    constexpr int NMF = 2 * NI + 4 * NC;         // fragment reads per step, two MFMAs each
+    constexpr int NPV = NMF / 2, EPM = 32 / NMF; // P V reads; exponentials per pair of MFMAs
+    static_assert(NMF == 16 || NMF == 32, "hd 64 or 128");
+    bf16x8 fr_[NMF];
+    // One step, P = t % NB at compile time. c indexes S of tile t + 1 and the P it becomes, n S of tile t
+    // + 2 and the P of tile t. Pairs of MFMAs (one per row tile) in a fixed order: P V (32-key group q / NI, O tile
+    // q % NI), then Q K (dims 32 (g / 4).., key tile g % 4, g = q - NPV); fragment q is read four pairs ahead of its
+    // use (0 to 3 in the step before). Past the last tile the stream runs on stale slots and S, unused.
+    // Exponential x is key tile x / 8, row tile (x / 4) % 2, entry x % 4; the empty asm pins it under these MFMAs.
+    auto read = [&](int r, const char *vb, const char *kb) __attribute__((always_inline)) {
+      const int g = r >= NPV ? r - NPV : 0;
+      if (r < NPV)
+        fr_[r] = vfrag(vb, r % NI, (r < NPV ? r : 0) / NI);
+      else
+        fr_[r] = *(const bf16x8 *)(kb + kro[g / 4] + (g % 4) * 16 * F::ROWB);
+    };
+#pragma unroll
+    for (int r = 0; r < 4; ++r) read(r, smem, smem);
+    auto step = [&](auto pc, int t) __attribute__((always_inline)) {
+      constexpr int P = decltype(pc)::value, cur = (P + 1) & 1, n = P & 1;
+      int issued = 0;
+      if (grp_a) {
+        if (t + 4 < tot) {
+          load_k(t + 4);
+          issued += TL::NS;
+        } else {
+          wv = wk;
+        }
+        if (t + 3 < tot) {
+          load_v(t + 3, wv);
+          issued += TL::NS;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const char *vb = smem + P * TB, *kb = smem + ((P + 2) % NB) * TB, *vn = smem + ((P + 1) % NB) * TB;
+      float ls[2] = {0.f, 0.f}, ex[2];
+      auto mma = [&](int q, int t_) __attribute__((always_inline)) {
+        if (q < NPV) {
+          o[q % NI][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], pf[n][t_][(q < NPV ? q : 0) / NI], o[q % NI][t_], 0, 0, 0);
+        } else {
+          const int g = q >= NPV ? q - NPV : 0;
+          S[n][g % 4][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], qf[t_][g / 4],
+                                                                    g < 4 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[n][g % 4][t_], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto expo = [&](int x) __attribute__((always_inline)) {
+        const int k = x / 8, t_ = (x / 4) % 2, e = x % 4;
+        float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[cur][k][t_][e], sc, -m[t_]));
+        asm volatile("" : "+v"(y));
+        return y;
+      };
+#pragma unroll
+      for (int q = 0; q < NMF; ++q) {
+        if constexpr (EPM == 2) {
+          ex[0] = expo(2 * q);
+          ex[1] = expo(2 * q + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mma(q, 0);
+        if constexpr (EPM == 1) {
+          ex[q & 1] = expo(q);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mma(q, 1);
+        if (q + 4 < NMF)
+          read(q + 4, vb, kb);
+        else                                     // the next step's first reads: V of tile t + 1
+          read(q + 4 - NMF, vn, kb);
+        __builtin_amdgcn_sched_barrier(0);
+        if (EPM == 2 || (q & 1)) {
+          const int x = EPM == 2 ? 2 * q : q - 1, k = x / 8, t_ = (x / 4) % 2, e = x % 4;
+          const bf16x2_t pr = {(__bf16)ex[0], (__bf16)ex[1]};
+          uint32_t u = __builtin_bit_cast(uint32_t, pr);
+          ls[t_] += ex[0] + ex[1];
+          asm volatile("" : "+v"(u), "+v"(ls[t_]));
+          u32x4_t w_ = __builtin_bit_cast(u32x4_t, pf[cur][t_][k / 2]);
+          w_[2 * (k & 1) + e / 2] = u;
+          pf[cur][t_][k / 2] = __builtin_bit_cast(bf16x8, w_);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      if (t + 1 < nf) {
+        if (__any(fmaxf(ls[0], ls[1]) > SUM_LIMIT)) {
+#pragma unroll
+          for (int t_ = 0; t_ < 2; ++t_) {
+            const float mx = rowmax<HD>(S[cur], t_) * sc, mn = mx > m[t_] + 8.f ? mx : m[t_];
+            const float al = __builtin_amdgcn_exp2f(m[t_] - mn);
+            m[t_] = mn;
+            l[t_] *= al;
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][t_][e] *= al;
+            ls[t_] = weights(S[cur], pf[cur][t_], t_, sc, m[t_]);
+          }
+        }
+        l[0] += ls[0];
+        l[1] += ls[1];
+      }
+      // the loads of earlier steps are done, and all reads but the four just issued
+      if (grp_a) {
+        if (issued == 2 * TL::NS)
+          wait_vm<2 * TL::NS>();
+        else if (issued == TL::NS)
+          wait_vm<TL::NS>();
+        else
+          wait_vm<0>();
+      }
+      asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(8) : "memory");
+    };
+    for (int t = 0; t < nf; t += NB) {
+      step(std::integral_constant<int, 0>{}, t);
+      if (t + 1 >= nf) break;
+      step(std::integral_constant<int, 1>{}, t + 1);
+      if (t + 2 >= nf) break;
+      step(std::integral_constant<int, 2>{}, t + 2);
+      if (t + 3 >= nf) break;
+      step(std::integral_constant<int, 3>{}, t + 3);
+    }
+  }
+
+  // masked tiles, one at a time: tile u with K and V of u + 1 and u + 2 under way
+  int lim[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int mr = m0 + 32 * wid + 16 * t + lr;
+    lim[t] = mr < count ? cache_limit(c, s, mr / group) : 0;
+  }
+  for (int u = nf; u < tot; ++u) {
+    if (grp_a) wait_vm<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (grp_a && u + 3 < tot) {
+      if (u > nf) load_k(u + 3);                 // at u = nf the pipeline has asked for it already
+      load_v(u + 3, wk);
+    }
+    const char *kb = smem + (u % NB) * TB, *vb = smem + (u % NB) * TB;   // vro holds V_BASE
+    // A key that a row does not see has weight 0, but 0 times an infinity or NaN of
+    // its V is NaN in a matrix product: a tile that holds one is multiplied key by key.
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < TB / (512 * 16); ++i) {
+      const uint4 x = *(const uint4 *)(vb + V_BASE + (i * 512 + tid) * 16);
+      const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) odd |= (y[q] & 0x7f80u) == 0x7f80u || (y[q] & 0x7f800000u) == 0x7f800000u;
+    }
+    odd = __syncthreads_or(odd);
+    const int key0 = KV * (t_first + u);
+    f32x4 S[4][2];
+    bf16x8 pf[2][2];
+    qk(S, kb);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key0 + 16 * k + 4 * lg + e >= lim[t]) S[k][t][e] = -INFINITY;
+      const float mx = rowmax<HD>(S, t) * sc;
+      if (__any(mx > m[t] + 8.f)) {
+        const float mn = fmaxf(m[t], mx), al = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
+        m[t] = mn;
+        l[t] *= al;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][t][e] *= al;
+      }
+      l[t] += weights(S, pf[t], t, sc, m[t] == -INFINITY ? 0.f : m[t]);
+    }
+    if (odd) {
+      for (int k = 0; k < 4; ++k)
+        for (int e = 0; e < 4; ++e)
+          for (int g = 0; g < 4; ++g) {
+            const int key = 16 * k + 4 * g + e;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              float p = 0.f;                     // of key and row lr, held by lane group g
+#pragma unroll
+              for (int q = 0; q < 16; ++q)
+                if (q == 4 * k + e) p = (float)pf[t][q >> 3][q & 7];
+              p = __shfl(p, 16 * g + lr, 64);
+              if (key0 + key < lim[t])
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+#pragma unroll
+                  for (int d = 0; d < 4; ++d) {
+                    const int col = 16 * i + 4 * lg + d;
+                    o[i][t][d] += p * bf2f(*(const bf16_t *)(vb + V_BASE + key * F::ROWB + ((col >> 3) ^ F::vkey(key)) * 16 + (col & 7) * 2));
+                  }
+            }
+          }
+    } else {
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const bf16x8 vf = vfrag(vb, i, p);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][p], o[i][t], 0, 0, 0);
+        }
+    }
+  }
+
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const float den = quad_sum(l[t]);
+    const int mr = m0 + 32 * wid + 16 * t + lr;
+    if (mr >= count) continue;
+    if (a.splits > 1) {
+      const int64_t at = ((int64_t)bh * a.splits + sp) * (c.max_q * group) + mr;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) *(f32x4 *)(a.part + at * HD + 16 * i + 4 * lg) = o[i][t];
+      if (lg == 0) {
+        float *pm = a.part + (int64_t)c.batch * c.kvh * a.splits * (c.max_q * group) * HD + 2 * at;
+        pm[0] = m[t];
+        pm[1] = den;
+      }
+      continue;
+    }
+    const float inv = 1.f / den;
+    const int i0 = mr / group, head = h * group + mr % group;
+    bf16_t *O = (bf16_t *)a.o + (int64_t)(s.q0 + i0) * a.ldo + (int64_t)head * HD + 4 * lg;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      bf16x4 y;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) y[d] = (__bf16)(den == 0.f ? 0.f : o[i][t][d] * inv);
+      *(bf16x4 *)(O + 16 * i) = y;
+    }
+    if (a.lse && lg == 0)
+      a.lse[(int64_t)(s.q0 + i0) * c.heads + head] = den == 0.f ? -INFINITY : (m[t] + log2f(den)) * LN2;
   }
 }
 
@@ -701,7 +1128,7 @@ __global__ __launch_bounds__(256) void k_cache_mass_combine(CacheMassArgs a) {
 int rows_per_block(int dtype, const CacheArgs &c) {
   if (dtype == 0) return 32;
   const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
-  return m <= 16 ? 16 : m <= 32 ? 32 : 64;
+  return m <= 16 ? 16 : m <= 32 ? 32 : m <= 128 ? 64 : 256;
 }
 int64_t attn_blocks(int dtype, const CacheArgs &c) {
   const int rpb = rows_per_block(dtype, c);
@@ -722,9 +1149,21 @@ hipError_t launch_few(const CacheAttnArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((k_cache_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(1, a.c) * a.splits)), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
+template <int HD, bool SMALL>
+hipError_t launch_many(const CacheAttnArgs &a, hipStream_t s) {
+  constexpr int LDS = 2 * NB * KV * Few<HD>::ROWB;
+  static DeviceOnce once;
+  const hipError_t lim = once_on_device(once, [] {
+    return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  });
+  if (lim != hipSuccess) return lim;
+  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL>), dim3((unsigned)(attn_blocks(1, a.c) * a.splits)), dim3(512), LDS, s, a);
+  return hipGetLastError();
+}
 template <int HD>
 hipError_t launch_bf16(const CacheAttnArgs &a, hipStream_t s) {
   const int rpb = rows_per_block(1, a.c);
+  if (rpb == 256) return a.c.plog < 6 ? launch_many<HD, true>(a, s) : launch_many<HD, false>(a, s);
   return rpb == 16 ? launch_few<HD, 1>(a, s) : rpb == 32 ? launch_few<HD, 2>(a, s) : launch_few<HD, 4>(a, s);
 }
 
