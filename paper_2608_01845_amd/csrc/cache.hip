@@ -167,150 +167,342 @@ __device__ __forceinline__ uint32_t mass_order(float m) {
 }
 
 constexpr int EVT = 1024, EVW = EVT / 64;   // threads and waves of a selection block
+constexpr int EVH = 4;                      // copies of a block's histogram, to spread equal digits over
+constexpr int EVP = 16;                     // parts of a long (sequence, kv head); one wave reads one part's histogram
+constexpr int EVB = 2048;                   // bins of a histogram
+constexpr int EVK = 8;                      // weights that a thread keeps in registers
+static_assert(EVP == EVW, "a wave per part");
+// digits of the order values, from the top: 11, 11 and 10 bits
+__device__ __forceinline__ int ev_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
+__device__ __forceinline__ int ev_bins(int d) { return d == 2 ? 1024 : 2048; }
+
+// Scratch of one (sequence, kv head), in 32-bit words: the number of moves, then
+// moves (to, from); with parts, two sets of their histograms and a few words each.
+__host__ __device__ inline int64_t evict_words(int moves, int parts) {
+  return 4 + 2 * (int64_t)moves + (parts > 1 ? 2 * EVP * EVB + 2 * EVP + 8 : 0);
+}
+
+// What one block of the selection works on: slots [s0, s1) of a (sequence, kv head) of n > keep keys
+struct EvictPart {
+  const CacheEvictArgs &a;
+  int h, b, n, s0, s1, low_len, high_len;
+  const int32_t *tab;
+  int32_t *list;
+  int j0, j1;        // the wave's slots: a contiguous run of them, so that lists in wave order are in slot order
+  // weights of slots j0 + 64 i + lane and their places in the pool (-1: on no page of the cache, read as one
+  // of its pages and never written); those of longer runs are read again where they are needed
+  float x[EVK];
+  int place[EVK];
+  uint32_t *words;   // histograms [2][EVP][EVB], keys above the threshold's digits so far [EVP], prefix and rank [2][2]
+  __device__ __forceinline__ EvictPart(const CacheEvictArgs &a_) : a(a_), h(blockIdx.y), b(blockIdx.z) {
+    const CacheArgs &c = a.c;
+    n = __builtin_amdgcn_readfirstlane(min(max(c.kv_len[b], 0), c.cap));
+    tab = c.table + (int64_t)b * c.table_ld;
+    list = a.list + ((int64_t)b * c.kvh + h) * evict_words(a.moves, a.parts);
+    words = (uint32_t *)list + 4 + 2 * (int64_t)a.moves;
+    low_len = (a.keep + a.low - 1) / a.low;
+    high_len = a.parts > a.low ? (max(n - a.keep, 0) + a.parts - a.low - 1) / (a.parts - a.low) : 0;
+    s0 = bound(blockIdx.x);
+    s1 = bound(blockIdx.x + 1);
+    const int run = ((s1 - s0 + 64 * EVW - 1) / (64 * EVW)) * 64;
+    j0 = min(s0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * run, s1);
+    j1 = min(j0 + run, s1);
+#pragma unroll
+    for (int i = 0; i < EVK; ++i)
+      if (j0 + 64 * i < j1) {
+        const int j = min(j0 + 64 * i + (int)(threadIdx.x & 63), j1 - 1), e = tab[j >> c.plog], at = spot(e, j);
+        x[i] = a.mass[at];
+        place[i] = (unsigned)e < (unsigned)c.pages ? at : -1;
+      }
+  }
+  // place in the pool of slot j with table entry e (pools hold fewer than 2^31 slots)
+  __device__ __forceinline__ int spot(int e, int j) const {
+    return ((cache_page(a.c, e) * a.c.kvh + h) << a.c.plog) + (j & ((1 << a.c.plog) - 1));
+  }
+  // f(slot, its weight, its place) for the wave's slots, 64 at a time in order; slots >= j1 come along
+  template <class F>
+  __device__ __forceinline__ void each(F &&f) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < EVK; ++i)
+      if (j0 + 64 * i < j1) f(j0 + 64 * i + lane, x[i], place[i]);
+    for (int j = j0 + 64 * EVK; j < j1; j += 64) {
+      const int jj = min(j + lane, j1 - 1), e = tab[jj >> a.c.plog], at = spot(e, jj);
+      f(j + lane, a.mass[at], (unsigned)e < (unsigned)a.c.pages ? at : -1);
+    }
+  }
+  // first slot of part p: parts [0, low) cut [0, keep) evenly, the others [keep, n)
+  __device__ __forceinline__ int bound(int p) const {
+    if (a.parts == 1) return p ? n : 0;
+    return p <= a.low ? min(p * low_len, min(n, a.keep)) : min(a.keep + (p - a.low) * high_len, n);
+  }
+  // slots that compete: behind the first `sink`, before the last `recent`
+  __device__ __forceinline__ bool middle(int j) const { return j >= a.sink && j < n - a.recent; }
+};
+
+// Histogram of digit d of the slots of the part that share the digits found so far
+__device__ __forceinline__ void evict_count(const EvictPart &p, uint32_t (*hist)[EVB], int d, uint32_t prefix,
+                                            uint32_t known) {
+  const int tid = threadIdx.x, w = tid >> 6;
+  for (int i = tid; i < EVH * EVB; i += EVT) (&hist[0][0])[i] = 0;
+  __syncthreads();
+  p.each([&](int j, float x, int) __attribute__((always_inline)) {
+    const uint32_t u = mass_order(x);
+    if (j < p.j1 && p.middle(j) && (u & known) == prefix)
+      atomicAdd(&hist[w % EVH][(u >> ev_shift(d)) & (ev_bins(d) - 1)], 1u);
+  });
+  __syncthreads();
+}
+
+// Bin in which the rank-th key from the top lies, and its rank there. Bins go
+// from the top: thread t brings bins top = bins - 1 - per t (first) and top - 1
+// (second, if per = 2). All threads get the results; *size: the keys of that bin.
+__device__ __forceinline__ void evict_pick(uint32_t first, uint32_t second, int top, int rank, int *bin, int *r,
+                                           int *size = nullptr) {
+  __shared__ uint32_t wsum[EVW];
+  __shared__ int got[3];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const uint32_t mine = first + second;
+  uint32_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t t = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += t;
+  }
+  if (lane == 63) wsum[w] = incl;
+  __syncthreads();
+  uint32_t before = incl - mine;
+  for (int i = 0; i < w; ++i) before += wsum[i];
+  if (before < (uint32_t)rank && before + mine >= (uint32_t)rank) {   // one thread
+    const uint32_t x = rank - before;
+    got[0] = x > first ? top - 1 : top;
+    got[1] = (int)(x > first ? x - first : x);
+    got[2] = (int)(x > first ? second : first);
+  }
+  __syncthreads();
+  *bin = got[0];
+  *r = got[1];
+  if (size) *size = got[2];
+  __syncthreads();
+}
+
+// The lists of one part, given the threshold in the digits `known`: slots whose order value is above it in
+// them are kept, of those equal to it the first `taken` (eq0 of them lie in parts before);
+// hr holes and mr movers lie in parts before. Each wave takes a contiguous run of slots,
+// and counts of runs are added in order, so every list is in slot order. Returns the part's holes.
+__device__ __forceinline__ void evict_lists(const EvictPart &p, uint32_t threshold, uint32_t known, bool any, int taken, int eq0, int hr,
+                                            int mr, bool count) {
+  __shared__ int wcnt[3][EVW];
+  const CacheEvictArgs &a = p.a;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), keep = a.keep;
+  int32_t *idx = a.index ? a.index + ((int64_t)p.b * a.c.kvh + p.h) * keep : nullptr;
+  const int j1 = p.j1;
+  const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
+  // class of slot j: 2 kept, 1 equal to the threshold, 0 dropped
+  auto cls = [&](int j, float x) {
+    if (j >= j1) return 0;
+    if (!p.middle(j)) return 2;
+    if (!any) return 0;
+    const uint32_t u = mass_order(x) & known;
+    return u > threshold ? 2 : u == threshold ? 1 : 0;
+  };
+  int eq = 0;
+  p.each([&](int j, float x, int) __attribute__((always_inline)) { eq += __popcll(__ballot(cls(j, x) == 1)); });
+  if (lane == 0) wcnt[0][w] = eq;
+  __syncthreads();
+  for (int i = 0; i < w; ++i) eq0 += wcnt[0][i];
+  // f(slot, weight, place, kept) in order
+  auto kept_each = [&](auto &&f) __attribute__((always_inline)) {
+    int er = eq0;
+    p.each([&](int j, float x, int place) __attribute__((always_inline)) {
+      const int cl = cls(j, x);
+      const uint64_t eb = __ballot(cl == 1);
+      f(j, x, place, cl == 2 || (cl == 1 && er + __popcll(eb & below) < taken));
+      er += __popcll(eb);
+    });
+  };
+  int holes = 0, movers = 0;
+  kept_each([&](int j, float, int, bool kept) __attribute__((always_inline)) {
+    holes += __popcll(__ballot(j < j1 && !kept && j < keep));
+    movers += __popcll(__ballot(j < j1 && kept && j >= keep));
+  });
+  if (lane == 0) {
+    wcnt[1][w] = holes;
+    wcnt[2][w] = movers;
+  }
+  __syncthreads();
+  int total = 0;
+  for (int i = 0; i < EVW; ++i) {
+    if (i < w) {
+      hr += wcnt[1][i];
+      mr += wcnt[2][i];
+    }
+    total += wcnt[1][i];
+  }
+  if (count && threadIdx.x == 0) p.list[0] = min(total, a.moves);
+  kept_each([&](int j, float x, int place, bool kept) __attribute__((always_inline)) {
+    const bool hole = j < j1 && !kept && j < keep, mover = j < j1 && kept && j >= keep;
+    const uint64_t hb = __ballot(hole), mb = __ballot(mover);
+    const int hx = hr + __popcll(hb & below), mx = mr + __popcll(mb & below);
+    if (hole && hx < a.moves) p.list[4 + 2 * hx] = j;
+    if (mover && mx < a.moves) p.list[5 + 2 * mx] = j;
+    if (j < j1 && kept && j < keep) {
+      if (a.out != a.mass && place >= 0) a.out[place] = x;
+      if (idx) idx[j] = j;
+    }
+    hr += __popcll(hb);
+    mr += __popcll(mb);
+  });
+}
+
+// A sequence that is short enough: everything stays
+__device__ __forceinline__ void evict_none(const EvictPart &p) {
+  const CacheEvictArgs &a = p.a;
+  int32_t *idx = a.index ? a.index + ((int64_t)p.b * a.c.kvh + p.h) * a.keep : nullptr;
+  const int first = blockIdx.x * EVT + threadIdx.x, step = gridDim.x * EVT;
+  for (int j = first; j < p.n; j += step) {
+    const int e = p.tab[j >> a.c.plog], at = p.spot(e, j);
+    if (a.out != a.mass && (unsigned)e < (unsigned)a.c.pages) a.out[at] = a.mass[at];
+    if (idx) idx[j] = j;
+  }
+  if (idx)
+    for (int j = p.n + first; j < a.keep; j += step) idx[j] = -1;
+  if (first == 0) p.list[0] = 0;
+}
 
 // The kept set of one (sequence, kv head). With m = keep - sink - recent places
 // for the n - sink - recent keys in between: the m-th largest weight is found digit by
-// digit (11, 11 and 10 bits, a histogram each), then the keys above it and the
-// first of those equal to it are kept. Each wave takes a contiguous run of
-// slots; counts of runs are added in order, so every list is in slot order.
-// Kept keys below `keep` stay; hole j below it takes kept key j from above, so
+// digit with a histogram each, then the keys above it and the first of those
+// equal to it are kept. Kept keys below `keep` stay; hole j below it takes kept key j from above, so
 // nothing that is still to be read is written and only those rows move.
+//
+// One block does it all for short sequences (STAGE -1). What bounds that form is
+// the instruction rate of one compute unit (67,320 slots: 189 us), so long ones are cut into EVP parts of one
+// block each and the steps become launches 0 to 3: stage d counts digit d of its part after every
+// block has found digit d - 1 from all parts' counts, and stage 3 writes the lists. The parts' counts also
+// give how many keys of each part are kept, hence the ranks that its lists start from; parts do not cross `keep`.
+template <int STAGE>
 __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
-  __shared__ uint32_t hist[2048];
-  __shared__ uint32_t wsum[EVW];
-  __shared__ int wcnt[3][EVW];
-  __shared__ uint32_t sh_prefix;
-  __shared__ int sh_rank;
-  const CacheArgs &c = a.c;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int n = min(max(c.kv_len[b], 0), c.cap);
-  const int keep = a.keep;
-  const int32_t *tab = c.table + (int64_t)b * c.table_ld;
-  int32_t *list = a.list + ((int64_t)b * c.kvh + h) * (1 + 2 * (int64_t)a.moves);
-  int32_t *idx = a.index ? a.index + ((int64_t)b * c.kvh + h) * keep : nullptr;
-  const int pmask = (1 << c.plog) - 1;
-  auto at = [&](int j) {
-    return (((int64_t)cache_page(c, tab[j >> c.plog]) * c.kvh + h) << c.plog) + (j & pmask);
-  };
-  // a slot on no page of the cache: read as one of its pages, never written
-  auto stored = [&](int j) { return (unsigned)tab[j >> c.plog] < (unsigned)c.pages; };
-  if (n <= keep) {
-    for (int j = tid; j < n; j += EVT) {
-      if (a.out != a.mass && stored(j)) a.out[at(j)] = a.mass[at(j)];
-      if (idx) idx[j] = j;
-    }
-    if (idx)
-      for (int j = n + tid; j < keep; j += EVT) idx[j] = -1;
-    if (tid == 0) list[0] = 0;
+  __shared__ uint32_t hist[EVH][EVB];
+  const EvictPart p(a);
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, part = blockIdx.x;
+  if (p.n <= a.keep) {
+    if (STAGE < 0 || STAGE == 3) evict_none(p);
     return;
   }
-  const int lo = a.sink, hi = n - a.recent, m = keep - a.sink - a.recent;
-  // the m-th largest order value of [lo, hi), and how many of its equals are taken
-  uint32_t prefix = 0, known = 0;
-  int rank = m;                          // rank among the keys that share the digits found so far
-  if (m > 0) {
-    const int shifts[3] = {21, 10, 0}, bins[3] = {2048, 2048, 1024};
-    for (int d = 0; d < 3; ++d) {
-      for (int i = tid; i < bins[d]; i += EVT) hist[i] = 0;
-      __syncthreads();
-      for (int j = lo + tid; j < hi; j += EVT) {
-        const uint32_t u = mass_order(a.mass[at(j)]);
-        if ((u & known) == prefix) atomicAdd(&hist[(u >> shifts[d]) & (bins[d] - 1)], 1u);
-      }
-      __syncthreads();
-      // bins from the top: thread t holds a pair of them (the last digit: one)
-      const int per = bins[d] / EVT, top = bins[d] - 1 - per * tid;
-      uint32_t mine = hist[top] + (per > 1 ? hist[top - 1] : 0u), incl = mine;
+  const int m = a.keep - a.sink - a.recent;
+  if constexpr (STAGE < 0) {
+    uint32_t prefix = 0, known = 0;
+    int rank = m, bin, size = m + 1;
+    for (int d = 0; d < 3 && m > 0 && size != rank; ++d) {   // until all of a bin are taken
+      evict_count(p, hist, d, prefix, known);
+      const int per = ev_bins(d) / EVT, top = ev_bins(d) - 1 - per * tid;
+      uint32_t first = 0, second = 0;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t t = __shfl_up(incl, o, 64);
-        if (lane >= o) incl += t;
+      for (int i = 0; i < EVH; ++i) {
+        first += hist[i][top];
+        if (per > 1) second += hist[i][top - 1];
       }
-      if (lane == 63) wsum[w] = incl;
-      __syncthreads();
-      uint32_t before = incl - mine;
-      for (int i = 0; i < w; ++i) before += wsum[i];
-      if (before < (uint32_t)rank && before + mine >= (uint32_t)rank) {   // one thread
-        int bin = top, r = rank - (int)before;
-        if (per > 1 && (uint32_t)r > hist[top]) {
-          r -= (int)hist[top];
-          bin = top - 1;
-        }
-        sh_prefix = prefix | ((uint32_t)bin << shifts[d]);
-        sh_rank = r;
-      }
-      __syncthreads();
-      prefix = sh_prefix;
-      rank = sh_rank;
-      known |= (uint32_t)(bins[d] - 1) << shifts[d];
-      __syncthreads();
+      evict_pick(first, second, top, rank, &bin, &rank, &size);
+      prefix |= (uint32_t)bin << ev_shift(d);
+      known |= (uint32_t)(ev_bins(d) - 1) << ev_shift(d);
     }
+    evict_lists(p, prefix, known, m > 0, rank, 0, 0, 0, true);
+    return;
   }
-  // runs of whole 64s per wave over [0, n)
-  const int run = ((n + 64 * EVW - 1) / (64 * EVW)) * 64;
-  const int j0 = min(w * run, n), j1 = min(j0 + run, n);
-  // class of slot j: 2 kept, 1 equal to the threshold, 0 dropped
-  auto cls = [&](int j, float x) {
-    if (j < lo || j >= hi) return 2;
-    if (m == 0) return 0;
-    const uint32_t u = mass_order(x);
-    return u > prefix ? 2 : u == prefix ? 1 : 0;
-  };
-  int eq = 0;
-  for (int j = j0; j < j1; j += 64) {
-    const int jj = j + lane;
-    eq += __popcll(__ballot(jj < j1 && cls(jj, a.mass[at(min(jj, n - 1))]) == 1));
+  // histograms of stage d lie in set d & 1
+  uint32_t *above = p.words + 2 * EVP * EVB, *found = above + 2 * EVP;
+  uint32_t prefix = 0, known = 0;
+  int rank = m, bin = 0;
+  if (STAGE > 1) {
+    prefix = found[2 * (STAGE & 1)];
+    rank = (int)found[2 * (STAGE & 1) + 1];
   }
-  if (lane == 0) wcnt[0][w] = eq;
-  __syncthreads();
-  int eq0 = 0;
-  for (int i = 0; i < w; ++i) eq0 += wcnt[0][i];
-  const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-  int holes = 0, movers = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    int er = eq0, hr = holes, mr = movers;   // pass 1: ranks before this run
-    for (int j = j0; j < j1; j += 64) {
-      const int jj = j + lane;
-      const bool in = jj < j1;
-      const float x = a.mass[at(min(jj, n - 1))];
-      const int cl = in ? cls(jj, x) : 0;
-      const uint64_t eb = __ballot(cl == 1);
-      const bool kept = cl == 2 || (cl == 1 && er + __popcll(eb & below) < rank);
-      er += __popcll(eb);
-      const bool hole = in && !kept && jj < keep, mover = in && kept && jj >= keep;
-      const uint64_t hb = __ballot(hole), mb = __ballot(mover);
-      if (pass == 1) {
-        if (hole) {
-          const int r = hr + __popcll(hb & below);
-          if (r < a.moves) list[1 + 2 * r] = jj;
-        }
-        if (mover) {
-          const int r = mr + __popcll(mb & below);
-          if (r < a.moves) list[2 + 2 * r] = jj;
-        }
-        if (in && kept && jj < keep) {
-          if (a.out != a.mass && stored(jj)) a.out[at(jj)] = x;
-          if (idx) idx[jj] = jj;
-        }
-      }
-      hr += __popcll(hb);
-      mr += __popcll(mb);
+  for (int d = 0; d < STAGE; ++d) known |= (uint32_t)(ev_bins(d) - 1) << ev_shift(d);
+  if (STAGE > 0 && m > 0) {
+    constexpr int D = STAGE - 1;
+    const uint32_t *g = p.words + (D & 1) * EVP * EVB;
+    const int bins = ev_bins(D), per = bins / EVT, top = bins - 1 - per * tid;
+    uint32_t first = 0, second = 0;
+#pragma unroll
+    for (int q = 0; q < EVP; ++q) {
+      first += g[q * EVB + top];
+      if (per > 1) second += g[q * EVB + top - 1];
     }
-    if (pass == 0) {
+    evict_pick(first, second, top, rank, &bin, &rank);
+    prefix |= (uint32_t)bin << ev_shift(D);
+    if (STAGE < 3 && part == 0 && tid == 0) {
+      found[2 * ((STAGE + 1) & 1)] = prefix;
+      found[2 * ((STAGE + 1) & 1) + 1] = (uint32_t)rank;
+    }
+    // keys of each part above the bin: of this part now, for stage 3 of all of them
+    __shared__ int gt[EVP], eq[EVP];
+    if (STAGE == 3 || w == part) {
+      int x = 0;
+#pragma unroll 16
+      for (int i = lane; i < bins; i += 64) {
+        const int y = (int)g[w * EVB + i];
+        if (i > bin) x += y;
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
       if (lane == 0) {
-        wcnt[1][w] = hr;
-        wcnt[2][w] = mr;
-      }
-      __syncthreads();
-      int total = 0;
-      for (int i = 0; i < EVW; ++i) {
-        if (i < w) {
-          holes += wcnt[1][i];
-          movers += wcnt[2][i];
+        if (STAGE < 3) {
+          above[w] = (uint32_t)x + (STAGE > 1 ? above[w] : 0u);
+        } else {
+          gt[w] = x + (int)above[w];
+          eq[w] = (int)g[w * EVB + bin];
         }
-        total += wcnt[1][i];
       }
-      if (tid == 0) list[0] = min(total, a.moves);
+    }
+    if (STAGE == 3) {
+      __syncthreads();
+      int eq0 = 0, hr = 0, mr = 0, my_eq = 0, my_hr = 0, my_mr = 0;
+      for (int q = 0; q < EVP; ++q) {
+        const int q0 = p.bound(q), q1 = p.bound(q + 1);
+        if (q == part) {
+          my_eq = eq0;
+          my_hr = hr;
+          my_mr = mr;
+        }
+        const int fixed = max(0, min(q1, a.sink) - q0) + max(0, q1 - max(q0, p.n - a.recent));
+        const int kept = fixed + gt[q] + min(eq[q], max(0, rank - eq0));
+        eq0 += eq[q];
+        if (q < a.low)
+          hr += q1 - q0 - kept;
+        else
+          mr += kept;
+      }
+      if (part == 0 && tid == 0) p.list[0] = min(hr, a.moves);
+      evict_lists(p, prefix, ~0u, true, rank, my_eq, my_hr, my_mr, false);
+      return;
+    }
+  } else if (STAGE == 3) {                       // m = 0: only what is protected stays
+    int hr = 0, mr = 0, my_hr = 0, my_mr = 0;
+    for (int q = 0; q < EVP; ++q) {
+      const int q0 = p.bound(q), q1 = p.bound(q + 1);
+      if (q == part) {
+        my_hr = hr;
+        my_mr = mr;
+      }
+      const int fixed = max(0, min(q1, a.sink) - q0) + max(0, q1 - max(q0, p.n - a.recent));
+      if (q < a.low)
+        hr += q1 - q0 - fixed;
+      else
+        mr += fixed;
+    }
+    if (part == 0 && tid == 0) p.list[0] = min(hr, a.moves);
+    evict_lists(p, 0, 0, false, 0, 0, my_hr, my_mr, false);
+    return;
+  }
+  if (STAGE < 3 && m > 0) {
+    evict_count(p, hist, STAGE, prefix, known);
+    uint32_t *g = p.words + ((STAGE & 1) * EVP + part) * EVB;
+    for (int i = tid; i < ev_bins(STAGE); i += EVT) {
+      uint32_t x = 0;
+#pragma unroll
+      for (int q = 0; q < EVH; ++q) x += hist[q][i];
+      g[i] = x;
     }
   }
 }
@@ -322,7 +514,7 @@ __global__ __launch_bounds__(256) void k_evict_move(CacheEvictArgs a) {
   constexpr int TPR = RB / 16, RPB = 256 / TPR;
   const CacheArgs &c = a.c;
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-  const int32_t *list = a.list + ((int64_t)b * c.kvh + h) * (1 + 2 * (int64_t)a.moves);
+  const int32_t *list = a.list + ((int64_t)b * c.kvh + h) * evict_words(a.moves, a.parts);
   const int32_t *tab = c.table + (int64_t)b * c.table_ld;
   const int cnt = list[0];
   const int pmask = (1 << c.plog) - 1;
@@ -335,7 +527,7 @@ __global__ __launch_bounds__(256) void k_evict_move(CacheEvictArgs a) {
   }
   const int e = (tid % TPR) * 16;
   for (int r = blockIdx.x * RPB + tid / TPR; r < cnt; r += gridDim.x * RPB) {
-    const int to = list[1 + 2 * r], from = list[2 + 2 * r];
+    const int to = list[4 + 2 * r], from = list[5 + 2 * r];
     if (e == 0 && a.index) a.index[((int64_t)b * c.kvh + h) * a.keep + to] = from;
     if ((unsigned)tab[to >> c.plog] >= (unsigned)c.pages) continue;   // a slot on no page of the cache
     const int64_t d = at(to), s = at(from);
@@ -354,16 +546,34 @@ hipError_t launch_cache_append(int dtype, const CacheAppendArgs &a, hipStream_t 
   return a.c.hd == 128 ? append<float, 128>(a, s) : append<float, 64>(a, s);
 }
 
-static int evict_moves(const CacheArgs &c, int keep) { return std::max(0, std::min(keep, c.cap - keep)); }
+// Moves and parts of a launch over these bounds. One block per (sequence, kv head) for up to 4,096 slots, and where
+// there are enough of them to fill the compute units.
+static void evict_plan(CacheEvictArgs &a) {
+  a.moves = std::max(0, std::min(a.keep, a.c.cap - a.keep));
+  a.parts = a.c.cap <= 4096 || a.moves == 0 || a.c.batch * a.c.kvh >= 256 ? 1 : EVP;
+  a.low = a.parts == 1 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(EVP - 1, (int64_t)EVP * a.keep / std::max(1, a.c.cap)));
+}
 
 size_t cache_evict_scratch(const CacheArgs &c, int keep) {
-  return (size_t)c.batch * c.kvh * (1 + 2 * (size_t)evict_moves(c, keep)) * sizeof(int32_t);
+  CacheEvictArgs a{};
+  a.c = c;
+  a.keep = keep;
+  evict_plan(a);
+  return (size_t)c.batch * c.kvh * (size_t)evict_words(a.moves, a.parts) * sizeof(int32_t);
 }
 
 hipError_t launch_cache_evict(int dtype, const CacheEvictArgs &in, hipStream_t s) {
   CacheEvictArgs a = in;
-  a.moves = evict_moves(a.c, a.keep);
-  hipLaunchKernelGGL(k_evict_select, dim3(a.c.kvh, a.c.batch), dim3(EVT), 0, s, a);
+  evict_plan(a);
+  const dim3 sel(a.parts, a.c.kvh, a.c.batch);
+  if (a.parts == 1) {
+    hipLaunchKernelGGL((k_evict_select<-1>), sel, dim3(EVT), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((k_evict_select<0>), sel, dim3(EVT), 0, s, a);
+    hipLaunchKernelGGL((k_evict_select<1>), sel, dim3(EVT), 0, s, a);
+    hipLaunchKernelGGL((k_evict_select<2>), sel, dim3(EVT), 0, s, a);
+    hipLaunchKernelGGL((k_evict_select<3>), sel, dim3(EVT), 0, s, a);
+  }
   const int rb = a.c.hd * (dtype == 1 ? 2 : 4), rpb = 256 / (rb / 16);
   const int per = std::max(1, 2048 / std::max(1, a.c.kvh * a.c.batch));
   const dim3 grid(std::max(1, std::min((a.moves + rpb - 1) / rpb, per)), a.c.kvh, a.c.batch);

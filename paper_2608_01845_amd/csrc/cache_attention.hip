@@ -9,6 +9,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 namespace wdc {
@@ -82,6 +83,27 @@ __device__ __forceinline__ CacheSeq uniform_seq(const CacheArgs &a, int b) {
   return s;
 }
 
+// Query rows of a block and its key range. The keys that the block's last row
+// sees are cut into ranges of a.range keys, one block each; a block that has none is not needed
+// (the first range always is: it writes zeros where nothing is seen).
+struct Range {
+  int lim_lo, lim_hi;   // keys seen by the first and the last row
+  int nr;               // ranges of this row block
+  __device__ __forceinline__ Range(const CacheAttnArgs &a, const CacheSeq &s, int group, int m0, int count) {
+    lim_lo = cache_limit(a.c, s, m0 / group);
+    lim_hi = cache_limit(a.c, s, (min(m0 + a.rpb, count) - 1) / group);
+    nr = a.splits > 1 ? max(1, (lim_hi + a.range - 1) / a.range) : 1;
+  }
+};
+// Part of range sp of packed row `row` and a head: HD unnormalised values at
+// part + slot * HD, its reference and sum at part + slots * HD + 2 slot
+__device__ __forceinline__ int64_t part_slot(const CacheAttnArgs &a, int sp, int row, int head) {
+  return ((int64_t)sp * a.c.rows + row) * a.c.heads + head;
+}
+__device__ __forceinline__ float *part_ml(const CacheAttnArgs &a, int64_t slot) {
+  return a.part + (int64_t)a.splits * a.c.rows * a.c.heads * a.c.hd + 2 * slot;
+}
+
 // Block of a launch over (sequence, kv head) x per blocks each. With the XCD order
 // the blocks of one (sequence, kv head) share an XCD, and so its K and V in that L2.
 __device__ __forceinline__ void cache_block(const CacheArgs &c, int per, int &bh, int &li) {
@@ -151,9 +173,10 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mlast = min(m0 + 16 * RT, count) - 1;
-  const int lim_lo = cache_limit(c, s, m0 / group), lim_hi = cache_limit(c, s, mlast / group);
-  const int tiles = (lim_hi + 31) / 32;
-  const int t0 = (int)((int64_t)sp * tiles / a.splits), t1 = (int)((int64_t)(sp + 1) * tiles / a.splits);
+  const Range rg(a, s, group, m0, count);
+  if (sp >= rg.nr) return;
+  const int lim_lo = rg.lim_lo, tiles = (rg.lim_hi + 31) / 32;
+  const int t0 = rg.nr > 1 ? sp * (a.range / 32) : 0, t1 = rg.nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
 
   const float sc = LOG2E / sqrtf((float)HD);
   bf16x8 qf[RT][NC];
@@ -353,18 +376,14 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) x[d] += wt * y[d];
     }
-    if (a.splits > 1) {
-      const int64_t at = ((int64_t)bh * a.splits + sp) * (c.max_q * group) + mr;
+    const int i = mr / group, head = h * group + mr % group;
+    if (rg.nr > 1) {
+      const int64_t at = part_slot(a, sp, s.q0 + i, head);
       *(f32x4 *)(a.part + at * HD + 4 * e) = x;
-      if (e == 0) {
-        float *pm = a.part + (int64_t)c.batch * c.kvh * a.splits * (c.max_q * group) * HD + 2 * at;
-        pm[0] = mx;
-        pm[1] = den;
-      }
+      if (e == 0) *(float2 *)part_ml(a, at) = make_float2(mx, den);
       continue;
     }
-    const float inv = den > 0.f ? 1.f / den : den != den ? den : 0.f;
-    const int i = mr / group, head = h * group + mr % group;
+    const float inv = 1.f / den;
     bf16x4 y;
 #pragma unroll
     for (int d = 0; d < 4; ++d) y[d] = (__bf16)(den == 0.f ? 0.f : x[d] * inv);
@@ -481,9 +500,10 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool grp_a = wid < 4;
   const int mlast = min(m0 + 256, count) - 1;
-  const int lim_lo = cache_limit(c, s, m0 / group), lim_hi = cache_limit(c, s, mlast / group);
-  const int tiles = (lim_hi + KV - 1) / KV;
-  const int t_first = (int)((int64_t)sp * tiles / a.splits), t_end = (int)((int64_t)(sp + 1) * tiles / a.splits);
+  const Range rg(a, s, group, m0, count);
+  if (sp >= rg.nr) return;
+  const int lim_lo = rg.lim_lo, tiles = (rg.lim_hi + KV - 1) / KV;
+  const int t_first = rg.nr > 1 ? sp * (a.range / KV) : 0, t_end = rg.nr > 1 ? min(t_first + a.range / KV, tiles) : tiles;
   // tiles of the range, relative to t_first: `nf` that every row sees whole, then masked ones
   const int tot = t_end - t_first, nf = min(max(lim_lo / KV - t_first, 0), tot);
 
@@ -770,19 +790,15 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
     const float den = quad_sum(l[t]);
     const int mr = m0 + 32 * wid + 16 * t + lr;
     if (mr >= count) continue;
-    if (a.splits > 1) {
-      const int64_t at = ((int64_t)bh * a.splits + sp) * (c.max_q * group) + mr;
+    const int i0 = mr / group, head = h * group + mr % group;
+    if (rg.nr > 1) {
+      const int64_t at = part_slot(a, sp, s.q0 + i0, head);
 #pragma unroll
       for (int i = 0; i < NI; ++i) *(f32x4 *)(a.part + at * HD + 16 * i + 4 * lg) = o[i][t];
-      if (lg == 0) {
-        float *pm = a.part + (int64_t)c.batch * c.kvh * a.splits * (c.max_q * group) * HD + 2 * at;
-        pm[0] = m[t];
-        pm[1] = den;
-      }
+      if (lg == 0) *(float2 *)part_ml(a, at) = make_float2(m[t], den);
       continue;
     }
     const float inv = 1.f / den;
-    const int i0 = mr / group, head = h * group + mr % group;
     bf16_t *O = (bf16_t *)a.o + (int64_t)(s.q0 + i0) * a.ldo + (int64_t)head * HD + 4 * lg;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -812,16 +828,19 @@ __global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
   const int b = bh / c.kvh, h = bh % c.kvh;
   const CacheSeq s = cache_seq(c, b);
   if (mr >= s.nq * group) return;
-  const int64_t at0 = (int64_t)bh * a.splits * rows + mr;
-  const float *pm = a.part + (int64_t)c.batch * c.kvh * a.splits * rows * HD;
+  const int nr = Range(a, s, group, mr / a.rpb * a.rpb, s.nq * group).nr;
+  if (nr == 1) return;                           // finished by its block
+  const int i = mr / group, head = h * group + mr % group;
+  const int64_t at0 = part_slot(a, 0, s.q0 + i, head), step = (int64_t)c.rows * c.heads;
   float mx = -INFINITY;
-  for (int u = 0; u < a.splits; ++u) mx = fmaxf(mx, pm[2 * (at0 + (int64_t)u * rows)]);
+  for (int u = 0; u < nr; ++u) mx = fmaxf(mx, *part_ml(a, at0 + u * step));
   const float ref = mx == -INFINITY ? 0.f : mx;
   float den = 0.f, x[8] = {};
-  for (int u = 0; u < a.splits; ++u) {
-    const int64_t at = at0 + (int64_t)u * rows;
-    const float wt = __builtin_amdgcn_exp2f(pm[2 * at] - ref);
-    den += wt * pm[2 * at + 1];
+  for (int u = 0; u < nr; ++u) {
+    const int64_t at = at0 + u * step;
+    const float2 ml = *(const float2 *)part_ml(a, at);
+    const float wt = __builtin_amdgcn_exp2f(ml.x - ref);
+    den += wt * ml.y;
     const f32x4 y0 = *(const f32x4 *)(a.part + at * HD + e), y1 = *(const f32x4 *)(a.part + at * HD + e + 4);
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
@@ -829,7 +848,6 @@ __global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
       x[4 + d] += wt * y1[d];
     }
   }
-  const int i = mr / group, head = h * group + mr % group;
   T *O = (T *)a.o + (int64_t)(s.q0 + i) * a.ldo + (int64_t)head * HD + e;
   if constexpr (sizeof(T) == 2) {
     bf16x8 y;
@@ -871,10 +889,11 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lg = lane >> 5;
   const int mlast = min(m0 + 32, count) - 1, mm = min(m0 + lr, mlast), row = mm / group;
-  const int lim_lo = cache_limit(c, s, m0 / group), lim_hi = cache_limit(c, s, mlast / group);
-  const int lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
-  const int tiles = (lim_hi + 31) / 32;
-  const int t0 = (int)((int64_t)sp * tiles / a.splits), t1 = (int)((int64_t)(sp + 1) * tiles / a.splits);
+  const Range rg(a, s, group, m0, count);
+  if (sp >= rg.nr) return;
+  const int lim_lo = rg.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
+  const int tiles = (rg.lim_hi + 31) / 32;
+  const int t0 = rg.nr > 1 ? sp * (a.range / 32) : 0, t1 = rg.nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
   const int32_t *tab = c.table + (int64_t)b * c.table_ld;
   const float *Q = (const float *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm % group) * HD + 4 * lg;
   const float *K = (const float *)c.k + 4 * lg, *V = (const float *)c.v + NI * lr;
@@ -986,8 +1005,8 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   }
   // wave w finishes entries e = 4 w .. 4 w + 3: NI x 4 consecutive dimensions per lane
   const int head = h * group + mm % group, dim0 = NI * (8 * w + 4 * lg);
-  const int64_t at = ((int64_t)bh * a.splits + sp) * (c.max_q * group) + mm;
-  float *O = a.splits > 1 ? a.part + at * HD + dim0
+  const int64_t at = part_slot(a, sp, s.q0 + row, head);
+  float *O = rg.nr > 1 ? a.part + at * HD + dim0
                           : (float *)a.o + (int64_t)(s.q0 + row) * a.ldo + (int64_t)head * HD + dim0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -996,13 +1015,11 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
       float y = 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u) y += wt[u] * po[u][i * 16 + 4 * w + e][lane];
-      O[NI * e + i] = a.splits > 1 ? y : den == 0.f ? 0.f : y / den;
+      O[NI * e + i] = rg.nr > 1 ? y : den == 0.f ? 0.f : y / den;
     }
   if (w != 0 || lg != 0) return;
-  if (a.splits > 1) {
-    float *pm = a.part + (int64_t)c.batch * c.kvh * a.splits * (c.max_q * group) * HD + 2 * at;
-    pm[0] = mx;
-    pm[1] = den;
+  if (rg.nr > 1) {
+    *(float2 *)part_ml(a, at) = make_float2(mx, den);
   } else if (a.lse) {
     a.lse[(int64_t)(s.q0 + row) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
   }
@@ -1128,14 +1145,34 @@ __global__ __launch_bounds__(256) void k_cache_mass_combine(CacheMassArgs a) {
 int rows_per_block(int dtype, const CacheArgs &c) {
   if (dtype == 0) return 32;
   const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
+  if (getenv("TUNE_RPB")) return atoi(getenv("TUNE_RPB"));
   return m <= 16 ? 16 : m <= 32 ? 32 : m <= 128 ? 64 : 256;
 }
-int64_t attn_blocks(int dtype, const CacheArgs &c) {
-  const int rpb = rows_per_block(dtype, c);
+// blocks of one range of keys
+int64_t attn_blocks(int rpb, const CacheArgs &c) {
   return (int64_t)c.batch * c.kvh * (((int64_t)c.max_q * (c.heads / c.kvh) + rpb - 1) / rpb);
 }
 size_t attn_part_bytes(const CacheArgs &c, int splits) {
-  return (size_t)c.batch * c.kvh * splits * c.max_q * (c.heads / c.kvh) * (c.hd + 2) * sizeof(float);
+  return (size_t)splits * c.rows * c.heads * (c.hd + 2) * sizeof(float);
+}
+// Rows per block and key ranges. Lengths are known on the device only; the host
+// has their bounds. Few blocks are given more ranges until they fill the compute
+// units; with several sequences of unlike length twice as many, so that a long one is not left to run alone.
+void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *range, int *splits) {
+  const int group = c.heads / c.kvh;
+  *rpb = rows_per_block(dtype, c);
+  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(attn_blocks(*rpb, c),
+                                                                c.kvh * ((int64_t)c.rows * group / *rpb + c.batch)));
+  const int64_t want = std::max<int64_t>(1, (int64_t)device_cus() * (c.batch > 1 ? 2 : 1) / blocks);
+  int64_t r = std::max<int64_t>(256, (c.cap + want - 1) / want);
+  if (getenv("TUNE_RANGE")) r = atoi(getenv("TUNE_RANGE"));
+  *range = (int)((r + 63) / 64 * 64);
+  *splits = (c.cap + *range - 1) / *range;
+  while (*splits > 1 && attn_part_bytes(c, *splits) > scratch) {
+    *range = (int)std::min<int64_t>((int64_t)*range * 2, 1 << 30);
+    *splits = (c.cap + *range - 1) / *range;
+  }
+  if (*splits < 1) *splits = 1;
 }
 
 template <int HD, int RT>
@@ -1146,7 +1183,7 @@ hipError_t launch_few(const CacheAttnArgs &a, hipStream_t s) {
     return hipFuncSetAttribute((const void *)k_cache_attn_few<HD, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(1, a.c) * a.splits)), dim3(256), LDS, s, a);
+  hipLaunchKernelGGL((k_cache_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD, bool SMALL>
@@ -1157,44 +1194,34 @@ hipError_t launch_many(const CacheAttnArgs &a, hipStream_t s) {
     return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL>), dim3((unsigned)(attn_blocks(1, a.c) * a.splits)), dim3(512), LDS, s, a);
+  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(512), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD>
 hipError_t launch_bf16(const CacheAttnArgs &a, hipStream_t s) {
-  const int rpb = rows_per_block(1, a.c);
+  const int rpb = a.rpb;
   if (rpb == 256) return a.c.plog < 6 ? launch_many<HD, true>(a, s) : launch_many<HD, false>(a, s);
   return rpb == 16 ? launch_few<HD, 1>(a, s) : rpb == 32 ? launch_few<HD, 2>(a, s) : launch_few<HD, 4>(a, s);
 }
 
 }  // namespace
 
-// Ranges of at least 256 keys, as many as fill the compute units once
-static int wanted_splits(int dtype, const CacheArgs &c) {
-  const int cus = device_cus();
-  const int64_t blocks = std::max<int64_t>(1, attn_blocks(dtype, c));
-  const int64_t fill = cus / blocks, most = ((int64_t)c.cap + 255) / 256;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(fill, most), 64));
-}
-int cache_attn_splits(int dtype, const CacheArgs &c, size_t scratch) {
-  int s = wanted_splits(dtype, c);
-  while (s > 1 && attn_part_bytes(c, s) > scratch) --s;
-  return s;
-}
 size_t cache_attn_scratch(int dtype, const CacheArgs &c) {
-  const int s = wanted_splits(dtype, c);
-  return s > 1 ? attn_part_bytes(c, s) : 0;
+  int rpb, range, splits;
+  attn_plan(dtype, c, ~(size_t)0, &rpb, &range, &splits);
+  return splits > 1 ? attn_part_bytes(c, splits) : 0;
 }
 
 hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_t s) {
   CacheAttnArgs a = in;
   a.c.xcd_order = a.c.batch * a.c.kvh % 8 == 0 ? 1 : 0;
-  if (attn_blocks(dtype, a.c) <= 0) return hipSuccess;
+  attn_plan(dtype, a.c, a.part ? a.part_bytes : 0, &a.rpb, &a.range, &a.splits);
+  if (attn_blocks(a.rpb, a.c) <= 0) return hipSuccess;
   hipError_t e;
   if (dtype == 1) {
     e = a.c.hd == 128 ? launch_bf16<128>(a, s) : launch_bf16<64>(a, s);
   } else {
-    const dim3 grid((unsigned)(attn_blocks(0, a.c) * a.splits));
+    const dim3 grid((unsigned)(attn_blocks(a.rpb, a.c) * a.splits));
     if (a.c.hd == 128)
       hipLaunchKernelGGL((k_cache_attn_f32<128>), grid, dim3(256), 0, s, a);
     else

@@ -246,11 +246,13 @@ struct CacheAttnArgs {
   void *o;
   int64_t ldo;
   float *lse;               // [rows, heads] or null
-  float *part;              // key-range parts of a split launch
-  int splits;
+  float *part;              // scratch (part_bytes) for key ranges, or null
+  size_t part_bytes;
+  // set by launch_cache_attention: rows per block; keys per range (a multiple of
+  // 64) and the most ranges of a row block, 1 = not split
+  int rpb, range, splits;
 };
-// Key ranges a launch over these bounds is split into, and the scratch bytes they need
-int cache_attn_splits(int dtype, const CacheArgs &c, size_t scratch);
+// scratch bytes that let a launch over these bounds split its keys as it would like to
 size_t cache_attn_scratch(int dtype, const CacheArgs &c);
 hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &a, hipStream_t s);
 
@@ -275,8 +277,10 @@ struct CacheEvictArgs {
   float *out;               // may be mass
   int32_t *len_out, *index; // index may be null
   int keep, sink, recent;
-  int32_t *list;            // scratch: per (sequence, kv head) a count, then moves (to, from)
-  int moves;                // most moves of a (sequence, kv head)
+  int32_t *list;            // scratch, see evict_layout
+  // set by launch_cache_evict: most moves of a (sequence, kv head); parts its
+  // slots are cut into, the first `low` of them below keep (1 part: one block does all)
+  int moves, parts, low;
 };
 size_t cache_evict_scratch(const CacheArgs &c, int keep);
 hipError_t launch_cache_evict(int dtype, const CacheEvictArgs &a, hipStream_t s);

@@ -1699,7 +1699,8 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
   while ((1 << plog) < p->page) ++plog;
   const int64_t cap = std::min<int64_t>(q->max_kv, (int64_t)q->table_ld << plog);
   const int64_t nrows = rows ? q->rows : 0, max_q = rows ? std::min(q->max_q, q->rows) : 0, heads = (int64_t)q->batch * p->kv_heads;
-  if (heads > 65535 || nrows * c->H > kCacheRows || max_q * q->batch * c->H > kCacheRows || heads * cap > kCacheKeys) {
+  if (heads > 65535 || nrows * c->H > kCacheRows || max_q * q->batch * c->H > kCacheRows || heads * cap > kCacheKeys ||
+      ((int64_t)p->pages * p->kv_heads << plog) > 0x7fffffff) {
     set_err(c, "cache call too large: %d sequences, %d kv heads, %lld rows, %lld keys", q->batch, p->kv_heads,
             (long long)nrows, (long long)cap);
     return WDC_E_SHAPE;
@@ -1812,7 +1813,7 @@ wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const
   a.ldo = ldo;
   a.lse = d_lse;
   a.part = (float *)d_scratch;
-  a.splits = cache_attn_splits(ctx->d.dtype, a.c, d_scratch ? scratch_bytes : 0);
+  a.part_bytes = d_scratch ? scratch_bytes : 0;
   HIPCHK(ctx, launch_cache_attention(ctx->d.dtype, a, ctx->stream));
   return WDC_OK;
 }

@@ -309,6 +309,11 @@ EVICT = [
     ("f32", 3, 64, 16, [100, 200], 64, 0, 33, "ties"),
     ("f32", 1, 128, 128, [900], 899, 1, 1, "random"),
     ("bf16", 1, 64, 64, [70000], 40000, 1000, 2000, "random"),
+    ("bf16", 2, 64, 16, [6000, 200, 4501, 0], 4500, 1000, 3500, "random"),
+    ("bf16", 2, 64, 32, [9000, 4000, 5000], 4200, 100, 200, "odd"),
+    ("f32", 1, 64, 64, [9000], 17, 5, 6, "ties"),
+    ("bf16", 1, 128, 256, [9000, 8999], 8990, 0, 0, "equal"),
+    ("bf16", 64, 64, 64, [4200] * 4, 4000, 10, 20, "ties"),
 ]
 
 
