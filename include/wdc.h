@@ -342,8 +342,8 @@ typedef struct {
  * values beyond them (or beyond the table's pages) are cut to them: rows past max_q of a chunk are
  * left out, keys past max_kv are not there. A slot whose table entry is not a page of the cache is read
  * as one of its pages and never written. Rows of no chunk are not written. batch * max_q * heads <= 2^26,
- * batch * kv_heads * (keys) <= 2^29, batch * kv_heads <= 65535 and pages * kv_heads * page < 2^31, else
- * WDC_E_SHAPE. */
+ * batch * kv_heads * (keys) <= 2^29, batch * kv_heads <= 65535, pages * kv_heads * page < 2^31 and row strides
+ * <= 2^22 elements, else WDC_E_SHAPE. */
 typedef struct {
   const int32_t *d_q_start, *d_kv_len, *d_table;
   int32_t batch, table_ld;

@@ -213,7 +213,7 @@ class PagedCache:
                              "[pages, kv_heads, page, head_dim]")
         if not (k.is_contiguous() and v.is_contiguous()):
             raise ValueError("k and v must be contiguous")
-        self.k, self.v = k, v
+        self.k, self.v, self.kv_heads, self.device = k, v, k.shape[1], k.get_device()
         self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], 0)
         self.ref = C.byref(self.desc)
 
@@ -231,6 +231,7 @@ class Chunks:
         if q_start.numel() != kv_len.numel() + 1 or table.shape[0] != kv_len.numel():
             raise ValueError("q_start [batch + 1], kv_len [batch] and table [batch, pages] disagree on the batch")
         self.q_start, self.kv_len, self.table = q_start, kv_len, table
+        self.rows, self.batch, self.device = rows, kv_len.numel(), kv_len.get_device()
         self.desc = ChunksDesc(q_start.data_ptr(), kv_len.data_ptr(), table.data_ptr(), kv_len.numel(), table.shape[1],
                                rows, rows if max_q is None else max_q, 0x7fffffff if max_kv is None else max_kv, 0)
         self.ref = C.byref(self.desc)
@@ -386,81 +387,72 @@ class Context:
         return out
 
     # ---------------------------------------------------------------- paged key/value cache
-    def _cache_check(self, cache, chunks, **tensors):
-        """Devices, types and shapes of a cache call: name=(tensor, dtype, shape); None in a shape: any length."""
-        if cache.k.dtype != self.tdtype or cache.k.shape[3] != self.cfg.head_dim:
+    def _cache_check(self, cache, chunks):
+        if cache.k.dtype is not self.tdtype or cache.k.shape[3] != self.cfg.head_dim:
             raise ValueError(f"cache of {cache.k.dtype}, head size {cache.k.shape[3]}: the context has {self.tdtype}, "
                              f"{self.cfg.head_dim}")
-        dev = cache.k.device
-        if dev != self.device and (self.device.index is not None or dev.type != self.device.type) or (
-                chunks.kv_len.device != dev):
+        if cache.device != chunks.device or cache.device != (
+                self.stream.device_index if self.device.index is None else self.device.index):
             raise ValueError(f"cache or chunks not on {self.device}")
-        for name, (t, dtype, shape) in tensors.items():
-            if t is None:
-                continue
-            if t.dtype != dtype or t.device != dev or t.dim() != len(shape) or any(
-                    n is not None and n != m for n, m in zip(shape, t.shape)):
-                raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, expected {shape} {dtype} on {dev}")
-            if t.stride(-1) != 1 if name in ("qkv", "q", "out") and t.dim() == 2 else not t.is_contiguous():
-                raise ValueError(f"{name}: unsupported strides {t.stride()}")
+
+    def _tensor(self, name, t, dtype, shape, device, strided=False):
+        """Pointer of an argument of this type, shape and device (an index); strided: rows may be apart."""
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+            raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, expected {shape} {dtype} on cuda:{device}")
+        if not t.is_contiguous() and not (strided and t.stride(1) == 1):
+            raise ValueError(f"{name}: unsupported strides {t.stride()}")
+        return t.data_ptr()
 
     def _scratch(self, nbytes: int):
         """Device memory that lives as long as the work just enqueued on this context's stream."""
         torch = _torch()
-        if not nbytes:
-            return None
         if torch.cuda.current_stream(self.device) == self.stream:
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
-    def _cache_call(self, fn, *args):
-        torch = _torch()
-        if torch.cuda.current_device() == self.device.index:
-            self._check(fn(self.h, *args))
-        else:
-            with torch.cuda.device(self.device):
-                self._check(fn(self.h, *args))
-
     def cache_append(self, cache: PagedCache, chunks: Chunks, qkv, q, pos=None, q_weight=None, k_weight=None):
         """Normalise and rotate q and k of qkv [rows, (heads + 2 kv_heads) head_dim], store k and v in the
         cache and write q [rows, heads head_dim]. Rows may be strided."""
         torch = _torch()
-        hd, kvh, rows = self.cfg.head_dim, cache.k.shape[1], chunks.desc.rows
-        self._cache_check(cache, chunks, qkv=(qkv, self.tdtype, (rows, (self.cfg.heads + 2 * kvh) * hd)),
-                          q=(q, self.tdtype, (rows, self.cfg.heads * hd)), pos=(pos, torch.int32, (rows, 3)),
-                          q_weight=(q_weight, torch.float32, (hd,)), k_weight=(k_weight, torch.float32, (hd,)))
-        self._cache_call(self.lib.wdc_cache_append, cache.ref, chunks.ref, _ptr(qkv), _ld(qkv), _ptr(pos),
-                         _ptr(q_weight), _ptr(k_weight), _ptr(q), _ld(q))
+        self._cache_check(cache, chunks)
+        hd, rows, dev, ptr = self.cfg.head_dim, chunks.rows, cache.device, self._tensor
+        qkv_p = ptr("qkv", qkv, self.tdtype, (rows, (self.cfg.heads + 2 * cache.kv_heads) * hd), dev, True)
+        q_p = ptr("q", q, self.tdtype, (rows, self.cfg.heads * hd), dev, True)
+        pos_p = pos if pos is None else ptr("pos", pos, torch.int32, (rows, 3), dev)
+        qw_p = q_weight if q_weight is None else ptr("q_weight", q_weight, torch.float32, (hd,), dev)
+        kw_p = k_weight if k_weight is None else ptr("k_weight", k_weight, torch.float32, (hd,), dev)
+        self._check(self.lib.wdc_cache_append(self.h, cache.ref, chunks.ref, qkv_p, _ld(qkv), pos_p, qw_p, kw_p, q_p,
+                                              _ld(q)))
         return q
 
     def cache_attention(self, cache: PagedCache, chunks: Chunks, q, out, frame: int = 0, lse=None):
         """Attention of the chunks' rows q [rows, heads head_dim] over the cache into out (same shape);
         lse [rows, heads] float32 takes the rows' log-sum-exp. frame: rows per frame (0: all see all)."""
-        torch = _torch()
-        rows, cols = chunks.desc.rows, self.cfg.heads * self.cfg.head_dim
-        self._cache_check(cache, chunks, q=(q, self.tdtype, (rows, cols)), out=(out, self.tdtype, (rows, cols)),
-                          lse=(lse, torch.float32, (rows, self.cfg.heads)))
-        nbytes = self.lib.wdc_cache_attention_scratch(self.h, cache.ref, chunks.ref)
-        scratch = self._scratch(nbytes)
-        self._cache_call(self.lib.wdc_cache_attention, cache.ref, chunks.ref, _ptr(q), _ld(q), frame, _ptr(out),
-                         _ld(out), _ptr(lse), _ptr(scratch), nbytes)
+        self._cache_check(cache, chunks)
+        shape, dev, ptr = (chunks.rows, self.cfg.heads * self.cfg.head_dim), cache.device, self._tensor
+        q_p, out_p = ptr("q", q, self.tdtype, shape, dev, True), ptr("out", out, self.tdtype, shape, dev, True)
+        lse_p = lse if lse is None else ptr("lse", lse, _torch().float32, (chunks.rows, self.cfg.heads), dev)
+        n = self.lib.wdc_cache_attention_scratch(self.h, cache.ref, chunks.ref)
+        scratch = self._scratch(n) if n else None
+        self._check(self.lib.wdc_cache_attention(self.h, cache.ref, chunks.ref, q_p, _ld(q), frame, out_p, _ld(out), lse_p,
+                                                 _ptr(scratch), n))
         return out
 
     def cache_mass(self, cache: PagedCache, chunks: Chunks, q, lse, mass, frame: int = 0, decay: float = 1.0, out=None):
         """out = decay * mass + the weight each cached key receives from the chunks' rows (out: mass itself
         if not given); mass [pages, kv_heads, page] float32, lse from cache_attention with the same frame."""
-        torch = _torch()
-        rows, shape = chunks.desc.rows, tuple(cache.k.shape[:3])
-        out = mass if out is None else out
-        self._cache_check(cache, chunks, q=(q, self.tdtype, (rows, self.cfg.heads * self.cfg.head_dim)),
-                          lse=(lse, torch.float32, (rows, self.cfg.heads)), mass=(mass, torch.float32, shape),
-                          out=(out, torch.float32, shape))
-        nbytes = self.lib.wdc_cache_mass_scratch(self.h, cache.ref, chunks.ref)
-        scratch = self._scratch(nbytes)
-        self._cache_call(self.lib.wdc_cache_mass, cache.ref, chunks.ref, _ptr(q), _ld(q), frame, _ptr(lse), decay,
-                         _ptr(mass), _ptr(out), _ptr(scratch), nbytes)
-        return out
+        f32, dev, ptr, shape = _torch().float32, cache.device, self._tensor, cache.k.shape[:3]
+        self._cache_check(cache, chunks)
+        q_p = ptr("q", q, self.tdtype, (chunks.rows, self.cfg.heads * self.cfg.head_dim), dev, True)
+        lse_p = ptr("lse", lse, f32, (chunks.rows, self.cfg.heads), dev)
+        mass_p = ptr("mass", mass, f32, shape, dev)
+        out_p = mass_p if out is None else ptr("out", out, f32, shape, dev)
+        n = self.lib.wdc_cache_mass_scratch(self.h, cache.ref, chunks.ref)
+        scratch = self._scratch(n) if n else None
+        self._check(self.lib.wdc_cache_mass(self.h, cache.ref, chunks.ref, q_p, _ld(q), frame, lse_p, decay, mass_p, out_p,
+                                            _ptr(scratch), n))
+        return mass if out is None else out
 
     def cache_evict(self, cache: PagedCache, chunks: Chunks, mass, keep: int, sink: int = 0, recent: int = 0,
                     kv_len_out=None, index=None, out=None):
@@ -468,17 +460,17 @@ class Context:
         largest mass. kv_len_out takes the new lengths (chunks.kv_len itself if not given), out the masses
         (mass itself), index [batch, kv_heads, keep] int32 the former slots."""
         torch = _torch()
-        shape = tuple(cache.k.shape[:3])
+        self._cache_check(cache, chunks)
+        dev, ptr, shape, batch = cache.device, self._tensor, cache.k.shape[:3], chunks.batch
         kv_len_out = chunks.kv_len if kv_len_out is None else kv_len_out
-        out = mass if out is None else out
-        batch = chunks.kv_len.numel()
-        self._cache_check(cache, chunks, mass=(mass, torch.float32, shape), out=(out, torch.float32, shape),
-                          kv_len_out=(kv_len_out, torch.int32, (batch,)),
-                          index=(index, torch.int32, (batch, shape[1], keep)))
-        nbytes = self.lib.wdc_cache_evict_scratch(self.h, cache.ref, chunks.ref, keep)
-        scratch = self._scratch(nbytes)
-        self._cache_call(self.lib.wdc_cache_evict, cache.ref, chunks.ref, _ptr(mass), _ptr(out), keep, sink, recent,
-                         _ptr(kv_len_out), _ptr(index), _ptr(scratch), nbytes)
+        mass_p = ptr("mass", mass, torch.float32, shape, dev)
+        out_p = mass_p if out is None else ptr("out", out, torch.float32, shape, dev)
+        len_p = ptr("kv_len_out", kv_len_out, torch.int32, (batch,), dev)
+        idx_p = index if index is None else ptr("index", index, torch.int32, (batch, cache.kv_heads, keep), dev)
+        n = self.lib.wdc_cache_evict_scratch(self.h, cache.ref, chunks.ref, keep)
+        scratch = self._scratch(n) if n else None
+        self._check(self.lib.wdc_cache_evict(self.h, cache.ref, chunks.ref, mass_p, out_p, keep, sink, recent, len_p, idx_p,
+                                             _ptr(scratch), n))
         return kv_len_out
 
     def set_timing(self, on: bool):

@@ -25,6 +25,9 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 __device__ __forceinline__ void lds_load16(__amdgpu_buffer_rsrc_t r, char *lds, int voff, int soff) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)lds, 16, voff, soff, 0, 0);
 }
+__device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, char *lds, int voff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)lds, 4, voff, 0, 0, 0);
+}
 // Four rows of 16 columns of 2 bytes, each read as 4 x 8 bytes by the lanes of a
 // group of 16 in row order, come back transposed: lane c of the group gets column c.
 __device__ __forceinline__ s16x4 lds_read_tr(const char *p) {
@@ -1045,14 +1048,139 @@ __device__ __forceinline__ void mass_store(const CacheMassArgs &a, const CacheSe
   a.out[at] = (key < s.start && a.decay != 0.f ? a.decay * a.mass[at] : 0.f) + sum;
 }
 
-// Four waves share KT keys and take every fourth tile of rows (16 of bf16, 32 of
-// float32). K stays in registers (A operand), rows stream past it as the B operand; a lane
-// holds one row and KT / 4 (float32: 16) keys, whose sums stay in its registers until the end.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_cache_mass(CacheMassArgs a) {
-  constexpr bool BF = sizeof(T) == 2;
-  constexpr int KT = BF ? 64 : 32, RQ = BF ? 16 : 32, NK = BF ? 4 : 1, NE = BF ? 4 : 16;
-  constexpr int NC = BF ? HD / 32 : HD / 8;
+// Rows of a key tile's launch part: tiles of `step` query rows from the first that sees key0
+struct MassRows {
+  int r0, r1;
+  __device__ __forceinline__ MassRows(const CacheMassArgs &a, const CacheSeq &s, int group, int key0, int step, int sp) {
+    const int lo = first_row(a.c, s, key0) * group / step, hi = (s.nq * group + step - 1) / step;
+    const int span = max(hi - lo, 0);
+    r0 = lo + (int)((int64_t)sp * span / a.splits);
+    r1 = lo + (int)((int64_t)(sp + 1) * span / a.splits);
+  }
+};
+
+// bf16: a block of four waves holds 256 keys, 64 a wave, in registers (A operand)
+// and streams the rows past them, 64 a stage through three LDS slots of direct loads; every wave
+// reads all rows (B operand). A lane holds one row and 16 keys of a tile of 16 x 64 and adds
+// exp2(sc x - lse) to its 16 sums: multiply-add, exponential and sum are 24 cycles for 64 weights
+// beside 16 (hd 128) of matrix work, so the vector units bound it.
+constexpr int MKT = 256, MST = 64, MNB = 3;
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
+  using F = Few<HD>;
+  constexpr int NC = HD / 32, NL = MST / (4 * F::RPL);   // loads of a wave per stage (4 or 2)
+  constexpr int QB = MST * F::ROWB;
+  __shared__ __attribute__((aligned(16))) char qs[MNB * QB];
+  __shared__ __attribute__((aligned(16))) float zs[MNB][4][MST];
+  const CacheArgs &c = a.c;
+  const int group = c.heads / c.kvh, nkt = (c.cap + MKT - 1) / MKT;
+  int bh, li;
+  cache_block(c, nkt * a.splits, bh, li);
+  const int sp = li % a.splits, kt = li / a.splits, b = bh / c.kvh, h = bh % c.kvh;
+  const CacheSeq s = uniform_seq(c, b);
+  const int key0 = kt * MKT;
+  if (key0 >= s.n) return;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int count = s.nq * group, kw = key0 + 64 * w;
+  const MassRows rows(a, s, group, key0, MST, sp);
+  const int32_t *tab = c.table + (int64_t)b * c.table_ld;
+  bf16x8 kf[4][NC];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const bf16_t *p = (const bf16_t *)c.k + slot_row(c, tab, h, min(kw + 16 * k + lr, s.n - 1)) + 8 * lg;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) kf[k][j] = *(const bf16x8 *)(p + 32 * j);
+  }
+  // stage r into slot j: row 64 r + m of the stage; rows past the last are read as the last
+  auto load = [&](int r, int j) {
+    const int i0 = r * MST / group;              // the stage's first chunk row: offsets from it stay below 2^31
+    const char *q = (const char *)a.q + ((int64_t)(s.q0 + i0) * a.ldq + (int64_t)h * group * HD) * 2;
+    const float *z = a.lse + (int64_t)(s.q0 + i0) * c.heads + h * group;
+    const __amdgpu_buffer_rsrc_t qd = __builtin_amdgcn_make_buffer_rsrc((void *)q, (short)0, 0x7fffffff, RSRC_WORD3);
+    const __amdgpu_buffer_rsrc_t zd = __builtin_amdgcn_make_buffer_rsrc((void *)z, (short)0, 0x7fffffff, RSRC_WORD3);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int x = (4 * i + w) * F::RPL + lane / (HD / 8), m = min(r * MST + x, count - 1);
+      const int row = m / group, ch = lane % (HD / 8);
+      lds_load16(qd, qs + j * QB + (4 * i + w) * 1024,
+                 (int)((row - i0) * a.ldq + (m - row * group) * HD) * 2 + (ch ^ F::kkey(x)) * 16, 0);
+    }
+    const int m = min(r * MST + lane, count - 1), row = m / group;
+    lds_load4(zd, (char *)zs[j][w], ((row - i0) * c.heads + m - row * group) * 4);
+  };
+  int qro[NC];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) qro[j] = lr * F::ROWB + ((4 * j + lg) ^ F::kkey(lr)) * 16;
+  const float sc = LOG2E / sqrtf((float)HD);
+  float sum[4][4] = {};
+  const int n = rows.r1 - rows.r0;
+  if (n > 0) load(rows.r0, 0);
+  if (n > 1) load(rows.r0 + 1, 1);
+  for (int t = 0; t < n; ++t) {
+    const int r = rows.r0 + t, j = t % MNB;
+    if (t + 1 < n)
+      wait_vm<NL + 1>();
+    else
+      wait_vm<0>();
+    asm volatile("s_barrier" ::: "memory");      // slot j is there, and the slot of stage t - 1 has been read
+    if (t + 2 < n) load(r + 2, (t + 2) % MNB);
+    // the stage's first row sees the fewest keys
+    const bool part = r * MST + MST > count || kw + 64 > cache_limit(c, s, r * MST / group);
+    const char *qb = qs + j * QB;
+    const float *zb = zs[j][w];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      bf16x8 qf[NC];
+#pragma unroll
+      for (int jj = 0; jj < NC; ++jj) qf[jj] = *(const bf16x8 *)(qb + q * 16 * F::ROWB + qro[jj]);
+      const float z = zb[16 * q + lr] * LOG2E;
+      f32x4 x[4];
+#pragma unroll
+      for (int jj = 0; jj < NC; ++jj)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          x[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][jj], qf[jj], jj == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x[k], 0, 0, 0);
+      if (part) {
+        const int m = r * MST + 16 * q + lr, lim = m < count ? cache_limit(c, s, m / group) : 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][e], sc, -z));
+            sum[k][e] += kw + 16 * k + 4 * lg + e < lim ? p : 0.f;
+          }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[k][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][e], sc, -z));
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): this wave's reads of the slot are done
+  }
+  // lane lr < 16 of each lane group: key 16 k + 4 lg + e with k = lr / 4, e = lr % 4
+  float mine = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float v = group_sum<16>(sum[k][e]);
+      if (lr == 4 * k + e) mine = v;
+    }
+  const int key = kw + 16 * (lr >> 2) + 4 * lg + (lr & 3);
+  if (key >= s.n) return;
+  if (a.splits > 1)
+    a.part[((int64_t)bh * a.splits + sp) * c.cap + key] = mine;
+  else
+    mass_store(a, s, b, h, key, mine);
+}
+
+// float32: four waves share 32 keys, held in registers, and take every fourth
+// tile of 32 rows, read straight from the caches: bound by the matrix instructions.
+template <int HD>
+__global__ __launch_bounds__(256) void k_cache_mass_f32(CacheMassArgs a) {
+  constexpr int KT = 32, NC = HD / 8;
   const CacheArgs &c = a.c;
   const int group = c.heads / c.kvh, nkt = (c.cap + KT - 1) / KT;
   int bh, li;
@@ -1062,65 +1190,44 @@ __global__ __launch_bounds__(256) void k_cache_mass(CacheMassArgs a) {
   const int key0 = kt * KT;
   if (key0 >= s.n) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane % RQ, lg = lane / RQ;
+  const int lr = lane & 31, lg = lane >> 5, count = s.nq * group;
+  const MassRows rows(a, s, group, key0, 32, sp);
   const int32_t *tab = c.table + (int64_t)b * c.table_ld;
-  const int count = s.nq * group;
-  const int r_lo = first_row(c, s, key0) * group / RQ, r_hi = (count + RQ - 1) / RQ;
-  const int span = max(r_hi - r_lo, 0);
-  const int r0 = r_lo + (int)((int64_t)sp * span / a.splits), r1 = r_lo + (int)((int64_t)(sp + 1) * span / a.splits);
-  typedef typename std::conditional<BF, bf16x8, f32x4>::type frag;
-  typedef typename std::conditional<BF, f32x4, f32x16>::type acc;
-  constexpr int STEP = BF ? 32 : 8, PER = BF ? 8 : 4;   // elements of a row per fragment: of the wave, of a lane
-  frag kf[NK][NC];
+  f32x4 kf[NC];
+  {
+    const float *p = (const float *)c.k + slot_row(c, tab, h, min(key0 + lr, s.n - 1)) + 4 * lg;
 #pragma unroll
-  for (int k = 0; k < NK; ++k) {
-    const T *p = (const T *)c.k + slot_row(c, tab, h, min(key0 + RQ * k + lr, s.n - 1)) + PER * lg;
-#pragma unroll
-    for (int j = 0; j < NC; ++j) kf[k][j] = *(const frag *)(p + STEP * j);
+    for (int j = 0; j < NC; ++j) kf[j] = *(const f32x4 *)(p + 8 * j);
   }
   const float sc = LOG2E / sqrtf((float)HD);
-  float sum[NK][NE] = {};
-  for (int r = r0 + w; r < r1; r += 4) {
-    const int m = r * RQ + lr, mm = min(m, count - 1), i = mm / group, head = h * group + mm % group;
-    const T *Q = (const T *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)head * HD + PER * lg;
-    const float lse = a.lse[(int64_t)(s.q0 + i) * c.heads + head] * LOG2E;
+  float sum[16] = {};
+  for (int r = rows.r0 + w; r < rows.r1; r += 4) {
+    const int m = r * 32 + lr, mm = min(m, count - 1), i = mm / group, head = h * group + mm % group;
+    const float *Q = (const float *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)head * HD + 4 * lg;
+    const float z = a.lse[(int64_t)(s.q0 + i) * c.heads + head] * LOG2E;
     const int lim = m < count ? cache_limit(c, s, i) : 0;
-    frag qf[NC];
+    f32x16 x;
 #pragma unroll
-    for (int j = 0; j < NC; ++j) qf[j] = *(const frag *)(Q + STEP * j);
-    const bool part = __any(key0 + KT > lim);
+    for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
-    for (int k = 0; k < NK; ++k) {
-      acc x;
+    for (int j = 0; j < NC; ++j) {
+      const f32x4 qf = *(const f32x4 *)(Q + 8 * j);
 #pragma unroll
-      for (int e = 0; e < NE; ++e) x[e] = 0.f;
+      for (int d = 0; d < 4; ++d) x = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j][d], qf[d], x, 0, 0, 0);
+    }
 #pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        if constexpr (BF) {
-          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][j], qf[j], x, 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int d = 0; d < 4; ++d) x = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[k][j][d], qf[j][d], x, 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        const int key = key0 + (BF ? 16 * k + 4 * lg + e : 8 * (e / 4) + 4 * lg + e % 4);
-        float p = BF ? __builtin_amdgcn_exp2f(x[e] * sc - lse) : exp2f(x[e] * sc - lse);
-        if (part && key >= lim) p = 0.f;
-        sum[k][e] += p;
-      }
+    for (int e = 0; e < 16; ++e) {
+      const float p = exp2f(x[e] * sc - z);
+      sum[e] += key0 + 8 * (e / 4) + 4 * lg + e % 4 < lim ? p : 0.f;
     }
   }
   __shared__ float ws[4][KT];
 #pragma unroll
-  for (int k = 0; k < NK; ++k)
-#pragma unroll
-    for (int e = 0; e < NE; ++e) {
-      float v = group_sum<16>(sum[k][e]);
-      if (!BF) v += __shfl_xor(v, 16, 64);
-      if (lr == 0) ws[w][BF ? 16 * k + 4 * lg + e : 8 * (e / 4) + 4 * lg + e % 4] = v;
-    }
+  for (int e = 0; e < 16; ++e) {
+    float v = group_sum<16>(sum[e]);
+    v += __shfl_xor(v, 16, 64);
+    if (lr == 0) ws[w][8 * (e / 4) + 4 * lg + e % 4] = v;
+  }
   __syncthreads();
   if (tid >= KT || key0 + tid >= s.n) return;
   const float total = ws[0][tid] + ws[1][tid] + ws[2][tid] + ws[3][tid];
@@ -1246,7 +1353,7 @@ hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_
 }
 
 static int64_t mass_blocks(int dtype, const CacheArgs &c) {
-  const int kt = dtype == 1 ? 64 : 32;
+  const int kt = dtype == 1 ? MKT : 32;
   return (int64_t)c.batch * c.kvh * (((int64_t)c.cap + kt - 1) / kt);
 }
 static size_t mass_part_bytes(const CacheArgs &c, int splits) {
@@ -1276,14 +1383,14 @@ hipError_t launch_cache_mass(int dtype, const CacheMassArgs &in, hipStream_t s) 
   const dim3 grid((unsigned)(blocks * a.splits));
   if (dtype == 1) {
     if (a.c.hd == 128)
-      hipLaunchKernelGGL((k_cache_mass<bf16_t, 128>), grid, dim3(256), 0, s, a);
+      hipLaunchKernelGGL((k_cache_mass_bf16<128>), grid, dim3(256), 0, s, a);
     else
-      hipLaunchKernelGGL((k_cache_mass<bf16_t, 64>), grid, dim3(256), 0, s, a);
+      hipLaunchKernelGGL((k_cache_mass_bf16<64>), grid, dim3(256), 0, s, a);
   } else {
     if (a.c.hd == 128)
-      hipLaunchKernelGGL((k_cache_mass<float, 128>), grid, dim3(256), 0, s, a);
+      hipLaunchKernelGGL((k_cache_mass_f32<128>), grid, dim3(256), 0, s, a);
     else
-      hipLaunchKernelGGL((k_cache_mass<float, 64>), grid, dim3(256), 0, s, a);
+      hipLaunchKernelGGL((k_cache_mass_f32<64>), grid, dim3(256), 0, s, a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits <= 1) return e;

@@ -1724,6 +1724,23 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
   return WDC_OK;
 }
 
+// The stream's device while a call launches: its kernels run there whatever device is current
+struct OnStreamDevice {
+  int old = -1;
+  explicit OnStreamDevice(hipStream_t s) {
+    int cur = -1;
+    hipDevice_t dev = -1;
+    if (s && hipGetDevice(&cur) == hipSuccess && hipStreamGetDevice(s, &dev) == hipSuccess && dev != cur &&
+        hipSetDevice(dev) == hipSuccess)
+      old = cur;
+  }
+  ~OnStreamDevice() {
+    if (old >= 0) (void)hipSetDevice(old);
+  }
+  OnStreamDevice(const OnStreamDevice &) = delete;
+  OnStreamDevice &operator=(const OnStreamDevice &) = delete;
+};
+
 // a row-major tensor of the model dtype read and written in 16-byte groups
 wdc_status cache_rows(wdc_ctx *c, const char *what, const void *p, int64_t ld, int64_t cols, int rows) {
   if ((!p && rows > 0) || ld < cols) {
@@ -1733,6 +1750,10 @@ wdc_status cache_rows(wdc_ctx *c, const char *what, const void *p, int64_t ld, i
   if (!aligned16(p) || ld * c->esz % 16) {
     set_err(c, "%s: pointer and row stride must be multiples of 16 bytes", what);
     return WDC_E_ALIGN;
+  }
+  if (ld > (int64_t(1) << 22)) {                 // offsets within a block's rows are 32-bit
+    set_err(c, "%s: row stride %lld above 2^22", what, (long long)ld);
+    return WDC_E_SHAPE;
   }
   return WDC_OK;
 }
@@ -1782,6 +1803,7 @@ wdc_status wdc_cache_append(wdc_ctx *ctx, const wdc_paged_cache *cache, const wd
       a.freq[p++] = std::pow(10000.0, -2.0 * j / dims[ax]) / (2.0 * 3.14159265358979323846);
     a.axis_end[ax] = p;
   }
+  const OnStreamDevice on(ctx->stream);
   HIPCHK(ctx, launch_cache_append(ctx->d.dtype, a, ctx->stream));
   return WDC_OK;
 }
@@ -1814,6 +1836,7 @@ wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const
   a.lse = d_lse;
   a.part = (float *)d_scratch;
   a.part_bytes = d_scratch ? scratch_bytes : 0;
+  const OnStreamDevice on(ctx->stream);
   HIPCHK(ctx, launch_cache_attention(ctx->d.dtype, a, ctx->stream));
   return WDC_OK;
 }
@@ -1847,6 +1870,7 @@ wdc_status wdc_cache_mass(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_
   a.decay = decay;
   a.part = (float *)d_scratch;
   a.splits = cache_mass_splits(ctx->d.dtype, a.c, d_scratch ? scratch_bytes : 0);
+  const OnStreamDevice on(ctx->stream);
   HIPCHK(ctx, launch_cache_mass(ctx->d.dtype, a, ctx->stream));
   return WDC_OK;
 }
@@ -1883,6 +1907,7 @@ wdc_status wdc_cache_evict(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc
   a.len_out = d_kv_len_out;
   a.index = d_index;
   a.list = (int32_t *)d_scratch;
+  const OnStreamDevice on(ctx->stream);
   HIPCHK(ctx, launch_cache_evict(ctx->d.dtype, a, ctx->stream));
   return WDC_OK;
 }
