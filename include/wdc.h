@@ -326,8 +326,8 @@ wdc_status wdc_linear(wdc_ctx *ctx, const void *d_a, int64_t lda, const void *d_
 
 /* Pages of one layer: slot p of page g and kv head h is row (g * kv_heads + h) *
  * page + p of d_k and d_v, [pages, kv_heads, page, head_dim] in the model dtype.
- * page is 16, 32, 64, 128 or 256 (else WDC_E_UNSUPPORTED); kv_heads divides heads:
- * query head i uses kv head i / (heads / kv_heads). */
+ * page is 16, 32, 64, 128 or 256; kv_heads divides heads, which are at most 64
+ * per kv head (else WDC_E_UNSUPPORTED): query head i uses kv head i / (heads / kv_heads). */
 typedef struct {
   void *d_k, *d_v;
   int32_t pages, page, kv_heads;

@@ -93,8 +93,8 @@ struct Range {
   int lim_lo, lim_hi;   // keys seen by the first and the last row
   int nr;               // ranges of this row block
   __device__ __forceinline__ Range(const CacheAttnArgs &a, const CacheSeq &s, int group, int m0, int count) {
-    lim_lo = cache_limit(a.c, s, m0 / group);
-    lim_hi = cache_limit(a.c, s, (min(m0 + a.rpb, count) - 1) / group);
+    lim_lo = cache_limit(a.c, s, cache_row(a.c, m0));
+    lim_hi = cache_limit(a.c, s, cache_row(a.c, min(m0 + a.rpb, count) - 1));
     nr = a.splits > 1 ? max(1, (lim_hi + a.range - 1) / a.range) : 1;
   }
 };
@@ -186,9 +186,9 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   int lim[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int m = m0 + 16 * t + lr, mm = min(m, mlast), i = mm / group;
+    const int m = m0 + 16 * t + lr, mm = min(m, mlast), i = cache_row(c, mm);
     lim[t] = m < count ? cache_limit(c, s, i) : 0;
-    const bf16_t *Q = (const bf16_t *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)(h * group + mm % group) * HD + 8 * lg;
+    const bf16_t *Q = (const bf16_t *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)(h * group + mm - i * group) * HD + 8 * lg;
 #pragma unroll
     for (int j = 0; j < NC; ++j) qf[t][j] = *(const bf16x8 *)(Q + 32 * j);
   }
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) x[d] += wt * y[d];
     }
-    const int i = mr / group, head = h * group + mr % group;
+    const int i = cache_row(c, mr), head = h * group + mr - i * group;
     if (rg.nr > 1) {
       const int64_t at = part_slot(a, sp, s.q0 + i, head);
       *(f32x4 *)(a.part + at * HD + 4 * e) = x;
@@ -514,8 +514,8 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
   bf16x8 qf[2][NC];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int mm = min(m0 + 32 * wid + 16 * t + lr, mlast), i = mm / group;
-    const bf16_t *Q = (const bf16_t *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)(h * group + mm % group) * HD + 8 * lg;
+    const int mm = min(m0 + 32 * wid + 16 * t + lr, mlast), i = cache_row(c, mm);
+    const bf16_t *Q = (const bf16_t *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)(h * group + mm - i * group) * HD + 8 * lg;
 #pragma unroll
     for (int j = 0; j < NC; ++j) qf[t][j] = *(const bf16x8 *)(Q + 32 * j);
   }
@@ -710,7 +710,7 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int mr = m0 + 32 * wid + 16 * t + lr;
-    lim[t] = mr < count ? cache_limit(c, s, mr / group) : 0;
+    lim[t] = mr < count ? cache_limit(c, s, cache_row(c, mr)) : 0;
   }
   for (int u = nf; u < tot; ++u) {
     if (grp_a) wait_vm<0>();
@@ -793,7 +793,7 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
     const float den = quad_sum(l[t]);
     const int mr = m0 + 32 * wid + 16 * t + lr;
     if (mr >= count) continue;
-    const int i0 = mr / group, head = h * group + mr % group;
+    const int i0 = cache_row(c, mr), head = h * group + mr - i0 * group;
     if (rg.nr > 1) {
       const int64_t at = part_slot(a, sp, s.q0 + i0, head);
 #pragma unroll
@@ -833,7 +833,7 @@ __global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
   if (mr >= s.nq * group) return;
   const int nr = Range(a, s, group, mr / a.rpb * a.rpb, s.nq * group).nr;
   if (nr == 1) return;                           // finished by its block
-  const int i = mr / group, head = h * group + mr % group;
+  const int i = cache_row(c, mr), head = h * group + mr - i * group;
   const int64_t at0 = part_slot(a, 0, s.q0 + i, head), step = (int64_t)c.rows * c.heads;
   float mx = -INFINITY;
   for (int u = 0; u < nr; ++u) mx = fmaxf(mx, *part_ml(a, at0 + u * step));
@@ -891,14 +891,14 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   if (m0 >= count) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lg = lane >> 5;
-  const int mlast = min(m0 + 32, count) - 1, mm = min(m0 + lr, mlast), row = mm / group;
+  const int mlast = min(m0 + 32, count) - 1, mm = min(m0 + lr, mlast), row = cache_row(c, mm);
   const Range rg(a, s, group, m0, count);
   if (sp >= rg.nr) return;
   const int lim_lo = rg.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
   const int tiles = (rg.lim_hi + 31) / 32;
   const int t0 = rg.nr > 1 ? sp * (a.range / 32) : 0, t1 = rg.nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
   const int32_t *tab = c.table + (int64_t)b * c.table_ld;
-  const float *Q = (const float *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm % group) * HD + 4 * lg;
+  const float *Q = (const float *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm - row * group) * HD + 4 * lg;
   const float *K = (const float *)c.k + 4 * lg, *V = (const float *)c.v + NI * lr;
   const float sc = LOG2E / sqrtf((float)HD);
   f32x4 qf[NC], kf[NC];
@@ -1007,7 +1007,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
     den += wt[u] * ml[u][1][lr];
   }
   // wave w finishes entries e = 4 w .. 4 w + 3: NI x 4 consecutive dimensions per lane
-  const int head = h * group + mm % group, dim0 = NI * (8 * w + 4 * lg);
+  const int head = h * group + mm - row * group, dim0 = NI * (8 * w + 4 * lg);
   const int64_t at = part_slot(a, sp, s.q0 + row, head);
   float *O = rg.nr > 1 ? a.part + at * HD + dim0
                           : (float *)a.o + (int64_t)(s.q0 + row) * a.ldo + (int64_t)head * HD + dim0;
@@ -1060,15 +1060,16 @@ struct MassRows {
 };
 
 // bf16: a block of four waves holds 256 keys, 64 a wave, in registers (A operand)
-// and streams the rows past them, 64 a stage through three LDS slots of direct loads; every wave
+// and streams the rows past them, 128 a stage through two LDS slots of direct loads; every wave
 // reads all rows (B operand). A lane holds one row and 16 keys of a tile of 16 x 64 and adds
 // exp2(sc x - lse) to its 16 sums: multiply-add, exponential and sum are 24 cycles for 64 weights
 // beside 16 (hd 128) of matrix work, so the vector units bound it.
-constexpr int MKT = 256, MST = 64, MNB = 3;
+constexpr int MKT = 256, MST = 128, MNB = 2;
 template <int HD>
 __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
   using F = Few<HD>;
-  constexpr int NC = HD / 32, NL = MST / (4 * F::RPL);   // loads of a wave per stage (4 or 2)
+  constexpr int NC = HD / 32, NL = MST / (4 * F::RPL);   // loads of a wave per stage (8 or 4)
+  constexpr int NZ = MST / 64, NQ = MST / 16;
   constexpr int QB = MST * F::ROWB;
   __shared__ __attribute__((aligned(16))) char qs[MNB * QB];
   __shared__ __attribute__((aligned(16))) float zs[MNB][4][MST];
@@ -1092,22 +1093,33 @@ __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
 #pragma unroll
     for (int j = 0; j < NC; ++j) kf[k][j] = *(const bf16x8 *)(p + 32 * j);
   }
-  // stage r into slot j: row 64 r + m of the stage; rows past the last are read as the last
+  // Stage r into slot j: its rows lie at fixed offsets from its first chunk row i0
+  // if the group divides 128; for other groups, and for rows past the last (read as the last), they are found per stage.
+  int qo[NL], zo[NZ];
+  auto place = [&](int r, int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int x = (4 * i + w) * F::RPL + lane / (HD / 8), m = min(r * MST + x, count - 1), row = cache_row(c, m);
+      qo[i] = (int)((row - i0) * a.ldq + (m - row * group) * HD) * 2 + ((lane % (HD / 8)) ^ F::kkey(x)) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < NZ; ++i) {
+      const int m = min(r * MST + 64 * i + lane, count - 1), row = cache_row(c, m);
+      zo[i] = ((row - i0) * c.heads + m - row * group) * 4;
+    }
+  };
+  const bool fixed = (group & (group - 1)) == 0;   // group <= 64
   auto load = [&](int r, int j) {
-    const int i0 = r * MST / group;              // the stage's first chunk row: offsets from it stay below 2^31
+    const int i0 = cache_row(c, r * MST);
+    if (!fixed || r * MST + MST > count) place(r, i0);
     const char *q = (const char *)a.q + ((int64_t)(s.q0 + i0) * a.ldq + (int64_t)h * group * HD) * 2;
     const float *z = a.lse + (int64_t)(s.q0 + i0) * c.heads + h * group;
     const __amdgpu_buffer_rsrc_t qd = __builtin_amdgcn_make_buffer_rsrc((void *)q, (short)0, 0x7fffffff, RSRC_WORD3);
     const __amdgpu_buffer_rsrc_t zd = __builtin_amdgcn_make_buffer_rsrc((void *)z, (short)0, 0x7fffffff, RSRC_WORD3);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int x = (4 * i + w) * F::RPL + lane / (HD / 8), m = min(r * MST + x, count - 1);
-      const int row = m / group, ch = lane % (HD / 8);
-      lds_load16(qd, qs + j * QB + (4 * i + w) * 1024,
-                 (int)((row - i0) * a.ldq + (m - row * group) * HD) * 2 + (ch ^ F::kkey(x)) * 16, 0);
-    }
-    const int m = min(r * MST + lane, count - 1), row = m / group;
-    lds_load4(zd, (char *)zs[j][w], ((row - i0) * c.heads + m - row * group) * 4);
+    for (int i = 0; i < NL; ++i) lds_load16(qd, qs + j * QB + (4 * i + w) * 1024, qo[i], 0);
+#pragma unroll
+    for (int i = 0; i < NZ; ++i) lds_load4(zd, (char *)(zs[j][w] + 64 * i), zo[i]);
   };
   int qro[NC];
 #pragma unroll
@@ -1115,48 +1127,64 @@ __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
   const float sc = LOG2E / sqrtf((float)HD);
   float sum[4][4] = {};
   const int n = rows.r1 - rows.r0;
-  if (n > 0) load(rows.r0, 0);
-  if (n > 1) load(rows.r0 + 1, 1);
+  // from this chunk row on, every row sees all of the wave's keys
+  const int whole = first_row(c, s, min(kw + 63, s.n - 1));
+  if (n > 0) {
+    place(rows.r0, cache_row(c, rows.r0 * MST));
+    load(rows.r0, 0);
+  }
   for (int t = 0; t < n; ++t) {
     const int r = rows.r0 + t, j = t % MNB;
-    if (t + 1 < n)
-      wait_vm<NL + 1>();
-    else
-      wait_vm<0>();
-    asm volatile("s_barrier" ::: "memory");      // slot j is there, and the slot of stage t - 1 has been read
-    if (t + 2 < n) load(r + 2, (t + 2) % MNB);
-    // the stage's first row sees the fewest keys
-    const bool part = r * MST + MST > count || kw + 64 > cache_limit(c, s, r * MST / group);
+    wait_vm<0>();
+    asm volatile("s_barrier" ::: "memory");      // slot j is there, and the other one has been read
+    if (t + 1 < n) load(r + 1, (t + 1) % MNB);
+    const bool part = r * MST + MST > count || cache_row(c, r * MST) < whole;
     const char *qb = qs + j * QB;
     const float *zb = zs[j][w];
+    // Row tile q's matrix products run in one stream with the exponentials of tile
+    // q - 1, so that a wave's vector work executes under its own MFMAs.
+    bf16x8 qf[2][NC];
+    f32x4 x[2][4];
+    float z[2];
+    int lim[2] = {0, 0};
+    auto fetch = [&](int q) __attribute__((always_inline)) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      bf16x8 qf[NC];
+      for (int jj = 0; jj < NC; ++jj) qf[q & 1][jj] = *(const bf16x8 *)(qb + q * 16 * F::ROWB + qro[jj]);
+    };
+    auto stream = [&](auto masked) __attribute__((always_inline)) {
+      constexpr bool M = decltype(masked)::value;
+      fetch(0);
 #pragma unroll
-      for (int jj = 0; jj < NC; ++jj) qf[jj] = *(const bf16x8 *)(qb + q * 16 * F::ROWB + qro[jj]);
-      const float z = zb[16 * q + lr] * LOG2E;
-      f32x4 x[4];
+      for (int q = 0; q <= NQ; ++q) {
+        if (q < NQ - 1) fetch(q + 1);
+        if (q < NQ) z[q & 1] = zb[16 * q + lr] * LOG2E;
+        if (M && q < NQ) {
+          const int m = r * MST + 16 * q + lr;
+          lim[q & 1] = m < count ? cache_limit(c, s, cache_row(c, m)) : 0;
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int jj = 0; jj < NC; ++jj)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          x[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][jj], qf[jj], jj == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x[k], 0, 0, 0);
-      if (part) {
-        const int m = r * MST + 16 * q + lr, lim = m < count ? cache_limit(c, s, m / group) : 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][e], sc, -z));
-            sum[k][e] += kw + 16 * k + 4 * lg + e < lim ? p : 0.f;
+        for (int i = 0; i < 16; ++i) {
+          if (q < NQ && i % (4 / NC) == 0) {
+            const int mm = i / (4 / NC), jj = mm / 4, k = mm % 4;
+            x[q & 1][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][jj], qf[q & 1][jj],
+                                                                  jj == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x[q & 1][k], 0, 0, 0);
           }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[k][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][e], sc, -z));
+          if (q > 0) {
+            const int p = (q - 1) & 1, k = i / 4, e = i % 4;
+            float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][k][e], sc, -z[p]));
+            if (M) y = kw + 16 * k + 4 * lg + e < lim[p] ? y : 0.f;
+            sum[k][e] += y;
+            asm volatile("" : "+v"(sum[k][e]));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-    }
+    };
+    if (part)
+      stream(std::true_type{});
+    else
+      stream(std::false_type{});
     __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): this wave's reads of the slot are done
   }
   // lane lr < 16 of each lane group: key 16 k + 4 lg + e with k = lr / 4, e = lr % 4
@@ -1202,7 +1230,7 @@ __global__ __launch_bounds__(256) void k_cache_mass_f32(CacheMassArgs a) {
   const float sc = LOG2E / sqrtf((float)HD);
   float sum[16] = {};
   for (int r = rows.r0 + w; r < rows.r1; r += 4) {
-    const int m = r * 32 + lr, mm = min(m, count - 1), i = mm / group, head = h * group + mm % group;
+    const int m = r * 32 + lr, mm = min(m, count - 1), i = cache_row(c, mm), head = h * group + mm - i * group;
     const float *Q = (const float *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)head * HD + 4 * lg;
     const float z = a.lse[(int64_t)(s.q0 + i) * c.heads + head] * LOG2E;
     const int lim = m < count ? cache_limit(c, s, i) : 0;
@@ -1359,9 +1387,9 @@ static int64_t mass_blocks(int dtype, const CacheArgs &c) {
 static size_t mass_part_bytes(const CacheArgs &c, int splits) {
   return (size_t)c.batch * c.kvh * splits * c.cap * sizeof(float);
 }
-// Row ranges of at least 256 rows, as many as give every compute unit two blocks
+// Row ranges of at least 256 rows, as many as give every compute unit a block
 static int mass_wanted(int dtype, const CacheArgs &c) {
-  const int64_t fill = 2 * device_cus() / std::max<int64_t>(1, mass_blocks(dtype, c));
+  const int64_t fill = device_cus() / std::max<int64_t>(1, mass_blocks(dtype, c));
   const int64_t most = ((int64_t)c.max_q * (c.heads / c.kvh) + 255) / 256;
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(fill, most), 64));
 }

@@ -199,8 +199,15 @@ struct CacheArgs {
   int batch, rows, max_q, table_ld;
   int cap;                  // most keys of a sequence: max_kv, or what the table's pages hold
   int heads, hd, frame;
+  uint32_t group_mul;       // see cache_row
   int xcd_order;            // 1: the blocks of one (sequence, kv head) run on one XCD
 };
+// Query row m of a (sequence, kv head) is chunk row m / group of query head m %
+// group, group = heads / kvh. Division by multiplication with ceil(2^32 / group):
+// exact while m * group < 2^32, and m < 2^26, group <= 64.
+__device__ __forceinline__ int cache_row(const CacheArgs &a, int m) {
+  return a.group_mul ? (int)__umulhi((uint32_t)m, a.group_mul) : m;   // 0: group is 1
+}
 
 struct CacheSeq {
   int q0, nq;  // first packed row, rows taken

@@ -1687,6 +1687,10 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
     set_err(c, "kv_heads (%d) must divide heads (%d)", p->kv_heads, c->H);
     return WDC_E_SHAPE;
   }
+  if (c->H / p->kv_heads > 64) {
+    set_err(c, "more than 64 query heads (%d) per kv head", c->H / p->kv_heads);
+    return WDC_E_UNSUPPORTED;
+  }
   if (!aligned16(p->d_k) || (values && !aligned16(p->d_v))) {
     set_err(c, "cache not 16-byte aligned");
     return WDC_E_ALIGN;
@@ -1721,6 +1725,8 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
   a->cap = (int)cap;
   a->heads = c->H;
   a->hd = c->hd;
+  const uint32_t group = c->H / p->kv_heads;
+  a->group_mul = group > 1 ? (uint32_t)(((uint64_t(1) << 32) + group - 1) / group) : 0;
   return WDC_OK;
 }
 
