@@ -18,25 +18,43 @@ namespace {
 constexpr int RSRC_WORD3 = 0x00020000;   // raw buffer descriptor word 3
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-__device__ __forceinline__ void lds_load16(__amdgpu_buffer_rsrc_t r, char *lds, int voff, int soff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)lds, 16, voff, soff, 0, 0);
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Buffer of `bytes` bytes from base + off: what lies outside reads as zero
+__device__ __forceinline__ u32x4_t buffer_at(const void *base, int64_t off, int bytes) {
+  const uint64_t p = (uint64_t)base + (uint64_t)off;
+  return u32x4_t{(uint32_t)uni((int)(uint32_t)p), (uint32_t)uni((int)(uint32_t)(p >> 32) & 0xffff), (uint32_t)uni(bytes),
+                 (uint32_t)RSRC_WORD3};
 }
-__device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, char *lds, int voff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)lds, 4, voff, 0, 0, 0);
+// Direct global -> LDS loads: lane l's 16 (4) bytes at `voff` of the buffer arrive
+// at lds + 16 l (4 l). Written as instructions because the compiler lets no transposed LDS read pass while one
+// of its own direct loads is under way (it waits for all of them); nothing is returned in
+// registers, and the waits for the data are wait_vm's. The kernels that use these use no others, so M0 is theirs.
+__device__ __forceinline__ void lds_load16(u32x4_t buf, uint32_t lds, int voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buf)
+               : "memory");
+}
+__device__ __forceinline__ void lds_load4(u32x4_t buf, uint32_t lds, int voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buf)
+               : "memory");
+}
+// LDS address of a pointer into it, the same in every lane
+__device__ __forceinline__ uint32_t lds_addr(const void *p) {
+  return (uint32_t)uni((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p);
+}
+// waits until at most N loads are under way
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 // Four rows of 16 columns of 2 bytes, each read as 4 x 8 bytes by the lanes of a
 // group of 16 in row order, come back transposed: lane c of the group gets column c.
 __device__ __forceinline__ s16x4 lds_read_tr(const char *p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
-}
-// s_waitcnt vmcnt(N), the other counters untouched
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
 __device__ __forceinline__ float quad_max(float v) {
@@ -53,7 +71,7 @@ __device__ __forceinline__ float quad_sum(float v) {
 }
 
 // Entries of one sequence's page table, asked for in rising order by a whole
-// wave: 64 entries in a register, the next 64 on their way.
+// wave: 64 entries in a register, the next 64 on their way in another.
 struct PageWalk {
   const int32_t *tab;
   int last, base, pages, cur, next;
@@ -79,10 +97,10 @@ struct PageWalk {
 // a sequence's lengths as wave-uniform values
 __device__ __forceinline__ CacheSeq uniform_seq(const CacheArgs &a, int b) {
   CacheSeq s = cache_seq(a, b);
-  s.q0 = __builtin_amdgcn_readfirstlane(s.q0);
-  s.nq = __builtin_amdgcn_readfirstlane(s.nq);
-  s.n = __builtin_amdgcn_readfirstlane(s.n);
-  s.start = __builtin_amdgcn_readfirstlane(s.start);
+  s.q0 = uni(s.q0);
+  s.nq = uni(s.nq);
+  s.n = uni(s.n);
+  s.start = uni(s.start);
   return s;
 }
 
@@ -107,28 +125,32 @@ __device__ __forceinline__ float *part_ml(const CacheAttnArgs &a, int64_t slot) 
   return a.part + (int64_t)a.splits * a.c.rows * a.c.heads * a.c.hd + 2 * slot;
 }
 
+// the same in every lane of a wave, as scalars
+__device__ __forceinline__ void uniform_range(Range &r) {
+  r.lim_lo = uni(r.lim_lo);
+  r.lim_hi = uni(r.lim_hi);
+  r.nr = uni(r.nr);
+}
+
 // Block of a launch over (sequence, kv head) x per blocks each. With the XCD order
 // the blocks of one (sequence, kv head) share an XCD, and so its K and V in that L2.
 __device__ __forceinline__ void cache_block(const CacheArgs &c, int per, int &bh, int &li) {
-  if (c.xcd_order) {
-    li = blockIdx.x >> 3;
-    bh = (blockIdx.x & 7) + 8 * (li / per);
-  } else {
-    li = blockIdx.x;
-    bh = li / per;
-  }
-  li %= per;
+  li = c.xcd_order ? blockIdx.x >> 3 : blockIdx.x;
+  const int q = uni(li / per);
+  li -= q * per;
+  bh = c.xcd_order ? (blockIdx.x & 7) + 8 * q : q;
 }
 
 // ---------------------------------------------------------------- bf16, few rows
 // RT tiles of 16 query rows per block of four waves; wave w takes key tiles w, w +
-// 4, .. of 32 keys of the block's range and the four partial softmaxes meet at the
-// end. What bounds it is the stream of K and V: a wave keeps one tile of 32 keys
-// under way (direct buffer loads into its own part of LDS, no block barrier) while it
-// works on the other: hd 128: 16 KB a tile, 64 to 128 KB under way per CU.
+// 4, .. of the block's range and the four partial softmaxes meet at the end. What
+// bounds it is the stream of K and V, so each wave keeps three tiles under way beside the
+// one it works on, without a block barrier: direct loads into its own part of LDS, 8 KB a
+// tile (32 keys of 64, 16 of 128). With two slots of 32 keys, one of them under way, a compute unit
+// reached 39 GB/s (hd 128): a tile per 1.7 us and wave.
 //
 // S^T = K Q^T (A: 16 keys, B: 16 rows) leaves lane (lr, lg) the keys 4 lg + e of
-// row lr; these values of two key tiles are the B operand of O^T = V^T P^T, whose A
+// row lr; these values of one (hd 128) or two key tiles are the B operand of O^T = V^T P^T, whose A
 // operand is V^T: rows 4 lg .. 4 lg + 3 of V read transposed from LDS.
 //
 // Softmax in base 2 with a reference m per row that moves when a score passes it
@@ -137,10 +159,13 @@ __device__ __forceinline__ void cache_block(const CacheArgs &c, int per, int &bh
 template <int HD>
 struct Few {
   static constexpr int ROWB = HD * 2;            // bytes of a row
-  static constexpr int RPL = 1024 / ROWB;        // rows per load of a wave (4 or 8)
-  static constexpr int LPT = 32 / RPL;           // loads per tile of 32 rows
-  static constexpr int TILE = 32 * ROWB;
-  static constexpr int WAVE = 4 * TILE;          // two K and two V tiles
+  static constexpr int RPL = 1024 / ROWB;        // rows per LDS load of a wave (4 or 8)
+  static constexpr int KT = HD == 128 ? 16 : 32; // keys per tile
+  static constexpr int NK = KT / 16;
+  static constexpr int LPH = 16 / RPL;           // LDS loads per 16 rows (4 or 2)
+  static constexpr int TILE = KT * ROWB;
+  static constexpr int NB = 4;                   // slots of a wave: one in use, three under way
+  static constexpr int WAVE = 2 * NB * TILE;     // K slots, V slots
   // 16-byte chunk c of row r lies at c ^ key(r): the 16 rows of a K fragment, and
   // the 4 rows that 16 lanes of a transposed V read take (a pair of chunks each), spread over the banks
   static __device__ __forceinline__ int kkey(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
@@ -159,7 +184,7 @@ __device__ __forceinline__ bf16x8 v_frag(const char *p) {
 template <int HD, int RT>
 __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   using F = Few<HD>;
-  constexpr int NC = HD / 32, NI = HD / 16;
+  constexpr int NC = HD / 32, NI = HD / 16, KT = F::KT;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ float ml[4][2][16 * RT];
   const CacheArgs &c = a.c;
@@ -167,8 +192,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   const int nrb = (c.max_q * group + 16 * RT - 1) / (16 * RT);
   int bh, li;                                    // (sequence, kv head); row block and key range
   cache_block(c, nrb * a.splits, bh, li);
-  const int sp = li % a.splits, rb = li / a.splits;
-  const int b = bh / c.kvh, h = bh % c.kvh;
+  const int rb = uni(li / a.splits), sp = li - rb * a.splits, b = uni(bh / c.kvh), h = bh - b * c.kvh;
   const CacheSeq s = uniform_seq(c, b);
   const int m0 = rb * 16 * RT, count = s.nq * group;
   if (m0 >= count) return;
@@ -176,10 +200,11 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mlast = min(m0 + 16 * RT, count) - 1;
-  const Range rg(a, s, group, m0, count);
+  Range rg(a, s, group, m0, count);
+  uniform_range(rg);
   if (sp >= rg.nr) return;
-  const int lim_lo = rg.lim_lo, tiles = (rg.lim_hi + 31) / 32;
-  const int t0 = rg.nr > 1 ? sp * (a.range / 32) : 0, t1 = rg.nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
+  const int lim_lo = rg.lim_lo, tiles = (rg.lim_hi + KT - 1) / KT;
+  const int t0 = rg.nr > 1 ? sp * (a.range / KT) : 0, t1 = rg.nr > 1 ? min(t0 + a.range / KT, tiles) : tiles;
 
   const float sc = LOG2E / sqrtf((float)HD);
   bf16x8 qf[RT][NC];
@@ -194,14 +219,15 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   }
 
   char *mine = smem + w * F::WAVE;
-  int kvo[F::LPT / 2], vvo[F::LPT / 2];          // byte offsets in 16 rows of K and V
+  const uint32_t lds0 = lds_addr(mine);
+  int kvo[F::LPH], vvo[F::LPH];                  // byte offsets in 16 rows of K and V
 #pragma unroll
-  for (int i = 0; i < F::LPT / 2; ++i) {
+  for (int i = 0; i < F::LPH; ++i) {
     const int r = i * F::RPL + lane / (HD / 8), ch = lane % (HD / 8);
     kvo[i] = r * F::ROWB + (ch ^ F::kkey(r)) * 16;
     vvo[i] = r * F::ROWB + (ch ^ F::vkey(r)) * 16;
   }
-  int kro[NC];                                   // K fragment of rows lr, dims 32 c + 8 lg
+  int kro[NC];                                   // K fragment of rows lr, dims 32 j + 8 lg
 #pragma unroll
   for (int j = 0; j < NC; ++j) kro[j] = lr * F::ROWB + ((4 * j + lg) ^ F::kkey(lr)) * 16;
   int vro[F::VR];                                // transposed V read of rows 4 lg .. + 3, dims 16 i ..
@@ -211,25 +237,25 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     for (int i = 0; i < F::VR; ++i) vro[i] = r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
   PageWalk pw;
-  pw.init(c, b, (32 * t0) >> c.plog);
+  pw.init(c, b, (KT * t0) >> c.plog);
   const int pmask = (1 << c.plog) - 1;
-  // tile t into slot j: halves of 16 rows, each on one page. Rows past the cache's
-  // end lie outside the buffer range and arrive as zeros, whatever they hold.
-  auto load = [&](int t, int j) {
+  // Tile t into slot j: halves of 16 rows, each on one page. Rows past the cache's
+  // end lie outside the buffer range and arrive as zeros, whatever they hold; so do tiles
+  // past the range, which are asked for like the others so that the count of loads under way is fixed.
+  auto load = [&](int t, int j) __attribute__((always_inline)) {
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const int key = 32 * t + 16 * hf;
-      const int pg = pw.get(key >> c.plog);
-      const int64_t off = (((((int64_t)pg * c.kvh + h) << c.plog) + (key & pmask)) * HD) * 2;
-      const int bytes = min(max(s.n - key, 0), 16) * F::ROWB;
-      const __amdgpu_buffer_rsrc_t kd = __builtin_amdgcn_make_buffer_rsrc((char *)c.k + off, (short)0, bytes, RSRC_WORD3);
-      const __amdgpu_buffer_rsrc_t vd = __builtin_amdgcn_make_buffer_rsrc((char *)c.v + off, (short)0, bytes, RSRC_WORD3);
+    for (int hf = 0; hf < F::NK; ++hf) {
+      const int key = KT * t + 16 * hf;
+      const bool live = t < t1;
+      const int pg = live ? pw.get(key >> c.plog) : 0;
+      const int64_t off = ((((int64_t)pg * c.kvh + h) << c.plog) + (key & pmask)) * F::ROWB;
+      const int bytes = live ? min(max(s.n - key, 0), 16) * F::ROWB : 0;
+      const u32x4_t kd = buffer_at(c.k, off, bytes), vd = buffer_at(c.v, off, bytes);
+      const uint32_t to = lds0 + j * F::TILE + hf * 16 * F::ROWB;
 #pragma unroll
-      for (int i = 0; i < F::LPT / 2; ++i)
-        lds_load16(kd, mine + j * F::TILE + hf * 16 * F::ROWB + i * 1024, kvo[i], 0);
+      for (int i = 0; i < F::LPH; ++i) lds_load16(kd, to + i * 1024, kvo[i]);
 #pragma unroll
-      for (int i = 0; i < F::LPT / 2; ++i)
-        lds_load16(vd, mine + (2 + j) * F::TILE + hf * 16 * F::ROWB + i * 1024, vvo[i], 0);
+      for (int i = 0; i < F::LPH; ++i) lds_load16(vd, to + F::NB * F::TILE + i * 1024, vvo[i]);
     }
   };
 
@@ -242,41 +268,38 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  int slot = 0;
-  if (t0 + w < t1) load(t0 + w, 0);
-  for (int t = t0 + w; t < t1; t += 4, slot ^= 1) {
-    if (t + 4 < t1) {
-      load(t + 4, slot ^ 1);
-      wait_vm<2 * F::LPT>();
-    } else {
-      wait_vm<0>();
-    }
+  constexpr int LT = 2 * F::NK * F::LPH;         // loads per tile
+  // tile t in slot J, with tile t + 4 (NB - 1) asked for
+  auto step = [&](auto jc, int t) __attribute__((always_inline)) {
+    constexpr int J = decltype(jc)::value;
+    load(t + 4 * (F::NB - 1), (J + F::NB - 1) % F::NB);
+    wait_vm<(F::NB - 1) * LT>();
     asm volatile("" ::: "memory");
-    const char *kt = mine + slot * F::TILE, *vt = mine + (2 + slot) * F::TILE;
-    f32x4 S[RT][2];
+    const char *kt = mine + J * F::TILE, *vt = kt + F::NB * F::TILE;
+    f32x4 S[RT][F::NK];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) S[r][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < F::NK; ++k) S[r][k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NC; ++j)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
+      for (int k = 0; k < F::NK; ++k) {
         const bf16x8 kf = *(const bf16x8 *)(kt + k * 16 * F::ROWB + kro[j]);
 #pragma unroll
         for (int r = 0; r < RT; ++r) S[r][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j], S[r][k], 0, 0, 0);
       }
-    const bool part = 32 * t + 32 > lim_lo;      // some row does not see the whole tile
-    bf16x8 pf[RT];
+    const bool part = KT * t + KT > lim_lo;      // some row does not see the whole tile
+    bf16x4 pf[RT][F::NK];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < F::NK; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float x = S[r][k][e] * sc;
-          if (part && 32 * t + 16 * k + 4 * lg + e >= lim[r]) x = -INFINITY;
+          if (KT * t + 16 * k + 4 * lg + e >= lim[r]) x = -INFINITY;
           S[r][k][e] = x;
           mx = fmaxf(mx, x);
         }
@@ -292,12 +315,12 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
       }
       const float ref = m[r] == -INFINITY ? 0.f : m[r];   // a row that has seen nothing yet
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < F::NK; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float p = __builtin_amdgcn_exp2f(S[r][k][e] - ref);
           l[r] += p;
-          pf[r][4 * k + e] = (__bf16)p;
+          pf[r][k][e] = (__bf16)p;
         }
     }
     // A key that a row does not see has weight 0, but 0 times an infinity or NaN
@@ -306,46 +329,71 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     bool odd = false;
     if (part) {
 #pragma unroll
-      for (int i = 0; i < F::LPT; ++i) {
-        const uint4 u = *(const uint4 *)(vt + i * 1024 + lane * 16);
-        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+      for (int i = 0; i < F::TILE / 1024; ++i) {
+        const u32x4_t u = *(const u32x4_t *)(vt + i * 1024 + lane * 16);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) odd |= (x[q] & 0x7f80u) == 0x7f80u || (x[q] & 0x7f800000u) == 0x7f800000u;
+        for (int q = 0; q < 4; ++q) odd |= (u[q] & 0x7f80u) == 0x7f80u || (u[q] & 0x7f800000u) == 0x7f800000u;
       }
       odd = __any(odd);
     }
     if (odd) {
-      for (int k = 0; k < 2; ++k)
-        for (int e = 0; e < 4; ++e)
-          for (int g = 0; g < 4; ++g) {
-            const int key = 16 * k + 4 * g + e;
+#pragma unroll 1
+      for (int x = 0; x < KT; ++x) {             // key 16 (q / 4) + 4 g + q % 4
+        const int q = x >> 2, g = x & 3, key = 16 * (q >> 2) + 4 * g + (q & 3);
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-              float p = 0.f;                     // of key and row lr, held by lane group g
+        for (int r = 0; r < RT; ++r) {
+          float p = 0.f;                         // of key and row lr, held by lane group g
 #pragma unroll
-              for (int q = 0; q < 8; ++q)
-                if (q == 4 * k + e) p = (float)pf[r][q];
-              p = __shfl(p, 16 * g + lr, 64);
-              if (32 * t + key < lim[r])
+          for (int y = 0; y < 4 * F::NK; ++y)
+            if (y == q) p = (float)pf[r][y / 4][y % 4];
+          p = __shfl(p, 16 * g + lr, 64);
+          if (KT * t + key < lim[r])
 #pragma unroll
-                for (int i = 0; i < NI; ++i)
+            for (int i = 0; i < NI; ++i)
 #pragma unroll
-                  for (int d = 0; d < 4; ++d) {
-                    const int col = 16 * i + 4 * lg + d;
-                    o[r][i][d] += p * bf2f(*(const bf16_t *)(vt + key * F::ROWB + ((col >> 3) ^ F::vkey(key)) * 16 + (col & 7) * 2));
-                  }
-            }
-          }
+              for (int d = 0; d < 4; ++d) {
+                const int col = 16 * i + 4 * lg + d;
+                o[r][i][d] += p * bf2f(*(const bf16_t *)(vt + key * F::ROWB + ((col >> 3) ^ F::vkey(key)) * 16 + (col & 7) * 2));
+              }
+        }
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const bf16x8 vf = v_frag<HD>(vt + vro[i % F::VR] + i / F::VR * F::VR * 32);
+        const char *vp = vt + vro[i % F::VR] + i / F::VR * F::VR * 32;
+        if constexpr (F::NK == 2) {
+          const bf16x8 vf = v_frag<HD>(vp);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][i], 0, 0, 0);
+          for (int r = 0; r < RT; ++r)
+            o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                vf, __builtin_shufflevector(pf[r][0], pf[r][F::NK - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[r][i], 0, 0, 0);
+        } else {
+          const s16x4 vf = lds_read_tr(vp);
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+            o[r][i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, __builtin_bit_cast(s16x4, pf[r][0]), o[r][i], 0, 0, 0);
+        }
       }
     }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): the slot has been read before it is loaded again
+  };
+  if (t0 + w < t1) {
+    static_assert(F::NB == 4, "slots of the unrolled steps");
+    load(t0 + w, 0);
+    load(t0 + w + 4, 1);
+    load(t0 + w + 8, 2);
+    for (int t = t0 + w; t < t1; t += 16) {
+      step(std::integral_constant<int, 0>{}, t);
+      if (t + 4 >= t1) break;
+      step(std::integral_constant<int, 1>{}, t + 4);
+      if (t + 8 >= t1) break;
+      step(std::integral_constant<int, 2>{}, t + 8);
+      if (t + 12 >= t1) break;
+      step(std::integral_constant<int, 3>{}, t + 12);
+    }
+    wait_vm<0>();                                // what is still under way goes to this wave's part of LDS
+    asm volatile("" ::: "memory");
   }
 
   // the four waves' parts: each leaves its rows in its own part of LDS
@@ -413,7 +461,6 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 constexpr int KV = 64, NB = 4;
 constexpr float SUM_LIMIT = 0x1p64f;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 // Loads of one wave (of four): stripe i of a tile is rows [(4 i + w) RPL, + RPL). SMALL:
 // pages of 16 or 32 slots, where every stripe has its own page; otherwise a tile lies on one page.
@@ -426,8 +473,8 @@ struct TileLoads {
     int64_t off[NP];                             // bytes from the pool to the tile (SMALL: the stripe's 16 rows)
     int bytes[NP];                               // what lies before the end of the cache
   };
-  PageWalk pw;
-  int kvo, vvo, w, h, n;
+  PageWalk pw;                                   // SMALL only
+  int kvo, w, h, n;                              // kvo: the lane's byte offset in its stripe's rows of K
   __device__ __forceinline__ void init(const CacheArgs &c, const CacheSeq &s, int b, int h_, int w_, int lane, int tile0) {
     w = w_;
     h = h_;
@@ -435,26 +482,35 @@ struct TileLoads {
     const int r = w * F::RPL + lane / (HD / 8), ch = lane % (HD / 8);
     const int at = SMALL ? r & 15 : r;
     kvo = at * F::ROWB + (ch ^ F::kkey(r)) * 16;
-    vvo = at * F::ROWB + (ch ^ F::vkey(r)) * 16;
-    pw.init(c, b, (KV * tile0) >> c.plog);
+    if (SMALL) pw.init(c, b, (KV * tile0) >> c.plog);
   }
-  __device__ __forceinline__ void find(const CacheArgs &c, int tile, Where &x) {
+  // the same of V, whose rows have another swizzle (found again each time: a register kept for it would spill)
+  __device__ __forceinline__ int vvo() const {
+    const int r = w * F::RPL + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)) / (HD / 8);
+    return kvo ^ ((F::kkey(r) ^ F::vkey(r)) * 16);
+  }
+  // page of a whole tile, by a scalar load (the table does not change during a launch)
+  __device__ __forceinline__ int page(const CacheArgs &c, int b, int tile) const {
+    typedef const __attribute__((address_space(4))) int32_t *scalar_ptr;
+    const int e = min((KV * tile) >> c.plog, c.table_ld - 1);
+    return cache_page(c, ((scalar_ptr)(uint64_t)(c.table + (int64_t)b * c.table_ld))[e]);
+  }
+  // where a tile lies; page: its page (unless SMALL)
+  __device__ __forceinline__ void find(const CacheArgs &c, int tile, int page, Where &x) {
     const int pmask = (1 << c.plog) - 1;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int key = KV * tile + (SMALL ? (4 * i + w) * F::RPL / 16 * 16 : 0);
-      const int pg = pw.get(key >> c.plog);
+      const int pg = SMALL ? pw.get(key >> c.plog) : page;
       x.off[i] = ((((int64_t)pg * c.kvh + h) << c.plog) + (key & pmask)) * F::ROWB;
       x.bytes[i] = min(max(n - key, 0), SMALL ? 16 : KV) * F::ROWB;
     }
   }
-  __device__ __forceinline__ void load(const void *pool, const Where &x, char *lds, int vo) const {
+  __device__ __forceinline__ void load(const void *pool, const Where &x, uint32_t lds, int vo) const {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc((char *)pool + x.off[SMALL ? i : 0], (short)0,
-                                                                        x.bytes[SMALL ? i : 0], RSRC_WORD3);
-      lds_load16(d, lds + i * 4096 + w * 1024, SMALL ? vo : vo + i * 4096, 0);
-    }
+    for (int i = 0; i < NS; ++i)
+      lds_load16(buffer_at(pool, x.off[SMALL ? i : 0], x.bytes[SMALL ? i : 0]), lds + i * 4096 + w * 1024,
+                 SMALL ? vo : vo + i * 4096);
   }
 };
 
@@ -494,7 +550,7 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
   const int nrb = (c.max_q * group + 255) / 256;
   int bh, li;
   cache_block(c, nrb * a.splits, bh, li);
-  const int sp = li % a.splits, rb = li / a.splits, b = bh / c.kvh, h = bh % c.kvh;
+  const int rb = uni(li / a.splits), sp = li - rb * a.splits, b = uni(bh / c.kvh), h = bh - b * c.kvh;
   const CacheSeq s = uniform_seq(c, b);
   const int m0 = rb * 256, count = s.nq * group;
   if (m0 >= count) return;
@@ -503,7 +559,8 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool grp_a = wid < 4;
   const int mlast = min(m0 + 256, count) - 1;
-  const Range rg(a, s, group, m0, count);
+  Range rg(a, s, group, m0, count);
+  uniform_range(rg);
   if (sp >= rg.nr) return;
   const int lim_lo = rg.lim_lo, tiles = (rg.lim_hi + KV - 1) / KV;
   const int t_first = rg.nr > 1 ? sp * (a.range / KV) : 0, t_end = rg.nr > 1 ? min(t_first + a.range / KV, tiles) : tiles;
@@ -528,14 +585,16 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < F::VR; ++i) vro[i] = V_BASE + r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
+  const uint32_t lds0 = lds_addr(smem);
   TL tl;
   typename TL::Where wk, wv;                     // of the latest K tile asked for, and of the one before
-  auto load_k = [&](int tile) {
+  auto page_of = [&](int tile) { return SMALL ? 0 : tl.page(c, b, t_first + tile); };
+  auto load_k = [&](int tile, int page) __attribute__((always_inline)) {
     wv = wk;
-    tl.find(c, t_first + tile, wk);
-    tl.load(c.k, wk, smem + (tile % NB) * TB, tl.kvo);
+    tl.find(c, t_first + tile, page, wk);
+    tl.load(c.k, wk, lds0 + (tile % NB) * TB, tl.kvo);
   };
-  auto load_v = [&](int tile, const typename TL::Where &x) { tl.load(c.v, x, smem + V_BASE + (tile % NB) * TB, tl.vvo); };
+  auto load_v = [&](int tile, const typename TL::Where &x) { tl.load(c.v, x, lds0 + V_BASE + (tile % NB) * TB, tl.vvo()); };
 
   if (grp_a) {                                   // K_0 .. K_3, V_0 .. V_2
     tl.init(c, s, b, h, wid, lane, t_first);
@@ -543,7 +602,7 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
 #pragma unroll
     for (int j = 0; j < NB; ++j)
       if (j < tot) {
-        load_k(j);
+        load_k(j, page_of(j));
         if (j < NB - 1) load_v(j, wk);
       }
     wait_vm<0>();
@@ -601,12 +660,12 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
     };
 #pragma unroll
     for (int r = 0; r < 4; ++r) read(r, smem, smem);
-    auto step = [&](auto pc, int t) __attribute__((always_inline)) {
+    auto step = [&](auto pc, int t, int page) __attribute__((always_inline)) {
       constexpr int P = decltype(pc)::value, cur = (P + 1) & 1, n = P & 1;
       int issued = 0;
       if (grp_a) {
         if (t + 4 < tot) {
-          load_k(t + 4);
+          load_k(t + 4, page);
           issued += TL::NS;
         } else {
           wv = wk;
@@ -694,14 +753,22 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
       }
       asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(8) : "memory");
     };
+    int page[NB];                                // of the K tiles that the next NB steps ask for
+#pragma unroll
+    for (int j = 0; j < NB; ++j) page[j] = page_of(NB + j);
     for (int t = 0; t < nf; t += NB) {
-      step(std::integral_constant<int, 0>{}, t);
+      int next[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) next[j] = page_of(t + 2 * NB + j);
+      step(std::integral_constant<int, 0>{}, t, page[0]);
       if (t + 1 >= nf) break;
-      step(std::integral_constant<int, 1>{}, t + 1);
+      step(std::integral_constant<int, 1>{}, t + 1, page[1]);
       if (t + 2 >= nf) break;
-      step(std::integral_constant<int, 2>{}, t + 2);
+      step(std::integral_constant<int, 2>{}, t + 2, page[2]);
       if (t + 3 >= nf) break;
-      step(std::integral_constant<int, 3>{}, t + 3);
+      step(std::integral_constant<int, 3>{}, t + 3, page[3]);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) page[j] = next[j];
     }
   }
 
@@ -716,7 +783,7 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
     if (grp_a) wait_vm<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (grp_a && u + 3 < tot) {
-      if (u > nf) load_k(u + 3);                 // at u = nf the pipeline has asked for it already
+      if (u > nf) load_k(u + 3, page_of(u + 3));                 // at u = nf the pipeline has asked for it already
       load_v(u + 3, wk);
     }
     const char *kb = smem + (u % NB) * TB, *vb = smem + (u % NB) * TB;   // vro holds V_BASE
@@ -725,8 +792,7 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < TB / (512 * 16); ++i) {
-      const uint4 x = *(const uint4 *)(vb + V_BASE + (i * 512 + tid) * 16);
-      const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+      const u32x4_t y = *(const u32x4_t *)(vb + V_BASE + (i * 512 + tid) * 16);
 #pragma unroll
       for (int q = 0; q < 4; ++q) odd |= (y[q] & 0x7f80u) == 0x7f80u || (y[q] & 0x7f800000u) == 0x7f800000u;
     }
@@ -885,14 +951,15 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   const int group = c.heads / c.kvh, nrb = (c.max_q * group + 31) / 32;
   int bh, li;
   cache_block(c, nrb * a.splits, bh, li);
-  const int sp = li % a.splits, rb = li / a.splits, b = bh / c.kvh, h = bh % c.kvh;
+  const int rb = uni(li / a.splits), sp = li - rb * a.splits, b = uni(bh / c.kvh), h = bh - b * c.kvh;
   const CacheSeq s = uniform_seq(c, b);
   const int m0 = rb * 32, count = s.nq * group;
   if (m0 >= count) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lg = lane >> 5;
   const int mlast = min(m0 + 32, count) - 1, mm = min(m0 + lr, mlast), row = cache_row(c, mm);
-  const Range rg(a, s, group, m0, count);
+  Range rg(a, s, group, m0, count);
+  uniform_range(rg);
   if (sp >= rg.nr) return;
   const int lim_lo = rg.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
   const int tiles = (rg.lim_hi + 31) / 32;
@@ -1077,7 +1144,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
   const int group = c.heads / c.kvh, nkt = (c.cap + MKT - 1) / MKT;
   int bh, li;
   cache_block(c, nkt * a.splits, bh, li);
-  const int sp = li % a.splits, kt = li / a.splits, b = bh / c.kvh, h = bh % c.kvh;
+  const int kt = uni(li / a.splits), sp = li - kt * a.splits, b = uni(bh / c.kvh), h = bh - b * c.kvh;
   const CacheSeq s = uniform_seq(c, b);
   const int key0 = kt * MKT;
   if (key0 >= s.n) return;
@@ -1096,6 +1163,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
   // Stage r into slot j: its rows lie at fixed offsets from its first chunk row i0
   // if the group divides 128; for other groups, and for rows past the last (read as the last), they are found per stage.
   int qo[NL], zo[NZ];
+  const uint32_t qa = lds_addr(qs), za = lds_addr(zs);
   auto place = [&](int r, int i0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
@@ -1112,14 +1180,12 @@ __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
   auto load = [&](int r, int j) {
     const int i0 = cache_row(c, r * MST);
     if (!fixed || r * MST + MST > count) place(r, i0);
-    const char *q = (const char *)a.q + ((int64_t)(s.q0 + i0) * a.ldq + (int64_t)h * group * HD) * 2;
-    const float *z = a.lse + (int64_t)(s.q0 + i0) * c.heads + h * group;
-    const __amdgpu_buffer_rsrc_t qd = __builtin_amdgcn_make_buffer_rsrc((void *)q, (short)0, 0x7fffffff, RSRC_WORD3);
-    const __amdgpu_buffer_rsrc_t zd = __builtin_amdgcn_make_buffer_rsrc((void *)z, (short)0, 0x7fffffff, RSRC_WORD3);
+    const u32x4_t qd = buffer_at(a.q, ((int64_t)(s.q0 + i0) * a.ldq + (int64_t)h * group * HD) * 2, 0x7fffffff);
+    const u32x4_t zd = buffer_at(a.lse, ((int64_t)(s.q0 + i0) * c.heads + h * group) * 4, 0x7fffffff);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) lds_load16(qd, qs + j * QB + (4 * i + w) * 1024, qo[i], 0);
+    for (int i = 0; i < NL; ++i) lds_load16(qd, qa + j * QB + (4 * i + w) * 1024, qo[i]);
 #pragma unroll
-    for (int i = 0; i < NZ; ++i) lds_load4(zd, (char *)(zs[j][w] + 64 * i), zo[i]);
+    for (int i = 0; i < NZ; ++i) lds_load4(zd, za + ((j * 4 + w) * MST + 64 * i) * 4, zo[i]);
   };
   int qro[NC];
 #pragma unroll
@@ -1213,7 +1279,7 @@ __global__ __launch_bounds__(256) void k_cache_mass_f32(CacheMassArgs a) {
   const int group = c.heads / c.kvh, nkt = (c.cap + KT - 1) / KT;
   int bh, li;
   cache_block(c, nkt * a.splits, bh, li);
-  const int sp = li % a.splits, kt = li / a.splits, b = bh / c.kvh, h = bh % c.kvh;
+  const int kt = uni(li / a.splits), sp = li - kt * a.splits, b = uni(bh / c.kvh), h = bh - b * c.kvh;
   const CacheSeq s = uniform_seq(c, b);
   const int key0 = kt * KT;
   if (key0 >= s.n) return;
@@ -1281,7 +1347,7 @@ int rows_per_block(int dtype, const CacheArgs &c) {
   if (dtype == 0) return 32;
   const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
   if (getenv("TUNE_RPB")) return atoi(getenv("TUNE_RPB"));
-  return m <= 16 ? 16 : m <= 32 ? 32 : m <= 128 ? 64 : 256;
+  return m <= 16 ? 16 : m <= 96 ? 32 : 256;
 }
 // blocks of one range of keys
 int64_t attn_blocks(int rpb, const CacheArgs &c) {
@@ -1298,7 +1364,9 @@ void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *ran
   *rpb = rows_per_block(dtype, c);
   const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(attn_blocks(*rpb, c),
                                                                 c.kvh * ((int64_t)c.rows * group / *rpb + c.batch)));
-  const int64_t want = std::max<int64_t>(1, (int64_t)device_cus() * (c.batch > 1 ? 2 : 1) / blocks);
+  int mul = c.batch > 1 ? 2 : 1;
+  if (getenv("TUNE_MUL")) mul = atoi(getenv("TUNE_MUL"));
+  const int64_t want = std::max<int64_t>(1, (int64_t)device_cus() * mul / blocks);
   int64_t r = std::max<int64_t>(256, (c.cap + want - 1) / want);
   if (getenv("TUNE_RANGE")) r = atoi(getenv("TUNE_RANGE"));
   *range = (int)((r + 63) / 64 * 64);
@@ -1336,7 +1404,7 @@ template <int HD>
 hipError_t launch_bf16(const CacheAttnArgs &a, hipStream_t s) {
   const int rpb = a.rpb;
   if (rpb == 256) return a.c.plog < 6 ? launch_many<HD, true>(a, s) : launch_many<HD, false>(a, s);
-  return rpb == 16 ? launch_few<HD, 1>(a, s) : rpb == 32 ? launch_few<HD, 2>(a, s) : launch_few<HD, 4>(a, s);
+  return rpb == 16 ? launch_few<HD, 1>(a, s) : launch_few<HD, 2>(a, s);
 }
 
 }  // namespace
