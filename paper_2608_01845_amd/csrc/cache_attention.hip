@@ -104,18 +104,12 @@ __device__ __forceinline__ CacheSeq uniform_seq(const CacheArgs &a, int b) {
   return s;
 }
 
-// Query rows of a block and its key range. The keys that the block's last row
-// sees are cut into ranges of a.range keys, one block each; a block that has none is not needed
-// (the first range always is: it writes zeros where nothing is seen).
-struct Range {
-  int lim_lo, lim_hi;   // keys seen by the first and the last row
-  int nr;               // ranges of this row block
-  __device__ __forceinline__ Range(const CacheAttnArgs &a, const CacheSeq &s, int group, int m0, int count) {
-    lim_lo = cache_limit(a.c, s, cache_row(a.c, m0));
-    lim_hi = cache_limit(a.c, s, cache_row(a.c, min(m0 + a.rpb, count) - 1));
-    nr = a.splits > 1 ? max(1, (lim_hi + a.range - 1) / a.range) : 1;
-  }
-};
+// Ranges of keys that the rows of a block which see up to `keys` of them are cut
+// into, one block each (the first is always there: it writes zeros where nothing is seen)
+__device__ __forceinline__ int range_count(const CacheAttnArgs &a, int keys) {
+  return a.splits > 1 ? max(1, (keys + a.range - 1) / a.range) : 1;
+}
+
 // Part of range sp of packed row `row` and a head: HD unnormalised values at
 // part + slot * HD, its reference and sum at part + slots * HD + 2 slot
 __device__ __forceinline__ int64_t part_slot(const CacheAttnArgs &a, int sp, int row, int head) {
@@ -125,12 +119,62 @@ __device__ __forceinline__ float *part_ml(const CacheAttnArgs &a, int64_t slot) 
   return a.part + (int64_t)a.splits * a.c.rows * a.c.heads * a.c.hd + 2 * slot;
 }
 
-// the same in every lane of a wave, as scalars
-__device__ __forceinline__ void uniform_range(Range &r) {
-  r.lim_lo = uni(r.lim_lo);
-  r.lim_hi = uni(r.lim_hi);
-  r.nr = uni(r.nr);
-}
+// What a block of an attention launch works on: query rows [m0, m0 + rpb) of
+// `count` of sequence b and kv head h, range sp of nr of the keys that they see.
+// Blocks are numbered sequence by sequence with the lengths of the device, so those that the host's bounds
+// allow for but no chunk needs come last. Within a sequence kv heads go fastest: with 8 (or a divisor
+// or multiple) of them the blocks of one run on one XCD (or its group) and share K and V in that L2.
+struct AttnBlock {
+  CacheSeq s;
+  int b, h, m0, count, group, sp, nr;
+  int lim_lo, lim_hi;   // keys seen by the first and the last row
+  bool live;
+  __device__ __forceinline__ explicit AttnBlock(const CacheAttnArgs &a) : b(0), live(false) {
+    const CacheArgs &c = a.c;
+    const int lane = threadIdx.x & 63;
+    group = c.heads / c.kvh;
+    int li = blockIdx.x;
+    if (c.batch > 1) {
+      bool found = false;
+      for (int e0 = 0; e0 < c.batch && !found; e0 += 64) {
+        int cnt = 0;
+        if (e0 + lane < c.batch) {
+          const CacheSeq q = cache_seq(c, e0 + lane);
+          cnt = (q.nq * group + a.rpb - 1) / a.rpb * range_count(a, q.n) * c.kvh;
+        }
+        int sum = cnt;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int t = __shfl_up(sum, o, 64);
+          if (lane >= o) sum += t;
+        }
+        const uint64_t past = __ballot(sum > li);
+        if (past) {
+          const int k = __builtin_ctzll(past);
+          b = e0 + k;
+          li -= __builtin_amdgcn_readlane(sum - cnt, k);
+          found = true;
+        } else {
+          li -= __builtin_amdgcn_readlane(sum, 63);
+        }
+      }
+      if (!found) return;
+    }
+    b = uni(b);
+    li = uni(li);
+    s = uniform_seq(c, b);
+    count = s.nq * group;
+    const int q = uni(li / c.kvh), nrb = range_count(a, s.n), rb = uni(q / nrb);
+    h = li - q * c.kvh;
+    sp = q - rb * nrb;
+    m0 = rb * a.rpb;
+    if (m0 >= count) return;
+    lim_lo = uni(cache_limit(c, s, cache_row(c, m0)));
+    lim_hi = uni(cache_limit(c, s, cache_row(c, min(m0 + a.rpb, count) - 1)));
+    nr = uni(range_count(a, lim_hi));
+    live = sp < nr;
+  }
+};
 
 // Block of a launch over (sequence, kv head) x per blocks each. With the XCD order
 // the blocks of one (sequence, kv head) share an XCD, and so its K and V in that L2.
@@ -188,23 +232,16 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ float ml[4][2][16 * RT];
   const CacheArgs &c = a.c;
-  const int group = c.heads / c.kvh;
-  const int nrb = (c.max_q * group + 16 * RT - 1) / (16 * RT);
-  int bh, li;                                    // (sequence, kv head); row block and key range
-  cache_block(c, nrb * a.splits, bh, li);
-  const int rb = uni(li / a.splits), sp = li - rb * a.splits, b = uni(bh / c.kvh), h = bh - b * c.kvh;
-  const CacheSeq s = uniform_seq(c, b);
-  const int m0 = rb * 16 * RT, count = s.nq * group;
-  if (m0 >= count) return;
+  const AttnBlock k_(a);
+  if (!k_.live) return;
+  const CacheSeq s = k_.s;
+  const int h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr;
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mlast = min(m0 + 16 * RT, count) - 1;
-  Range rg(a, s, group, m0, count);
-  uniform_range(rg);
-  if (sp >= rg.nr) return;
-  const int lim_lo = rg.lim_lo, tiles = (rg.lim_hi + KT - 1) / KT;
-  const int t0 = rg.nr > 1 ? sp * (a.range / KT) : 0, t1 = rg.nr > 1 ? min(t0 + a.range / KT, tiles) : tiles;
+  const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KT - 1) / KT;
+  const int t0 = nr > 1 ? sp * (a.range / KT) : 0, t1 = nr > 1 ? min(t0 + a.range / KT, tiles) : tiles;
 
   const float sc = LOG2E / sqrtf((float)HD);
   bf16x8 qf[RT][NC];
@@ -237,7 +274,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     for (int i = 0; i < F::VR; ++i) vro[i] = r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
   PageWalk pw;
-  pw.init(c, b, (KT * t0) >> c.plog);
+  pw.init(c, k_.b, (KT * t0) >> c.plog);
   const int pmask = (1 << c.plog) - 1;
   // Tile t into slot j: halves of 16 rows, each on one page. Rows past the cache's
   // end lie outside the buffer range and arrive as zeros, whatever they hold; so do tiles
@@ -428,7 +465,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
       for (int d = 0; d < 4; ++d) x[d] += wt * y[d];
     }
     const int i = cache_row(c, mr), head = h * group + mr - i * group;
-    if (rg.nr > 1) {
+    if (nr > 1) {
       const int64_t at = part_slot(a, sp, s.q0 + i, head);
       *(f32x4 *)(a.part + at * HD + 4 * e) = x;
       if (e == 0) *(float2 *)part_ml(a, at) = make_float2(mx, den);
@@ -546,24 +583,17 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
   constexpr int V_BASE = NB * TB;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const CacheArgs &c = a.c;
-  const int group = c.heads / c.kvh;
-  const int nrb = (c.max_q * group + 255) / 256;
-  int bh, li;
-  cache_block(c, nrb * a.splits, bh, li);
-  const int rb = uni(li / a.splits), sp = li - rb * a.splits, b = uni(bh / c.kvh), h = bh - b * c.kvh;
-  const CacheSeq s = uniform_seq(c, b);
-  const int m0 = rb * 256, count = s.nq * group;
-  if (m0 >= count) return;
+  const AttnBlock k_(a);
+  if (!k_.live) return;
+  const CacheSeq s = k_.s;
+  const int b = k_.b, h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr;
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool grp_a = wid < 4;
   const int mlast = min(m0 + 256, count) - 1;
-  Range rg(a, s, group, m0, count);
-  uniform_range(rg);
-  if (sp >= rg.nr) return;
-  const int lim_lo = rg.lim_lo, tiles = (rg.lim_hi + KV - 1) / KV;
-  const int t_first = rg.nr > 1 ? sp * (a.range / KV) : 0, t_end = rg.nr > 1 ? min(t_first + a.range / KV, tiles) : tiles;
+  const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KV - 1) / KV;
+  const int t_first = nr > 1 ? sp * (a.range / KV) : 0, t_end = nr > 1 ? min(t_first + a.range / KV, tiles) : tiles;
   // tiles of the range, relative to t_first: `nf` that every row sees whole, then masked ones
   const int tot = t_end - t_first, nf = min(max(lim_lo / KV - t_first, 0), tot);
 
@@ -596,18 +626,28 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
   };
   auto load_v = [&](int tile, const typename TL::Where &x) { tl.load(c.v, x, lds0 + V_BASE + (tile % NB) * TB, tl.vvo()); };
 
-  if (grp_a) {                                   // K_0 .. K_3, V_0 .. V_2
+  int page[NB];                                  // of the K tiles that the next NB steps ask for
+  if (grp_a) {                                   // K_0 .. K_3, V_0 .. V_2; the first products wait for K_0 and K_1 alone
     tl.init(c, s, b, h, wid, lane, t_first);
     wk = typename TL::Where{};
+    int first[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) first[j] = page_of(j);
 #pragma unroll
     for (int j = 0; j < NB; ++j)
       if (j < tot) {
-        load_k(j, page_of(j));
-        if (j < NB - 1) load_v(j, wk);
+        load_k(j, first[j]);
+        if (j > 0) load_v(j - 1, wv);
       }
-    wait_vm<0>();
+    if (tot < NB && tot > 0) load_v(tot - 1, wk);
+    if (nf >= 2 && tot >= NB)
+      wait_vm<(NB + 1) * TL::NS>();              // K_0, V_0's neighbour K_1
+    else
+      wait_vm<0>();
   }
-  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < NB; ++j) page[j] = page_of(NB + j);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
   f32x4 o[NI][2];
 #pragma unroll
@@ -641,6 +681,12 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
       l[t] = weights(S[0], pf[0][t], t, sc, m[t]);
     }
     if (nf > 1) qk(S[1], smem + TB);
+    if (grp_a) {                                 // K_2 and V_1: at most K_3 and V_2 are still under way
+      if (tot >= NB)
+        wait_vm<2 * TL::NS>();
+      else
+        wait_vm<0>();
+    }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // step 0 refills the slot of K_0
     constexpr int NMF = 2 * NI + 4 * NC;         // fragment reads per step, two MFMAs each
     constexpr int NPV = NMF / 2, EPM = 32 / NMF; // P V reads; exponentials per pair of MFMAs
@@ -753,9 +799,6 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
       }
       asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(8) : "memory");
     };
-    int page[NB];                                // of the K tiles that the next NB steps ask for
-#pragma unroll
-    for (int j = 0; j < NB; ++j) page[j] = page_of(NB + j);
     for (int t = 0; t < nf; t += NB) {
       int next[NB];
 #pragma unroll
@@ -860,7 +903,7 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
     const int mr = m0 + 32 * wid + 16 * t + lr;
     if (mr >= count) continue;
     const int i0 = cache_row(c, mr), head = h * group + mr - i0 * group;
-    if (rg.nr > 1) {
+    if (nr > 1) {
       const int64_t at = part_slot(a, sp, s.q0 + i0, head);
 #pragma unroll
       for (int i = 0; i < NI; ++i) *(f32x4 *)(a.part + at * HD + 16 * i + 4 * lg) = o[i][t];
@@ -883,49 +926,53 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
 
 // ---------------------------------------------------------------- parts of a split launch
 // o = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s with M the largest m_s, ranges
-// in order; thread: one row, 8 columns.
+// in order; thread: one row, 4 columns.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
-  constexpr int TPR = HD / 8;
+  constexpr int TPR = HD / 4;
   const CacheArgs &c = a.c;
-  const int group = c.heads / c.kvh, rows = c.max_q * group;
+  const int group = c.heads / c.kvh, b = blockIdx.y;
   const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int e = 8 * (int)(gid % TPR);
-  const int64_t q = gid / TPR;
-  const int bh = (int)(q / rows), mr = (int)(q % rows);
-  if (bh >= c.batch * c.kvh) return;
-  const int b = bh / c.kvh, h = bh % c.kvh;
+  const int e = 4 * (int)(gid % TPR), q = (int)(gid / TPR);   // q: chunk row x heads + head
   const CacheSeq s = cache_seq(c, b);
-  if (mr >= s.nq * group) return;
-  const int nr = Range(a, s, group, mr / a.rpb * a.rpb, s.nq * group).nr;
+  if (q >= s.nq * c.heads) return;
+  const int i = q / c.heads, head = q - i * c.heads, h = head / group, mr = i * group + head - h * group;
+  const int last = min(mr / a.rpb * a.rpb + a.rpb, s.nq * group) - 1;   // of the row's block
+  const int nr = range_count(a, cache_limit(c, s, cache_row(c, last)));
   if (nr == 1) return;                           // finished by its block
-  const int i = cache_row(c, mr), head = h * group + mr - i * group;
   const int64_t at0 = part_slot(a, 0, s.q0 + i, head), step = (int64_t)c.rows * c.heads;
-  float mx = -INFINITY;
-  for (int u = 0; u < nr; ++u) mx = fmaxf(mx, *part_ml(a, at0 + u * step));
-  const float ref = mx == -INFINITY ? 0.f : mx;
-  float den = 0.f, x[8] = {};
-  for (int u = 0; u < nr; ++u) {
-    const int64_t at = at0 + u * step;
-    const float2 ml = *(const float2 *)part_ml(a, at);
-    const float wt = __builtin_amdgcn_exp2f(ml.x - ref);
-    den += wt * ml.y;
-    const f32x4 y0 = *(const f32x4 *)(a.part + at * HD + e), y1 = *(const f32x4 *)(a.part + at * HD + e + 4);
+  float mx = -INFINITY, den = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int u0 = 0; u0 < nr; u0 += 8) {           // eight ranges' loads at a time
+    float2 ml[8];
+    f32x4 y[8];
 #pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      x[d] += wt * y0[d];
-      x[4 + d] += wt * y1[d];
-    }
+    for (int u = 0; u < 8; ++u)
+      if (u0 + u < nr) {
+        const int64_t at = at0 + (u0 + u) * step;
+        ml[u] = *(const float2 *)part_ml(a, at);
+        y[u] = *(const f32x4 *)(a.part + at * HD + e);
+      }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (u0 + u < nr) {
+        const float mn = fmaxf(mx, ml[u].x), ref = mn == -INFINITY ? 0.f : mn;
+        const float wo = __builtin_amdgcn_exp2f(mx - ref), wn = __builtin_amdgcn_exp2f(ml[u].x - ref);
+        mx = mn;
+        den = wo * den + wn * ml[u].y;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) x[d] = wo * x[d] + wn * y[u][d];
+      }
   }
   T *O = (T *)a.o + (int64_t)(s.q0 + i) * a.ldo + (int64_t)head * HD + e;
   if constexpr (sizeof(T) == 2) {
-    bf16x8 y;
+    bf16x4 y;
 #pragma unroll
-    for (int d = 0; d < 8; ++d) y[d] = (__bf16)(den == 0.f ? 0.f : x[d] / den);
-    *(bf16x8 *)O = y;
+    for (int d = 0; d < 4; ++d) y[d] = (__bf16)(den == 0.f ? 0.f : x[d] / den);
+    *(bf16x4 *)O = y;
   } else {
 #pragma unroll
-    for (int d = 0; d < 8; ++d) O[d] = den == 0.f ? 0.f : x[d] / den;
+    for (int d = 0; d < 4; ++d) O[d] = den == 0.f ? 0.f : x[d] / den;
   }
   if (a.lse && e == 0)
     a.lse[(int64_t)(s.q0 + i) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
@@ -948,22 +995,16 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   constexpr int NI = HD / 32, NC = HD / 8;
   typedef __attribute__((ext_vector_type(NI))) float vecn;
   const CacheArgs &c = a.c;
-  const int group = c.heads / c.kvh, nrb = (c.max_q * group + 31) / 32;
-  int bh, li;
-  cache_block(c, nrb * a.splits, bh, li);
-  const int rb = uni(li / a.splits), sp = li - rb * a.splits, b = uni(bh / c.kvh), h = bh - b * c.kvh;
-  const CacheSeq s = uniform_seq(c, b);
-  const int m0 = rb * 32, count = s.nq * group;
-  if (m0 >= count) return;
+  const AttnBlock k_(a);
+  if (!k_.live) return;
+  const CacheSeq s = k_.s;
+  const int b = k_.b, h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lg = lane >> 5;
   const int mlast = min(m0 + 32, count) - 1, mm = min(m0 + lr, mlast), row = cache_row(c, mm);
-  Range rg(a, s, group, m0, count);
-  uniform_range(rg);
-  if (sp >= rg.nr) return;
-  const int lim_lo = rg.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
-  const int tiles = (rg.lim_hi + 31) / 32;
-  const int t0 = rg.nr > 1 ? sp * (a.range / 32) : 0, t1 = rg.nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
+  const int lim_lo = k_.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
+  const int tiles = (k_.lim_hi + 31) / 32;
+  const int t0 = nr > 1 ? sp * (a.range / 32) : 0, t1 = nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
   const int32_t *tab = c.table + (int64_t)b * c.table_ld;
   const float *Q = (const float *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm - row * group) * HD + 4 * lg;
   const float *K = (const float *)c.k + 4 * lg, *V = (const float *)c.v + NI * lr;
@@ -1076,7 +1117,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   // wave w finishes entries e = 4 w .. 4 w + 3: NI x 4 consecutive dimensions per lane
   const int head = h * group + mm - row * group, dim0 = NI * (8 * w + 4 * lg);
   const int64_t at = part_slot(a, sp, s.q0 + row, head);
-  float *O = rg.nr > 1 ? a.part + at * HD + dim0
+  float *O = nr > 1 ? a.part + at * HD + dim0
                           : (float *)a.o + (int64_t)(s.q0 + row) * a.ldo + (int64_t)head * HD + dim0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -1085,10 +1126,10 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
       float y = 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u) y += wt[u] * po[u][i * 16 + 4 * w + e][lane];
-      O[NI * e + i] = rg.nr > 1 ? y : den == 0.f ? 0.f : y / den;
+      O[NI * e + i] = nr > 1 ? y : den == 0.f ? 0.f : y / den;
     }
   if (w != 0 || lg != 0) return;
-  if (rg.nr > 1) {
+  if (nr > 1) {
     *(float2 *)part_ml(a, at) = make_float2(mx, den);
   } else if (a.lse) {
     a.lse[(int64_t)(s.q0 + row) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
@@ -1349,9 +1390,10 @@ int rows_per_block(int dtype, const CacheArgs &c) {
   if (getenv("TUNE_RPB")) return atoi(getenv("TUNE_RPB"));
   return m <= 16 ? 16 : m <= 96 ? 32 : 256;
 }
-// blocks of one range of keys
+// most blocks of one range of keys each
 int64_t attn_blocks(int rpb, const CacheArgs &c) {
-  return (int64_t)c.batch * c.kvh * (((int64_t)c.max_q * (c.heads / c.kvh) + rpb - 1) / rpb);
+  const int64_t group = c.heads / c.kvh, per = (c.max_q * group + rpb - 1) / rpb;
+  return c.kvh * std::min<int64_t>(c.batch * per, c.rows * group / rpb + c.batch);
 }
 size_t attn_part_bytes(const CacheArgs &c, int splits) {
   return (size_t)splits * c.rows * c.heads * (c.hd + 2) * sizeof(float);
@@ -1360,10 +1402,8 @@ size_t attn_part_bytes(const CacheArgs &c, int splits) {
 // has their bounds. Few blocks are given more ranges until they fill the compute
 // units; with several sequences of unlike length twice as many, so that a long one is not left to run alone.
 void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *range, int *splits) {
-  const int group = c.heads / c.kvh;
   *rpb = rows_per_block(dtype, c);
-  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(attn_blocks(*rpb, c),
-                                                                c.kvh * ((int64_t)c.rows * group / *rpb + c.batch)));
+  const int64_t blocks = std::max<int64_t>(1, attn_blocks(*rpb, c));
   int mul = c.batch > 1 ? 2 : 1;
   if (getenv("TUNE_MUL")) mul = atoi(getenv("TUNE_MUL"));
   const int64_t want = std::max<int64_t>(1, (int64_t)device_cus() * mul / blocks);
@@ -1417,9 +1457,8 @@ size_t cache_attn_scratch(int dtype, const CacheArgs &c) {
 
 hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_t s) {
   CacheAttnArgs a = in;
-  a.c.xcd_order = a.c.batch * a.c.kvh % 8 == 0 ? 1 : 0;
   attn_plan(dtype, a.c, a.part ? a.part_bytes : 0, &a.rpb, &a.range, &a.splits);
-  if (attn_blocks(a.rpb, a.c) <= 0) return hipSuccess;
+  if (a.c.rows <= 0 || a.c.max_q <= 0) return hipSuccess;
   hipError_t e;
   if (dtype == 1) {
     e = a.c.hd == 128 ? launch_bf16<128>(a, s) : launch_bf16<64>(a, s);
@@ -1432,8 +1471,8 @@ hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.splits <= 1) return e;
-  const int64_t items = (int64_t)a.c.batch * a.c.max_q * a.c.heads * (a.c.hd / 8);
-  const dim3 grid((unsigned)((items + 255) / 256));
+  const int64_t items = (int64_t)a.c.max_q * a.c.heads * (a.c.hd / 4);
+  const dim3 grid((unsigned)((items + 255) / 256), a.c.batch);
   if (dtype == 1) {
     if (a.c.hd == 128)
       hipLaunchKernelGGL((k_cache_attn_combine<bf16_t, 128>), grid, dim3(256), 0, s, a);
