@@ -406,7 +406,8 @@ class Context:
     def _scratch(self, nbytes: int):
         """Device memory that lives as long as the work just enqueued on this context's stream."""
         torch = _torch()
-        if torch.cuda.current_stream(self.device) == self.stream:
+        # (torch.cuda.current_stream() builds a Stream object: 1.9 us a call, this 0.1)
+        if torch._C._cuda_getCurrentRawStream(self.stream.device_index) == self.stream.cuda_stream:
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)

@@ -241,15 +241,17 @@ struct EvictPart {
 };
 
 // Histogram of digit d of the slots of the part that share the digits found so far
+// (in COPIES copies)
+template <int COPIES>
 __device__ __forceinline__ void evict_count(const EvictPart &p, uint32_t (*hist)[EVB], int d, uint32_t prefix,
                                             uint32_t known) {
   const int tid = threadIdx.x, w = tid >> 6;
-  for (int i = tid; i < EVH * EVB; i += EVT) (&hist[0][0])[i] = 0;
+  for (int i = tid; i < COPIES * EVB; i += EVT) (&hist[0][0])[i] = 0;
   __syncthreads();
   p.each([&](int j, float x, int) __attribute__((always_inline)) {
     const uint32_t u = mass_order(x);
     if (j < p.j1 && p.middle(j) && (u & known) == prefix)
-      atomicAdd(&hist[w % EVH][(u >> ev_shift(d)) & (ev_bins(d) - 1)], 1u);
+      atomicAdd(&hist[w % COPIES][(u >> ev_shift(d)) & (ev_bins(d) - 1)], 1u);
   });
   __syncthreads();
 }
@@ -395,11 +397,13 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
     uint32_t prefix = 0, known = 0;
     int rank = m, bin, size = m + 1;
     for (int d = 0; d < 3 && m > 0 && size != rank; ++d) {   // until all of a bin are taken
-      evict_count(p, hist, d, prefix, known);
+      if (d == 0)
+        evict_count<EVH>(p, hist, d, prefix, known);
+      else
+        evict_count<1>(p, hist, d, prefix, known);
       const int per = ev_bins(d) / EVT, top = ev_bins(d) - 1 - per * tid;
       uint32_t first = 0, second = 0;
-#pragma unroll
-      for (int i = 0; i < EVH; ++i) {
+      for (int i = 0; i < (d == 0 ? EVH : 1); ++i) {
         first += hist[i][top];
         if (per > 1) second += hist[i][top - 1];
       }
@@ -410,34 +414,45 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
     evict_lists(p, prefix, known, m > 0, rank, 0, 0, 0, true);
     return;
   }
-  // histograms of stage d lie in set d & 1
+  // Histograms of stage d lie in set d & 1. found: the threshold's digits and rank after each stage's pick, and whether
+  // all keys of its bin are taken, so that no further digit is needed.
   uint32_t *above = p.words + 2 * EVP * EVB, *found = above + 2 * EVP;
   uint32_t prefix = 0, known = 0;
-  int rank = m, bin = 0;
-  if (STAGE > 1) {
-    prefix = found[2 * (STAGE & 1)];
-    rank = (int)found[2 * (STAGE & 1) + 1];
+  int rank = m, bin = 0, size = 0, digit = STAGE - 1;   // digit: the last one picked
+  bool done = m == 0;
+  if (STAGE > 1 && !done) {
+    const uint32_t *f = found + 4 * (STAGE - 2);
+    prefix = f[0];
+    rank = (int)f[1];
+    bin = (int)f[3];
+    done = f[2] != 0;
+    if (done) digit = STAGE - 2;                 // (of the stage before at the earliest: stage 2 may pass it on)
+    if (STAGE == 3 && done) digit = (int)f[2] - 1;
   }
-  for (int d = 0; d < STAGE; ++d) known |= (uint32_t)(ev_bins(d) - 1) << ev_shift(d);
-  if (STAGE > 0 && m > 0) {
-    constexpr int D = STAGE - 1;
-    const uint32_t *g = p.words + (D & 1) * EVP * EVB;
-    const int bins = ev_bins(D), per = bins / EVT, top = bins - 1 - per * tid;
+  const uint32_t *g = p.words + (digit & 1) * EVP * EVB;
+  if (STAGE > 0 && !done) {
+    const int bins = ev_bins(digit), per = bins / EVT, top = bins - 1 - per * tid;
     uint32_t first = 0, second = 0;
 #pragma unroll
     for (int q = 0; q < EVP; ++q) {
       first += g[q * EVB + top];
       if (per > 1) second += g[q * EVB + top - 1];
     }
-    evict_pick(first, second, top, rank, &bin, &rank);
-    prefix |= (uint32_t)bin << ev_shift(D);
-    if (STAGE < 3 && part == 0 && tid == 0) {
-      found[2 * ((STAGE + 1) & 1)] = prefix;
-      found[2 * ((STAGE + 1) & 1) + 1] = (uint32_t)rank;
+    evict_pick(first, second, top, rank, &bin, &rank, &size);
+    prefix |= (uint32_t)bin << ev_shift(digit);
+  }
+  for (int d = 0; d <= digit; ++d) known |= (uint32_t)(ev_bins(d) - 1) << ev_shift(d);
+  if (STAGE > 0 && STAGE < 3) {
+    if (part == 0 && tid == 0) {
+      uint32_t *f = found + 4 * (STAGE - 1);
+      f[0] = prefix;
+      f[1] = (uint32_t)rank;
+      f[2] = done || size == rank ? digit + 1 : 0;
+      f[3] = (uint32_t)bin;
     }
-    // keys of each part above the bin: of this part now, for stage 3 of all of them
-    __shared__ int gt[EVP], eq[EVP];
-    if (STAGE == 3 || w == part) {
+    // keys of this part above the bin
+    if (!done && w == part) {
+      const int bins = ev_bins(digit);
       int x = 0;
 #pragma unroll 16
       for (int i = lane; i < bins; i += 64) {
@@ -446,65 +461,63 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
       }
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-      if (lane == 0) {
-        if (STAGE < 3) {
-          above[w] = (uint32_t)x + (STAGE > 1 ? above[w] : 0u);
-        } else {
-          gt[w] = x + (int)above[w];
-          eq[w] = (int)g[w * EVB + bin];
-        }
-      }
+      if (lane == 0) above[w] = (uint32_t)x + (STAGE > 1 ? above[w] : 0u);
     }
-    if (STAGE == 3) {
-      __syncthreads();
-      int eq0 = 0, hr = 0, mr = 0, my_eq = 0, my_hr = 0, my_mr = 0;
-      for (int q = 0; q < EVP; ++q) {
-        const int q0 = p.bound(q), q1 = p.bound(q + 1);
-        if (q == part) {
-          my_eq = eq0;
-          my_hr = hr;
-          my_mr = mr;
-        }
-        const int fixed = max(0, min(q1, a.sink) - q0) + max(0, q1 - max(q0, p.n - a.recent));
-        const int kept = fixed + gt[q] + min(eq[q], max(0, rank - eq0));
-        eq0 += eq[q];
-        if (q < a.low)
-          hr += q1 - q0 - kept;
-        else
-          mr += kept;
-      }
-      if (part == 0 && tid == 0) p.list[0] = min(hr, a.moves);
-      evict_lists(p, prefix, ~0u, true, rank, my_eq, my_hr, my_mr, false);
-      return;
-    }
-  } else if (STAGE == 3) {                       // m = 0: only what is protected stays
-    int hr = 0, mr = 0, my_hr = 0, my_mr = 0;
-    for (int q = 0; q < EVP; ++q) {
-      const int q0 = p.bound(q), q1 = p.bound(q + 1);
-      if (q == part) {
-        my_hr = hr;
-        my_mr = mr;
-      }
-      const int fixed = max(0, min(q1, a.sink) - q0) + max(0, q1 - max(q0, p.n - a.recent));
-      if (q < a.low)
-        hr += q1 - q0 - fixed;
-      else
-        mr += fixed;
-    }
-    if (part == 0 && tid == 0) p.list[0] = min(hr, a.moves);
-    evict_lists(p, 0, 0, false, 0, 0, my_hr, my_mr, false);
-    return;
+    done = done || size == rank;
   }
-  if (STAGE < 3 && m > 0) {
-    evict_count(p, hist, STAGE, prefix, known);
-    uint32_t *g = p.words + ((STAGE & 1) * EVP + part) * EVB;
+  if (STAGE < 3) {
+    if (done) return;
+    if (STAGE == 0)
+      evict_count<EVH>(p, hist, STAGE, prefix, known);
+    else
+      evict_count<1>(p, hist, STAGE, prefix, known);
+    uint32_t *to = p.words + ((STAGE & 1) * EVP + part) * EVB;
     for (int i = tid; i < ev_bins(STAGE); i += EVT) {
       uint32_t x = 0;
 #pragma unroll
-      for (int q = 0; q < EVH; ++q) x += hist[q][i];
-      g[i] = x;
+      for (int q = 0; q < (STAGE == 0 ? EVH : 1); ++q) x += hist[q][i];
+      to[i] = x;
+    }
+    return;
+  }
+  // stage 3: what each part keeps, from its counts above and in the threshold's bin
+  __shared__ int gt[EVP], eq[EVP];
+  {
+    int x = 0;
+    if (m > 0 && !done) {
+      const int bins = ev_bins(digit);
+#pragma unroll 16
+      for (int i = lane; i < bins; i += 64) {
+        const int y = (int)g[w * EVB + i];
+        if (i > bin) x += y;
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    }
+    if (lane == 0) {
+      gt[w] = m > 0 ? x + (int)above[w] : 0;
+      eq[w] = m > 0 ? (int)g[w * EVB + bin] : 0;
     }
   }
+  __syncthreads();
+  // lane q (of every wave): part q; sums over the parts before it
+  const int q = lane % EVP, q0 = p.bound(q), q1 = p.bound(q + 1), my = eq[q];
+  auto before = [&](int x) {
+    int sum = x;
+#pragma unroll
+    for (int o = 1; o < EVP; o <<= 1) {
+      const int t = __shfl_up(sum, o, EVP);
+      if (q >= o) sum += t;
+    }
+    return sum - x;
+  };
+  const int eq0 = before(my);
+  const int fixed = max(0, min(q1, a.sink) - q0) + max(0, q1 - max(q0, p.n - a.recent));
+  const int kept = fixed + gt[q] + min(my, max(0, rank - eq0));
+  const int holes = q < a.low ? q1 - q0 - kept : 0, movers = q < a.low ? 0 : kept;
+  const int hr = before(holes), mr = before(movers);
+  if (part == 0 && tid == EVP - 1) p.list[0] = min(hr + holes, a.moves);
+  evict_lists(p, prefix, known, m > 0, rank, __shfl(eq0, part, EVP), __shfl(hr, part, EVP), __shfl(mr, part, EVP), false);
 }
 
 // The moves that k_evict_select listed. RB bytes of a row: 16 per thread, the
