@@ -194,7 +194,7 @@ struct EvictPart {
   float x[EVK];
   int place[EVK];
   uint32_t *words;   // histograms [2][EVP][EVB], keys above the threshold's digits so far [EVP], prefix and rank [2][2]
-  __device__ __forceinline__ EvictPart(const CacheEvictArgs &a_) : a(a_), h(blockIdx.y), b(blockIdx.z) {
+  __device__ __forceinline__ EvictPart(const CacheEvictArgs &a_) : a(a_), h(blockIdx.x), b(blockIdx.z) {
     const CacheArgs &c = a.c;
     n = __builtin_amdgcn_readfirstlane(min(max(c.kv_len[b], 0), c.cap));
     tab = c.table + (int64_t)b * c.table_ld;
@@ -202,8 +202,8 @@ struct EvictPart {
     words = (uint32_t *)list + 4 + 2 * (int64_t)a.moves;
     low_len = (a.keep + a.low - 1) / a.low;
     high_len = a.parts > a.low ? (max(n - a.keep, 0) + a.parts - a.low - 1) / (a.parts - a.low) : 0;
-    s0 = bound(blockIdx.x);
-    s1 = bound(blockIdx.x + 1);
+    s0 = bound(blockIdx.y);
+    s1 = bound(blockIdx.y + 1);
     const int run = ((s1 - s0 + 64 * EVW - 1) / (64 * EVW)) * 64;
     j0 = min(s0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * run, s1);
     j1 = min(j0 + run, s1);
@@ -274,7 +274,8 @@ __device__ __forceinline__ void evict_pick(uint32_t first, uint32_t second, int 
   if (lane == 63) wsum[w] = incl;
   __syncthreads();
   uint32_t before = incl - mine;
-  for (int i = 0; i < w; ++i) before += wsum[i];
+#pragma unroll
+  for (int i = 0; i < EVW; ++i) before += i < w ? wsum[i] : 0u;
   if (before < (uint32_t)rank && before + mine >= (uint32_t)rank) {   // one thread
     const uint32_t x = rank - before;
     got[0] = x > first ? top - 1 : top;
@@ -312,7 +313,8 @@ __device__ __forceinline__ void evict_lists(const EvictPart &p, uint32_t thresho
   p.each([&](int j, float x, int) __attribute__((always_inline)) { eq += __popcll(__ballot(cls(j, x) == 1)); });
   if (lane == 0) wcnt[0][w] = eq;
   __syncthreads();
-  for (int i = 0; i < w; ++i) eq0 += wcnt[0][i];
+#pragma unroll
+  for (int i = 0; i < EVW; ++i) eq0 += i < w ? wcnt[0][i] : 0;
   // f(slot, weight, place, kept) in order
   auto kept_each = [&](auto &&f) __attribute__((always_inline)) {
     int er = eq0;
@@ -334,11 +336,10 @@ __device__ __forceinline__ void evict_lists(const EvictPart &p, uint32_t thresho
   }
   __syncthreads();
   int total = 0;
+#pragma unroll
   for (int i = 0; i < EVW; ++i) {
-    if (i < w) {
-      hr += wcnt[1][i];
-      mr += wcnt[2][i];
-    }
+    hr += i < w ? wcnt[1][i] : 0;
+    mr += i < w ? wcnt[2][i] : 0;
     total += wcnt[1][i];
   }
   if (count && threadIdx.x == 0) p.list[0] = min(total, a.moves);
@@ -361,7 +362,7 @@ __device__ __forceinline__ void evict_lists(const EvictPart &p, uint32_t thresho
 __device__ __forceinline__ void evict_none(const EvictPart &p) {
   const CacheEvictArgs &a = p.a;
   int32_t *idx = a.index ? a.index + ((int64_t)p.b * a.c.kvh + p.h) * a.keep : nullptr;
-  const int first = blockIdx.x * EVT + threadIdx.x, step = gridDim.x * EVT;
+  const int first = blockIdx.y * EVT + threadIdx.x, step = gridDim.y * EVT;
   for (int j = first; j < p.n; j += step) {
     const int e = p.tab[j >> a.c.plog], at = p.spot(e, j);
     if (a.out != a.mass && (unsigned)e < (unsigned)a.c.pages) a.out[at] = a.mass[at];
@@ -387,7 +388,7 @@ template <int STAGE>
 __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
   __shared__ uint32_t hist[EVH][EVB];
   const EvictPart p(a);
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, part = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, part = blockIdx.y;
   if (p.n <= a.keep) {
     if (STAGE < 0 || STAGE == 3) evict_none(p);
     return;
@@ -433,10 +434,16 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
   if (STAGE > 0 && !done) {
     const int bins = ev_bins(digit), per = bins / EVT, top = bins - 1 - per * tid;
     uint32_t first = 0, second = 0;
+    if (per > 1) {
 #pragma unroll
-    for (int q = 0; q < EVP; ++q) {
-      first += g[q * EVB + top];
-      if (per > 1) second += g[q * EVB + top - 1];
+      for (int q = 0; q < EVP; ++q) {
+        const uint2 x = *(const uint2 *)(g + q * EVB + top - 1);
+        first += x.y;
+        second += x.x;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < EVP; ++q) first += g[q * EVB + top];
     }
     evict_pick(first, second, top, rank, &bin, &rank, &size);
     prefix |= (uint32_t)bin << ev_shift(digit);
@@ -578,7 +585,7 @@ size_t cache_evict_scratch(const CacheArgs &c, int keep) {
 hipError_t launch_cache_evict(int dtype, const CacheEvictArgs &in, hipStream_t s) {
   CacheEvictArgs a = in;
   evict_plan(a);
-  const dim3 sel(a.parts, a.c.kvh, a.c.batch);
+  const dim3 sel(a.c.kvh, a.parts, a.c.batch);   // with 8 kv heads the parts of one share an XCD, and their counts its L2
   if (a.parts == 1) {
     hipLaunchKernelGGL((k_evict_select<-1>), sel, dim3(EVT), 0, s, a);
   } else {
