@@ -122,7 +122,8 @@ __device__ __forceinline__ float *part_ml(const CacheAttnArgs &a, int64_t slot) 
 // `count` of sequence b and kv head h, range sp of nr of the keys that they see.
 // Blocks are numbered sequence by sequence with the lengths of the device, so those that the host's bounds
 // allow for but no chunk needs come last. Within a sequence kv heads go fastest: with 8 (or a divisor
-// or multiple) of them the blocks of one run on one XCD (or its group) and share K and V in that L2.
+// or multiple) of them the blocks of one run on one XCD (or its group) and share K and V in that L2; the last rows,
+// which see the most, come first (8,192 rows causal over themselves, 16 heads of 128: 312 us from the first, 271 so).
 struct AttnBlock {
   CacheSeq s;
   int b, h, m0, count, group, sp, nr;
@@ -163,11 +164,11 @@ struct AttnBlock {
     li = uni(li);
     s = uniform_seq(c, b);
     count = s.nq * group;
-    const int q = uni(li / c.kvh), nrb = range_count(a, s.n), rb = uni(q / nrb);
+    const int q = uni(li / c.kvh), nrg = range_count(a, s.n), back = uni(q / nrg), rb = (count + a.rpb - 1) / a.rpb - 1 - back;
     h = li - q * c.kvh;
-    sp = q - rb * nrb;
+    sp = q - back * nrg;
     m0 = rb * a.rpb;
-    if (m0 >= count) return;
+    if (m0 < 0) return;
     lim_lo = uni(cache_limit(c, s, cache_row(c, m0)));
     lim_hi = uni(cache_limit(c, s, cache_row(c, min(m0 + a.rpb, count) - 1)));
     nr = uni(range_count(a, lim_hi));

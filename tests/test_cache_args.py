@@ -93,6 +93,7 @@ def test_tensors_are_refused(wdc):
             h, c, q, a, ld, pos, qw, kw, o, ldq)
         assert app(a=None) == ARG and app(o=None) == ARG and app(ld=760) == ARG and app(ldq=248) == ARG
         assert app(a=odd) == app(o=odd) == app(ld=772) == app(ldq=260) == app(qw=odd) == app(kw=odd) == app(pos=two) == ALIGN
+        assert app(ld=(1 << 22) + 8) == app(ldq=(1 << 22) + 8) == SHAPE
         att = lambda x=p, ld=256, f=0, o=p, ldo=256, z=None, sc=None: lib.wdc_cache_attention(  # noqa: E731
             h, c, q, x, ld, f, o, ldo, z, sc, 64)
         assert att(x=None) == att(o=None) == att(ld=248) == att(ldo=248) == att(f=-1) == ARG
