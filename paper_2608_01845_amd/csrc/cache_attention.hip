@@ -208,8 +208,6 @@ struct Few {
   static constexpr int NK = KT / 16;
   static constexpr int LPH = 16 / RPL;           // LDS loads per 16 rows (4 or 2)
   static constexpr int TILE = KT * ROWB;
-  static constexpr int NB = 4;                   // slots of a wave: one in use, three under way
-  static constexpr int WAVE = 2 * NB * TILE;     // K slots, V slots
   // 16-byte chunk c of row r lies at c ^ key(r): the 16 rows of a K fragment, and
   // the 4 rows that 16 lanes of a transposed V read take (a pair of chunks each), spread over the banks
   static __device__ __forceinline__ int kkey(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
@@ -225,10 +223,14 @@ __device__ __forceinline__ bf16x8 v_frag(const char *p) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Slots of a wave's K and V tiles: one in use, the others under way. One row tile waits for memory; with two, a
+// second block per compute unit does more than a deeper queue.
+constexpr int few_slots(int rt) { return rt == 1 ? 4 : 2; }
+
 template <int HD, int RT>
 __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   using F = Few<HD>;
-  constexpr int NC = HD / 32, NI = HD / 16, KT = F::KT;
+  constexpr int NC = HD / 32, NI = HD / 16, KT = F::KT, NB = few_slots(RT), WAVE = 2 * NB * F::TILE;   // K slots, V slots
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ float ml[4][2][16 * RT];
   const CacheArgs &c = a.c;
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     for (int j = 0; j < NC; ++j) qf[t][j] = *(const bf16x8 *)(Q + 32 * j);
   }
 
-  char *mine = smem + w * F::WAVE;
+  char *mine = smem + w * WAVE;
   const uint32_t lds0 = lds_addr(mine);
   int kvo[F::LPH], vvo[F::LPH];                  // byte offsets in 16 rows of K and V
 #pragma unroll
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 #pragma unroll
       for (int i = 0; i < F::LPH; ++i) lds_load16(kd, to + i * 1024, kvo[i]);
 #pragma unroll
-      for (int i = 0; i < F::LPH; ++i) lds_load16(vd, to + F::NB * F::TILE + i * 1024, vvo[i]);
+      for (int i = 0; i < F::LPH; ++i) lds_load16(vd, to + NB * F::TILE + i * 1024, vvo[i]);
     }
   };
 
@@ -309,10 +311,10 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   // tile t in slot J, with tile t + 4 (NB - 1) asked for
   auto step = [&](auto jc, int t) __attribute__((always_inline)) {
     constexpr int J = decltype(jc)::value;
-    load(t + 4 * (F::NB - 1), (J + F::NB - 1) % F::NB);
-    wait_vm<(F::NB - 1) * LT>();
+    load(t + 4 * (NB - 1), (J + NB - 1) % NB);
+    wait_vm<(NB - 1) * LT>();
     asm volatile("" ::: "memory");
-    const char *kt = mine + J * F::TILE, *vt = kt + F::NB * F::TILE;
+    const char *kt = mine + J * F::TILE, *vt = kt + NB * F::TILE;
     f32x4 S[RT][F::NK];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -416,18 +418,19 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): the slot has been read before it is loaded again
   };
   if (t0 + w < t1) {
-    static_assert(F::NB == 4, "slots of the unrolled steps");
-    load(t0 + w, 0);
-    load(t0 + w + 4, 1);
-    load(t0 + w + 8, 2);
-    for (int t = t0 + w; t < t1; t += 16) {
+    static_assert(NB == 4 || NB == 2, "slots of the unrolled steps");
+#pragma unroll
+    for (int j = 0; j < NB - 1; ++j) load(t0 + w + 4 * j, j);
+    for (int t = t0 + w; t < t1; t += 4 * NB) {
       step(std::integral_constant<int, 0>{}, t);
       if (t + 4 >= t1) break;
       step(std::integral_constant<int, 1>{}, t + 4);
-      if (t + 8 >= t1) break;
-      step(std::integral_constant<int, 2>{}, t + 8);
-      if (t + 12 >= t1) break;
-      step(std::integral_constant<int, 3>{}, t + 12);
+      if constexpr (NB == 4) {
+        if (t + 8 >= t1) break;
+        step(std::integral_constant<int, 2 % NB>{}, t + 8);
+        if (t + 12 >= t1) break;
+        step(std::integral_constant<int, 3 % NB>{}, t + 12);
+      }
     }
     wait_vm<0>();                                // what is still under way goes to this wave's part of LDS
     asm volatile("" ::: "memory");
@@ -460,7 +463,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     for (int u = 0; u < 4; ++u) {
       const float wt = __builtin_amdgcn_exp2f(ml[u][0][r] - ref);
       den += wt * ml[u][1][r];
-      const f32x4 y = *(const f32x4 *)(smem + u * F::WAVE + (r * HD + 4 * (e ^ (r & 7))) * 4);
+      const f32x4 y = *(const f32x4 *)(smem + u * WAVE + (r * HD + 4 * (e ^ (r & 7))) * 4);
 #pragma unroll
       for (int d = 0; d < 4; ++d) x[d] += wt * y[d];
     }
@@ -482,8 +485,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 }
 
 // ---------------------------------------------------------------- bf16, many rows
-// 256 query rows per block of eight waves, 32 each (two tiles of 16), two waves per
-// SIMD; key tiles of 64 reach four K and four V slots of LDS by direct buffer loads
+// 32 query rows (two tiles of 16) a wave, W = 8 or 4 waves a block, two waves per SIMD at 8; key tiles of 64 reach four K and four V slots of LDS by direct buffer loads
 // of waves 0 to 3, up to four tiles ahead. Bound by the matrix cores, with the
 // exponentials close behind.
 //
@@ -574,8 +576,8 @@ __device__ __forceinline__ float weights(const f32x4 (&S)[4][2], bf16x8 (&pf)[2]
   return ls;
 }
 
-template <int HD, bool SMALL>
-__global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
+template <int HD, bool SMALL, int W>
+__global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs a) {
   using F = Few<HD>;
   using TL = TileLoads<HD, SMALL>;
   constexpr int NC = HD / 32, NI = HD / 16;
@@ -591,7 +593,7 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool grp_a = wid < 4;
-  const int mlast = min(m0 + 256, count) - 1;
+  const int mlast = min(m0 + 32 * W, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KV - 1) / KV;
   const int t_first = nr > 1 ? sp * (a.range / KV) : 0, t_end = nr > 1 ? min(t_first + a.range / KV, tiles) : tiles;
   // tiles of the range, relative to t_first: `nf` that every row sees whole, then masked ones
@@ -834,8 +836,8 @@ __global__ __launch_bounds__(512, 1) void k_cache_attn_many(CacheAttnArgs a) {
     // its V is NaN in a matrix product: a tile that holds one is multiplied key by key.
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < TB / (512 * 16); ++i) {
-      const u32x4_t y = *(const u32x4_t *)(vb + V_BASE + (i * 512 + tid) * 16);
+    for (int i = 0; i < TB / (1024 * W); ++i) {
+      const u32x4_t y = *(const u32x4_t *)(vb + V_BASE + (i * 64 * W + tid) * 16);
 #pragma unroll
       for (int q = 0; q < 4; ++q) odd |= (y[q] & 0x7f80u) == 0x7f80u || (y[q] & 0x7f800000u) == 0x7f800000u;
     }
@@ -1384,12 +1386,6 @@ __global__ __launch_bounds__(256) void k_cache_mass_combine(CacheMassArgs a) {
 }
 
 // ---------------------------------------------------------------- launches
-int rows_per_block(int dtype, const CacheArgs &c) {
-  if (dtype == 0) return 32;
-  const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
-  // (8,192 keys, 16 heads of 128: 64 rows 33 us in blocks of 32 rows, 40 of 256; 128 rows 47 and 43)
-  return m <= 16 ? 16 : m <= 96 ? 32 : 256;
-}
 // most blocks of one range of keys each
 int64_t attn_blocks(int rpb, const CacheArgs &c) {
   const int64_t group = c.heads / c.kvh, per = (c.max_q * group + rpb - 1) / rpb;
@@ -1399,28 +1395,60 @@ size_t attn_part_bytes(const CacheArgs &c, int splits) {
   return (size_t)splits * c.rows * c.heads * (c.hd + 2) * sizeof(float);
 }
 // Rows per block and key ranges. Lengths are known on the device only; the host
-// has their bounds. Few blocks are given more ranges until they fill the compute
-// units; with several sequences of unlike length twice as many, so that a long one is not left to run alone
-// (1 x 8,192 keys, 16 heads of 128, one row: 20.8 us, 25.5 with twice as many; ragged chunks 33.0 against 29.5).
-// A second launch and its reads cost about 5 us: 16 rows and fewer are not cut below 65,536 / hd keys (1,000 keys, 16
-// heads of 64, one row: 10.1 us whole, 13.0 in four), blocks with more work per key not below 256.
+// has their bounds.
+//
+// Up to 64 rows, and float32: blocks of 16 or 32 rows, and enough ranges to fill
+// the compute units; with several sequences of unlike length twice as many, so that a long
+// one is not left to run alone (one row over 8,192 keys, 16 heads of 128: 20.8 us, 25.5 with
+// twice as many; eight tokens over 1 to 32,768 keys 87 us, 104 with half). A second launch and its reads
+// cost about 5 us: 16 rows and fewer are not cut below 65,536 / hd keys (1,000 keys, 16 heads
+// of 64, one row: 10.1 us whole, 13.0 in four), others not below 256.
+//
+// More rows: blocks of 128 or 256 rows and the number of ranges by estimate: rounds of blocks on
+// the compute units, a start and end of 7 us each and a time per tile of 64 keys (measured alone
+// on a compute unit: 256 rows 1.0 us at hd 64, 1.45 at hd 128; 128 rows 0.77 and 1.05), then the
+// second launch and the scratch written and read. 384 rows over 3,456 keys, 16 heads of 64: 256 rows 26.6 us, 128 rows 23.0;
+// over 8,192 keys, 16 heads of 128: 49.6 against 58.8.
 void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *range, int *splits) {
-  *rpb = rows_per_block(dtype, c);
-  const int64_t blocks = std::max<int64_t>(1, attn_blocks(*rpb, c));
-  const int64_t want = std::max<int64_t>(1, (int64_t)device_cus() * (c.batch > 1 ? 2 : 1) / blocks);
-  const int64_t r = std::max<int64_t>(*rpb == 16 ? 65536 / c.hd : 256, (c.cap + want - 1) / want);
-  *range = (int)((r + 63) / 64 * 64);
-  *splits = (c.cap + *range - 1) / *range;
+  const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
+  // of several sequences about half the ranges that the bounds allow for are there
+  const int64_t slots = (int64_t)std::max(1, device_cus()) * (c.batch > 1 ? 2 : 1);
+  auto set = [&](int r, int64_t keys) {
+    *rpb = r;
+    *range = (int)((std::max<int64_t>(keys, 64) + 63) / 64 * 64);
+    *splits = std::max(1, (c.cap + *range - 1) / *range);
+  };
+  if (dtype == 0 || m <= 64) {
+    const int r = dtype == 1 && m <= 16 ? 16 : 32;
+    const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
+    const int64_t want = std::max<int64_t>(1, slots / blocks);
+    set(r, std::max<int64_t>(r == 16 ? 65536 / c.hd : 256, (c.cap + want - 1) / want));
+  } else {
+    const int64_t tiles = (c.cap + 63) / 64;
+    double best = 0;
+    for (int r = 256; r >= 128; r -= 128) {
+      const double tile = (r == 256 ? 1.0 : 0.77) * (c.hd == 128 ? 1.4 : 1.0);
+      const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
+      for (int64_t n = 1; n <= 32 && (n == 1 || tiles >= 4 * n); ++n) {
+        const double rounds = (double)((blocks * n + slots - 1) / slots);
+        double t = rounds * ((double)((tiles + n - 1) / n) * tile + 7.0);
+        if (n > 1) t += 5.0 + (double)attn_part_bytes(c, (int)n) * 2 / 4e6;
+        if (best == 0 || t < best) {
+          best = t;
+          set(r, (tiles + n - 1) / n * 64);
+        }
+      }
+    }
+  }
   while (*splits > 1 && attn_part_bytes(c, *splits) > scratch) {
     *range = (int)std::min<int64_t>((int64_t)*range * 2, 1 << 30);
     *splits = (c.cap + *range - 1) / *range;
   }
-  if (*splits < 1) *splits = 1;
 }
 
 template <int HD, int RT>
 hipError_t launch_few(const CacheAttnArgs &a, hipStream_t s) {
-  constexpr int LDS = 4 * Few<HD>::WAVE;
+  constexpr int LDS = 4 * 2 * few_slots(RT) * Few<HD>::TILE;
   static DeviceOnce once;
   const hipError_t lim = once_on_device(once, [] {
     return hipFuncSetAttribute((const void *)k_cache_attn_few<HD, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
@@ -1429,21 +1457,22 @@ hipError_t launch_few(const CacheAttnArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((k_cache_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
-template <int HD, bool SMALL>
+template <int HD, bool SMALL, int W>
 hipError_t launch_many(const CacheAttnArgs &a, hipStream_t s) {
   constexpr int LDS = 2 * NB * KV * Few<HD>::ROWB;
   static DeviceOnce once;
   const hipError_t lim = once_on_device(once, [] {
-    return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL, W>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(512), LDS, s, a);
+  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL, W>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(64 * W), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD>
 hipError_t launch_bf16(const CacheAttnArgs &a, hipStream_t s) {
   const int rpb = a.rpb;
-  if (rpb == 256) return a.c.plog < 6 ? launch_many<HD, true>(a, s) : launch_many<HD, false>(a, s);
+  if (rpb == 256) return a.c.plog < 6 ? launch_many<HD, true, 8>(a, s) : launch_many<HD, false, 8>(a, s);
+  if (rpb == 128) return a.c.plog < 6 ? launch_many<HD, true, 4>(a, s) : launch_many<HD, false, 4>(a, s);
   return rpb == 16 ? launch_few<HD, 1>(a, s) : launch_few<HD, 2>(a, s);
 }
 
