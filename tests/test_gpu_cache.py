@@ -165,6 +165,10 @@ ids = lambda c: f"{c[0]}-{c[1]}x{c[2]}x{c[3]}-p{c[4]}-{c[5]}-{c[6]}-f{c[7]}"  # 
 
 @pytest.mark.parametrize("case", ATTENTION, ids=ids)
 def test_attention_matches_definition(case):
+    check_attention(case)
+
+
+def check_attention(case):
     dtype, heads, kvh, hd, page, q, kv, frame = case
     s = cu.state(dtype, heads, kvh, hd, page, q, kv, seed=5, tail_rows=3)
     wdc, ctx = ctx_of(s)
@@ -180,6 +184,23 @@ def test_attention_matches_definition(case):
         if with_lse:
             within(z[:n], lse[:n], lse_bound[:n] + 4 * EPS32 * lse[:n].abs(), "lse")
             assert (z[n:] == 7).all()
+
+
+# Rows enough for blocks of 256 (16 query heads per kv head): each head dim, pages shorter than a tile of 64
+# keys and not, one range and several, a short sequence beside a long one
+ATTENTION_WIDE = [
+    ("bf16", 16, 1, 64, 16, [4090], [4200], 64),
+    ("bf16", 16, 1, 64, 64, [2500, 0, 2000], [3000, 40, 2001], 7),
+    ("bf16", 16, 1, 64, 128, [2500, 2000], [9000, 100], 100),     # ranges; rows before the first key
+    ("bf16", 16, 1, 128, 32, [2600, 2500], [2700, 2650], 0),
+    ("bf16", 16, 1, 128, 256, [4000, 96], [4050, 700], 33),
+    ("bf16", 12, 1, 128, 16, [5000], [5200], 1000),               # a group that does not divide the block's rows
+]
+
+
+@pytest.mark.parametrize("case", ATTENTION_WIDE, ids=ids)
+def test_attention_of_many_rows_matches_definition(case):
+    check_attention(case)
 
 
 @pytest.mark.parametrize("dtype,hd,q,kv,frame", [("bf16", 64, [40], [200], 8), ("bf16", 128, [1, 90], [5, 91], 1),
@@ -373,23 +394,6 @@ def test_evict_bad_pages_are_not_written():
 # ---------------------------------------------------------------- together
 
 
-def _roll(ctx, wdc, s, data, frame, cap, keep, out, lse, index):
-    """One chunk per entry of data: append, attend, accumulate, and trim to keep when the cache passes cap."""
-    cache, results = wdc.PagedCache(s.k, s.v), []
-    for qkv, pos in data:
-        n = qkv.shape[0]
-        s.kv_len += n // 2
-        ch = wdc.Chunks(s.q_start, s.kv_len, s.table, rows=n, max_q=n, max_kv=s.table.shape[1] * s.page)
-        q = torch.empty((n, s.heads * s.hd), dtype=s.td, device="cuda")
-        ctx.cache_append(cache, ch, qkv, q, pos=pos)
-        ctx.cache_attention(cache, ch, q, out, frame=frame, lse=lse)
-        ctx.cache_mass(cache, ch, q, lse, s.mass, frame=frame, decay=0.9)
-        results.append((q, out.clone(), lse.clone()))
-        if int(s.kv_len.max()) > cap:
-            ctx.cache_evict(cache, ch, s.mass, keep, sink=8, recent=n // 2, index=index)
-    return results
-
-
 @pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("f32", 64)])
 def test_rollout_of_chunks_append_attend_accumulate_evict(dtype, hd):
     """Two sequences, chunks of two frames each, a bounded cache; every step against float64 on the cache as it is."""
@@ -407,7 +411,14 @@ def test_rollout_of_chunks_append_attend_accumulate_evict(dtype, hd):
         pos = torch.stack([2 * step + i // frame, i % frame // 5, i % 5], 1).to(torch.int32).cuda()
         before = s.mass.clone()
         prev = s.kv_len.tolist()
-        ((q, o, z),) = _roll(ctx, wdc, s, [(qkv, pos)], frame, 1 << 30, 120, out, lse, index)
+        s.kv_len += n
+        cache = wdc.PagedCache(s.k, s.v)
+        ch = wdc.Chunks(s.q_start, s.kv_len, s.table, rows=2 * n, max_q=2 * n, max_kv=s.table.shape[1] * page)
+        q = torch.empty((2 * n, heads * hd), dtype=s.td, device="cuda")
+        ctx.cache_append(cache, ch, qkv, q, pos=pos)
+        ctx.cache_attention(cache, ch, q, out, frame=frame, lse=lse)
+        ctx.cache_mass(cache, ch, q, lse, s.mass, frame=frame, decay=0.9)
+        o, z = out, lse
         s.kv, s.x, s.q = s.kv_len.tolist(), q, [n, n]
         assert s.kv == [p + n for p in prev]
         s.rows = 2 * n
