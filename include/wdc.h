@@ -341,8 +341,10 @@ typedef struct {
  * The host gives bounds: rows of the packed tensors, the longest chunk and the longest cache. Device
  * values beyond them (or beyond the table's pages) are cut to them: rows past max_q of a chunk are
  * left out, keys past max_kv are not there. A slot whose table entry is not a page of the cache is read
- * as one of its pages and never written. Rows of no chunk are not written. batch * max_q * heads <= 2^26,
- * batch * kv_heads * (keys) <= 2^29, batch * kv_heads <= 65535, pages * kv_heads * page < 2^31 and row strides
+ * as one of its pages and never written. Rows of no chunk are not written. Sequences may share the pages
+ * of a common past for append (below the chunks' own slots) and attention; mass and eviction write every
+ * key's slot, so there a page is in one sequence. batch * max_q * heads <= 2^26,
+ * batch * kv_heads * (keys) <= 2^28, batch * kv_heads <= 65535, pages * kv_heads * page < 2^31 and row strides
  * <= 2^22 elements, else WDC_E_SHAPE. */
 typedef struct {
   const int32_t *d_q_start, *d_kv_len, *d_table;
@@ -369,7 +371,7 @@ wdc_status wdc_cache_append(wdc_ctx *ctx, const wdc_paged_cache *cache, const wd
  * frames of `frame` rows those up to its own (frame = 1: up to itself; 0: all).
  * What a row does not see has no influence on it, whatever its value; a row that sees nothing gets
  * zeros. d_q [rows, ldq], d_o [rows, ldo], head h at columns [h * head_dim, ..), multiples of 16
- * bytes; d_lse [rows, heads] float32 (or NULL): ln sum exp of the scores, -inf for a row that sees
+ * bytes (d_o may be d_q with ldo = ldq); d_lse [rows, heads] float32 (or NULL): ln sum exp of the scores, -inf for a row that sees
  * nothing. float32 accumulation and statistics; bf16: attention weights rounded to bf16 before the product
  * with v. d_scratch: memory for splitting the keys of few rows over the device,
  * wdc_cache_attention_scratch() bytes; with less (or NULL) the call runs with fewer parts. */

@@ -203,6 +203,13 @@ def _torch():
     return torch
 
 
+def _int32(**values):
+    """Refuse what a 32-bit argument would cut."""
+    for name, x in values.items():
+        if not 0 <= x <= 0x7fffffff:
+            raise ValueError(f"{name} = {x}: need 0 <= {name} < 2^31")
+
+
 class PagedCache:
     """Pages of one layer's keys and values: k, v [pages, kv_heads, page, head_dim]
     contiguous device tensors (wdc_paged_cache)."""
@@ -230,10 +237,12 @@ class Chunks:
                 raise ValueError(f"{name}: a contiguous int32 tensor of {dim} dimension(s) on one device is needed")
         if q_start.numel() != kv_len.numel() + 1 or table.shape[0] != kv_len.numel():
             raise ValueError("q_start [batch + 1], kv_len [batch] and table [batch, pages] disagree on the batch")
+        max_q, max_kv = rows if max_q is None else max_q, 0x7fffffff if max_kv is None else max_kv
+        _int32(rows=rows, max_q=max_q, max_kv=max_kv)
         self.q_start, self.kv_len, self.table = q_start, kv_len, table
         self.rows, self.batch, self.device = rows, kv_len.numel(), kv_len.get_device()
         self.desc = ChunksDesc(q_start.data_ptr(), kv_len.data_ptr(), table.data_ptr(), kv_len.numel(), table.shape[1],
-                               rows, rows if max_q is None else max_q, 0x7fffffff if max_kv is None else max_kv, 0)
+                               rows, max_q, max_kv, 0)
         self.ref = C.byref(self.desc)
 
 
@@ -412,6 +421,14 @@ class Context:
         with torch.cuda.stream(self.stream):
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
+    def _launch(self, call, *args):
+        """One call; the null stream is the current device's, so that device has to be this context's."""
+        torch, dev = _torch(), self.stream.device_index
+        if torch._C._cuda_getDevice() == dev:
+            return self._check(call(self.h, *args))
+        with torch.cuda.device(dev):
+            self._check(call(self.h, *args))
+
     def cache_append(self, cache: PagedCache, chunks: Chunks, qkv, q, pos=None, q_weight=None, k_weight=None):
         """Normalise and rotate q and k of qkv [rows, (heads + 2 kv_heads) head_dim], store k and v in the
         cache and write q [rows, heads head_dim]. Rows may be strided."""
@@ -423,21 +440,22 @@ class Context:
         pos_p = pos if pos is None else ptr("pos", pos, torch.int32, (rows, 3), dev)
         qw_p = q_weight if q_weight is None else ptr("q_weight", q_weight, torch.float32, (hd,), dev)
         kw_p = k_weight if k_weight is None else ptr("k_weight", k_weight, torch.float32, (hd,), dev)
-        self._check(self.lib.wdc_cache_append(self.h, cache.ref, chunks.ref, qkv_p, _ld(qkv), pos_p, qw_p, kw_p, q_p,
-                                              _ld(q)))
+        self._launch(self.lib.wdc_cache_append, cache.ref, chunks.ref, qkv_p, _ld(qkv), pos_p, qw_p, kw_p, q_p, _ld(q))
         return q
 
     def cache_attention(self, cache: PagedCache, chunks: Chunks, q, out, frame: int = 0, lse=None):
         """Attention of the chunks' rows q [rows, heads head_dim] over the cache into out (same shape);
-        lse [rows, heads] float32 takes the rows' log-sum-exp. frame: rows per frame (0: all see all)."""
+        lse [rows, heads] float32 takes the rows' log-sum-exp. frame: rows per frame (0: all see all).
+        out may be q itself."""
         self._cache_check(cache, chunks)
+        _int32(frame=frame)
         shape, dev, ptr = (chunks.rows, self.cfg.heads * self.cfg.head_dim), cache.device, self._tensor
         q_p, out_p = ptr("q", q, self.tdtype, shape, dev, True), ptr("out", out, self.tdtype, shape, dev, True)
         lse_p = lse if lse is None else ptr("lse", lse, _torch().float32, (chunks.rows, self.cfg.heads), dev)
         n = self.lib.wdc_cache_attention_scratch(self.h, cache.ref, chunks.ref)
         scratch = self._scratch(n) if n else None
-        self._check(self.lib.wdc_cache_attention(self.h, cache.ref, chunks.ref, q_p, _ld(q), frame, out_p, _ld(out), lse_p,
-                                                 _ptr(scratch), n))
+        self._launch(self.lib.wdc_cache_attention, cache.ref, chunks.ref, q_p, _ld(q), frame, out_p, _ld(out), lse_p,
+                     _ptr(scratch), n)
         return out
 
     def cache_mass(self, cache: PagedCache, chunks: Chunks, q, lse, mass, frame: int = 0, decay: float = 1.0, out=None):
@@ -445,14 +463,15 @@ class Context:
         if not given); mass [pages, kv_heads, page] float32, lse from cache_attention with the same frame."""
         f32, dev, ptr, shape = _torch().float32, cache.device, self._tensor, cache.k.shape[:3]
         self._cache_check(cache, chunks)
+        _int32(frame=frame)
         q_p = ptr("q", q, self.tdtype, (chunks.rows, self.cfg.heads * self.cfg.head_dim), dev, True)
         lse_p = ptr("lse", lse, f32, (chunks.rows, self.cfg.heads), dev)
         mass_p = ptr("mass", mass, f32, shape, dev)
         out_p = mass_p if out is None else ptr("out", out, f32, shape, dev)
         n = self.lib.wdc_cache_mass_scratch(self.h, cache.ref, chunks.ref)
         scratch = self._scratch(n) if n else None
-        self._check(self.lib.wdc_cache_mass(self.h, cache.ref, chunks.ref, q_p, _ld(q), frame, lse_p, decay, mass_p, out_p,
-                                            _ptr(scratch), n))
+        self._launch(self.lib.wdc_cache_mass, cache.ref, chunks.ref, q_p, _ld(q), frame, lse_p, decay, mass_p, out_p,
+                     _ptr(scratch), n)
         return mass if out is None else out
 
     def cache_evict(self, cache: PagedCache, chunks: Chunks, mass, keep: int, sink: int = 0, recent: int = 0,
@@ -462,6 +481,7 @@ class Context:
         (mass itself), index [batch, kv_heads, keep] int32 the former slots."""
         torch = _torch()
         self._cache_check(cache, chunks)
+        _int32(keep=keep, sink=sink, recent=recent)
         dev, ptr, shape, batch = cache.device, self._tensor, cache.k.shape[:3], chunks.batch
         kv_len_out = chunks.kv_len if kv_len_out is None else kv_len_out
         mass_p = ptr("mass", mass, torch.float32, shape, dev)
@@ -470,8 +490,8 @@ class Context:
         idx_p = index if index is None else ptr("index", index, torch.int32, (batch, cache.kv_heads, keep), dev)
         n = self.lib.wdc_cache_evict_scratch(self.h, cache.ref, chunks.ref, keep)
         scratch = self._scratch(n) if n else None
-        self._check(self.lib.wdc_cache_evict(self.h, cache.ref, chunks.ref, mass_p, out_p, keep, sink, recent, len_p, idx_p,
-                                             _ptr(scratch), n))
+        self._launch(self.lib.wdc_cache_evict, cache.ref, chunks.ref, mass_p, out_p, keep, sink, recent, len_p, idx_p,
+                     _ptr(scratch), n)
         return kv_len_out
 
     def set_timing(self, on: bool):

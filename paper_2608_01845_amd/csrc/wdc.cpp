@@ -1665,7 +1665,7 @@ wdc_status wdc_linear(wdc_ctx *ctx, const void *d_a, int64_t lda, const void *d_
 }  // extern "C"
 
 namespace {
-constexpr int64_t kCacheRows = int64_t(1) << 26, kCacheKeys = int64_t(1) << 29;
+constexpr int64_t kCacheRows = int64_t(1) << 26, kCacheKeys = int64_t(1) << 28;   // (launches stay below 2^32 threads)
 
 // Descriptor checks shared by the cache operators; fills *a. `rows`: the call takes chunk rows.
 wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q, bool rows, bool values, CacheArgs *a) {

@@ -39,7 +39,7 @@ BAD = [
     (dict(table_ld=0), ARG), (dict(max_kv=-1), ARG), (dict(page=48), UNSUPPORTED), (dict(page=8), UNSUPPORTED),
     (dict(page=512), UNSUPPORTED), (dict(kv_heads=3), SHAPE), (dict(kv_heads=0), SHAPE), (dict(d_k=4104), ALIGN),
     (dict(d_table=66), ALIGN), (dict(d_kv_len=65), ALIGN), (dict(batch=20000), SHAPE),
-    (dict(max_kv=0x7fffffff, table_ld=0x7fffffff), SHAPE),
+    (dict(max_kv=0x7fffffff, table_ld=0x7fffffff), SHAPE), (dict(batch=1, max_kv=(1 << 26) + 1, table_ld=1 << 22), SHAPE),
 ]
 ROWS = [(dict(d_q_start=None), ARG), (dict(rows=-1), ARG), (dict(max_q=-1), ARG), (dict(d_q_start=62), ALIGN),
         (dict(rows=1 << 25, max_q=1), SHAPE), (dict(batch=1000, rows=1 << 20, max_q=1 << 20, max_kv=10), SHAPE)]
@@ -145,3 +145,11 @@ def test_python_descriptors_check_tensors(wdc):
               (i(6)[::2], i(2), i(2, 5)), (i(3), i(2), i(5, 2).T)):
         with pytest.raises(ValueError):
             wdc.Chunks(*a, rows=4)
+
+
+@pytest.mark.parametrize("bad", [dict(rows=1 << 32), dict(rows=-1), dict(max_q=1 << 31), dict(max_kv=1 << 32), dict(max_kv=-1)],
+                         ids=str)
+def test_bounds_that_32_bits_would_cut_are_refused(wdc, bad):
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError):
+        wdc.Chunks(i(3), i(2), i(2, 5), **{**dict(rows=4), **bad})

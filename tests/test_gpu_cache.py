@@ -28,6 +28,15 @@ def within(got, want, bound, what):
     assert not bad.any(), (what, int(bad.sum()), got[bad][:4].tolist(), want[bad][:4].tolist())
 
 
+def few(x):
+    """A list in a test's name: itself, or its length."""
+    return x if len(x) <= 8 else f"{len(x)}seqs"
+
+
+# more sequences than a wave has lanes: chunks of none to three rows, caches of none to 85 keys
+MANY_Q = [(3 * i + i // 7) % 4 for i in range(150)]
+MANY_KV = [q + 11 * i % 83 for i, q in enumerate(MANY_Q)]
+
 # ---------------------------------------------------------------- append
 
 
@@ -64,10 +73,12 @@ APPEND = [
     ("bf16", 4, 4, 64, 32, [50, 3], [20, 3], True, False, "near", (32, 16, 16)),   # a chunk longer than its cache
     ("f32", 4, 2, 64, 16, [5, 0, 1, 33], [5, 7, 100, 40], True, True, "far", None),
     ("f32", 5, 5, 128, 128, [1500], [1501], True, False, "far", None),
+    ("bf16", 4, 2, 64, 16, MANY_Q, MANY_KV, True, False, "near", None),
+    ("f32", 4, 2, 64, 16, [7 * x for x in MANY_Q], [7 * x for x in MANY_KV], True, True, "near", None),
 ]
 
 
-@pytest.mark.parametrize("case", APPEND, ids=lambda c: f"{c[0]}-{c[1]}x{c[2]}x{c[3]}-p{c[4]}-{c[5]}")
+@pytest.mark.parametrize("case", APPEND, ids=lambda c: f"{c[0]}-{c[1]}x{c[2]}x{c[3]}-p{c[4]}-{few(c[5])}")
 def test_append_matches_definition(case):
     dtype, heads, kvh, hd, page, q, kv, norm, weights, pos, rope = case
     s = cu.state(dtype, heads, kvh, hd, page, q, kv, seed=1, tail_rows=2)
@@ -159,8 +170,11 @@ ATTENTION = [
     ("f32", 4, 2, 64, 32, [100, 0, 33], [400, 5, 33], 1),
     ("f32", 3, 1, 128, 64, [70, 40], [333, 25], 16),
     ("f32", 2, 2, 128, 16, [20], [0], 0),
+    ("bf16", 4, 2, 64, 16, MANY_Q, MANY_KV, 1),
+    ("bf16", 4, 1, 128, 16, [20 * x for x in MANY_Q], [20 * x for x in MANY_KV], 7),
+    ("f32", 4, 2, 64, 16, MANY_Q, MANY_KV, 2),
 ]
-ids = lambda c: f"{c[0]}-{c[1]}x{c[2]}x{c[3]}-p{c[4]}-{c[5]}-{c[6]}-f{c[7]}"  # noqa: E731
+ids = lambda c: f"{c[0]}-{c[1]}x{c[2]}x{c[3]}-p{c[4]}-{few(c[5])}-{few(c[6])}-f{c[7]}"  # noqa: E731
 
 
 @pytest.mark.parametrize("case", ATTENTION, ids=ids)
@@ -335,10 +349,11 @@ EVICT = [
     ("f32", 1, 64, 64, [9000], 17, 5, 6, "ties"),
     ("bf16", 1, 128, 256, [9000, 8999], 8990, 0, 0, "equal"),
     ("bf16", 64, 64, 64, [4200] * 4, 4000, 10, 20, "ties"),
+    ("bf16", 2, 64, 16, MANY_KV, 20, 3, 4, "random"),
 ]
 
 
-@pytest.mark.parametrize("case", EVICT, ids=lambda c: f"{c[0]}-{c[1]}x{c[2]}-p{c[3]}-{c[4]}-keep{c[5]}-{c[6]}-{c[7]}-{c[8]}")
+@pytest.mark.parametrize("case", EVICT, ids=lambda c: f"{c[0]}-{c[1]}x{c[2]}-p{c[3]}-{few(c[4])}-keep{c[5]}-{c[6]}-{c[7]}-{c[8]}")
 @pytest.mark.parametrize("in_place", [False, True])
 def test_evict_matches_definition(case, in_place):
     dtype, kvh, hd, page, kv, keep, sink, recent, kind = case
@@ -389,6 +404,94 @@ def test_evict_bad_pages_are_not_written():
     own[[int(p) for p in s.table[0].tolist() if 0 <= p < s.pages]] = True
     assert torch.equal(s.k[~own.cuda()], k0[~own.cuda()]) and torch.equal(s.mass[~own.cuda()], m0[~own.cuda()])
     assert s.kv_len.tolist() == [100]
+
+
+# ---------------------------------------------------------------- edges of all four
+
+
+def run_all(ctx, wdc, s, frame=5, keep=20, **kw):
+    """append, attention, mass, eviction on state s; every result."""
+    cache, ch = wdc.PagedCache(s.k, s.v), cu.chunks(wdc, s, **kw)
+    q, out = torch.full_like(s.x, 7.0), torch.full_like(s.x, 7.0)
+    lse = torch.full((s.rows, s.heads), 7.0, device="cuda")
+    pos = torch.arange(3 * s.rows, dtype=torch.int32, device="cuda").reshape(s.rows, 3)
+    index = torch.empty((len(s.q), s.kvh, keep), dtype=torch.int32, device="cuda")
+    ctx.cache_append(cache, ch, s.qkv, q, pos=pos)
+    ctx.cache_attention(cache, ch, q, out, frame=frame, lse=lse)
+    ctx.cache_mass(cache, ch, q, lse, s.mass, frame=frame, decay=0.5)
+    mass = s.mass.clone()
+    ctx.cache_evict(cache, ch, s.mass, keep, 3, 4, index=index)
+    return q, out, lse, mass, index
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_rows_and_no_keys(dtype):
+    """Calls without rows change masses by the decay only; rows over no keys at all get zeros, however many they are."""
+    s = cu.state(dtype, 4, 2, 64, 16, [0, 0], [30, 0], seed=21)
+    wdc, ctx = ctx_of(s)
+    k0, m0 = s.k.clone(), s.mass.clone()
+    run_all(ctx, wdc, s, keep=40)
+    assert torch.equal(s.k.nan_to_num(9), k0.nan_to_num(9))
+    pg, sl = cu.where(s, 0)
+    assert torch.equal(s.mass[pg, :, sl], 0.5 * m0[pg, :, sl])
+    for rows in (5, 20, 300, 2000):
+        s = cu.state(dtype, 4, 1, 64, 16, [rows], [0], seed=22)
+        q, out, lse, _, index = run_all(ctx_of(s)[1], wdc, s, keep=40)
+        assert torch.isfinite(q).all() and (out == 0).all() and (lse == -math.inf).all() and (index == -1).all()
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 64)])
+def test_pool_beyond_32_bit_offsets(dtype, hd):
+    """Pages past 4 GiB of a pool: the results of the same pages in a small pool."""
+    q, kv, page = [3, 200], [400, 300], 64
+    small = cu.state(dtype, 4, 2, hd, page, q, kv, seed=23, fill=0.0)
+    wdc, ctx = ctx_of(small)
+    td = small.td
+    pages = (1 << 33) // (2 * page * hd * td.itemsize)            # 8 GiB each of k and v
+    far = torch.tensor([pages - 1 - 37 * i for i in range(small.pages)], device="cuda")
+    big = cu.state(dtype, 4, 2, hd, page, q, kv, seed=23, fill=0.0)
+    big.k, big.v = (torch.empty((pages, 2, page, hd), dtype=td, device="cuda") for _ in range(2))
+    big.mass = torch.zeros((pages, 2, page), device="cuda")
+    big.k[far], big.v[far], big.mass[far] = small.k, small.v, small.mass
+    big.table = torch.where(small.table < 0, -1, far[small.table.clamp(min=0).long()]).to(torch.int32)
+    for a, b in zip(run_all(ctx, wdc, small, keep=250), run_all(ctx, wdc, big, keep=250)):
+        assert torch.equal(a, b[far] if a.shape != b.shape else b)
+    for a, b in ((small.k, big.k), (small.v, big.v), (small.mass, big.mass)):
+        assert torch.equal(a, b[far])
+
+
+@pytest.mark.parametrize("dtype,heads,kvh,hd,q,kv", [("bf16", 4, 4, 64, 3, 900), ("bf16", 6, 2, 128, 40, 300),
+                                                     ("bf16", 16, 1, 64, 300, 700), ("f32", 4, 2, 64, 50, 400)])
+def test_attention_in_place_shared_pages_and_a_long_frame(dtype, heads, kvh, hd, q, kv):
+    """out may be q; two sequences may share the pages of their past; a frame longer than any chunk is one frame."""
+    s = cu.state(dtype, heads, kvh, hd, 16, [q, q], [kv, kv], seed=24, fill=0.0)
+    shared = (kv - q) // 16
+    s.table[1, :shared] = s.table[0, :shared]
+    wdc, ctx = ctx_of(s)
+    cache, ch = wdc.PagedCache(s.k, s.v), cu.chunks(wdc, s)
+    o, lse, pv, qk = cu.attention64(s, 0)
+    bound, _ = attention_bound(s, pv, o, qk, kv)
+    ref = ctx.cache_attention(cache, ch, s.x, torch.empty_like(s.x))
+    within(ref.reshape(o.shape), o, bound, "o")
+    assert torch.equal(ref, ctx.cache_attention(cache, ch, s.x, torch.empty_like(s.x), frame=0x7fffffff))
+    x = s.x.clone()
+    ctx.cache_attention(cache, ch, x, x)
+    assert torch.equal(x, ref)
+
+
+def test_bounds_that_32_bits_would_cut_are_refused():
+    s = cu.state("bf16", 4, 2, 64, 16, [2], [20], seed=25)
+    wdc, ctx = ctx_of(s)
+    cache, ch, x = wdc.PagedCache(s.k, s.v), cu.chunks(wdc, s), s.x
+    lse = torch.zeros((2, 4), device="cuda")
+    for frame in (1 << 32, -1):
+        with pytest.raises(ValueError):
+            ctx.cache_attention(cache, ch, x, x, frame=frame)
+        with pytest.raises(ValueError):
+            ctx.cache_mass(cache, ch, x, lse, s.mass, frame=frame)
+    for a in (((1 << 32) + 9, 0, 0), (9, 1 << 32, 0), (9, 0, 1 << 32)):
+        with pytest.raises(ValueError):
+            ctx.cache_evict(cache, ch, s.mass, *a)
 
 
 # ---------------------------------------------------------------- together
