@@ -181,39 +181,46 @@ __device__ __forceinline__ uint32_t mass_order(float m) {
 }
 
 constexpr int EVT = 1024, EVW = EVT / 64;   // threads and waves of a selection block
-constexpr int EVH = 4;                      // copies of a block's histogram, to spread equal digits over
-constexpr int EVP = 16;                     // parts of a long (sequence, kv head); one wave reads one part's histogram
-constexpr int EVB = 2048;                   // bins of a histogram
+constexpr int EVP = 16;                     // parts of a long (sequence, kv head); one wave sums up one part
 constexpr int EVK = 8;                      // weights that a thread keeps in registers
+constexpr int EVA = 8192;                   // keys that share digit 0 with the threshold, listed as they come
+constexpr int EVH = 4096;                   // words of LDS for histograms: copies of one, to spread equal digits over
 static_assert(EVP == EVW, "a wave per part");
-// digits of the order values, from the top: 11, 11 and 10 bits
-__device__ __forceinline__ int ev_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
-__device__ __forceinline__ int ev_bins(int d) { return d == 2 ? 1024 : 2048; }
+// digits of the order values, from the top: 10, 11 and 11 bits
+__device__ __forceinline__ constexpr int ev_shift(int d) { return d == 0 ? 22 : d == 1 ? 11 : 0; }
+__device__ __forceinline__ constexpr int ev_bins(int d) { return d == 0 ? 1024 : 2048; }
 
-// Scratch of one (sequence, kv head), in 32-bit words: the number of moves, then
-// moves (to, from); with parts, two sets of their histograms and a few words each.
-__host__ __device__ inline int64_t evict_words(int moves, int parts) {
-  return 4 + 2 * (int64_t)moves + (parts > 1 ? 2 * EVP * EVB + 2 * EVP + 8 : 0);
+// Scratch of one (sequence, kv head), in 32-bit words: the number of moves, then moves (to, from); with parts,
+// their histograms of digit 0 and cumulated ones of digit 1, the order values of all slots, those that share
+// digit 0 with the threshold (part by part, from the part's first slot) and a few words each.
+__host__ __device__ inline int64_t evict_words(int moves, int parts, int cap) {
+  const int64_t slots = ((int64_t)cap + 3) / 4 * 4;
+  return 4 + 2 * (((int64_t)moves + 1) / 2 * 2) + (parts > 1 ? EVP * (1024 + 2048) + 2 * slots + 2 * EVP + 4 : 0);
 }
 
-// What one block of the selection works on: slots [s0, s1) of a (sequence, kv head) of n > keep keys
+// What one block of the selection works on: slots [s0, s1) of a (sequence, kv head) of n > keep
+// keys. STORED: the order values of the weights are read from the scratch (else from the masses).
+template <bool STORED>
 struct EvictPart {
   const CacheEvictArgs &a;
   int h, b, n, s0, s1, low_len, high_len;
   const int32_t *tab;
   int32_t *list;
   int j0, j1;        // the wave's slots: a contiguous run of them, so that lists in wave order are in slot order
-  // weights of slots j0 + 64 i + lane and their places in the pool (-1: on no page of the cache, read as one
-  // of its pages and never written); those of longer runs are read again where they are needed
-  float x[EVK];
-  int place[EVK];
-  uint32_t *words;   // histograms [2][EVP][EVB], keys above the threshold's digits so far [EVP], prefix and rank [2][2]
+  uint32_t u[EVK];   // order values of slots j0 + 64 i + lane; those of longer runs are read where they are needed
+  uint32_t *hist, *from, *order, *alike, *above, *count, *found;
   __device__ __forceinline__ EvictPart(const CacheEvictArgs &a_) : a(a_), h(blockIdx.x), b(blockIdx.z) {
     const CacheArgs &c = a.c;
     n = __builtin_amdgcn_readfirstlane(min(max(c.kv_len[b], 0), c.cap));
     tab = c.table + (int64_t)b * c.table_ld;
-    list = a.list + ((int64_t)b * c.kvh + h) * evict_words(a.moves, a.parts);
-    words = (uint32_t *)list + 4 + 2 * (int64_t)a.moves;
+    list = a.list + ((int64_t)b * c.kvh + h) * evict_words(a.moves, a.parts, c.cap);
+    hist = (uint32_t *)list + 4 + 2 * (((int64_t)a.moves + 1) / 2 * 2);
+    from = hist + EVP * ev_bins(0);
+    order = from + EVP * ev_bins(1);
+    alike = order + ((int64_t)c.cap + 3) / 4 * 4;
+    above = alike + ((int64_t)c.cap + 3) / 4 * 4;   // [EVP] keys of a part above the threshold's digit 0
+    count = above + EVP;                         // [EVP] keys of a part that share it
+    found = count + EVP;                         // the threshold's digit 0, its rank among those that share it, their number
     low_len = (a.keep + a.low - 1) / a.low;
     high_len = a.parts > a.low ? (max(n - a.keep, 0) + a.parts - a.low - 1) / (a.parts - a.low) : 0;
     s0 = bound(blockIdx.y);
@@ -221,29 +228,54 @@ struct EvictPart {
     const int run = ((s1 - s0 + 64 * EVW - 1) / (64 * EVW)) * 64;
     j0 = min(s0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * run, s1);
     j1 = min(j0 + run, s1);
+    if (STORED) {
+#pragma unroll
+      for (int i = 0; i < EVK; ++i)
+        if (j0 + 64 * i < j1) u[i] = read(j0 + 64 * i);
+      return;
+    }
+    // The masses; those of slots below keep go to `out`, if it is not mass itself: most stay, k_evict_move
+    // replaces the others.
+    float x[EVK];
+    int at[EVK];
 #pragma unroll
     for (int i = 0; i < EVK; ++i)
       if (j0 + 64 * i < j1) {
-        const int j = min(j0 + 64 * i + (int)(threadIdx.x & 63), j1 - 1), e = tab[j >> c.plog], at = spot(e, j);
-        x[i] = a.mass[at];
-        place[i] = (unsigned)e < (unsigned)c.pages ? at : -1;
+        x[i] = weight(j0 + 64 * i, at[i]);
+        u[i] = mass_order(x[i]);
       }
+    if (a.out == a.mass) return;
+#pragma unroll
+    for (int i = 0; i < EVK; ++i)
+      if (j0 + 64 * i < j1 && at[i] >= 0) a.out[at[i]] = x[i];
+    for (int j = j0 + 64 * EVK; j < j1; j += 64) {
+      const float y = weight(j, at[0]);
+      if (at[0] >= 0) a.out[at[0]] = y;
+    }
   }
   // place in the pool of slot j with table entry e (pools hold fewer than 2^31 slots)
   __device__ __forceinline__ int spot(int e, int j) const {
     return ((cache_page(a.c, e) * a.c.kvh + h) << a.c.plog) + (j & ((1 << a.c.plog) - 1));
   }
-  // f(slot, its weight, its place) for the wave's slots, 64 at a time in order; slots >= j1 come along
+  // weight of slot first + lane, or of the run's last; at: its place in `out`, -1: none
+  __device__ __forceinline__ float weight(int first, int &at) const {
+    const int own = first + (int)(threadIdx.x & 63), j = min(own, j1 - 1), e = tab[j >> a.c.plog], x = spot(e, j);
+    at = own < min(j1, a.keep) && (unsigned)e < (unsigned)a.c.pages ? x : -1;
+    return a.mass[x];
+  }
+  // its order value
+  __device__ __forceinline__ uint32_t read(int first) const {
+    int at;
+    return STORED ? order[min(first + (int)(threadIdx.x & 63), j1 - 1)] : mass_order(weight(first, at));
+  }
+  // f(slot, its order value) for the wave's slots, 64 at a time in order; slots >= j1 come along
   template <class F>
   __device__ __forceinline__ void each(F &&f) const {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int i = 0; i < EVK; ++i)
-      if (j0 + 64 * i < j1) f(j0 + 64 * i + lane, x[i], place[i]);
-    for (int j = j0 + 64 * EVK; j < j1; j += 64) {
-      const int jj = min(j + lane, j1 - 1), e = tab[jj >> a.c.plog], at = spot(e, jj);
-      f(j + lane, a.mass[at], (unsigned)e < (unsigned)a.c.pages ? at : -1);
-    }
+      if (j0 + 64 * i < j1) f(j0 + 64 * i + lane, u[i]);
+    for (int j = j0 + 64 * EVK; j < j1; j += 64) f(j + lane, read(j));
   }
   // first slot of part p: parts [0, low) cut [0, keep) evenly, the others [keep, n)
   __device__ __forceinline__ int bound(int p) const {
@@ -254,42 +286,68 @@ struct EvictPart {
   __device__ __forceinline__ bool middle(int j) const { return j >= a.sink && j < n - a.recent; }
 };
 
-// Histogram of digit d of the slots of the part that share the digits found so far
-// (in COPIES copies)
-template <int COPIES>
-__device__ __forceinline__ void evict_count(const EvictPart &p, uint32_t (*hist)[EVB], int d, uint32_t prefix,
-                                            uint32_t known) {
-  const int tid = threadIdx.x, w = tid >> 6;
-  for (int i = tid; i < COPIES * EVB; i += EVT) (&hist[0][0])[i] = 0;
+// hist[d] += 1 for lanes with d >= 0; a lane's place among those with its d (from hist[d] on). Lanes that share the
+// first one's d are added up first: of masses that are all alike every lane would add to one word, one
+// after the other.
+__device__ __forceinline__ uint32_t evict_tally(uint32_t *hist, int d) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t live = __ballot(d >= 0);
+  if (!live) return 0;
+  const int first = __builtin_ctzll(live), same = __builtin_amdgcn_readlane(d, first);
+  const uint64_t alike = __ballot(d == same);
+  uint32_t at = 0;
+  if (d >= 0 && (lane == first || d != same)) at = atomicAdd(&hist[d], d == same ? (uint32_t)__popcll(alike) : 1u);
+  const uint32_t base = __builtin_amdgcn_readlane(at, first);
+  return d == same ? base + __popcll(alike & (lane ? ~0ull >> (64 - lane) : 0ull)) : at;
+}
+
+// Histogram of digit d of the block's slots that share the digits found so far, in EVH / bins copies
+template <bool STORED>
+__device__ __forceinline__ void evict_count(const EvictPart<STORED> &p, uint32_t *hist, int d, uint32_t prefix, uint32_t known) {
+  const int tid = threadIdx.x, copy = (tid >> 6) % (EVH / ev_bins(d)) * ev_bins(d);
+  for (int i = tid; i < EVH; i += EVT) hist[i] = 0;
   __syncthreads();
-  p.each([&](int j, float x, int) __attribute__((always_inline)) {
-    const uint32_t u = mass_order(x);
-    if (j < p.j1 && p.middle(j) && (u & known) == prefix)
-      atomicAdd(&hist[w % COPIES][(u >> ev_shift(d)) & (ev_bins(d) - 1)], 1u);
+  p.each([&](int j, uint32_t u) __attribute__((always_inline)) {
+    const bool in = j < p.j1 && p.middle(j) && (u & known) == prefix;
+    evict_tally(hist, in ? copy + (int)((u >> ev_shift(d)) & (ev_bins(d) - 1)) : -1);
   });
   __syncthreads();
+}
+
+// Sums over the lanes up to this one: of its 16 (data-parallel primitives, no trip through LDS), of the wave
+__device__ __forceinline__ int row_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  return x;
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  const int row = (threadIdx.x & 63) >> 4;
+  x = row_scan(x);
+  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31), r2 = __builtin_amdgcn_readlane(x, 47);
+  return x + (row > 0 ? r0 : 0) + (row > 1 ? r1 : 0) + (row > 2 ? r2 : 0);
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+
+// Sum of x over the threads before this one
+__device__ __forceinline__ uint32_t block_before(uint32_t x) {
+  __shared__ uint32_t wsum[EVW];
+  const uint32_t incl = (uint32_t)wave_scan((int)x);
+  if ((threadIdx.x & 63) == 63) wsum[threadIdx.x >> 6] = incl;
+  __syncthreads();
+  uint32_t before = incl - x;
+#pragma unroll
+  for (int i = 0; i < EVW; ++i) before += i < (int)(threadIdx.x >> 6) ? wsum[i] : 0u;
+  return before;
 }
 
 // Bin in which the rank-th key from the top lies, and its rank there. Bins go
 // from the top: thread t brings bins top = bins - 1 - per t (first) and top - 1
 // (second, if per = 2). All threads get the results; *size: the keys of that bin.
-__device__ __forceinline__ void evict_pick(uint32_t first, uint32_t second, int top, int rank, int *bin, int *r,
-                                           int *size = nullptr) {
-  __shared__ uint32_t wsum[EVW];
+__device__ __forceinline__ void evict_pick(uint32_t first, uint32_t second, int top, int rank, int *bin, int *r, int *size) {
   __shared__ int got[3];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const uint32_t mine = first + second;
-  uint32_t incl = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t t = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += t;
-  }
-  if (lane == 63) wsum[w] = incl;
-  __syncthreads();
-  uint32_t before = incl - mine;
-#pragma unroll
-  for (int i = 0; i < EVW; ++i) before += i < w ? wsum[i] : 0u;
+  const uint32_t mine = first + second, before = block_before(mine);
   if (before < (uint32_t)rank && before + mine >= (uint32_t)rank) {   // one thread
     const uint32_t x = rank - before;
     got[0] = x > first ? top - 1 : top;
@@ -299,50 +357,53 @@ __device__ __forceinline__ void evict_pick(uint32_t first, uint32_t second, int 
   __syncthreads();
   *bin = got[0];
   *r = got[1];
-  if (size) *size = got[2];
+  *size = got[2];
   __syncthreads();
 }
 
 // The lists of one part, given the threshold in the digits `known`: slots whose order value is above it in
-// them are kept, of those equal to it the first `taken` (eq0 of them lie in parts before);
-// hr holes and mr movers lie in parts before. Each wave takes a contiguous run of slots,
-// and counts of runs are added in order, so every list is in slot order. Returns the part's holes.
-__device__ __forceinline__ void evict_lists(const EvictPart &p, uint32_t threshold, uint32_t known, bool any, int taken, int eq0, int hr,
-                                            int mr, bool count) {
+// them are kept, of the part's `eqn` equal to it those that are among the first `taken` of all (eq0 of them lie in
+// parts before); hr holes and mr movers lie in parts before. Each wave takes a contiguous run of slots,
+// and counts of runs are added in order, so every list is in slot order.
+template <bool STORED>
+__device__ __forceinline__ void evict_lists(const EvictPart<STORED> &p, uint32_t threshold, uint32_t known, bool any,
+                                            int taken, int eq0, int eqn, int hr, int mr) {
   __shared__ int wcnt[3][EVW];
   const CacheEvictArgs &a = p.a;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), keep = a.keep;
   int32_t *idx = a.index ? a.index + ((int64_t)p.b * a.c.kvh + p.h) * keep : nullptr;
   const int j1 = p.j1;
   const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-  // class of slot j: 2 kept, 1 equal to the threshold, 0 dropped
-  auto cls = [&](int j, float x) {
-    if (j >= j1) return 0;
-    if (!p.middle(j)) return 2;
-    if (!any) return 0;
-    const uint32_t u = mass_order(x) & known;
-    return u > threshold ? 2 : u == threshold ? 1 : 0;
-  };
-  int eq = 0;
-  p.each([&](int j, float x, int) __attribute__((always_inline)) { eq += __popcll(__ballot(cls(j, x) == 1)); });
-  if (lane == 0) wcnt[0][w] = eq;
-  __syncthreads();
+  // Kept: above `limit`. Only where some of a part's equal ones stay and others not they have to be numbered.
+  // (Order values are at least 0x7fffff, NaN and -inf, so the threshold is not 0.)
+  const bool mixed = __builtin_amdgcn_readfirstlane(any && taken > eq0 && taken < eq0 + eqn);
+  const uint32_t limit = !any ? ~0u : taken >= eq0 + eqn ? threshold - 1 : threshold | ~known;
+  auto equal = [&](int j, uint32_t u) { return j < j1 && p.middle(j) && (u & known) == threshold; };
+  if (mixed) {
+    int eq = 0;
+    p.each([&](int j, uint32_t u) __attribute__((always_inline)) { eq += __popcll(__ballot(equal(j, u))); });
+    if (lane == 0) wcnt[0][w] = eq;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < EVW; ++i) eq0 += i < w ? wcnt[0][i] : 0;
-  // f(slot, weight, place, kept) in order
+    for (int i = 0; i < EVW; ++i) eq0 += i < w ? wcnt[0][i] : 0;
+  }
+  // f(slot, kept) in order
   auto kept_each = [&](auto &&f) __attribute__((always_inline)) {
     int er = eq0;
-    p.each([&](int j, float x, int place) __attribute__((always_inline)) {
-      const int cl = cls(j, x);
-      const uint64_t eb = __ballot(cl == 1);
-      f(j, x, place, cl == 2 || (cl == 1 && er + __popcll(eb & below) < taken));
-      er += __popcll(eb);
+    p.each([&](int j, uint32_t u) __attribute__((always_inline)) {
+      bool kept = j < j1 && (!p.middle(j) || u > limit);
+      if (mixed) {
+        const uint64_t eb = __ballot(equal(j, u));
+        kept = kept || (eb >> lane & 1 && er + __popcll(eb & below) < taken);
+        er += __popcll(eb);
+      }
+      f(j, kept);
     });
   };
   int holes = 0, movers = 0;
-  kept_each([&](int j, float, int, bool kept) __attribute__((always_inline)) {
+  kept_each([&](int j, bool kept) __attribute__((always_inline)) {
     holes += __popcll(__ballot(j < j1 && !kept && j < keep));
-    movers += __popcll(__ballot(j < j1 && kept && j >= keep));
+    movers += __popcll(__ballot(kept && j >= keep));
   });
   if (lane == 0) {
     wcnt[1][w] = holes;
@@ -356,34 +417,29 @@ __device__ __forceinline__ void evict_lists(const EvictPart &p, uint32_t thresho
     mr += i < w ? wcnt[2][i] : 0;
     total += wcnt[1][i];
   }
-  if (count && threadIdx.x == 0) p.list[0] = min(total, a.moves);
-  kept_each([&](int j, float x, int place, bool kept) __attribute__((always_inline)) {
-    const bool hole = j < j1 && !kept && j < keep, mover = j < j1 && kept && j >= keep;
+  if (!STORED && threadIdx.x == 0) p.list[0] = min(total, a.moves);
+  kept_each([&](int j, bool kept) __attribute__((always_inline)) {
+    const bool hole = j < j1 && !kept && j < keep, mover = kept && j >= keep;
     const uint64_t hb = __ballot(hole), mb = __ballot(mover);
     const int hx = hr + __popcll(hb & below), mx = mr + __popcll(mb & below);
     if (hole && hx < a.moves) p.list[4 + 2 * hx] = j;
     if (mover && mx < a.moves) p.list[5 + 2 * mx] = j;
-    if (j < j1 && kept && j < keep) {
-      if (a.out != a.mass && place >= 0) a.out[place] = x;
-      if (idx) idx[j] = j;
-    }
+    if (idx && kept && j < keep) idx[j] = j;
     hr += __popcll(hb);
     mr += __popcll(mb);
   });
 }
 
 // A sequence that is short enough: everything stays
-__device__ __forceinline__ void evict_none(const EvictPart &p) {
+template <bool STORED>
+__device__ __forceinline__ void evict_none(const EvictPart<STORED> &p) {
   const CacheEvictArgs &a = p.a;
   int32_t *idx = a.index ? a.index + ((int64_t)p.b * a.c.kvh + p.h) * a.keep : nullptr;
   const int first = blockIdx.y * EVT + threadIdx.x, step = gridDim.y * EVT;
-  for (int j = first; j < p.n; j += step) {
-    const int e = p.tab[j >> a.c.plog], at = p.spot(e, j);
-    if (a.out != a.mass && (unsigned)e < (unsigned)a.c.pages) a.out[at] = a.mass[at];
-    if (idx) idx[j] = j;
-  }
-  if (idx)
+  if (idx) {
+    for (int j = first; j < p.n; j += step) idx[j] = j;
     for (int j = p.n + first; j < a.keep; j += step) idx[j] = -1;
+  }
   if (first == 0) p.list[0] = 0;
 }
 
@@ -395,150 +451,195 @@ __device__ __forceinline__ void evict_none(const EvictPart &p) {
 //
 // One block does it all for short sequences (STAGE -1). What bounds that form is
 // the instruction rate of one compute unit (67,320 slots: 189 us), so long ones are cut into EVP parts of one
-// block each and the steps become launches 0 to 3: stage d counts digit d of its part after every
-// block has found digit d - 1 from all parts' counts, and stage 3 writes the lists. The parts' counts also
-// give how many keys of each part are kept, hence the ranks that its lists start from; parts do not cross `keep`.
+// block each and the steps become launches. 0: order values stored, digit 0 counted. 1: digit 0 of the
+// threshold from all parts' counts; the keys that share it listed, those above it counted. 2: the other digits from
+// the listed keys of all parts, how many keys of each part are kept, hence the ranks that its lists start
+// from, and the lists. Parts do not cross `keep`. Keys listed in stage 1 are few unless most masses are alike:
+// more than EVA of them are sorted by digit 1 within their part, with the number of keys from
+// each bin on, so that stage 2 reads those of one bin only. 16 heads, 67,320 slots, 61,200 kept: 8.5, 6 and
+// 11 us, launches and the latency of a dozen dependent steps (masses over many binades; within one 48 us in all,
+// all equal 58). Reading all 16 parts' counts of every digit in every block instead took 15 us more.
 template <int STAGE>
 __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
-  __shared__ uint32_t hist[EVH][EVB];
-  const EvictPart p(a);
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, part = blockIdx.y;
+  __shared__ uint32_t hist[EVH];
+  const EvictPart<(STAGE > 0)> p(a);
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), part = blockIdx.y;
   if (p.n <= a.keep) {
-    if (STAGE < 0 || STAGE == 3) evict_none(p);
+    if (STAGE < 0 || STAGE == 2) evict_none(p);
     return;
   }
   const int m = a.keep - a.sink - a.recent;
+  // evict_pick from the LDS histogram of digit d
+  auto pick = [&](int d, int rank, int *bin, int *r, int *size) __attribute__((always_inline)) {
+    const int per = ev_bins(d) / EVT, top = ev_bins(d) - 1 - per * tid;
+    uint32_t first = 0, second = 0;
+    for (int i = 0; i < EVH; i += ev_bins(d)) {
+      first += hist[i + top];
+      if (per > 1) second += hist[i + top - 1];
+    }
+    evict_pick(first, second, top, rank, bin, r, size);
+  };
   if constexpr (STAGE < 0) {
     uint32_t prefix = 0, known = 0;
     int rank = m, bin, size = m + 1;
     for (int d = 0; d < 3 && m > 0 && size != rank; ++d) {   // until all of a bin are taken
-      if (d == 0)
-        evict_count<EVH>(p, hist, d, prefix, known);
-      else
-        evict_count<1>(p, hist, d, prefix, known);
-      const int per = ev_bins(d) / EVT, top = ev_bins(d) - 1 - per * tid;
-      uint32_t first = 0, second = 0;
-      for (int i = 0; i < (d == 0 ? EVH : 1); ++i) {
-        first += hist[i][top];
-        if (per > 1) second += hist[i][top - 1];
-      }
-      evict_pick(first, second, top, rank, &bin, &rank, &size);
+      evict_count(p, hist, d, prefix, known);
+      pick(d, rank, &bin, &rank, &size);
       prefix |= (uint32_t)bin << ev_shift(d);
       known |= (uint32_t)(ev_bins(d) - 1) << ev_shift(d);
     }
-    evict_lists(p, prefix, known, m > 0, rank, 0, 0, 0, true);
-    return;
-  }
-  // Histograms of stage d lie in set d & 1. found: the threshold's digits and rank after each stage's pick, and whether
-  // all keys of its bin are taken, so that no further digit is needed.
-  uint32_t *above = p.words + 2 * EVP * EVB, *found = above + 2 * EVP;
-  uint32_t prefix = 0, known = 0;
-  int rank = m, bin = 0, size = 0, digit = STAGE - 1;   // digit: the last one picked
-  bool done = m == 0;
-  if (STAGE > 1 && !done) {
-    const uint32_t *f = found + 4 * (STAGE - 2);
-    prefix = f[0];
-    rank = (int)f[1];
-    bin = (int)f[3];
-    done = f[2] != 0;
-    if (done) digit = STAGE - 2;                 // (of the stage before at the earliest: stage 2 may pass it on)
-    if (STAGE == 3 && done) digit = (int)f[2] - 1;
-  }
-  const uint32_t *g = p.words + (digit & 1) * EVP * EVB;
-  if (STAGE > 0 && !done) {
-    const int bins = ev_bins(digit), per = bins / EVT, top = bins - 1 - per * tid;
-    uint32_t first = 0, second = 0;
-    if (per > 1) {
+    evict_lists(p, prefix, known, m > 0, rank, 0, size, 0, 0);
+  } else if constexpr (STAGE == 0) {
+    if (m == 0) return;
+    evict_count(p, hist, 0, 0, 0);
+    p.each([&](int j, uint32_t u) __attribute__((always_inline)) {
+      if (j < p.j1) p.order[j] = u;
+    });
+    static_assert(ev_bins(0) == EVT && EVH == 4 * EVT, "a thread per bin");
+    p.hist[part * EVT + tid] = hist[tid] + hist[EVT + tid] + hist[2 * EVT + tid] + hist[3 * EVT + tid];
+  } else if constexpr (STAGE == 1) {
+    __shared__ uint32_t listed, over;
+    if (m == 0) return;
+    const int top = EVT - 1 - tid;
+    uint32_t sum = 0;
 #pragma unroll
-      for (int q = 0; q < EVP; ++q) {
-        const uint2 x = *(const uint2 *)(g + q * EVB + top - 1);
-        first += x.y;
-        second += x.x;
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < EVP; ++q) first += g[q * EVB + top];
-    }
-    evict_pick(first, second, top, rank, &bin, &rank, &size);
-    prefix |= (uint32_t)bin << ev_shift(digit);
-  }
-  for (int d = 0; d <= digit; ++d) known |= (uint32_t)(ev_bins(d) - 1) << ev_shift(d);
-  if (STAGE > 0 && STAGE < 3) {
+    for (int q = 0; q < EVP; ++q) sum += p.hist[q * EVT + top];
+    if (tid == 0) listed = over = 0;
+    for (int i = tid; i < ev_bins(1); i += EVT) hist[i] = 0;
+    int bin, rank, size;
+    evict_pick(sum, 0u, top, m, &bin, &rank, &size);
     if (part == 0 && tid == 0) {
-      uint32_t *f = found + 4 * (STAGE - 1);
-      f[0] = prefix;
-      f[1] = (uint32_t)rank;
-      f[2] = done || size == rank ? digit + 1 : 0;
-      f[3] = (uint32_t)bin;
+      p.found[0] = (uint32_t)bin << ev_shift(0);
+      p.found[1] = (uint32_t)rank;
+      p.found[2] = (uint32_t)size;
     }
-    // keys of this part above the bin
-    if (!done && w == part) {
-      const int bins = ev_bins(digit);
-      int x = 0;
-#pragma unroll 16
-      for (int i = lane; i < bins; i += 64) {
-        const int y = (int)g[w * EVB + i];
-        if (i > bin) x += y;
+    auto digit0 = [&](int j, uint32_t u) { return j < p.j1 && p.middle(j) ? (int)(u >> ev_shift(0)) : -1; };
+    auto digit1 = [&](int j, uint32_t u) { return digit0(j, u) == bin ? (int)(u >> ev_shift(1)) & (ev_bins(1) - 1) : -1; };
+    if (size > EVA) {
+      p.each([&](int j, uint32_t u) __attribute__((always_inline)) { evict_tally(hist, digit1(j, u)); });
+      __syncthreads();
+      const int b1 = ev_bins(1) - 1 - 2 * tid;   // from bins b1 and b1 - 1 on; hist: where they begin in the list
+      const uint32_t x = hist[b1], y = hist[b1 - 1], before = block_before(x + y);
+      *(uint2 *)(p.from + part * ev_bins(1) + b1 - 1) = make_uint2(before + x + y, before + x);
+      hist[b1] = before;
+      hist[b1 - 1] = before + x;
+      __syncthreads();
+    }
+    p.each([&](int j, uint32_t u) __attribute__((always_inline)) {
+      const int d = digit0(j, u);
+      const uint64_t same = __ballot(d == bin), more = __ballot(d > bin);
+      uint32_t at = 0;
+      if (lane == 0) {
+        if (more) atomicAdd(&over, (uint32_t)__popcll(more));
+        if (same) at = atomicAdd(&listed, (uint32_t)__popcll(same));
+      }
+      if (size > EVA)
+        at = evict_tally(hist, digit1(j, u));
+      else
+        at = __builtin_amdgcn_readfirstlane(at) + __popcll(same & (lane ? ~0ull >> (64 - lane) : 0ull));
+      if (d == bin) p.alike[p.s0 + at] = u;
+    });
+    __syncthreads();
+    if (tid == 0) {
+      p.count[part] = listed;
+      p.above[part] = over;
+    }
+  } else {
+    __shared__ int gt[EVP], eq[EVP];
+    constexpr int NA = 4;                        // listed keys that a thread keeps in registers
+    uint32_t prefix = 0;
+    int rank = 0;
+    if (m > 0) {
+      const uint32_t *al = p.alike + p.bound(w);   // wave w has those of part w
+      int more = __builtin_amdgcn_readfirstlane((int)p.count[w]);
+      uint32_t x[NA];
+      auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+          if (64 * i < more) x[i] = al[min(64 * i + lane, more - 1)];
+      };
+      load();
+      prefix = p.found[0];
+      rank = (int)p.found[1];
+      const bool sorted = p.found[2] > EVA;
+      int up = (int)p.above[w], equal = 0, over = 0, bin, size;
+      auto alike = [&](auto &&f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+          if (64 * i < more) f(x[i], 64 * i + lane < more);
+#pragma unroll 8
+        for (int i = 64 * NA; i < more; i += 64) f(al[min(i + lane, more - 1)], i + lane < more);
+      };
+      if (sorted) {                              // total number of keys from each bin on
+        uint2 sum = make_uint2(0u, 0u);
+#pragma unroll
+        for (int q = 0; q < EVP; ++q) {
+          const uint2 y = *(const uint2 *)(p.from + q * ev_bins(1) + 2 * tid);
+          sum.x += y.x;
+          sum.y += y.y;
+        }
+        *(uint2 *)(hist + 2 * tid) = sum;
+        if (tid == 0) hist[ev_bins(1)] = 0;
+        __syncthreads();
+        const uint32_t next = hist[2 * tid + 2];
+        const bool one = sum.y >= (uint32_t)rank && next < (uint32_t)rank, two = sum.x >= (uint32_t)rank && sum.y < (uint32_t)rank;
+        if (one || two) {                        // one thread
+          gt[0] = 2 * tid + (one ? 1 : 0);
+          gt[1] = rank - (int)(one ? next : sum.y);
+        }
+        __syncthreads();
+        bin = gt[0];
+        rank = gt[1];
+        __syncthreads();
+        prefix |= (uint32_t)bin << ev_shift(1);
+        const uint32_t *f = p.from + w * ev_bins(1) + bin;
+        const int skip = bin + 1 < ev_bins(1) ? __builtin_amdgcn_readfirstlane((int)f[1]) : 0;
+        more = __builtin_amdgcn_readfirstlane((int)f[0]) - skip;
+        up += skip;
+        al += skip;
+        load();
       }
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-      if (lane == 0) above[w] = (uint32_t)x + (STAGE > 1 ? above[w] : 0u);
-    }
-    done = done || size == rank;
-  }
-  if (STAGE < 3) {
-    if (done) return;
-    if (STAGE == 0)
-      evict_count<EVH>(p, hist, STAGE, prefix, known);
-    else
-      evict_count<1>(p, hist, STAGE, prefix, known);
-    uint32_t *to = p.words + ((STAGE & 1) * EVP + part) * EVB;
-    for (int i = tid; i < ev_bins(STAGE); i += EVT) {
-      uint32_t x = 0;
-#pragma unroll
-      for (int q = 0; q < (STAGE == 0 ? EVH : 1); ++q) x += hist[q][i];
-      to[i] = x;
-    }
-    return;
-  }
-  // stage 3: what each part keeps, from its counts above and in the threshold's bin
-  __shared__ int gt[EVP], eq[EVP];
-  {
-    int x = 0;
-    if (m > 0 && !done) {
-      const int bins = ev_bins(digit);
-#pragma unroll 16
-      for (int i = lane; i < bins; i += 64) {
-        const int y = (int)g[w * EVB + i];
-        if (i > bin) x += y;
+      for (int d = 1; d < 3; ++d) {
+        if (d == 1 && sorted) continue;
+        const int copy = w % (EVH / ev_bins(d)) * ev_bins(d);
+        const uint32_t known = ~0u << ev_shift(d - 1);
+        for (int i = tid; i < EVH; i += EVT) hist[i] = 0;
+        __syncthreads();
+        alike([&](uint32_t y, bool in) __attribute__((always_inline)) {
+          evict_tally(hist, in && (y & known) == prefix ? copy + (int)((y >> ev_shift(d)) & (ev_bins(d) - 1)) : -1);
+        });
+        __syncthreads();
+        pick(d, rank, &bin, &rank, &size);
+        prefix |= (uint32_t)bin << ev_shift(d);
       }
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+      alike([&](uint32_t y, bool in) __attribute__((always_inline)) {
+        over += in && y > prefix ? 1 : 0;
+        equal += in && y == prefix ? 1 : 0;
+      });
+      up += wave_sum(over);
+      equal = wave_sum(equal);
+      if (lane == 0) {                           // what the wave's part keeps for sure, and may
+        gt[w] = up;
+        eq[w] = equal;
+      }
+    } else if (lane == 0) {
+      gt[w] = eq[w] = 0;
     }
-    if (lane == 0) {
-      gt[w] = m > 0 ? x + (int)above[w] : 0;
-      eq[w] = m > 0 ? (int)g[w * EVB + bin] : 0;
-    }
+    __syncthreads();
+    // lane q (of every wave): part q; sums over the parts before it
+    const int q = lane % EVP, q0 = p.bound(q), q1 = p.bound(q + 1), my = eq[q];
+    static_assert(EVP == 16, "row_scan");
+    auto before = [&](int x) { return row_scan(x) - x; };
+    const int eq0 = before(my);
+    const int fixed = max(0, min(q1, a.sink) - q0) + max(0, q1 - max(q0, p.n - a.recent));
+    const int kept = fixed + gt[q] + min(my, max(0, rank - eq0));
+    const int holes = q < a.low ? q1 - q0 - kept : 0, movers = q < a.low ? 0 : kept;
+    const int hr = before(holes), mr = before(movers);
+    if (part == 0 && tid == EVP - 1) p.list[0] = min(hr + holes, a.moves);
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, part); };
+    evict_lists(p, prefix, ~0u, m > 0, rank, of(eq0), of(my), of(hr), of(mr));
   }
-  __syncthreads();
-  // lane q (of every wave): part q; sums over the parts before it
-  const int q = lane % EVP, q0 = p.bound(q), q1 = p.bound(q + 1), my = eq[q];
-  auto before = [&](int x) {
-    int sum = x;
-#pragma unroll
-    for (int o = 1; o < EVP; o <<= 1) {
-      const int t = __shfl_up(sum, o, EVP);
-      if (q >= o) sum += t;
-    }
-    return sum - x;
-  };
-  const int eq0 = before(my);
-  const int fixed = max(0, min(q1, a.sink) - q0) + max(0, q1 - max(q0, p.n - a.recent));
-  const int kept = fixed + gt[q] + min(my, max(0, rank - eq0));
-  const int holes = q < a.low ? q1 - q0 - kept : 0, movers = q < a.low ? 0 : kept;
-  const int hr = before(holes), mr = before(movers);
-  if (part == 0 && tid == EVP - 1) p.list[0] = min(hr + holes, a.moves);
-  evict_lists(p, prefix, known, m > 0, rank, __shfl(eq0, part, EVP), __shfl(hr, part, EVP), __shfl(mr, part, EVP), false);
 }
 
 // The moves that k_evict_select listed. RB bytes of a row: 16 per thread, the
@@ -548,7 +649,7 @@ __global__ __launch_bounds__(256) void k_evict_move(CacheEvictArgs a) {
   constexpr int TPR = RB / 16, RPB = 256 / TPR;
   const CacheArgs &c = a.c;
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-  const int32_t *list = a.list + ((int64_t)b * c.kvh + h) * evict_words(a.moves, a.parts);
+  const int32_t *list = a.list + ((int64_t)b * c.kvh + h) * evict_words(a.moves, a.parts, c.cap);
   const int32_t *tab = c.table + (int64_t)b * c.table_ld;
   const int cnt = list[0];
   const int pmask = (1 << c.plog) - 1;
@@ -593,7 +694,7 @@ size_t cache_evict_scratch(const CacheArgs &c, int keep) {
   a.c = c;
   a.keep = keep;
   evict_plan(a);
-  return (size_t)c.batch * c.kvh * (size_t)evict_words(a.moves, a.parts) * sizeof(int32_t);
+  return (size_t)c.batch * c.kvh * (size_t)evict_words(a.moves, a.parts, c.cap) * sizeof(int32_t);
 }
 
 hipError_t launch_cache_evict(int dtype, const CacheEvictArgs &in, hipStream_t s) {
@@ -606,7 +707,6 @@ hipError_t launch_cache_evict(int dtype, const CacheEvictArgs &in, hipStream_t s
     hipLaunchKernelGGL((k_evict_select<0>), sel, dim3(EVT), 0, s, a);
     hipLaunchKernelGGL((k_evict_select<1>), sel, dim3(EVT), 0, s, a);
     hipLaunchKernelGGL((k_evict_select<2>), sel, dim3(EVT), 0, s, a);
-    hipLaunchKernelGGL((k_evict_select<3>), sel, dim3(EVT), 0, s, a);
   }
   const int rb = a.c.hd * (dtype == 1 ? 2 : 4), rpb = 256 / (rb / 16);
   const int per = std::max(1, 2048 / std::max(1, a.c.kvh * a.c.batch));

@@ -350,6 +350,9 @@ EVICT = [
     ("bf16", 1, 128, 256, [9000, 8999], 8990, 0, 0, "equal"),
     ("bf16", 64, 64, 64, [4200] * 4, 4000, 10, 20, "ties"),
     ("bf16", 2, 64, 16, MANY_KV, 20, 3, 4, "random"),
+    ("bf16", 2, 64, 64, [30000, 9000, 21000], 20000, 100, 200, "near"),
+    ("f32", 1, 64, 32, [40000], 12345, 0, 0, "near"),
+    ("bf16", 1, 64, 32, [40000], 39000, 50, 60, "ties"),
 ]
 
 
@@ -360,6 +363,8 @@ def test_evict_matches_definition(case, in_place):
     s = cu.state(dtype, kvh, kvh, hd, page, [0] * len(kv), kv, seed=11)
     if kind == "ties":
         s.mass = torch.round(s.mass)
+    elif kind == "near":                               # distinct, within a factor of 1.2
+        s.mass = torch.where(torch.isnan(s.mass), s.mass, 1 + 0.2 * torch.rand_like(s.mass))
     elif kind == "equal":
         s.mass = torch.where(torch.isnan(s.mass), s.mass, 0.5)
     elif kind == "odd":
