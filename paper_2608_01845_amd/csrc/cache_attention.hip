@@ -485,9 +485,16 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 }
 
 // ---------------------------------------------------------------- bf16, many rows
-// 32 query rows (two tiles of 16) a wave, W = 8 or 4 waves a block, two waves per SIMD at 8; key tiles of 64 reach four K and four V slots of LDS by direct buffer loads
-// of waves 0 to 3, up to four tiles ahead. Bound by the matrix cores, with the
+// 32 query rows (two tiles of 16) a wave; key tiles of 64 reach four K and four V slots of LDS by direct buffer loads
+// of four waves, up to four tiles ahead. Bound by the matrix cores, with the
 // exponentials close behind.
+//
+// Blocks of 256 rows are 8 waves, two per SIMD: 1.0 us a tile at hd 64, 1.4 at hd 128. Few rows or keys leave
+// compute units idle with them, so there are blocks of 128 rows too. At hd 128 they are 4 waves, 1.05 us a tile: one
+// wave alone on a SIMD waits for its own results (1,720 cycles, of which 960 issue). At hd 64 two
+// tiles fit into LDS at a time: KG = 2 groups of 4 waves take every second one each, 0.58 us a
+// tile (0.77 with 4 waves), and their softmaxes meet at the end (2,048 rows causal over themselves, 16 heads: 26.7 us,
+// 38.4 with 256 rows; 4,096 over 4,096 in full: 88.6, 77.4 with 256).
 //
 // Tiles that all rows see whole run through a software pipeline: step t holds the P V
 // products of tile t, the Q K products of tile t + 2 and, in the same instruction
@@ -576,7 +583,7 @@ __device__ __forceinline__ float weights(const f32x4 (&S)[4][2], bf16x8 (&pf)[2]
   return ls;
 }
 
-template <int HD, bool SMALL, int W>
+template <int HD, bool SMALL, int W, int KG>
 __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs a) {
   using F = Few<HD>;
   using TL = TileLoads<HD, SMALL>;
@@ -592,18 +599,20 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool grp_a = wid < 4;
-  const int mlast = min(m0 + 32 * W, count) - 1;
-  const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KV - 1) / KV;
-  const int t_first = nr > 1 ? sp * (a.range / KV) : 0, t_end = nr > 1 ? min(t_first + a.range / KV, tiles) : tiles;
-  // tiles of the range, relative to t_first: `nf` that every row sees whole, then masked ones
-  const int tot = t_end - t_first, nf = min(max(lim_lo / KV - t_first, 0), tot);
+  constexpr int WR = W / KG;                     // waves over the block's rows
+  const int wr = wid % WR, kg = wid / WR;
+  const bool grp_a = KG == 2 || wid < 4;         // loads tiles
+  const int mlast = min(m0 + 32 * WR, count) - 1;
+  const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KG * KV - 1) / (KG * KV);   // in steps of KG tiles
+  const int range = a.range / (KG * KV), t_first = nr > 1 ? sp * range : 0, t_end = nr > 1 ? min(t_first + range, tiles) : tiles;
+  // steps of the range, relative to t_first: `nf` that every row sees whole, then masked ones
+  const int tot = t_end - t_first, nf = min(max(lim_lo / (KG * KV) - t_first, 0), tot);
 
   const float sc = LOG2E / sqrtf((float)HD);
   bf16x8 qf[2][NC];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int mm = min(m0 + 32 * wid + 16 * t + lr, mlast), i = cache_row(c, mm);
+    const int mm = min(m0 + 32 * wr + 16 * t + lr, mlast), i = cache_row(c, mm);
     const bf16_t *Q = (const bf16_t *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)(h * group + mm - i * group) * HD + 8 * lg;
 #pragma unroll
     for (int j = 0; j < NC; ++j) qf[t][j] = *(const bf16x8 *)(Q + 32 * j);
@@ -617,20 +626,21 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
 #pragma unroll
     for (int i = 0; i < F::VR; ++i) vro[i] = V_BASE + r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
-  const uint32_t lds0 = lds_addr(smem);
+  char *ring = smem + kg * 2 * NB * TB;
+  const uint32_t lds0 = lds_addr(ring);
   TL tl;
   typename TL::Where wk, wv;                     // of the latest K tile asked for, and of the one before
-  auto page_of = [&](int tile) { return SMALL ? 0 : tl.page(c, b, t_first + tile); };
-  auto load_k = [&](int tile, int page) __attribute__((always_inline)) {
+  auto page_of = [&](int t) { return SMALL ? 0 : tl.page(c, b, KG * (t_first + t) + kg); };
+  auto load_k = [&](int t, int page) __attribute__((always_inline)) {
     wv = wk;
-    tl.find(c, t_first + tile, page, wk);
-    tl.load(c.k, wk, lds0 + (tile % NB) * TB, tl.kvo);
+    tl.find(c, KG * (t_first + t) + kg, page, wk);
+    tl.load(c.k, wk, lds0 + (t % NB) * TB, tl.kvo);
   };
-  auto load_v = [&](int tile, const typename TL::Where &x) { tl.load(c.v, x, lds0 + V_BASE + (tile % NB) * TB, tl.vvo()); };
+  auto load_v = [&](int t, const typename TL::Where &x) { tl.load(c.v, x, lds0 + V_BASE + (t % NB) * TB, tl.vvo()); };
 
   int page[NB];                                  // of the K tiles that the next NB steps ask for
   if (grp_a) {                                   // K_0 .. K_3, V_0 .. V_2; the first products wait for K_0 and K_1 alone
-    tl.init(c, s, b, h, wid, lane, t_first);
+    tl.init(c, s, b, h, wid & 3, lane, KG * t_first + kg);
     wk = typename TL::Where{};
     int first[NB];
 #pragma unroll
@@ -676,13 +686,13 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   if (nf > 0) {
     f32x4 S[2][4][2];                            // S of tiles t + 1 and t + 2 (index tile & 1)
     bf16x8 pf[2][2][2];                          // P of tiles t and t + 1 (index tile & 1), [row tile][32-key group]
-    qk(S[0], smem);
+    qk(S[0], ring);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       m[t] = fmaxf(rowmax<HD>(S[0], t) * sc, -1e30f);
       l[t] = weights(S[0], pf[0][t], t, sc, m[t]);
     }
-    if (nf > 1) qk(S[1], smem + TB);
+    if (nf > 1) qk(S[1], ring + TB);
     if (grp_a) {                                 // K_2 and V_1: at most K_3 and V_2 are still under way
       if (tot >= NB)
         wait_vm<2 * TL::NS>();
@@ -707,7 +717,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
         fr_[r] = *(const bf16x8 *)(kb + kro[g / 4] + (g % 4) * 16 * F::ROWB);
     };
 #pragma unroll
-    for (int r = 0; r < 4; ++r) read(r, smem, smem);
+    for (int r = 0; r < 4; ++r) read(r, ring, ring);
     auto step = [&](auto pc, int t, int page) __attribute__((always_inline)) {
       constexpr int P = decltype(pc)::value, cur = (P + 1) & 1, n = P & 1;
       int issued = 0;
@@ -724,7 +734,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      const char *vb = smem + P * TB, *kb = smem + ((P + 2) % NB) * TB, *vn = smem + ((P + 1) % NB) * TB;
+      const char *vb = ring + P * TB, *kb = ring + ((P + 2) % NB) * TB, *vn = ring + ((P + 1) % NB) * TB;
       float ls[2] = {0.f, 0.f}, ex[2];
       auto mma = [&](int q, int t_) __attribute__((always_inline)) {
         if (q < NPV) {
@@ -821,7 +831,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   int lim[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int mr = m0 + 32 * wid + 16 * t + lr;
+    const int mr = m0 + 32 * wr + 16 * t + lr;
     lim[t] = mr < count ? cache_limit(c, s, cache_row(c, mr)) : 0;
   }
   for (int u = nf; u < tot; ++u) {
@@ -831,18 +841,18 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
       if (u > nf) load_k(u + 3, page_of(u + 3));                 // at u = nf the pipeline has asked for it already
       load_v(u + 3, wk);
     }
-    const char *kb = smem + (u % NB) * TB, *vb = smem + (u % NB) * TB;   // vro holds V_BASE
+    const char *kb = ring + (u % NB) * TB, *vb = ring + (u % NB) * TB;   // vro holds V_BASE
     // A key that a row does not see has weight 0, but 0 times an infinity or NaN of
     // its V is NaN in a matrix product: a tile that holds one is multiplied key by key.
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < TB / (1024 * W); ++i) {
-      const u32x4_t y = *(const u32x4_t *)(vb + V_BASE + (i * 64 * W + tid) * 16);
+    for (int i = 0; i < TB / (1024 * WR); ++i) {
+      const u32x4_t y = *(const u32x4_t *)(vb + V_BASE + (i * 64 * WR + 64 * wr + lane) * 16);
 #pragma unroll
       for (int q = 0; q < 4; ++q) odd |= (y[q] & 0x7f80u) == 0x7f80u || (y[q] & 0x7f800000u) == 0x7f800000u;
     }
     odd = __syncthreads_or(odd);
-    const int key0 = KV * (t_first + u);
+    const int key0 = KV * (KG * (t_first + u) + kg);
     f32x4 S[4][2];
     bf16x8 pf[2][2];
     qk(S, kb);
@@ -899,10 +909,39 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
     }
   }
 
+  if constexpr (KG == 2) {                       // the two softmaxes of every row meet
+    f32x4 *xo = (f32x4 *)smem + (wr * 2 * NI) * 64 + lane;
+    float2 *xm = (float2 *)((f32x4 *)smem + WR * 2 * NI * 64) + wr * 128 + lane;
+    __syncthreads();
+    if (kg == 1) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) xo[(t * NI + i) * 64] = o[i][t];
+        xm[64 * t] = make_float2(m[t], l[t]);
+      }
+    }
+    __syncthreads();
+    if (kg == 1) return;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float2 y = xm[64 * t];
+      const float mn = fmaxf(m[t], y.x), ref = mn == -INFINITY ? 0.f : mn;
+      const float a0 = __builtin_amdgcn_exp2f(m[t] - ref), a1 = __builtin_amdgcn_exp2f(y.x - ref);
+      m[t] = mn;
+      l[t] = a0 * l[t] + a1 * y.y;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const f32x4 z = xo[(t * NI + i) * 64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][t][e] = a0 * o[i][t][e] + a1 * z[e];
+      }
+    }
+  }
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const float den = quad_sum(l[t]);
-    const int mr = m0 + 32 * wid + 16 * t + lr;
+    const int mr = m0 + 32 * wr + 16 * t + lr;
     if (mr >= count) continue;
     const int i0 = cache_row(c, mr), head = h * group + mr - i0 * group;
     if (nr > 1) {
@@ -1403,22 +1442,29 @@ size_t attn_part_bytes(const CacheArgs &c, int splits) {
 // twice as many; eight tokens over 1 to 32,768 keys 87 us, 104 with half). A second launch and its reads
 // cost about 5 us: 16 rows and fewer are not cut below 65,536 / hd keys (1,000 keys, 16 heads
 // of 64, one row: 10.1 us whole, 13.0 in four), others not below 256.
+// Of hd 128 only up to 32 rows where there is much to read (64 rows, 16 heads, eight sequences of 1,000 keys: 34
+// us, 28.6 in blocks of 128 rows; one of 3,456 keys: 19.4 and 20.8).
 //
 // More rows: blocks of 128 or 256 rows and the number of ranges by estimate: rounds of blocks on
 // the compute units, a start and end of 7 us each and a time per tile of 64 keys (measured alone
-// on a compute unit: 256 rows 1.0 us at hd 64, 1.45 at hd 128; 128 rows 0.77 and 1.05), then the
-// second launch and the scratch written and read. 384 rows over 3,456 keys, 16 heads of 64: 256 rows 26.6 us, 128 rows 23.0;
-// over 8,192 keys, 16 heads of 128: 49.6 against 58.8.
+// on a compute unit: 256 rows 1.03 us at hd 64, 1.4 at hd 128; 128 rows 0.58 and 1.08), then the
+// second launch and the scratch written and read. 384 rows over 3,456 keys, 16 heads of 64: 256 rows 27.1 us, 128 rows 23.9;
+// 1,024 over 8,192 keys, 16 heads of 128: 77 against 84. Three chunks of 333 rows over 3,456 keys:
+// 55 us if half of the ranges are taken to be there, 41 as they fill their bound.
 void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *range, int *splits) {
   const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
-  // of several sequences about half the ranges that the bounds allow for are there
-  const int64_t slots = (int64_t)std::max(1, device_cus()) * (c.batch > 1 ? 2 : 1);
+  // Of several sequences not all ranges that the bounds allow for are there: of few rows each about half; else
+  // the fewer the less the chunks fill their bound (unlike chunks going with unlike lengths)
+  const bool few = dtype == 0 || m <= 32 || (m <= 64 && (c.hd == 64 || (int64_t)c.batch * c.kvh * c.cap < 100000));
+  const int64_t cus = std::max(1, device_cus()), most = std::max<int64_t>(1, (int64_t)c.batch * c.max_q);
+  const int64_t slots = c.batch == 1 ? cus : few ? 2 * cus : cus + cus * 7 / 10 * (most - std::min<int64_t>(most, c.rows)) / most;
   auto set = [&](int r, int64_t keys) {
     *rpb = r;
-    *range = (int)((std::max<int64_t>(keys, 64) + 63) / 64 * 64);
+    const int64_t step = r == 128 && c.hd == 64 ? 128 : 64;   // keys that a block works on at a time
+    *range = (int)((std::max<int64_t>(keys, 64) + step - 1) / step * step);
     *splits = std::max(1, (c.cap + *range - 1) / *range);
   };
-  if (dtype == 0 || m <= 64) {
+  if (few) {
     const int r = dtype == 1 && m <= 16 ? 16 : 32;
     const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
     const int64_t want = std::max<int64_t>(1, slots / blocks);
@@ -1427,7 +1473,7 @@ void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *ran
     const int64_t tiles = (c.cap + 63) / 64;
     double best = 0;
     for (int r = 256; r >= 128; r -= 128) {
-      const double tile = (r == 256 ? 1.0 : 0.77) * (c.hd == 128 ? 1.4 : 1.0);
+      const double tile = c.hd == 128 ? (r == 256 ? 1.4 : 1.08) : (r == 256 ? 1.03 : 0.58);
       const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
       for (int64_t n = 1; n <= 32 && (n == 1 || tiles >= 4 * n); ++n) {
         const double rounds = (double)((blocks * n + slots - 1) / slots);
@@ -1457,22 +1503,23 @@ hipError_t launch_few(const CacheAttnArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((k_cache_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
-template <int HD, bool SMALL, int W>
+template <int HD, bool SMALL, int W, int KG>
 hipError_t launch_many(const CacheAttnArgs &a, hipStream_t s) {
-  constexpr int LDS = 2 * NB * KV * Few<HD>::ROWB;
+  constexpr int LDS = KG * 2 * NB * KV * Few<HD>::ROWB;
   static DeviceOnce once;
   const hipError_t lim = once_on_device(once, [] {
-    return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL, W>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL, W, KG>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL, W>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(64 * W), LDS, s, a);
+  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL, W, KG>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(64 * W), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD>
 hipError_t launch_bf16(const CacheAttnArgs &a, hipStream_t s) {
+  constexpr int W128 = HD == 64 ? 8 : 4, KG = HD == 64 ? 2 : 1;   // of blocks of 128 rows
   const int rpb = a.rpb;
-  if (rpb == 256) return a.c.plog < 6 ? launch_many<HD, true, 8>(a, s) : launch_many<HD, false, 8>(a, s);
-  if (rpb == 128) return a.c.plog < 6 ? launch_many<HD, true, 4>(a, s) : launch_many<HD, false, 4>(a, s);
+  if (rpb == 256) return a.c.plog < 6 ? launch_many<HD, true, 8, 1>(a, s) : launch_many<HD, false, 8, 1>(a, s);
+  if (rpb == 128) return a.c.plog < 6 ? launch_many<HD, true, W128, KG>(a, s) : launch_many<HD, false, W128, KG>(a, s);
   return rpb == 16 ? launch_few<HD, 1>(a, s) : launch_few<HD, 2>(a, s);
 }
 

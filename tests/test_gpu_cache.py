@@ -209,6 +209,11 @@ ATTENTION_WIDE = [
     ("bf16", 16, 1, 128, 32, [2600, 2500], [2700, 2650], 0),
     ("bf16", 16, 1, 128, 256, [4000, 96], [4050, 700], 33),
     ("bf16", 12, 1, 128, 16, [5000], [5200], 1000),               # a group that does not divide the block's rows
+    ("bf16", 16, 16, 64, 64, [1024], [8192], 256),                # ranges of blocks of 256
+    ("bf16", 16, 16, 128, 32, [1024], [8192], 0),
+    ("bf16", 16, 16, 64, 128, [384], [3457], 1),                  # blocks of 128, an odd number of tiles of 64
+    ("bf16", 4, 4, 64, 16, [1000, 130], [1000, 4001], 1),
+    ("bf16", 16, 16, 128, 64, [200, 64], [2000, 1999], 64),
 ]
 
 
