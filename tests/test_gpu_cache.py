@@ -489,6 +489,52 @@ def test_attention_in_place_shared_pages_and_a_long_frame(dtype, heads, kvh, hd,
     assert torch.equal(x, ref)
 
 
+@pytest.mark.parametrize("dtype,heads,kvh,hd,q,kv", [("bf16", 4, 4, 128, [1, 1], [9000, 5000]), ("bf16", 4, 4, 64, [300], [9000]),
+                                                     ("bf16", 4, 2, 128, [700, 90], [3000, 2000]),
+                                                     ("bf16", 2, 2, 64, [40, 3], [4000, 9000]), ("f32", 4, 2, 64, [50], [4000])])
+def test_less_scratch_and_no_byte_behind_it(dtype, heads, kvh, hd, q, kv):
+    """Attention and masses with all, half, a seventh and none of the scratch; eviction with exactly its own."""
+    import ctypes as C
+    s = cu.state(dtype, heads, kvh, hd, 16, q, kv, seed=26)
+    wdc, ctx = ctx_of(s)
+    lib, cache, ch = ctx.lib, wdc.PagedCache(s.k, s.v), cu.chunks(wdc, s)
+    o, lse, pv, qk = cu.attention64(s, 7)
+    bound, lse_bound = attention_bound(s, pv, o, qk, max(kv))
+    z32 = lse.float()
+    want, add = cu.mass64(s, 7, z32, 0.5)
+    ld, ptr = heads * hd, lambda t: C.c_void_p(t.data_ptr())
+    rel = (hd + 8) * EPS32 * qk.max().item() + 4 * EPS32 * (lse.abs().max().item() + qk.max().item()) + 2.0 ** -21
+    rel += (max(q) * heads / kvh + 8) * EPS32
+    need = lib.wdc_cache_attention_scratch(ctx.h, cache.ref, ch.ref)
+    need_m = lib.wdc_cache_mass_scratch(ctx.h, cache.ref, ch.ref)
+    assert need > 0
+
+    def area(n):
+        return torch.full((n + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
+
+    for part in (1, 2, 7, 0):
+        n, m = (need // part // 16 * 16, need_m // part // 16 * 16) if part else (0, 0)
+        mem, out, z = area(n), torch.full_like(s.x, 7.0), torch.empty((s.rows, heads), device="cuda")
+        assert lib.wdc_cache_attention(ctx.h, cache.ref, ch.ref, ptr(s.x), ld, 7, ptr(out), ld, ptr(z), ptr(mem) if n else None,
+                                       n) == 0
+        within(out.reshape(o.shape), o, bound, "o")
+        within(z, lse, lse_bound + 4 * EPS32 * lse.abs(), "lse")
+        assert (mem[n:] == 0x5a).all()
+        mem, got = area(m), torch.zeros_like(s.mass)
+        assert lib.wdc_cache_mass(ctx.h, cache.ref, ch.ref, ptr(s.x), ld, 7, ptr(z32), 0.5, ptr(s.mass), ptr(got),
+                                  ptr(mem) if m else None, m) == 0
+        for b in range(len(kv)):
+            pg, sl = cu.where(s, b)
+            within(got[pg, :, sl], want[pg, :, sl], rel * add[pg, :, sl] + 4 * EPS32 * want[pg, :, sl].abs(), "mass")
+        assert (mem[m:] == 0x5a).all()
+    n = lib.wdc_cache_evict_scratch(ctx.h, cache.ref, ch.ref, 2000)
+    mem, index = area(n), torch.empty((len(kv), kvh, 2000), dtype=torch.int32, device="cuda")
+    want_idx = cu.evict64(s, s.mass, 2000, 5, 6)
+    assert lib.wdc_cache_evict(ctx.h, cache.ref, ch.ref, ptr(s.mass), ptr(s.mass), 2000, 5, 6, ptr(s.kv_len), ptr(index), ptr(mem),
+                               n) == 0
+    assert index.tolist() == want_idx and (mem[n:] == 0x5a).all()
+
+
 def test_bounds_that_32_bits_would_cut_are_refused():
     s = cu.state("bf16", 4, 2, 64, 16, [2], [20], seed=25)
     wdc, ctx = ctx_of(s)
@@ -618,3 +664,51 @@ def test_another_stream_than_the_current_one():
         torch.full((1 << 22,), 3.0, device="cuda")                # the current stream's allocations take what is free
     side.synchronize()
     assert all(torch.equal(o, ref) for o in outs)
+
+
+def test_two_graphs_in_flight():
+    """Two captured chains on the same cache, replayed on two streams at once, several times: each has its own scratch."""
+    import paper_2608_01845_amd as wdc
+    torch_cuda()
+    s = cu.state("bf16", 8, 2, 128, 64, [4, 4], [7000, 6000], seed=27)
+    ref_ctx = wdc.Context(cu.config("bf16", 8, 128), allocate_weights=False)
+    cache, ch = wdc.PagedCache(s.k, s.v), cu.chunks(wdc, s)
+    xs = [s.x, s.x.flip(0).contiguous()]
+
+    def calls(ctx, x, out, lse, mass):
+        ctx.cache_attention(cache, ch, x, out, lse=lse)
+        ctx.cache_mass(cache, ch, x, lse, s.mass, out=mass)
+
+    def buffers():
+        return [torch.zeros_like(s.x), torch.zeros((s.rows, 8), device="cuda"), torch.zeros_like(s.mass)]
+
+    want, got, graphs, streams, ctxs = [], [], [], [], []
+    for x in xs:
+        want.append(buffers())
+        calls(ref_ctx, x, *want[-1])
+    torch.cuda.synchronize()
+    for x in xs:
+        side = torch.cuda.Stream()
+        ctx = wdc.Context(cu.config("bf16", 8, 128), allocate_weights=False, stream=side)
+        b = buffers()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            calls(ctx, x, *b)
+        got.append(b), graphs.append(g), streams.append(side), ctxs.append(ctx)
+    for _ in range(5):
+        for b in got:
+            for t in b:
+                t.fill_(7)
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for g, st in zip(graphs, streams):
+                with torch.cuda.stream(st):
+                    g.replay()
+        torch.cuda.synchronize()
+        live = torch.zeros(s.mass.shape, dtype=torch.bool, device="cuda")
+        for i in range(2):
+            pg, sl = cu.where(s, i)
+            live[pg, :, sl] = True
+        for a, b in zip(want, got):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and torch.equal(a[2][live], b[2][live])
