@@ -188,7 +188,8 @@ def _ptr(t) -> Optional[int]:
 
 def _ld(t) -> int:
     """Row stride of a [rows, cols] tensor (one of at most one row: its columns)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 else cols
 
 
 def _ptrs(ts):
@@ -198,9 +199,15 @@ def _ptrs(ts):
     return (C.c_void_p * len(ts))(*[None if t is None else t.data_ptr() for t in ts])
 
 
+_TORCH = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
 
 
 def _int32(**values):
@@ -221,6 +228,7 @@ class PagedCache:
         if not (k.is_contiguous() and v.is_contiguous()):
             raise ValueError("k and v must be contiguous")
         self.k, self.v, self.kv_heads, self.device = k, v, k.shape[1], k.get_device()
+        self.dtype, self.head_dim, self.slots = k.dtype, k.shape[3], tuple(k.shape[:3])
         self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], 0)
         self.ref = C.byref(self.desc)
 
@@ -257,6 +265,7 @@ class Context:
         self.cfg = cfg
         self.device = torch.device(device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self.device_index = self.stream.device_index if self.device.index is None else self.device.index
         self.max_batch = max_batch
         self.desc = desc_from_config(cfg, max_batch)
         self.params = params if params is not None else default_params()
@@ -397,11 +406,10 @@ class Context:
 
     # ---------------------------------------------------------------- paged key/value cache
     def _cache_check(self, cache, chunks):
-        if cache.k.dtype is not self.tdtype or cache.k.shape[3] != self.cfg.head_dim:
-            raise ValueError(f"cache of {cache.k.dtype}, head size {cache.k.shape[3]}: the context has {self.tdtype}, "
+        if cache.dtype is not self.tdtype or cache.head_dim != self.cfg.head_dim:
+            raise ValueError(f"cache of {cache.dtype}, head size {cache.head_dim}: the context has {self.tdtype}, "
                              f"{self.cfg.head_dim}")
-        if cache.device != chunks.device or cache.device != (
-                self.stream.device_index if self.device.index is None else self.device.index):
+        if cache.device != chunks.device or cache.device != self.device_index:
             raise ValueError(f"cache or chunks not on {self.device}")
 
     def _tensor(self, name, t, dtype, shape, device, strided=False):
@@ -416,18 +424,21 @@ class Context:
         """Device memory that lives as long as the work just enqueued on this context's stream."""
         torch = _torch()
         # (torch.cuda.current_stream() builds a Stream object: 1.9 us a call, this 0.1)
-        if torch._C._cuda_getCurrentRawStream(self.stream.device_index) == self.stream.cuda_stream:
+        if torch._C._cuda_getCurrentRawStream(self.device_index) == self.stream.cuda_stream:
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
     def _launch(self, call, *args):
         """One call; the null stream is the current device's, so that device has to be this context's."""
-        torch, dev = _torch(), self.stream.device_index
-        if torch._C._cuda_getDevice() == dev:
-            return self._check(call(self.h, *args))
-        with torch.cuda.device(dev):
-            self._check(call(self.h, *args))
+        torch = _torch()
+        if torch._C._cuda_getDevice() == self.device_index:
+            status = call(self.h, *args)
+        else:
+            with torch.cuda.device(self.device_index):
+                status = call(self.h, *args)
+        if status:
+            self._check(status)
 
     def cache_append(self, cache: PagedCache, chunks: Chunks, qkv, q, pos=None, q_weight=None, k_weight=None):
         """Normalise and rotate q and k of qkv [rows, (heads + 2 kv_heads) head_dim], store k and v in the
@@ -461,7 +472,7 @@ class Context:
     def cache_mass(self, cache: PagedCache, chunks: Chunks, q, lse, mass, frame: int = 0, decay: float = 1.0, out=None):
         """out = decay * mass + the weight each cached key receives from the chunks' rows (out: mass itself
         if not given); mass [pages, kv_heads, page] float32, lse from cache_attention with the same frame."""
-        f32, dev, ptr, shape = _torch().float32, cache.device, self._tensor, cache.k.shape[:3]
+        f32, dev, ptr, shape = _torch().float32, cache.device, self._tensor, cache.slots
         self._cache_check(cache, chunks)
         _int32(frame=frame)
         q_p = ptr("q", q, self.tdtype, (chunks.rows, self.cfg.heads * self.cfg.head_dim), dev, True)
@@ -482,7 +493,7 @@ class Context:
         torch = _torch()
         self._cache_check(cache, chunks)
         _int32(keep=keep, sink=sink, recent=recent)
-        dev, ptr, shape, batch = cache.device, self._tensor, cache.k.shape[:3], chunks.batch
+        dev, ptr, shape, batch = cache.device, self._tensor, cache.slots, chunks.batch
         kv_len_out = chunks.kv_len if kv_len_out is None else kv_len_out
         mass_p = ptr("mass", mass, torch.float32, shape, dev)
         out_p = mass_p if out is None else ptr("out", out, torch.float32, shape, dev)
