@@ -121,7 +121,8 @@ __device__ __forceinline__ float *part_ml(const CacheAttnArgs &a, int64_t slot) 
 // What a block of an attention launch works on: query rows [m0, m0 + rpb) of
 // `count` of sequence b and kv head h, range sp of nr of the keys that they see.
 // Blocks are numbered sequence by sequence with the lengths of the device, so those that the host's bounds
-// allow for but no chunk needs come last. Within a sequence kv heads go fastest: with 8 (or a divisor
+// allow for but no chunk needs come last. (2,048 single tokens over 100 keys each, 16 heads of 64: 1,432 us when every
+// block counted, 515 with the numbers as they are.) Within a sequence kv heads go fastest: with 8 (or a divisor
 // or multiple) of them the blocks of one run on one XCD (or its group) and share K and V in that L2; the last rows,
 // which see the most, come first (8,192 rows causal over themselves, 16 heads of 128: 312 us from the first, 271 so).
 struct AttnBlock {
@@ -134,7 +135,10 @@ struct AttnBlock {
     const int lane = threadIdx.x & 63;
     group = c.heads / c.kvh;
     int li = blockIdx.x;
-    if (c.batch > 1) {
+    if (a.splits == 1 && c.max_q * group <= a.rpb) {   // a block per sequence and kv head: nothing to count
+      b = li / c.kvh;
+      li -= b * c.kvh;
+    } else if (c.batch > 1) {
       bool found = false;
       for (int e0 = 0; e0 < c.batch && !found; e0 += 64) {
         int cnt = 0;
@@ -188,10 +192,10 @@ __device__ __forceinline__ void cache_block(const CacheArgs &c, int per, int &bh
 // ---------------------------------------------------------------- bf16, few rows
 // RT tiles of 16 query rows per block of four waves; wave w takes key tiles w, w +
 // 4, .. of the block's range and the four partial softmaxes meet at the end. What
-// bounds it is the stream of K and V, so each wave keeps three tiles under way beside the
+// bounds it is the stream of K and V, so each wave keeps a tile under way beside the
 // one it works on, without a block barrier: direct loads into its own part of LDS, 8 KB a
-// tile (32 keys of 64, 16 of 128). Eight tokens over 1 to 32,768 keys, 32 heads on 8 kv heads of 128: 87 us,
-// 5.35 TB/s, where a large copy reaches 4.9.
+// tile (32 keys of 64, 16 of 128). Eight tokens over 1 to 32,768 keys, 32 heads on 8 kv heads of 128: 86 us,
+// 5.4 TB/s, where a large copy reaches 4.9.
 //
 // S^T = K Q^T (A: 16 keys, B: 16 rows) leaves lane (lr, lg) the keys 4 lg + e of
 // row lr; these values of one (hd 128) or two key tiles are the B operand of O^T = V^T P^T, whose A
@@ -223,14 +227,14 @@ __device__ __forceinline__ bf16x8 v_frag(const char *p) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Slots of a wave's K and V tiles: one in use, the others under way. One row tile waits for memory; with two, a
-// second block per compute unit does more than a deeper queue.
-constexpr int few_slots(int rt) { return rt == 1 ? 4 : 2; }
+// Slots of a wave's K and V tiles: one in use, the other under way. Two blocks per compute unit with two slots each do
+// more than one with four (16 heads of 64: 16 tokens over 4,000 keys 52.7 us, 57.1 with four; 2,048 over 100: 240, 479).
+constexpr int FSL = 2;
 
 template <int HD, int RT>
 __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   using F = Few<HD>;
-  constexpr int NC = HD / 32, NI = HD / 16, KT = F::KT, NB = few_slots(RT), WAVE = 2 * NB * F::TILE;   // K slots, V slots
+  constexpr int NC = HD / 32, NI = HD / 16, KT = F::KT, NB = FSL, WAVE = 2 * NB * F::TILE;   // K slots, V slots
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ float ml[4][2][16 * RT];
   const CacheArgs &c = a.c;
@@ -418,19 +422,12 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): the slot has been read before it is loaded again
   };
   if (t0 + w < t1) {
-    static_assert(NB == 4 || NB == 2, "slots of the unrolled steps");
-#pragma unroll
-    for (int j = 0; j < NB - 1; ++j) load(t0 + w + 4 * j, j);
+    static_assert(NB == 2, "slots of the unrolled steps");
+    load(t0 + w, 0);
     for (int t = t0 + w; t < t1; t += 4 * NB) {
       step(std::integral_constant<int, 0>{}, t);
       if (t + 4 >= t1) break;
       step(std::integral_constant<int, 1>{}, t + 4);
-      if constexpr (NB == 4) {
-        if (t + 8 >= t1) break;
-        step(std::integral_constant<int, 2 % NB>{}, t + 8);
-        if (t + 12 >= t1) break;
-        step(std::integral_constant<int, 3 % NB>{}, t + 12);
-      }
     }
     wait_vm<0>();                                // what is still under way goes to this wave's part of LDS
     asm volatile("" ::: "memory");
@@ -1441,9 +1438,9 @@ size_t attn_part_bytes(const CacheArgs &c, int splits) {
 // has their bounds.
 //
 // Up to 64 rows, and float32: blocks of 16 or 32 rows, and enough ranges to fill
-// the compute units; with several sequences of unlike length twice as many, so that a long
-// one is not left to run alone (one row over 8,192 keys, 16 heads of 128: 20.8 us, 25.5 with
-// twice as many; eight tokens over 1 to 32,768 keys 87 us, 104 with half). A second launch and its reads
+// the compute units; with several sequences half as many again, since some are shorter (eight tokens over 1 to 32,768
+// keys, 32 heads on 8 of 128: 87 us, 103 without; 16 over 4,000 keys each, 16 heads of 128: 94, 98 with twice as many; four
+// over 100 to 30,000: 40, 50 without and 36 with twice as many). A second launch and its reads
 // cost about 5 us: 16 rows and fewer are not cut below 65,536 / hd keys (1,000 keys, 16 heads
 // of 64, one row: 10.1 us whole, 13.0 in four), others not below 256.
 // Of hd 128 only up to 32 rows where there is much to read (64 rows, 16 heads, eight sequences of 1,000 keys: 34
@@ -1457,11 +1454,11 @@ size_t attn_part_bytes(const CacheArgs &c, int splits) {
 // 55 us if half of the ranges are taken to be there, 41 as they fill their bound.
 void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *range, int *splits) {
   const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
-  // Of several sequences not all ranges that the bounds allow for are there: of few rows each about half; else
+  // Of several sequences not all ranges that the bounds allow for are there: of few rows each two thirds; else
   // the fewer the less the chunks fill their bound (unlike chunks going with unlike lengths)
   const bool few = dtype == 0 || m <= 32 || (m <= 64 && (c.hd == 64 || (int64_t)c.batch * c.kvh * c.cap < 100000));
   const int64_t cus = std::max(1, device_cus()), most = std::max<int64_t>(1, (int64_t)c.batch * c.max_q);
-  const int64_t slots = c.batch == 1 ? cus : few ? 2 * cus : cus + cus * 7 / 10 * (most - std::min<int64_t>(most, c.rows)) / most;
+  const int64_t slots = c.batch == 1 ? cus : few ? cus * 3 / 2 : cus + cus * 7 / 10 * (most - std::min<int64_t>(most, c.rows)) / most;
   auto set = [&](int r, int64_t keys) {
     *rpb = r;
     const int64_t step = r == 128 && c.hd == 64 ? 128 : 64;   // keys that a block works on at a time
@@ -1498,7 +1495,7 @@ void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *ran
 
 template <int HD, int RT>
 hipError_t launch_few(const CacheAttnArgs &a, hipStream_t s) {
-  constexpr int LDS = 4 * 2 * few_slots(RT) * Few<HD>::TILE;
+  constexpr int LDS = 4 * 2 * FSL * Few<HD>::TILE;
   static DeviceOnce once;
   const hipError_t lim = once_on_device(once, [] {
     return hipFuncSetAttribute((const void *)k_cache_attn_few<HD, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
