@@ -314,22 +314,6 @@ __device__ __forceinline__ void evict_count(const EvictPart<STORED> &p, uint32_t
   __syncthreads();
 }
 
-// Sums over the lanes up to this one: of its 16 (data-parallel primitives, no trip through LDS), of the wave
-__device__ __forceinline__ int row_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-  return x;
-}
-__device__ __forceinline__ int wave_scan(int x) {
-  const int row = (threadIdx.x & 63) >> 4;
-  x = row_scan(x);
-  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31), r2 = __builtin_amdgcn_readlane(x, 47);
-  return x + (row > 0 ? r0 : 0) + (row > 1 ? r1 : 0) + (row > 2 ? r2 : 0);
-}
-__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
-
 // Sum of x over the threads before this one
 __device__ __forceinline__ uint32_t block_before(uint32_t x) {
   __shared__ uint32_t wsum[EVW];

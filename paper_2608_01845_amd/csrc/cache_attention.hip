@@ -122,7 +122,7 @@ __device__ __forceinline__ float *part_ml(const CacheAttnArgs &a, int64_t slot) 
 // `count` of sequence b and kv head h, range sp of nr of the keys that they see.
 // Blocks are numbered sequence by sequence with the lengths of the device, so those that the host's bounds
 // allow for but no chunk needs come last. (2,048 single tokens over 100 keys each, 16 heads of 64: 1,432 us when every
-// block counted, 515 with the numbers as they are.) Within a sequence kv heads go fastest: with 8 (or a divisor
+// block counted the sequences before its own, 515 without.) Within a sequence kv heads go fastest: with 8 (or a divisor
 // or multiple) of them the blocks of one run on one XCD (or its group) and share K and V in that L2; the last rows,
 // which see the most, come first (8,192 rows causal over themselves, 16 heads of 128: 312 us from the first, 271 so).
 struct AttnBlock {
@@ -146,12 +146,7 @@ struct AttnBlock {
           const CacheSeq q = cache_seq(c, e0 + lane);
           cnt = (q.nq * group + a.rpb - 1) / a.rpb * range_count(a, q.n) * c.kvh;
         }
-        int sum = cnt;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int t = __shfl_up(sum, o, 64);
-          if (lane >= o) sum += t;
-        }
+        const int sum = wave_scan(cnt);
         const uint64_t past = __ballot(sum > li);
         if (past) {
           const int k = __builtin_ctzll(past);
