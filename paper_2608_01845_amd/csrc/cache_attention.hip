@@ -135,15 +135,19 @@ struct AttnBlock {
     const int lane = threadIdx.x & 63;
     group = c.heads / c.kvh;
     int li = blockIdx.x;
-    if (a.splits == 1 && c.max_q * group <= a.rpb) {   // a block per sequence and kv head: nothing to count
-      b = li / c.kvh;
-      li -= b * c.kvh;
-    } else if (c.batch > 1) {
+    if (c.batch == 1 || (a.splits == 1 && c.max_q * group <= a.rpb)) {   // one sequence, or a block for each and kv head
+      if (c.batch > 1) {
+        b = uni(li / c.kvh);
+        li -= b * c.kvh;
+      }
+      s = uniform_seq(c, b);
+    } else {
       bool found = false;
       for (int e0 = 0; e0 < c.batch && !found; e0 += 64) {
         int cnt = 0;
+        CacheSeq q{};
         if (e0 + lane < c.batch) {
-          const CacheSeq q = cache_seq(c, e0 + lane);
+          q = cache_seq(c, e0 + lane);
           cnt = (q.nq * group + a.rpb - 1) / a.rpb * range_count(a, q.n) * c.kvh;
         }
         const int sum = wave_scan(cnt);
@@ -152,6 +156,10 @@ struct AttnBlock {
           const int k = __builtin_ctzll(past);
           b = e0 + k;
           li -= __builtin_amdgcn_readlane(sum - cnt, k);
+          s.q0 = __builtin_amdgcn_readlane(q.q0, k);
+          s.nq = __builtin_amdgcn_readlane(q.nq, k);
+          s.n = __builtin_amdgcn_readlane(q.n, k);
+          s.start = __builtin_amdgcn_readlane(q.start, k);
           found = true;
         } else {
           li -= __builtin_amdgcn_readlane(sum, 63);
@@ -161,7 +169,6 @@ struct AttnBlock {
     }
     b = uni(b);
     li = uni(li);
-    s = uniform_seq(c, b);
     count = s.nq * group;
     const int q = uni(li / c.kvh), nrg = range_count(a, s.n), back = uni(q / nrg), rb = (count + a.rpb - 1) / a.rpb - 1 - back;
     h = li - q * c.kvh;
