@@ -69,27 +69,37 @@ __device__ __forceinline__ float quad_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Entries of one sequence's page table, asked for in rising order by a whole
-// wave: 64 entries in a register, the next 64 on their way in another.
+// First slots in the pool of one sequence's pages and a kv head, asked for in rising order by a whole
+// wave: 64 table entries in a register, the next 64 on their way in another. EARLY: slots are found for all 64
+// at once (long chunks over small pages: 59 -> 56 us for 2,048 rows of 16 heads of 128; single
+// tokens, which touch few entries of a page table, lose by it: 86 -> 93).
+template <bool EARLY>
 struct PageWalk {
   const int32_t *tab;
-  int last, base, pages, cur, next;
+  int last, base, cur, next;
   __device__ __forceinline__ int fetch(int i) const { return tab[min(i + (int)(threadIdx.x & 63), last)]; }
-  __device__ __forceinline__ void init(const CacheArgs &a, int b, int first) {
+  __device__ __forceinline__ static int slot(const CacheArgs &a, int h, int entry) {   // (pools hold fewer than 2^31)
+    return (cache_page(a, entry) * a.kvh + h) << a.plog;
+  }
+  __device__ __forceinline__ void init(const CacheArgs &a, int b, int h, int first) {
     tab = a.table + (int64_t)b * a.table_ld;
     last = a.table_ld - 1;
-    pages = a.pages;
     base = first;
     cur = fetch(base);
     next = fetch(base + 64);
+    if (EARLY) cur = slot(a, h, cur);
   }
-  __device__ __forceinline__ int get(int i) {
+  // before get(i); the entries that share i's group of 64 from the first on need no further call
+  __device__ __forceinline__ void advance(const CacheArgs &a, int h, int i) {
     while (i - base >= 64) {
-      cur = next;
+      cur = EARLY ? slot(a, h, next) : next;
       base += 64;
       next = fetch(base + 64);
     }
-    return min(max(__builtin_amdgcn_readlane(cur, i - base), 0), pages - 1);
+  }
+  __device__ __forceinline__ int get(const CacheArgs &a, int h, int i) const {
+    const int x = __builtin_amdgcn_readlane(cur, i - base);
+    return EARLY ? x : slot(a, h, x);
   }
 };
 
@@ -281,8 +291,8 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < F::VR; ++i) vro[i] = r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
-  PageWalk pw;
-  pw.init(c, k_.b, (KT * t0) >> c.plog);
+  PageWalk<false> pw;
+  pw.init(c, k_.b, h, (KT * t0) >> c.plog);
   const int pmask = (1 << c.plog) - 1;
   // Tile t into slot j: halves of 16 rows, each on one page. Rows past the cache's
   // end lie outside the buffer range and arrive as zeros, whatever they hold; so do tiles
@@ -292,8 +302,8 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     for (int hf = 0; hf < F::NK; ++hf) {
       const int key = KT * t + 16 * hf;
       const bool live = t < t1;
-      const int pg = live ? pw.get(key >> c.plog) : 0;
-      const int64_t off = ((((int64_t)pg * c.kvh + h) << c.plog) + (key & pmask)) * F::ROWB;
+      if (live) pw.advance(c, h, key >> c.plog);
+      const int64_t off = (int64_t)(live ? pw.get(c, h, key >> c.plog) + (key & pmask) : 0) * F::ROWB;
       const int bytes = live ? min(max(s.n - key, 0), 16) * F::ROWB : 0;
       const u32x4_t kd = buffer_at(c.k, off, bytes), vd = buffer_at(c.v, off, bytes);
       const uint32_t to = lds0 + j * F::TILE + hf * 16 * F::ROWB;
@@ -520,21 +530,31 @@ struct TileLoads {
     int64_t off[NP];                             // bytes from the pool to the tile (SMALL: the stripe's 16 rows)
     int bytes[NP];                               // what lies before the end of the cache
   };
-  PageWalk pw;                                   // SMALL only
-  int kvo, w, h, n;                              // kvo: the lane's byte offset in its stripe's rows of K
+  PageWalk<true> pw;                             // SMALL only
+  int kvo_, w, h, n;                             // kvo_: the lane's byte offset in its stripe's rows of K
   __device__ __forceinline__ void init(const CacheArgs &c, const CacheSeq &s, int b, int h_, int w_, int lane, int tile0) {
     w = w_;
     h = h_;
     n = s.n;
-    const int r = w * F::RPL + lane / (HD / 8), ch = lane % (HD / 8);
-    const int at = SMALL ? r & 15 : r;
-    kvo = at * F::ROWB + (ch ^ F::kkey(r)) * 16;
-    if (SMALL) pw.init(c, b, (KV * tile0) >> c.plog);
+    kvo_ = offset(lane);
+    if (SMALL) pw.init(c, b, h, (KV * tile0) >> c.plog);
   }
-  // the same of V, whose rows have another swizzle (found again each time: a register kept for it would spill)
+  __device__ __forceinline__ int offset(int lane) const {
+    const int r = w * F::RPL + lane / (HD / 8), ch = lane % (HD / 8);
+    return (SMALL ? r & 15 : r) * F::ROWB + (ch ^ F::kkey(r)) * 16;
+  }
+  // With small pages it is found again each time: a register kept for it would spill, and its reload would wait
+  // for all loads under way. (The lane's number by an instruction that is not moved out of the loop.)
+  __device__ __forceinline__ int kvo() const {
+    if (!SMALL || HD == 64) return kvo_;
+    int lane;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+    return offset(lane);
+  }
+  // the same of V, whose rows have another swizzle
   __device__ __forceinline__ int vvo() const {
     const int r = w * F::RPL + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)) / (HD / 8);
-    return kvo ^ ((F::kkey(r) ^ F::vkey(r)) * 16);
+    return kvo() ^ ((F::kkey(r) ^ F::vkey(r)) * 16);
   }
   // page of a whole tile, by a scalar load (the table does not change during a launch)
   __device__ __forceinline__ int page(const CacheArgs &c, int b, int tile) const {
@@ -544,13 +564,14 @@ struct TileLoads {
   }
   // where a tile lies; page: its page (unless SMALL)
   __device__ __forceinline__ void find(const CacheArgs &c, int tile, int page, Where &x) {
-    const int pmask = (1 << c.plog) - 1;
+    const int pmask = (1 << c.plog) - 1, key0 = KV * tile, rest = n - key0;
+    if (SMALL) pw.advance(c, h, key0 >> c.plog);   // a tile's pages are of one group of 64
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int key = KV * tile + (SMALL ? (4 * i + w) * F::RPL / 16 * 16 : 0);
-      const int pg = SMALL ? pw.get(key >> c.plog) : page;
-      x.off[i] = ((((int64_t)pg * c.kvh + h) << c.plog) + (key & pmask)) * F::ROWB;
-      x.bytes[i] = min(max(n - key, 0), SMALL ? 16 : KV) * F::ROWB;
+      const int at = SMALL ? (4 * i + w) * F::RPL / 16 * 16 : 0, key = key0 + at;
+      const int slot = SMALL ? pw.get(c, h, key >> c.plog) : ((page * c.kvh + h) << c.plog);   // (pools hold fewer than 2^31)
+      x.off[i] = (int64_t)(slot + (key & pmask)) * F::ROWB;
+      x.bytes[i] = rest >= KV ? (SMALL ? 16 : KV) * F::ROWB : min(max(rest - at, 0), SMALL ? 16 : KV) * F::ROWB;
     }
   }
   __device__ __forceinline__ void load(const void *pool, const Where &x, uint32_t lds, int vo) const {
@@ -635,7 +656,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   auto load_k = [&](int t, int page) __attribute__((always_inline)) {
     wv = wk;
     tl.find(c, KG * (t_first + t) + kg, page, wk);
-    tl.load(c.k, wk, lds0 + (t % NB) * TB, tl.kvo);
+    tl.load(c.k, wk, lds0 + (t % NB) * TB, tl.kvo());
   };
   auto load_v = [&](int t, const typename TL::Where &x) { tl.load(c.v, x, lds0 + V_BASE + (t % NB) * TB, tl.vvo()); };
 
@@ -1573,10 +1594,11 @@ static int64_t mass_blocks(int dtype, const CacheArgs &c) {
 static size_t mass_part_bytes(const CacheArgs &c, int splits) {
   return (size_t)c.batch * c.kvh * splits * c.cap * sizeof(float);
 }
-// Row ranges of at least 256 rows, as many as give every compute unit a block
+// Row ranges of at least 256 rows, as many as give every compute unit a block (300 rows over 1,000 keys, 4 heads of 64:
+// 11.3 us, 14.5 in two ranges; 600: 13.9 and 12.8)
 static int mass_wanted(int dtype, const CacheArgs &c) {
   const int64_t fill = device_cus() / std::max<int64_t>(1, mass_blocks(dtype, c));
-  const int64_t most = ((int64_t)c.max_q * (c.heads / c.kvh) + 255) / 256;
+  const int64_t most = (int64_t)c.max_q * (c.heads / c.kvh) / 256;
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(fill, most), 64));
 }
 int cache_mass_splits(int dtype, const CacheArgs &c, size_t scratch) {
