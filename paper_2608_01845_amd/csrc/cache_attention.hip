@@ -1465,7 +1465,8 @@ size_t attn_part_bytes(const CacheArgs &c, int splits) {
 // keys, 32 heads on 8 of 128: 87 us, 103 without; 16 over 4,000 keys each, 16 heads of 128: 94, 98 with twice as many; four
 // over 100 to 30,000: 40, 50 without and 36 with twice as many). A second launch and its reads
 // cost about 5 us: 16 rows and fewer are not cut below 65,536 / hd keys (1,000 keys, 16 heads
-// of 64, one row: 10.1 us whole, 13.0 in four), others not below 256.
+// of 64, one row: 10.1 us whole, 13.0 in four), others not below 256, float32 beyond 256 keys not below 128 (its tile
+// of 32 keys is 2 us of matrix instructions, 4 at hd 128: one row over 642 keys, 8 heads, 16.5 and 22.9 us with 256, 13.7 and 17.9 so).
 // Of hd 128 only up to 32 rows where there is much to read (64 rows, 16 heads, eight sequences of 1,000 keys: 34
 // us, 28.6 in blocks of 128 rows; one of 3,456 keys: 19.4 and 20.8).
 //
@@ -1492,7 +1493,8 @@ void attn_plan(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *ran
     const int r = dtype == 1 && m <= 16 ? 16 : 32;
     const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
     const int64_t want = std::max<int64_t>(1, slots / blocks);
-    set(r, std::max<int64_t>(r == 16 ? 65536 / c.hd : 256, (c.cap + want - 1) / want));
+    const int64_t least = r == 16 ? 65536 / c.hd : dtype == 1 || c.cap <= 256 ? 256 : 128;
+    set(r, std::max(least, (c.cap + want - 1) / want));
   } else {
     const int64_t tiles = (c.cap + 63) / 64;
     double best = 0;
