@@ -5,6 +5,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace wdc {
 namespace {
@@ -180,11 +181,12 @@ __device__ __forceinline__ uint32_t mass_order(float m) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int EVT = 1024, EVW = EVT / 64;   // threads and waves of a selection block
+constexpr int EVT = 1024, EVW = EVT / 64;   // threads and waves of a selection block (256 and 4 for short sequences) (of one part, see evict_plan: fewer)
 constexpr int EVP = 16;                     // parts of a long (sequence, kv head); one wave sums up one part
 constexpr int EVK = 8;                      // weights that a thread keeps in registers
 constexpr int EVA = 8192;                   // keys that share digit 0 with the threshold, listed as they come
-constexpr int EVH = 4096;                   // words of LDS for histograms: copies of one, to spread equal digits over
+// words of LDS for histograms: copies of one, to spread equal digits over
+constexpr int ev_words(int threads) { return threads == EVT ? 4096 : 2048; }
 static_assert(EVP == EVW, "a wave per part");
 // digits of the order values, from the top: 10, 11 and 11 bits
 __device__ __forceinline__ constexpr int ev_shift(int d) { return d == 0 ? 22 : d == 1 ? 11 : 0; }
@@ -200,8 +202,9 @@ __host__ __device__ inline int64_t evict_words(int moves, int parts, int cap) {
 
 // What one block of the selection works on: slots [s0, s1) of a (sequence, kv head) of n > keep
 // keys. STORED: the order values of the weights are read from the scratch (else from the masses).
-template <bool STORED>
+template <bool STORED, int T>
 struct EvictPart {
+  static constexpr int W = T / 64;
   const CacheEvictArgs &a;
   int h, b, n, s0, s1, low_len, high_len;
   const int32_t *tab;
@@ -225,7 +228,7 @@ struct EvictPart {
     high_len = a.parts > a.low ? (max(n - a.keep, 0) + a.parts - a.low - 1) / (a.parts - a.low) : 0;
     s0 = bound(blockIdx.y);
     s1 = bound(blockIdx.y + 1);
-    const int run = ((s1 - s0 + 64 * EVW - 1) / (64 * EVW)) * 64;
+    const int run = ((s1 - s0 + T - 1) / T) * 64;
     j0 = min(s0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * run, s1);
     j1 = min(j0 + run, s1);
     if (STORED) {
@@ -301,11 +304,12 @@ __device__ __forceinline__ uint32_t evict_tally(uint32_t *hist, int d) {
   return d == same ? base + __popcll(alike & (lane ? ~0ull >> (64 - lane) : 0ull)) : at;
 }
 
-// Histogram of digit d of the block's slots that share the digits found so far, in EVH / bins copies
-template <bool STORED>
-__device__ __forceinline__ void evict_count(const EvictPart<STORED> &p, uint32_t *hist, int d, uint32_t prefix, uint32_t known) {
-  const int tid = threadIdx.x, copy = (tid >> 6) % (EVH / ev_bins(d)) * ev_bins(d);
-  for (int i = tid; i < EVH; i += EVT) hist[i] = 0;
+// Histogram of digit d of the block's slots that share the digits found so far, in as many copies as there is room for
+template <bool STORED, int T>
+__device__ __forceinline__ void evict_count(const EvictPart<STORED, T> &p, uint32_t *hist, int d, uint32_t prefix,
+                                            uint32_t known) {
+  const int tid = threadIdx.x, copy = (tid >> 6) % (ev_words(T) / ev_bins(d)) * ev_bins(d);
+  for (int i = tid; i < ev_words(T); i += T) hist[i] = 0;
   __syncthreads();
   p.each([&](int j, uint32_t u) __attribute__((always_inline)) {
     const bool in = j < p.j1 && p.middle(j) && (u & known) == prefix;
@@ -315,28 +319,44 @@ __device__ __forceinline__ void evict_count(const EvictPart<STORED> &p, uint32_t
 }
 
 // Sum of x over the threads before this one
+template <int T>
 __device__ __forceinline__ uint32_t block_before(uint32_t x) {
-  __shared__ uint32_t wsum[EVW];
+  __shared__ uint32_t wsum[T / 64];
   const uint32_t incl = (uint32_t)wave_scan((int)x);
   if ((threadIdx.x & 63) == 63) wsum[threadIdx.x >> 6] = incl;
   __syncthreads();
   uint32_t before = incl - x;
 #pragma unroll
-  for (int i = 0; i < EVW; ++i) before += i < (int)(threadIdx.x >> 6) ? wsum[i] : 0u;
+  for (int i = 0; i < T / 64; ++i) before += i < (int)(threadIdx.x >> 6) ? wsum[i] : 0u;
   return before;
 }
 
 // Bin in which the rank-th key from the top lies, and its rank there. Bins go
-// from the top: thread t brings bins top = bins - 1 - per t (first) and top - 1
-// (second, if per = 2). All threads get the results; *size: the keys of that bin.
-__device__ __forceinline__ void evict_pick(uint32_t first, uint32_t second, int top, int rank, int *bin, int *r, int *size) {
+// from the top: thread t has bins top = bins - 1 - PER t, top - 1, .. with count(0), count(1), .. keys.
+// All threads get the results; *size: the keys of that bin.
+template <int T, int PER, class F>
+__device__ __forceinline__ void evict_pick(F &&count, int top, int rank, int *bin, int *r, int *size) {
   __shared__ int got[3];
-  const uint32_t mine = first + second, before = block_before(mine);
+  uint32_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mine += count(i);
+  const uint32_t before = block_before<T>(mine);
   if (before < (uint32_t)rank && before + mine >= (uint32_t)rank) {   // one thread
-    const uint32_t x = rank - before;
-    got[0] = x > first ? top - 1 : top;
-    got[1] = (int)(x > first ? x - first : x);
-    got[2] = (int)(x > first ? second : first);
+    uint32_t x = rank - before, at = 0, n = 0;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t c = count(i);
+      if (!found && x <= c) {
+        found = true;
+        at = i;
+        n = c;
+      }
+      if (!found) x -= c;
+    }
+    got[0] = top - (int)at;
+    got[1] = (int)x;
+    got[2] = (int)n;
   }
   __syncthreads();
   *bin = got[0];
@@ -349,10 +369,10 @@ __device__ __forceinline__ void evict_pick(uint32_t first, uint32_t second, int 
 // them are kept, of the part's `eqn` equal to it those that are among the first `taken` of all (eq0 of them lie in
 // parts before); hr holes and mr movers lie in parts before. Each wave takes a contiguous run of slots,
 // and counts of runs are added in order, so every list is in slot order.
-template <bool STORED>
-__device__ __forceinline__ void evict_lists(const EvictPart<STORED> &p, uint32_t threshold, uint32_t known, bool any,
+template <bool STORED, int T>
+__device__ __forceinline__ void evict_lists(const EvictPart<STORED, T> &p, uint32_t threshold, uint32_t known, bool any,
                                             int taken, int eq0, int eqn, int hr, int mr) {
-  __shared__ int wcnt[3][EVW];
+  __shared__ int wcnt[3][(T / 64)];
   const CacheEvictArgs &a = p.a;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), keep = a.keep;
   int32_t *idx = a.index ? a.index + ((int64_t)p.b * a.c.kvh + p.h) * keep : nullptr;
@@ -369,7 +389,7 @@ __device__ __forceinline__ void evict_lists(const EvictPart<STORED> &p, uint32_t
     if (lane == 0) wcnt[0][w] = eq;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < EVW; ++i) eq0 += i < w ? wcnt[0][i] : 0;
+    for (int i = 0; i < (T / 64); ++i) eq0 += i < w ? wcnt[0][i] : 0;
   }
   // f(slot, kept) in order
   auto kept_each = [&](auto &&f) __attribute__((always_inline)) {
@@ -396,7 +416,7 @@ __device__ __forceinline__ void evict_lists(const EvictPart<STORED> &p, uint32_t
   __syncthreads();
   int total = 0;
 #pragma unroll
-  for (int i = 0; i < EVW; ++i) {
+  for (int i = 0; i < (T / 64); ++i) {
     hr += i < w ? wcnt[1][i] : 0;
     mr += i < w ? wcnt[2][i] : 0;
     total += wcnt[1][i];
@@ -415,11 +435,11 @@ __device__ __forceinline__ void evict_lists(const EvictPart<STORED> &p, uint32_t
 }
 
 // A sequence that is short enough: everything stays
-template <bool STORED>
-__device__ __forceinline__ void evict_none(const EvictPart<STORED> &p) {
+template <bool STORED, int T>
+__device__ __forceinline__ void evict_none(const EvictPart<STORED, T> &p) {
   const CacheEvictArgs &a = p.a;
   int32_t *idx = a.index ? a.index + ((int64_t)p.b * a.c.kvh + p.h) * a.keep : nullptr;
-  const int first = blockIdx.y * EVT + threadIdx.x, step = gridDim.y * EVT;
+  const int first = blockIdx.y * T + threadIdx.x, step = gridDim.y * T;
   if (idx) {
     for (int j = first; j < p.n; j += step) idx[j] = j;
     for (int j = p.n + first; j < a.keep; j += step) idx[j] = -1;
@@ -433,7 +453,9 @@ __device__ __forceinline__ void evict_none(const EvictPart<STORED> &p) {
 // equal to it are kept. Kept keys below `keep` stay; hole j below it takes kept key j from above, so
 // nothing that is still to be read is written and only those rows move.
 //
-// One block does it all for short sequences (STAGE -1). What bounds that form is
+// One block does it all for short sequences (STAGE -1), of 256 threads for the shortest, whose time is barriers (12
+// kv heads, 76 keys: 13.5 us with the moves, 16.6 with 1,024; 2,048 sequences of 100 keys, 16 heads: 172, 752; but four
+// of 2,000 keys: 19.3, 17.0). What bounds that form on long ones is
 // the instruction rate of one compute unit (67,320 slots: 189 us), so long ones are cut into EVP parts of one
 // block each and the steps become launches. 0: order values stored, digit 0 counted. 1: digit 0 of the
 // threshold from all parts' counts; the keys that share it listed, those above it counted. 2: the other digits from
@@ -443,10 +465,11 @@ __device__ __forceinline__ void evict_none(const EvictPart<STORED> &p) {
 // each bin on, so that stage 2 reads those of one bin only. 16 heads, 67,320 slots, 61,200 kept: 8.5, 6 and
 // 11 us, launches and the latency of a dozen dependent steps (masses over many binades; within one 48 us in all,
 // all equal 58). Reading all 16 parts' counts of every digit in every block instead took 15 us more.
-template <int STAGE>
-__global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
+template <int STAGE, int T>
+__global__ __launch_bounds__(T) void k_evict_select(CacheEvictArgs a) {
+  constexpr int EVH = ev_words(T);
   __shared__ uint32_t hist[EVH];
-  const EvictPart<(STAGE > 0)> p(a);
+  const EvictPart<(STAGE > 0), T> p(a);
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), part = blockIdx.y;
   if (p.n <= a.keep) {
     if (STAGE < 0 || STAGE == 2) evict_none(p);
@@ -454,21 +477,25 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
   }
   const int m = a.keep - a.sink - a.recent;
   // evict_pick from the LDS histogram of digit d
-  auto pick = [&](int d, int rank, int *bin, int *r, int *size) __attribute__((always_inline)) {
-    const int per = ev_bins(d) / EVT, top = ev_bins(d) - 1 - per * tid;
-    uint32_t first = 0, second = 0;
-    for (int i = 0; i < EVH; i += ev_bins(d)) {
-      first += hist[i + top];
-      if (per > 1) second += hist[i + top - 1];
-    }
-    evict_pick(first, second, top, rank, bin, r, size);
+  auto pick = [&](auto dc, int rank, int *bin, int *r, int *size) __attribute__((always_inline)) {
+    constexpr int D = decltype(dc)::value, PER = ev_bins(D) / T;
+    const int top = ev_bins(D) - 1 - PER * tid;
+    evict_pick<T, PER>([&](int i) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int q = 0; q < EVH; q += ev_bins(D)) n += hist[q + top - i];
+      return n;
+    }, top, rank, bin, r, size);
   };
   if constexpr (STAGE < 0) {
     uint32_t prefix = 0, known = 0;
     int rank = m, bin, size = m + 1;
     for (int d = 0; d < 3 && m > 0 && size != rank; ++d) {   // until all of a bin are taken
       evict_count(p, hist, d, prefix, known);
-      pick(d, rank, &bin, &rank, &size);
+      if (d == 0)
+        pick(std::integral_constant<int, 0>{}, rank, &bin, &rank, &size);
+      else
+        pick(std::integral_constant<int, 1>{}, rank, &bin, &rank, &size);   // (digit 2 has as many bins)
       prefix |= (uint32_t)bin << ev_shift(d);
       known |= (uint32_t)(ev_bins(d) - 1) << ev_shift(d);
     }
@@ -479,7 +506,7 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
     p.each([&](int j, uint32_t u) __attribute__((always_inline)) {
       if (j < p.j1) p.order[j] = u;
     });
-    static_assert(ev_bins(0) == EVT && EVH == 4 * EVT, "a thread per bin");
+    static_assert(ev_bins(0) == T && T == EVT && EVH == 4 * EVT, "a thread per bin");
     p.hist[part * EVT + tid] = hist[tid] + hist[EVT + tid] + hist[2 * EVT + tid] + hist[3 * EVT + tid];
   } else if constexpr (STAGE == 1) {
     __shared__ uint32_t listed, over;
@@ -491,7 +518,7 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
     if (tid == 0) listed = over = 0;
     for (int i = tid; i < ev_bins(1); i += EVT) hist[i] = 0;
     int bin, rank, size;
-    evict_pick(sum, 0u, top, m, &bin, &rank, &size);
+    evict_pick<T, 1>([&](int) { return sum; }, top, m, &bin, &rank, &size);
     if (part == 0 && tid == 0) {
       p.found[0] = (uint32_t)bin << ev_shift(0);
       p.found[1] = (uint32_t)rank;
@@ -503,7 +530,7 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
       p.each([&](int j, uint32_t u) __attribute__((always_inline)) { evict_tally(hist, digit1(j, u)); });
       __syncthreads();
       const int b1 = ev_bins(1) - 1 - 2 * tid;   // from bins b1 and b1 - 1 on; hist: where they begin in the list
-      const uint32_t x = hist[b1], y = hist[b1 - 1], before = block_before(x + y);
+      const uint32_t x = hist[b1], y = hist[b1 - 1], before = block_before<T>(x + y);
       *(uint2 *)(p.from + part * ev_bins(1) + b1 - 1) = make_uint2(before + x + y, before + x);
       hist[b1] = before;
       hist[b1 - 1] = before + x;
@@ -594,7 +621,7 @@ __global__ __launch_bounds__(EVT) void k_evict_select(CacheEvictArgs a) {
           evict_tally(hist, in && (y & known) == prefix ? copy + (int)((y >> ev_shift(d)) & (ev_bins(d) - 1)) : -1);
         });
         __syncthreads();
-        pick(d, rank, &bin, &rank, &size);
+        pick(std::integral_constant<int, 1>{}, rank, &bin, &rank, &size);
         prefix |= (uint32_t)bin << ev_shift(d);
       }
       alike([&](uint32_t y, bool in) __attribute__((always_inline)) {
@@ -686,11 +713,14 @@ hipError_t launch_cache_evict(int dtype, const CacheEvictArgs &in, hipStream_t s
   evict_plan(a);
   const dim3 sel(a.c.kvh, a.parts, a.c.batch);   // with 8 kv heads the parts of one share an XCD, and their counts its L2
   if (a.parts == 1) {
-    hipLaunchKernelGGL((k_evict_select<-1>), sel, dim3(EVT), 0, s, a);
+    if (a.c.cap <= (a.c.batch * a.c.kvh >= 512 ? 2048 : 1024))
+      hipLaunchKernelGGL((k_evict_select<-1, 256>), sel, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_evict_select<-1, EVT>), sel, dim3(EVT), 0, s, a);
   } else {
-    hipLaunchKernelGGL((k_evict_select<0>), sel, dim3(EVT), 0, s, a);
-    hipLaunchKernelGGL((k_evict_select<1>), sel, dim3(EVT), 0, s, a);
-    hipLaunchKernelGGL((k_evict_select<2>), sel, dim3(EVT), 0, s, a);
+    hipLaunchKernelGGL((k_evict_select<0, EVT>), sel, dim3(EVT), 0, s, a);
+    hipLaunchKernelGGL((k_evict_select<1, EVT>), sel, dim3(EVT), 0, s, a);
+    hipLaunchKernelGGL((k_evict_select<2, EVT>), sel, dim3(EVT), 0, s, a);
   }
   const int rb = a.c.hd * (dtype == 1 ? 2 : 4), rpb = 256 / (rb / 16);
   const int per = std::max(1, 2048 / std::max(1, a.c.kvh * a.c.batch));

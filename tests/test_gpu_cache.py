@@ -355,6 +355,11 @@ EVICT = [
     ("bf16", 1, 128, 256, [9000, 8999], 8990, 0, 0, "equal"),
     ("bf16", 64, 64, 64, [4200] * 4, 4000, 10, 20, "ties"),
     ("bf16", 2, 64, 16, MANY_KV, 20, 3, 4, "random"),
+    ("bf16", 2, 64, 16, [1024, 1000, 257, 255, 64, 65], 250, 3, 4, "odd"),       # blocks of 256 threads
+    ("bf16", 2, 64, 16, [1024, 700], 600, 0, 0, "near"),
+    ("bf16", 2, 64, 16, [1025, 700], 600, 0, 0, "ties"),
+    ("bf16", 128, 64, 64, [2048, 2000, 1999, 3], 1500, 700, 800, "equal"),
+    ("bf16", 128, 64, 64, [2048, 2000, 1999, 3], 1500, 7, 80, "ties"),
     ("bf16", 2, 64, 64, [30000, 9000, 21000], 20000, 100, 200, "near"),
     ("f32", 1, 64, 32, [40000], 12345, 0, 0, "near"),
     ("bf16", 1, 64, 32, [40000], 39000, 50, 60, "ties"),
