@@ -692,11 +692,14 @@ hipError_t launch_cache_append(int dtype, const CacheAppendArgs &a, hipStream_t 
   return a.c.hd == 128 ? append<float, 128>(a, s) : append<float, 64>(a, s);
 }
 
-// Moves and parts of a launch over these bounds. One block per (sequence, kv head) for up to 4,096 slots, and where
-// there are enough of them to fill the compute units.
+// Moves and parts of a launch over these bounds. One block per (sequence, kv head) for up to 8,192 slots (16 heads: 8,000
+// slots 20.8 us, in parts 20.9; 12,000: 31.4 and 22.1), for more where there are more of them, which share the compute
+// units (four sequences of 10,000, 8 heads: 31.0 and 34.8; of 16,000, eight of 4 heads: 46.9 and 37.5; twelve of 5,000, 16
+// heads: 36.8 and 162), and always where they fill these.
 static void evict_plan(CacheEvictArgs &a) {
   a.moves = std::max(0, std::min(a.keep, a.c.cap - a.keep));
-  a.parts = a.c.cap <= 4096 || a.moves == 0 || a.c.batch * a.c.kvh >= 256 ? 1 : EVP;
+  const int heads = a.c.batch * a.c.kvh;
+  a.parts = a.c.cap <= 8192 + 256 * std::max(0, heads - 16) || a.moves == 0 || heads >= 256 ? 1 : EVP;
   a.low = a.parts == 1 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(EVP - 1, (int64_t)EVP * a.keep / std::max(1, a.c.cap)));
 }
 
