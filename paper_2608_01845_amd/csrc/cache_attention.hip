@@ -215,7 +215,12 @@ __device__ __forceinline__ void cache_block(const CacheArgs &c, int per, int &bh
 //
 // Softmax in base 2 with a reference m per row that moves when a score passes it
 // by more than 8: scores are scaled by log2(e)/sqrt(hd) in float32, weights are summed in
-// float32 and rounded to bf16 once for the product with V (as its operand type).
+// float32 and rounded to bf16 once for the product with V (as its operand type). The rounded ones are summed as well
+// and O is scaled by the ratio of the two sums: then it is a mean of V whatever their rounding, so that a key which
+// has nearly all of the weight comes out as it is (else off by up to half a bf16 step, 1.6 times the error of a single
+// rounding over keys of which a few dominate).
+__device__ __forceinline__ float unround(float sum, float rounded) { return rounded == 0.f ? 1.f : sum / rounded; }
+
 template <int HD>
 struct Few {
   static constexpr int ROWB = HD * 2;            // bytes of a row
@@ -315,11 +320,11 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   };
 
   f32x4 o[RT][NI];
-  float m[RT], l[RT];
+  float m[RT], l[RT], d[RT];                     // d: sum of the rounded weights
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     m[t] = -INFINITY;
-    l[t] = 0.f;
+    l[t] = d[t] = 0.f;
 #pragma unroll
     for (int i = 0; i < NI; ++i) o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -363,6 +368,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
         const float mn = fmaxf(m[r], mx), al = mn == m[r] ? 1.f : __builtin_amdgcn_exp2f(m[r] - mn);
         m[r] = mn;
         l[r] *= al;
+        d[r] *= al;
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -376,6 +382,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
           const float p = __builtin_amdgcn_exp2f(S[r][k][e] - ref);
           l[r] += p;
           pf[r][k][e] = (__bf16)p;
+          d[r] += (float)pf[r][k][e];
         }
     }
     // A key that a row does not see has weight 0, but 0 times an infinity or NaN
@@ -450,8 +457,9 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     l[t] = quad_sum(l[t]);
+    const float f = unround(l[t], quad_sum(d[t]));
 #pragma unroll
-    for (int i = 0; i < NI; ++i) *(f32x4 *)(po + (16 * t + lr) * HD + 4 * ((4 * i + lg) ^ (lr & 7))) = o[t][i];
+    for (int i = 0; i < NI; ++i) *(f32x4 *)(po + (16 * t + lr) * HD + 4 * ((4 * i + lg) ^ (lr & 7))) = o[t][i] * f;
     if (lg == 0) {
       ml[w][0][16 * t + lr] = m[t];
       ml[w][1][16 * t + lr] = l[t];
@@ -514,7 +522,9 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 // maximum, moved only when a lane's sum of weights over a tile passes 2^64 (then O and the
 // sum are rescaled and P is taken again); any reference gives the same result.
 // Tiles that some row sees in part, and the cache's last, partial one, follow one at a
-// time with their masks.
+// time with their masks. There m is the row's largest score so far, so that a key with nearly all
+// of the weight of a row that sees few has weight 1, without rounding. (Summing the rounded weights too, as with few
+// rows, spills at hd 128: 5% on the call above, 20% on 2,048 rows causal over themselves.)
 constexpr int KV = 64, NB = 4;
 constexpr float SUM_LIMIT = 0x1p64f;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
@@ -886,7 +896,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
         for (int e = 0; e < 4; ++e)
           if (key0 + 16 * k + 4 * lg + e >= lim[t]) S[k][t][e] = -INFINITY;
       const float mx = rowmax<HD>(S, t) * sc;
-      if (__any(mx > m[t] + 8.f)) {
+      if (__any(mx > m[t])) {                    // the largest itself: its weight is 1, without rounding
         const float mn = fmaxf(m[t], mx), al = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
         m[t] = mn;
         l[t] *= al;
