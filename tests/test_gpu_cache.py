@@ -248,6 +248,20 @@ def test_attention_unseen_keys_have_no_influence(dtype, hd, q, kv, frame):
     within(z[fine], lse[fine], (lse_bound + 4 * EPS32 * lse.abs())[fine], "lse")
 
 
+@pytest.mark.parametrize("heads,kvh,hd,q", [(4, 4, 64, 1), (4, 2, 128, 7), (4, 4, 64, 40), (4, 4, 128, 40), (4, 2, 64, 200),
+                                           (4, 2, 128, 200), (16, 1, 64, 4090), (16, 1, 128, 4090)])
+def test_attention_over_one_key_is_its_value(heads, kvh, hd, q):
+    """The first row of a chunk at the start of a cache sees one key: whatever its weight's rounding, the result is v. (The
+    weight over its sum is 1 up to a few float32 steps, which do not reach half a bf16 step.)"""
+    s = cu.state("bf16", heads, kvh, hd, 16, [q, 1], [q, 1], seed=28, scale=1.3)
+    wdc, ctx = ctx_of(s)
+    out = ctx.cache_attention(wdc.PagedCache(s.k, s.v), cu.chunks(wdc, s), s.x, torch.empty_like(s.x), frame=1)
+    for b, row in ((0, 0), (1, q)):
+        pg, sl = cu.where(s, b)
+        v = s.v[pg[0], :, sl[0]].repeat_interleave(heads // kvh, 0)
+        assert torch.equal(out[row].reshape(heads, hd), v)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_large_scores_and_rising_maxima(dtype):
     """Scores of some hundreds, rising along the keys: the softmax reference has to move, late and far."""
