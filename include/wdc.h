@@ -397,7 +397,8 @@ wdc_status wdc_cache_mass(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_
  * of the other slots below keep takes the j-th kept key from above (k, v and mass), so the order of
  * the keys changes (attention does not depend on it) and `recent` means what was appended last only
  * while it is at most the rows appended since the last eviction. d_kv_len_out [batch] = min(n, keep)
- * (may be d_kv_len). d_index [batch, kv_heads, keep] int32 or NULL: the former slot of every slot, -1 past n.
+ * (may be d_kv_len). d_index [batch, kv_heads, keep] int32 or NULL: the former slot of every slot, -1 past n
+ * (batch * kv_heads * keep <= 2^28, else WDC_E_SHAPE).
  * d_mass_out as in wdc_cache_mass: the kept keys' masses. sink + recent <= keep, keep >= 1.
  * d_scratch: wdc_cache_evict_scratch() bytes, required (else WDC_E_WORKSPACE). Of d_chunks only batch,
  * d_kv_len, d_table, table_ld and max_kv are used. */

@@ -181,7 +181,7 @@ __device__ __forceinline__ uint32_t mass_order(float m) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int EVT = 1024, EVW = EVT / 64;   // threads and waves of a selection block (256 and 4 for short sequences) (of one part, see evict_plan: fewer)
+constexpr int EVT = 1024, EVW = EVT / 64;   // threads and waves of a selection block (256 and 4 for short sequences)
 constexpr int EVP = 16;                     // parts of a long (sequence, kv head); one wave sums up one part
 constexpr int EVK = 8;                      // weights that a thread keeps in registers
 constexpr int EVA = 8192;                   // keys that share digit 0 with the threshold, listed as they come
@@ -204,7 +204,6 @@ __host__ __device__ inline int64_t evict_words(int moves, int parts, int cap) {
 // keys. STORED: the order values of the weights are read from the scratch (else from the masses).
 template <bool STORED, int T>
 struct EvictPart {
-  static constexpr int W = T / 64;
   const CacheEvictArgs &a;
   int h, b, n, s0, s1, low_len, high_len;
   const int32_t *tab;

@@ -300,7 +300,7 @@ struct CacheEvictArgs {
   float *out;               // may be mass
   int32_t *len_out, *index; // index may be null
   int keep, sink, recent;
-  int32_t *list;            // scratch, see evict_layout
+  int32_t *list;            // scratch, see evict_words
   // set by launch_cache_evict: most moves of a (sequence, kv head); parts its
   // slots are cut into, the first `low` of them below keep (1 part: one block does all)
   int moves, parts, low;

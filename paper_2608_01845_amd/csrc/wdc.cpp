@@ -1900,6 +1900,10 @@ wdc_status wdc_cache_evict(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc
     set_err(ctx, "keep %d, sink %d, recent %d: need keep >= 1 and sink + recent <= keep", keep, sink, recent);
     return WDC_E_ARG;
   }
+  if (d_index && (int64_t)a.c.batch * a.c.kvh * keep > kCacheKeys) {
+    set_err(ctx, "index of %lld entries is too large", (long long)a.c.batch * a.c.kvh * keep);
+    return WDC_E_SHAPE;
+  }
   if (!d_scratch || scratch_bytes < cache_evict_scratch(a.c, keep)) {
     set_err(ctx, "scratch too small: %zu < %zu", d_scratch ? scratch_bytes : (size_t)0, cache_evict_scratch(a.c, keep));
     return WDC_E_WORKSPACE;

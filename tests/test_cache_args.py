@@ -107,6 +107,7 @@ def test_tensors_are_refused(wdc):
             h, c, q, m, o, k, s, r, n, i, sc, b)
         assert ev(m=None) == ev(o=None) == ev(n=None) == ev(k=0) == ev(s=-1) == ev(r=-1) == ev(s=3, r=2) == ARG
         assert ev(s=0x7fffffff, r=0x7fffffff) == ARG
+        assert ev(k=0x7fffffff, i=p) == ev(k=(1 << 25) + 1, i=p) == SHAPE
         assert ev(sc=None) == ev(b=8) == WORKSPACE
         assert ev(m=two) == ev(o=two) == ev(n=two) == ev(i=two) == ev(sc=odd) == ALIGN
         need = lib.wdc_cache_evict_scratch(h, c, q, 50)
