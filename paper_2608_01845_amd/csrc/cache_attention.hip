@@ -32,14 +32,17 @@ __device__ __forceinline__ u32x4_t buffer_at(const void *base, int64_t off, int 
 // Direct global -> LDS loads: lane l's 16 (4) bytes at `voff` of the buffer arrive
 // at lds + 16 l (4 l). Written as instructions because the compiler lets no transposed LDS read pass while one
 // of its own direct loads is under way (it waits for all of them); nothing is returned in
-// registers, and the waits for the data are wait_vm's. The kernels that use these use no others, so M0 is theirs.
+// registers, and the waits for the data are wait_vm's. The wait states are ours as well, since the compiler
+// looks for hazards between its own instructions only: a scalar register written by a vector instruction
+// (v_readfirstlane makes the descriptor's words) is there for a memory instruction five wait states later, one
+// of s_mov_b32 and four of s_nop 3; M0 needs one of them.
 __device__ __forceinline__ void lds_load16(u32x4_t buf, uint32_t lds, int voff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buf)
-               : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buf)
+               : "memory", "m0");
 }
 __device__ __forceinline__ void lds_load4(u32x4_t buf, uint32_t lds, int voff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buf)
-               : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buf)
+               : "memory", "m0");
 }
 // LDS address of a pointer into it, the same in every lane
 __device__ __forceinline__ uint32_t lds_addr(const void *p) {
