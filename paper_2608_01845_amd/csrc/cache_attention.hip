@@ -9,6 +9,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 namespace wdc {
@@ -523,7 +524,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 // stream, the vector work of tile t + 1 (P = exp2(sc S - m), its row sum in float32, its
 // rounding to bf16). m is a reference per row, not a running maximum: the first tile's
 // maximum, moved only when a lane's sum of weights over a tile passes 2^64 (then O and the
-// sum are rescaled and P is taken again); any reference gives the same result.
+// sum are rescaled and P is taken again). With scores beyond 2^20 in a wave's rows every tile's P is taken again (see far_out).
 // Tiles that some row sees in part, and the cache's last, partial one, follow one at a
 // time with their masks. There m is the row's largest score so far, so that a key with nearly all
 // of the weight of a row that sees few has weight 1, without rounding. (Summing the rounded weights too, as with few
@@ -604,9 +605,19 @@ __device__ __forceinline__ float rowmax(const f32x4 (&S)[4][2], int t) {
     for (int e = 0; e < 4; ++e) mx = fmaxf(mx, S[k][t][e]);
   return quad_max(mx);
 }
-// P of one row tile, its lane sums
-__device__ __forceinline__ float weights(const f32x4 (&S)[4][2], bf16x8 (&pf)[2], int t, float sc, float m) {
+// Whether a row of the wave has a reference so large that its rounding, half a step of m = sc max S, changes what
+// fma(S, sc, -m) is for the largest S by more than 2^-4: the weights of such a row would pass float32's range or all vanish.
+__device__ __forceinline__ bool far_out(float m) { return __any(fabsf(m) > 0x1p20f); }
+
+// P of one row tile, its lane sums. Far out S sc is rounded like the reference before m is taken off (S is scaled in
+// place), so that the largest score has weight 1.
+__device__ __forceinline__ float weights(f32x4 (&S)[4][2], bf16x8 (&pf)[2], int t, float sc, float m) {
   float ls = 0.f;
+  if (far_out(m)) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) S[k][t] *= sc;
+    sc = 1.f;
+  }
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -724,9 +735,11 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
     qk(S[0], ring);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      m[t] = fmaxf(rowmax<HD>(S[0], t) * sc, -1e30f);
+      m[t] = fmaxf(rowmax<HD>(S[0], t) * sc, -FLT_MAX);   // (scores of -inf: weight 0)
       l[t] = weights(S[0], pf[0][t], t, sc, m[t]);
     }
+    // a lane's sum of weights above which a tile's weights are taken again; far out all are
+    float limit = far_out(fmaxf(fabsf(m[0]), fabsf(m[1]))) ? -1.f : SUM_LIMIT;
     if (nf > 1) qk(S[1], ring + TB);
     if (grp_a) {                                 // K_2 and V_1: at most K_3 and V_2 are still under way
       if (tot >= NB)
@@ -818,7 +831,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
         }
       }
       if (t + 1 < nf) {
-        if (__any(fmaxf(ls[0], ls[1]) > SUM_LIMIT)) {
+        if (__any(!(fmaxf(ls[0], ls[1]) <= limit))) {
 #pragma unroll
           for (int t_ = 0; t_ < 2; ++t_) {
             const float mx = rowmax<HD>(S[cur], t_) * sc, mn = mx > m[t_] + 8.f ? mx : m[t_];
@@ -831,6 +844,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
               for (int e = 0; e < 4; ++e) o[i][t_][e] *= al;
             ls[t_] = weights(S[cur], pf[cur][t_], t_, sc, m[t_]);
           }
+          limit = far_out(fmaxf(fabsf(m[0]), fabsf(m[1]))) ? -1.f : SUM_LIMIT;
         }
         l[0] += ls[0];
         l[1] += ls[1];
