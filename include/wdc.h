@@ -373,7 +373,8 @@ wdc_status wdc_cache_append(wdc_ctx *ctx, const wdc_paged_cache *cache, const wd
  * zeros. d_q [rows, ldq], d_o [rows, ldo], head h at columns [h * head_dim, ..), multiples of 16
  * bytes (d_o may be d_q with ldo = ldq); d_lse [rows, heads] float32 (or NULL): ln sum exp of the scores, -inf for a row that sees
  * nothing. float32 accumulation and statistics; bf16: attention weights rounded to bf16 before the product
- * with v. d_scratch: memory for splitting the keys of few rows over the device,
+ * with v. Sums of weights times v are divided at the end, with weights of up to 2^16: they stay finite while |v|
+ * is below 2^112 / (keys). d_scratch: memory for splitting the keys of few rows over the device,
  * wdc_cache_attention_scratch() bytes; with less (or NULL) the call runs with fewer parts. */
 size_t wdc_cache_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks);
 wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_q,

@@ -523,14 +523,15 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 // products of tile t, the Q K products of tile t + 2 and, in the same instruction
 // stream, the vector work of tile t + 1 (P = exp2(sc S - m), its row sum in float32, its
 // rounding to bf16). m is a reference per row, not a running maximum: the first tile's
-// maximum, moved only when a lane's sum of weights over a tile passes 2^64 (then O and the
-// sum are rescaled and P is taken again). With scores beyond 2^20 in a wave's rows every tile's P is taken again (see far_out).
+// maximum, moved only when a lane's sum of weights over a tile passes 2^16 (then O and the
+// sum are rescaled and P is taken again): weights of up to that are as exact as those below 1, and sums of them times v
+// stay within float32 while |v| is below 2^112 over the number of keys. With scores beyond 2^20 in a wave's rows every tile's P is taken again (see far_out).
 // Tiles that some row sees in part, and the cache's last, partial one, follow one at a
 // time with their masks. There m is the row's largest score so far, so that a key with nearly all
 // of the weight of a row that sees few has weight 1, without rounding. (Summing the rounded weights too, as with few
 // rows, spills at hd 128: 5% on the call above, 20% on 2,048 rows causal over themselves.)
 constexpr int KV = 64, NB = 4;
-constexpr float SUM_LIMIT = 0x1p64f;
+constexpr float SUM_LIMIT = 0x1p16f;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 
 // Loads of one wave (of four): stripe i of a tile is rows [(4 i + w) RPL, + RPL). SMALL:

@@ -84,3 +84,24 @@ def test_scores_of_minus_infinity_have_weight_zero(form):
     bound, lse_bound = attention_bound(s, pv, o, qk, kv)
     within(out, o, bound, "o")
     within(z, lse, lse_bound + 4 * EPS32 * lse.abs(), "lse")
+
+
+@forms
+@pytest.mark.parametrize("frame", [0, 24])
+@pytest.mark.parametrize("ramp,size", [(3, 1.0), (40, 1.0), (12, 2.0 ** 80), (40, 2.0 ** 80)], ids=str)
+def test_rising_scores_move_the_reference(form, frame, ramp, size):
+    """Scores rise along the keys to some 15 to 200 (in half of the rows they fall): the softmax reference moves once or
+    in every tile. Values of 2^80 times weights far above 1 would pass float32's range."""
+    dtype, heads, kvh, hd, page, q, kv = form
+    s = cu.state(dtype, heads, kvh, hd, page, [q], [kv], seed=34)
+    pg, sl = cu.where(s, 0)
+    rise = torch.linspace(0.1, ramp * (64 / hd) ** 0.5, kv, device="cuda")[:, None, None]
+    s.k[pg, :, sl] = (s.k[pg, :, sl].float().abs() * rise).to(s.td)
+    s.v *= size
+    s.x = s.x.abs()
+    s.x[1::2] *= -1
+    o, lse, pv, qk = cu.attention64(s, frame)
+    bound, lse_bound = attention_bound(s, pv, o, qk, kv)
+    out, z = attend(s, frame)
+    within(out, o, bound, "o")
+    within(z, lse, lse_bound + 4 * EPS32 * lse.abs(), "lse")
