@@ -210,8 +210,8 @@ __device__ __forceinline__ void cache_block(const CacheArgs &c, int per, int &bh
 // 4, .. of the block's range and the four partial softmaxes meet at the end. What
 // bounds it is the stream of K and V, so each wave keeps a tile under way beside the
 // one it works on, without a block barrier: direct loads into its own part of LDS, 8 KB a
-// tile (32 keys of 64, 16 of 128). Eight tokens over 1 to 32,768 keys, 32 heads on 8 kv heads of 128: 86 us,
-// 5.4 TB/s, where a large copy reaches 4.9.
+// tile (32 keys of 64, 16 of 128). Eight tokens over 1 to 32,768 keys, 32 heads on 8 kv heads of 128: 85 to 87 us,
+// 5.4 TB/s, also over four caches in turn, more than the last-level cache holds (a large copy, which writes too: 4.9).
 //
 // S^T = K Q^T (A: 16 keys, B: 16 rows) leaves lane (lr, lg) the keys 4 lg + e of
 // row lr; these values of one (hd 128) or two key tiles are the B operand of O^T = V^T P^T, whose A
@@ -508,8 +508,8 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 // ---------------------------------------------------------------- bf16, many rows
 // 32 query rows (two tiles of 16) a wave; key tiles of 64 reach four K and four V slots of LDS by direct buffer loads
 // of four waves, up to four tiles ahead. Bound by the matrix cores, with the
-// exponentials close behind, and by the power that both draw: 4,080 rows over 67,320 keys, 16 heads of 128, 1,780 us,
-// 1,250 TFLOP/s (a large library product: 1,200 to 1,580), the matrix cores busy in 66% of the
+// exponentials close behind, and by the power that both draw: 4,080 rows over 67,320 keys, 16 heads of 128, 1,750 to 1,860 us
+// by box, 1,190 to 1,260 TFLOP/s (a large library product: 1,200 to 1,580), the matrix cores busy in 65% of the
 // cycles of a clock that falls to 1.8 GHz.
 //
 // Blocks of 256 rows are 8 waves, two per SIMD: 1.0 us a tile at hd 64, 1.4 at hd 128. Few rows or keys leave
@@ -529,7 +529,9 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 // Tiles that some row sees in part, and the cache's last, partial one, follow one at a
 // time with their masks. There m is the row's largest score so far, so that a key with nearly all
 // of the weight of a row that sees few has weight 1, without rounding. (Summing the rounded weights too, as with few
-// rows, spills at hd 128: 5% on the call above, 20% on 2,048 rows causal over themselves.)
+// rows, costs 5% on the call above and 20% on 2,048 rows causal over themselves.) At hd 128 a wave's 256 registers do not
+// hold everything: 148 bytes a lane are in scratch, what only the masked tiles need: 21 to 23 reloads in each of them; none
+// in the pipeline over pages of 64 slots and more, two a step over smaller ones.
 constexpr int KV = 64, NB = 4;
 constexpr float SUM_LIMIT = 0x1p16f;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
@@ -558,8 +560,8 @@ struct TileLoads {
     const int r = w * F::RPL + lane / (HD / 8), ch = lane % (HD / 8);
     return (SMALL ? r & 15 : r) * F::ROWB + (ch ^ F::kkey(r)) * 16;
   }
-  // With small pages it is found again each time: a register kept for it would spill, and its reload would wait
-  // for all loads under way. (The lane's number by an instruction that is not moved out of the loop.)
+  // With small pages it is found again each time: a register kept for it would be spilled as well, and its reload in every
+  // step would wait for all loads under way. (The lane's number by an instruction that is not moved out of the loop.)
   __device__ __forceinline__ int kvo() const {
     if (!SMALL || HD == 64) return kvo_;
     int lane;
@@ -1081,7 +1083,8 @@ __device__ __forceinline__ int64_t slot_row(const CacheArgs &c, const int32_t *t
 // operand. Bound by the matrix instructions, so K and V come straight from the
 // caches: K of the next tile is asked for under this tile's softmax and P V. Keys past
 // the cache's end are read as its last key and get weight 0. Chunks of 256 and 100 rows over 1,500 and 777 keys, 4 heads of 64:
-// 15 us and 4 of the parts' launch; a wave has two tiles there, most of it latency.
+// 14 us and 4 of the parts' launch; a wave has two tiles there, most of it latency. 2,040 rows over 10,200 keys, 8 heads of
+// 128: 786 us, 108 TFLOP/s of a library product's 153.
 template <int HD>
 __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   constexpr int NI = HD / 32, NC = HD / 8;
@@ -1262,9 +1265,10 @@ struct MassRows {
 // bf16: a block of four waves holds 256 keys, 64 a wave, in registers (A operand)
 // and streams the rows past them, 128 a stage through two LDS slots of direct loads; every wave
 // reads all rows (B operand). A lane holds one row and 16 keys of a tile of 16 x 64 and adds
-// exp2(sc x - lse) to its 16 sums: multiply-add, exponential and sum are 24 cycles for 64 weights
-// beside 16 (hd 128) of matrix work, so the vector units bound it: 2,040 rows over 34,680 keys, 16 heads of 128, 290
-// us (990 TFLOP/s of matrix work; two waves per SIMD that share the rows' tiles: 339).
+// exp2(sc x - lse) to its 16 sums. Multiply-add, exponential and sum are 16 cycles for 64 weights, as many as hd 128's
+// matrix work; the vector units are busy in 69% of the cycles and the matrix cores in 48%. What is lost: the blocks' last
+// round, and in each stage one turn of nine without exponentials and one without products. 2,040 rows over 34,680 keys, 16
+// heads of 128, 287 to 310 us by box and load (1,010 to 930 TFLOP/s; two waves per SIMD that share the rows' tiles: 339).
 constexpr int MKT = 256, MST = 128, MNB = 2;
 template <int HD>
 __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
@@ -1405,7 +1409,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
 }
 
 // float32: four waves share 32 keys, held in registers, and take every fourth
-// tile of 32 rows, read straight from the caches: bound by the matrix instructions (64 cycles each).
+// tile of 32 rows, read straight from the caches: bound by the matrix instructions (64 cycles each): 2,040 rows over 10,200
+// keys, 8 heads of 128, 425 us, 100 TFLOP/s of a library product's 153; 356 rows over 1,500 and 777 keys 11 us, latency.
 template <int HD>
 __global__ __launch_bounds__(256) void k_cache_mass_f32(CacheMassArgs a) {
   constexpr int KT = 32, NC = HD / 8;
