@@ -489,8 +489,9 @@ class Context:
                     kv_len_out=None, index=None, out=None):
         """Trim every sequence to `keep` keys in place: the first `sink` slots, the last `recent` and the others of
         largest mass. Kept keys fill holes, so slots are not in order of age afterwards: the last `recent` slots are the
-        newest keys only while `recent` is at most the rows appended since the last eviction. kv_len_out takes the new lengths (chunks.kv_len itself if not given), out the masses
-        (mass itself), index [batch, kv_heads, keep] int32 the former slots."""
+        newest keys only while `recent` is at most the rows appended since the last eviction. kv_len_out takes the
+        new lengths (chunks.kv_len itself if not given), out the masses (mass itself), index [batch, kv_heads, keep]
+        int32 the former slots."""
         torch = _torch()
         self._cache_check(cache, chunks)
         _int32(keep=keep, sink=sink, recent=recent)

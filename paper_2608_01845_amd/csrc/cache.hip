@@ -48,11 +48,13 @@ __device__ __forceinline__ void store8(T *p, const float (&x)[8]) {
 // sines of each are found once and shared by all heads through LDS. The angle is
 // coordinate x frequency in float64 turns, reduced to half a turn before it is
 // rounded: far into a long rollout a float32 angle would be off by whole
-// fractions of a turn. What that rounding takes off (up to 2^-25 pi, three half steps of a sine) is put back to first order.
+// fractions of a turn. What that rounding takes off (up to 2^-25 pi, three half steps of a sine) is put back to
+// first order.
 //
 // Bound by memory: 4,080 rows of 16 + 2 x 16 heads of 128 (100 MB) 21.9 us, 4.6 TB/s, where a large copy
-// reaches 4.9 (four inputs in turn, more than the last-level cache holds: 25.5 us); blocks of 1 row 22.7 us, of 4 rows 24.4. Fewer than 1,024 rows take
-// a row a block and split its heads over blocks: one launch of 4 us, most of it latency.
+// reaches 4.9 (four inputs in turn, more than the last-level cache holds: 25.5 us); blocks of 1 row 22.7 us, of 4
+// rows 24.4. Fewer than 1,024 rows take a row a block and split its heads over blocks: one launch of 4 us, most of
+// it latency.
 template <typename T, int HD, int R>
 __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
   constexpr int TPH = HD / 8, HALF = HD / 2;

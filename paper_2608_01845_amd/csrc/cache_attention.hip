@@ -525,7 +525,8 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 // rounding to bf16). m is a reference per row, not a running maximum: the first tile's
 // maximum, moved only when a lane's sum of weights over a tile passes 2^16 (then O and the
 // sum are rescaled and P is taken again): weights of up to that are as exact as those below 1, and sums of them times v
-// stay within float32 while |v| is below 2^112 over the number of keys. With scores beyond 2^20 in a wave's rows every tile's P is taken again (see far_out).
+// stay within float32 while |v| is below 2^112 over the number of keys. Where a wave has references beyond 2^20, every
+// tile's P is taken again (see far_out).
 // Tiles that some row sees in part, and the cache's last, partial one, follow one at a
 // time with their masks. There m is the row's largest score so far, so that a key with nearly all
 // of the weight of a row that sees few has weight 1, without rounding. (Summing the rounded weights too, as with few
