@@ -386,7 +386,8 @@ wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const
  * with the chunk, frame and d_lse of wdc_cache_attention. The chunk's own keys have no past: their
  * mass[j] is not read, nor is any with decay 0. lse is float32: weights are relatively off by about |lse| 2^-22.
  * d_mass and d_mass_out: [pages, kv_heads, page] float32 (they may be the same); slots of no cached key are not
- * touched. decay is finite. d_scratch as above, wdc_cache_mass_scratch() bytes. d_v of the cache is not used. Sums in float32 in a fixed order. */
+ * touched. decay is finite. d_scratch as above, wdc_cache_mass_scratch() bytes. d_v of the cache is not used. Sums
+ * in float32 in a fixed order. */
 size_t wdc_cache_mass_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks);
 wdc_status wdc_cache_mass(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_q,
                           int64_t ldq, int32_t frame, const float *d_lse, float decay, const float *d_mass,

@@ -509,7 +509,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 // 32 query rows (two tiles of 16) a wave; key tiles of 64 reach four K and four V slots of LDS by direct buffer loads
 // of four waves, up to four tiles ahead. Bound by the matrix cores, with the
 // exponentials close behind, and by the power that both draw: 4,080 rows over 67,320 keys, 16 heads of 128, 1,750 to 1,860 us
-// by box, 1,190 to 1,260 TFLOP/s (a large library product: 1,200 to 1,580), the matrix cores busy in 65% of the
+// by device, 1,190 to 1,260 TFLOP/s (a large library product: 1,200 to 1,580), the matrix cores busy in 65% of the
 // cycles of a clock that falls to 1.8 GHz.
 //
 // Blocks of 256 rows are 8 waves, two per SIMD: 1.0 us a tile at hd 64, 1.4 at hd 128. Few rows or keys leave
@@ -1269,7 +1269,7 @@ struct MassRows {
 // exp2(sc x - lse) to its 16 sums. Multiply-add, exponential and sum are 16 cycles for 64 weights, as many as hd 128's
 // matrix work; the vector units are busy in 69% of the cycles and the matrix cores in 48%. What is lost: the blocks' last
 // round, and in each stage one turn of nine without exponentials and one without products. 2,040 rows over 34,680 keys, 16
-// heads of 128, 287 to 310 us by box and load (1,010 to 930 TFLOP/s; two waves per SIMD that share the rows' tiles: 339).
+// heads of 128, 287 to 310 us by device and load (1,010 to 930 TFLOP/s; two waves per SIMD that share the rows' tiles: 339).
 constexpr int MKT = 256, MST = 128, MNB = 2;
 template <int HD>
 __global__ __launch_bounds__(256, 2) void k_cache_mass_bf16(CacheMassArgs a) {
