@@ -204,9 +204,10 @@ def prepare(case, seed):
 
 
 def _quantised(x):
-    """Codes and exponent bytes of heads x [..., hd] float32: the smallest power of two that keeps them within 448."""
+    """Codes and exponent bytes of heads x [..., hd] float32: the smallest power of two, from 2^-117 on, that keeps them
+    within 448 (so that every value is a normal number)."""
     m, e = torch.frexp(torch.where(torch.isfinite(x), x.abs(), 0).amax(-1))
-    e = torch.where(m == 0, -126, (e - 9 + (m > 0.875)).clamp(min=-126))
+    e = torch.where(m == 0, -117, (e - 9 + (m > 0.875)).clamp(min=-117))
     return torch.ldexp(x, -e[..., None]).to(E4M3), (e + 127).to(torch.uint8)
 
 
@@ -394,7 +395,7 @@ def work(case):
 
 def _power64(x):
     """The cache's power of two for heads x [..., hd] float64."""
-    big = torch.where(torch.isfinite(x), x.abs(), 0).amax(-1, keepdim=True).clamp(min=448 * 2.0 ** -126)
+    big = torch.where(torch.isfinite(x), x.abs(), 0).amax(-1, keepdim=True).clamp(min=448 * 2.0 ** -117)
     p = torch.exp2(torch.floor(torch.log2(big)) - 8)           # 448 is 1.75 * 2^8
     return torch.where(big > 448 * p, 2 * p, p)
 
