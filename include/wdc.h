@@ -409,6 +409,58 @@ wdc_status wdc_cache_evict(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc
                            float *d_mass_out, int32_t keep, int32_t sink, int32_t recent, int32_t *d_kv_len_out,
                            int32_t *d_index, void *d_scratch, size_t scratch_bytes);
 
+/* Attention from sequences that share a past: rollouts that branch off one clip. d_group_start [groups + 1]
+ * rises from 0 to batch; the sequences of group g are [d_group_start[g], d_group_start[g + 1]), so their rows
+ * are consecutive in the packed tensors. The first d_prefix_len[g] slots, cut to whole pages and to the first sequence's keys, are
+ * those of the group's first sequence: every row of the group sees all of them, whatever its own table's
+ * entries there. From there on a sequence has its own slots, seen as in wdc_cache_attention. The host
+ * gives bounds: the longest prefix and the most own keys of a sequence; device values beyond them are cut to them.
+ * groups * kv_heads <= 65535 and groups * kv_heads * (prefix keys) <= 2^28, else WDC_E_SHAPE. */
+typedef struct {
+  const int32_t *d_group_start, *d_prefix_len;
+  int32_t groups, max_prefix, max_own;
+  int32_t pad_;
+} wdc_prefix;
+
+/* wdc_cache_attention where groups share a past: the same result up to the order of float32 sums, with every shared
+ * key read for all rows of a group at once. d_scratch: wdc_cache_attention_shared_scratch() bytes, required (else WDC_E_WORKSPACE). */
+size_t wdc_cache_attention_shared_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks,
+                                          const wdc_prefix *prefix);
+wdc_status wdc_cache_attention_shared(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks,
+                                      const wdc_prefix *prefix, const void *d_q, int64_t ldq, int32_t frame, void *d_o,
+                                      int64_t ldo, float *d_lse, void *d_scratch, size_t scratch_bytes);
+
+/* The same cache in 8 bits, for contexts of either dtype: d_k and d_v are e4m3 codes (no infinities, largest 448),
+ * [pages, kv_heads, page, head_dim]; d_scale [pages, kv_heads, page, 2] holds the exponent bytes of
+ * each slot's key and value: element = code * 2^(byte - 127), exact in bf16 and float32 for bytes 10 to 247 as wdc_cache8_append
+ * writes them. Alignment and limits as above (d_scale 16-byte aligned). */
+typedef struct {
+  void *d_k, *d_v, *d_scale;
+  int32_t pages, page, kv_heads;
+  int32_t pad_;
+} wdc_paged_cache8;
+
+/* wdc_cache_append into such a cache. Keys (normalised and turned) and values of a row and kv head get the smallest power of two,
+ * from 2^-117 on, that keeps their finite elements within 448 times it, and are rounded once, to nearest even; infinities and
+ * NaN are stored as NaN, and finite values that round to 2^128 read back as infinity. */
+wdc_status wdc_cache8_append(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks, const void *d_qkv,
+                             int64_t ld, const int32_t *d_pos, const float *d_q_weight, const float *d_k_weight,
+                             void *d_q, int64_t ldq);
+
+/* The chunks' keys and values back in the model dtype: row i of a chunk of q rows over n keys is slot n - q + i, d_k
+ * [rows, ldk] and d_v [rows, ldv] with kv head h at columns [h * head_dim, ..), either may be NULL. A row whose
+ * slot is negative or on no page is zeros. Pointers and row strides: multiples of 16 bytes. */
+wdc_status wdc_cache8_read(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks, void *d_k, int64_t ldk,
+                           void *d_v, int64_t ldv);
+
+/* wdc_cache_attention over such a cache, on the values that its codes stand for, or with a prefix (may be NULL)
+ * wdc_cache_attention_shared, whose scratch is required. */
+size_t wdc_cache8_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks,
+                                    const wdc_prefix *prefix);
+wdc_status wdc_cache8_attention(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks,
+                                const wdc_prefix *prefix, const void *d_q, int64_t ldq, int32_t frame, void *d_o,
+                                int64_t ldo, float *d_lse, void *d_scratch, size_t scratch_bytes);
+
 /* Kernel timing for benchmarks. While timing is on (wdc_set_timing(ctx, 1),
  * which also clears the totals), every launch of the classes below on the
  * context's stream is bracketed by HIP events; wdc_timing synchronises the

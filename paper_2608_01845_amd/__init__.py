@@ -6,6 +6,6 @@ control; this package is its ctypes binding. Build it with
 """
 from ._binding import (  # noqa: F401
     MODE_ALL_EXACT, MODE_FORCED, MODE_PERIODIC, MODE_RISK, OBS_KERNEL, OBS_LINEAR, POST_EXACT, POST_SURROGATE,
-    PRE_DECISION, SURROGATE_LIFTED, SURROGATE_SECANT, TIMING_CLASSES, Chunks, Context, ModelDesc, PagedCache, Params,
-    State, StepLog, WdcError, default_params, desc_from_config, exported_symbols, load,
+    PRE_DECISION, SURROGATE_LIFTED, SURROGATE_SECANT, TIMING_CLASSES, Chunks, Context, ModelDesc, PagedCache, PagedCache8,
+    Params, Prefix, State, StepLog, WdcError, default_params, desc_from_config, exported_symbols, load,
 )

@@ -86,6 +86,18 @@ class CacheDesc(C.Structure):
     _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p)] + [(n, C.c_int32) for n in ("pages", "page", "kv_heads", "pad_")]
 
 
+class Cache8Desc(C.Structure):
+    """wdc_paged_cache8"""
+    _fields_ = [(n, C.c_void_p) for n in ("d_k", "d_v", "d_scale")] + [(n, C.c_int32) for n in (
+        "pages", "page", "kv_heads", "pad_")]
+
+
+class PrefixDesc(C.Structure):
+    """wdc_prefix"""
+    _fields_ = [(n, C.c_void_p) for n in ("d_group_start", "d_prefix_len")] + [(n, C.c_int32) for n in (
+        "groups", "max_prefix", "max_own", "pad_")]
+
+
 class ChunksDesc(C.Structure):
     """wdc_chunks"""
     _fields_ = [(n, C.c_void_p) for n in ("d_q_start", "d_kv_len", "d_table")] + [(n, C.c_int32) for n in (
@@ -104,7 +116,7 @@ def load() -> C.CDLL:
         raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2608_01845_amd.build`")
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64, sz, dbl, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_double, C.c_float
-    pc, pq = C.POINTER(CacheDesc), C.POINTER(ChunksDesc)
+    pc, pq, pc8, pp = C.POINTER(CacheDesc), C.POINTER(ChunksDesc), C.POINTER(Cache8Desc), C.POINTER(PrefixDesc)
     sig = {
         "wdc_params_default": (None, [C.POINTER(Params)]),
         "wdc_create": (i32, [C.POINTER(ModelDesc), C.POINTER(Params), vp, C.POINTER(vp)]),
@@ -145,6 +157,12 @@ def load() -> C.CDLL:
         "wdc_cache_mass": (i32, [vp, pc, pq, vp, i64, i32, vp, f32, vp, vp, vp, sz]),
         "wdc_cache_evict_scratch": (sz, [vp, pc, pq, i32]),
         "wdc_cache_evict": (i32, [vp, pc, pq, vp, vp, i32, i32, i32, vp, vp, vp, sz]),
+        "wdc_cache_attention_shared_scratch": (sz, [vp, pc, pq, pp]),
+        "wdc_cache_attention_shared": (i32, [vp, pc, pq, pp, vp, i64, i32, vp, i64, vp, vp, sz]),
+        "wdc_cache8_append": (i32, [vp, pc8, pq, vp, i64, vp, vp, vp, vp, i64]),
+        "wdc_cache8_read": (i32, [vp, pc8, pq, vp, i64, vp, i64]),
+        "wdc_cache8_attention_scratch": (sz, [vp, pc8, pq, pp]),
+        "wdc_cache8_attention": (i32, [vp, pc8, pq, pp, vp, i64, i32, vp, i64, vp, vp, sz]),
         "wdc_set_timing": (i32, [vp, i32]),
         "wdc_timing": (i32, [vp, C.POINTER(dbl), C.POINTER(i64), C.POINTER(dbl)]),
     }
@@ -165,6 +183,8 @@ def exported_symbols() -> List[str]:
         "wdc_surrogate_step", "wdc_surrogate_step_noalloc", "wdc_risk_update", "wdc_rollout", "wdc_rollout_batch", "wdc_attn_pad", "wdc_attention", "wdc_attention_plan", "wdc_linear",
         "wdc_cache_append", "wdc_cache_attention_scratch", "wdc_cache_attention", "wdc_cache_mass_scratch",
         "wdc_cache_mass", "wdc_cache_evict_scratch", "wdc_cache_evict",
+        "wdc_cache_attention_shared_scratch", "wdc_cache_attention_shared", "wdc_cache8_append", "wdc_cache8_read",
+        "wdc_cache8_attention_scratch", "wdc_cache8_attention",
         "wdc_set_timing", "wdc_timing"]
 
 
@@ -230,6 +250,46 @@ class PagedCache:
         self.k, self.v, self.kv_heads, self.device = k, v, k.shape[1], k.get_device()
         self.dtype, self.head_dim, self.slots = k.dtype, k.shape[3], tuple(k.shape[:3])
         self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], 0)
+        self.ref = C.byref(self.desc)
+
+
+class PagedCache8:
+    """Pages of one layer's keys and values in 8 bits: k, v [pages, kv_heads, page, head_dim] float8_e4m3fn and scale
+    [pages, kv_heads, page, 2] uint8, the exponent bytes of keys and values (wdc_paged_cache8): an element is its code
+    times 2^(byte - 127). Contiguous device tensors."""
+
+    def __init__(self, k, v, scale):
+        torch = _torch()
+        if k.dim() != 4 or k.shape != v.shape or any(t.dtype != torch.float8_e4m3fn for t in (k, v)):
+            raise ValueError(f"k {tuple(k.shape)} {k.dtype} and v {tuple(v.shape)} {v.dtype} must be alike, "
+                             "[pages, kv_heads, page, head_dim] float8_e4m3fn")
+        if scale.shape != (*k.shape[:3], 2) or scale.dtype != torch.uint8:
+            raise ValueError(f"scale {tuple(scale.shape)} {scale.dtype} must be [pages, kv_heads, page, 2] uint8")
+        if not (k.device == v.device == scale.device) or not all(t.is_contiguous() for t in (k, v, scale)):
+            raise ValueError("k, v and scale must be contiguous and on one device")
+        self.k, self.v, self.scale, self.kv_heads, self.device = k, v, scale, k.shape[1], k.get_device()
+        self.head_dim, self.slots = k.shape[3], tuple(k.shape[:3])
+        self.desc = Cache8Desc(k.data_ptr(), v.data_ptr(), scale.data_ptr(), k.shape[0], k.shape[2], k.shape[1], 0)
+        self.ref = C.byref(self.desc)
+
+
+class Prefix:
+    """Groups of sequences that share a past (wdc_prefix): group_start [groups + 1] and prefix_len [groups] int32
+    device tensors, read when the work runs. Group g is the sequences from group_start[g] to group_start[g + 1]; their first
+    prefix_len[g] slots (whole pages) are those of its first one. max_prefix and max_own bound the prefixes and the keys
+    that a sequence has past its prefix (all of them, if not given; tight bounds are faster)."""
+
+    def __init__(self, group_start, prefix_len, max_prefix: Optional[int] = None, max_own: Optional[int] = None):
+        torch = _torch()
+        for name, t in (("group_start", group_start), ("prefix_len", prefix_len)):
+            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != prefix_len.device:
+                raise ValueError(f"{name}: a contiguous int32 tensor of 1 dimension on one device is needed")
+        if group_start.numel() != prefix_len.numel() + 1:
+            raise ValueError("group_start [groups + 1] and prefix_len [groups] disagree on the groups")
+        max_prefix, max_own = (0x7fffffff if x is None else x for x in (max_prefix, max_own))
+        _int32(max_prefix=max_prefix, max_own=max_own)
+        self.group_start, self.prefix_len, self.device = group_start, prefix_len, prefix_len.get_device()
+        self.desc = PrefixDesc(group_start.data_ptr(), prefix_len.data_ptr(), prefix_len.numel(), max_prefix, max_own, 0)
         self.ref = C.byref(self.desc)
 
 
@@ -406,9 +466,18 @@ class Context:
 
     # ---------------------------------------------------------------- paged key/value cache
     def _cache_check(self, cache, chunks):
-        if cache.dtype is not self.tdtype or cache.head_dim != self.cfg.head_dim:
-            raise ValueError(f"cache of {cache.dtype}, head size {cache.head_dim}: the context has {self.tdtype}, "
+        if not isinstance(cache, PagedCache) or cache.dtype is not self.tdtype or cache.head_dim != self.cfg.head_dim:
+            raise ValueError(f"cache of {cache.k.dtype}, head size {cache.head_dim}: the context has {self.tdtype}, "
                              f"{self.cfg.head_dim}")
+        self._cache_device(cache, chunks)
+
+    def _cache8_check(self, cache, chunks):
+        if not isinstance(cache, PagedCache8) or cache.head_dim != self.cfg.head_dim:
+            raise ValueError(f"cache of {cache.k.dtype}, head size {cache.head_dim}: a PagedCache8 of head size "
+                             f"{self.cfg.head_dim} is needed")
+        self._cache_device(cache, chunks)
+
+    def _cache_device(self, cache, chunks):
         if cache.device != chunks.device or cache.device != self.device_index:
             raise ValueError(f"cache or chunks not on {self.device}")
 
@@ -443,15 +512,18 @@ class Context:
     def cache_append(self, cache: PagedCache, chunks: Chunks, qkv, q, pos=None, q_weight=None, k_weight=None):
         """Normalise and rotate q and k of qkv [rows, (heads + 2 kv_heads) head_dim], store k and v in the
         cache and write q [rows, heads head_dim]. Rows may be strided."""
-        torch = _torch()
         self._cache_check(cache, chunks)
+        return self._append(self.lib.wdc_cache_append, cache, chunks, qkv, q, pos, q_weight, k_weight)
+
+    def _append(self, call, cache, chunks, qkv, q, pos, q_weight, k_weight):
+        torch = _torch()
         hd, rows, dev, ptr = self.cfg.head_dim, chunks.rows, cache.device, self._tensor
         qkv_p = ptr("qkv", qkv, self.tdtype, (rows, (self.cfg.heads + 2 * cache.kv_heads) * hd), dev, True)
         q_p = ptr("q", q, self.tdtype, (rows, self.cfg.heads * hd), dev, True)
         pos_p = pos if pos is None else ptr("pos", pos, torch.int32, (rows, 3), dev)
         qw_p = q_weight if q_weight is None else ptr("q_weight", q_weight, torch.float32, (hd,), dev)
         kw_p = k_weight if k_weight is None else ptr("k_weight", k_weight, torch.float32, (hd,), dev)
-        self._launch(self.lib.wdc_cache_append, cache.ref, chunks.ref, qkv_p, _ld(qkv), pos_p, qw_p, kw_p, q_p, _ld(q))
+        self._launch(call, cache.ref, chunks.ref, qkv_p, _ld(qkv), pos_p, qw_p, kw_p, q_p, _ld(q))
         return q
 
     def cache_attention(self, cache: PagedCache, chunks: Chunks, q, out, frame: int = 0, lse=None):
@@ -459,15 +531,53 @@ class Context:
         lse [rows, heads] float32 takes the rows' log-sum-exp. frame: rows per frame (0: all see all).
         out may be q itself."""
         self._cache_check(cache, chunks)
+        return self._attend(self.lib.wdc_cache_attention, self.lib.wdc_cache_attention_scratch, cache, chunks, (), q, out,
+                            frame, lse)
+
+    def cache_attention_shared(self, cache: PagedCache, chunks: Chunks, prefix: Prefix, q, out, frame: int = 0, lse=None):
+        """cache_attention of sequences whose first slots are those of their group's first one: every shared
+        key is read once for all rows of its group."""
+        self._cache_check(cache, chunks)
+        return self._attend(self.lib.wdc_cache_attention_shared, self.lib.wdc_cache_attention_shared_scratch, cache, chunks,
+                            (self._prefix(prefix, cache),), q, out, frame, lse)
+
+    def _prefix(self, prefix, cache):
+        if prefix.device != cache.device:
+            raise ValueError(f"prefix not on {self.device}")
+        return prefix.ref
+
+    def _attend(self, call, need, cache, chunks, prefix, q, out, frame, lse):
         _int32(frame=frame)
         shape, dev, ptr = (chunks.rows, self.cfg.heads * self.cfg.head_dim), cache.device, self._tensor
         q_p, out_p = ptr("q", q, self.tdtype, shape, dev, True), ptr("out", out, self.tdtype, shape, dev, True)
         lse_p = lse if lse is None else ptr("lse", lse, _torch().float32, (chunks.rows, self.cfg.heads), dev)
-        n = self.lib.wdc_cache_attention_scratch(self.h, cache.ref, chunks.ref)
+        n = need(self.h, cache.ref, chunks.ref, *prefix)
         scratch = self._scratch(n) if n else None
-        self._launch(self.lib.wdc_cache_attention, cache.ref, chunks.ref, q_p, _ld(q), frame, out_p, _ld(out), lse_p,
-                     _ptr(scratch), n)
+        self._launch(call, cache.ref, chunks.ref, *prefix, q_p, _ld(q), frame, out_p, _ld(out), lse_p, _ptr(scratch), n)
         return out
+
+    def cache8_append(self, cache: PagedCache8, chunks: Chunks, qkv, q, pos=None, q_weight=None, k_weight=None):
+        """cache_append into a cache in 8 bits: keys and values are rounded to codes with a power of two per slot and
+        kv head."""
+        self._cache8_check(cache, chunks)
+        return self._append(self.lib.wdc_cache8_append, cache, chunks, qkv, q, pos, q_weight, k_weight)
+
+    def cache8_read(self, cache: PagedCache8, chunks: Chunks, k=None, v=None):
+        """The chunks' rows of a cache in 8 bits back in the model's type: k and/or v [rows, kv_heads head_dim].
+        Rows may be strided."""
+        self._cache8_check(cache, chunks)
+        shape, dev = (chunks.rows, cache.kv_heads * self.cfg.head_dim), cache.device
+        k_p, v_p = (t if t is None else self._tensor(name, t, self.tdtype, shape, dev, True) for name, t in (("k", k), ("v", v)))
+        self._launch(self.lib.wdc_cache8_read, cache.ref, chunks.ref, k_p, 0 if k is None else _ld(k), v_p,
+                     0 if v is None else _ld(v))
+        return k, v
+
+    def cache8_attention(self, cache: PagedCache8, chunks: Chunks, q, out, frame: int = 0, lse=None,
+                         prefix: Optional[Prefix] = None):
+        """cache_attention (with a prefix cache_attention_shared) over the values of a cache in 8 bits."""
+        self._cache8_check(cache, chunks)
+        return self._attend(self.lib.wdc_cache8_attention, self.lib.wdc_cache8_attention_scratch, cache, chunks,
+                            (None if prefix is None else self._prefix(prefix, cache),), q, out, frame, lse)
 
     def cache_mass(self, cache: PagedCache, chunks: Chunks, q, lse, mass, frame: int = 0, decay: float = 1.0, out=None):
         """out = decay * mass + the weight each cached key receives from the chunks' rows (out: mass itself

@@ -39,6 +39,28 @@ __device__ __forceinline__ void store8(T *p, const float (&x)[8]) {
   }
 }
 
+// Eight elements of a head over HD / 8 lanes as e4m3 codes of x 2^-E, with E the smallest exponent, from -117 on, that keeps
+// the head's finite elements within 448 2^E (448: the largest code). Returns E + 127. A power of two changes no
+// digit of a floating-point code, and from 2^-117 on every value code 2^E is a normal number in bf16 as in float32: what
+// reads the cache has the values exactly. The one rounding is to nearest even; infinities and NaN become NaN.
+template <int HD>
+__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint2 &codes) {
+  float big = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[e]) < INFINITY ? fabsf(x[e]) : 0.f);
+  const uint32_t u = __float_as_uint(group_max<HD / 8>(big));
+  const int byte = max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), 10);
+  const float down = __uint_as_float((uint32_t)(254 - byte) << 23);
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = fabsf(x[e]) < INFINITY ? x[e] * down : NAN;
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
+  codes = make_uint2((uint32_t)lo, (uint32_t)hi);
+  return (uint32_t)byte;
+}
+
 // x -> x / sqrt(mean(x^2) + 1e-6) [* w] over a head, pair (2p, 2p + 1) turned by
 // the row's angle of p, in float32, rounded once. A thread takes 8 consecutive
 // elements of one head, so a head's sum of squares is one butterfly over HD / 8
@@ -55,7 +77,7 @@ __device__ __forceinline__ void store8(T *p, const float (&x)[8]) {
 // reaches 4.9 (four inputs in turn, more than the last-level cache holds: 25.5 us); blocks of 1 row 22.7 us, of 4
 // rows 24.4. Fewer than 1,024 rows take a row a block and split its heads over blocks: one launch of 4 us, most of
 // it latency.
-template <typename T, int HD, int R>
+template <typename T, int HD, int R, bool CODES>
 __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
   constexpr int TPH = HD / 8, HALF = HD / 2;
   const CacheArgs &c = a.c;
@@ -101,7 +123,7 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
         }
       }
       dst[lane] = d;
-      live[lane] = ok;
+      live[lane] = !ok ? 0 : a.pos && a.pos[3 * (int64_t)row] >= 0 ? 2 : 1;   // 2: turned
     }
   }
   for (int e = tid; e < R * HALF; e += 256) {
@@ -145,6 +167,7 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
         if (w)
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[r][e] *= wt[e];
+        if (CODES && live[r] == 1) continue;     // (turned by nothing an infinity would make its neighbour NaN)
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
           const float2 t = cs[r][e8 / 2 + p];
@@ -161,21 +184,106 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
         store8((T *)a.q + (int64_t)(row0 + r) * a.ldq + (int64_t)h * HD + e8, x[r]);
       } else if (dst[r] >= 0) {
         const int kh = h < nqk ? h - c.heads : h - nqk;
+        if constexpr (CODES) {
+          const int64_t at = dst[r] / HD + ((int64_t)kh << c.plog);
+          uint2 codes;
+          const uint32_t byte = quantise8<HD>(x[r], codes);
+          *(uint2 *)((uint8_t *)(h < nqk ? c.k : c.v) + at * HD + e8) = codes;
+          if (e8 == 0) c.scale[2 * at + (h < nqk ? 0 : 1)] = (uint8_t)byte;
+          continue;
+        }
         store8((T *)(h < nqk ? c.k : c.v) + dst[r] + (((int64_t)kh << c.plog) * HD) + e8, x[r]);
       }
     }
   }
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool CODES>
 hipError_t append(const CacheAppendArgs &a, hipStream_t s) {
   const int chunks = (a.c.heads + 2 * a.c.kvh) * (HD / 8);
   if (a.c.rows >= 1024) {
-    hipLaunchKernelGGL((k_cache_append<T, HD, 2>), dim3((a.c.rows + 1) / 2), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_cache_append<T, HD, 2, CODES>), dim3((a.c.rows + 1) / 2), dim3(256), 0, s, a);
   } else {
     const int split = std::min((chunks + 255) / 256, std::max(1, 512 / a.c.rows));
-    hipLaunchKernelGGL((k_cache_append<T, HD, 1>), dim3(a.c.rows, split), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_cache_append<T, HD, 1, CODES>), dim3(a.c.rows, split), dim3(256), 0, s, a);
   }
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- read
+// Stored rows back in the model dtype: row i of a chunk of q rows over n keys is slot n - q + i. A
+// thread takes 16 codes, a block R rows.
+template <typename T, int HD, int R>
+__global__ __launch_bounds__(256) void k_cache8_read(Cache8ReadArgs a) {
+  constexpr int TPH = HD / 16;
+  const CacheArgs &c = a.c;
+  __shared__ int64_t src[R];             // (page, kv head 0, slot); -1: on no page, -2: row of no chunk
+  const int tid = threadIdx.x, lane = tid & 63, row0 = blockIdx.x * R;
+  if (tid < 64) {
+    int cnt[R] = {};
+    for (int e0 = 0; e0 < c.batch; e0 += 64) {
+      const int end = e0 + lane < c.batch ? c.q_start[e0 + lane + 1] : 0x7fffffff;
+#pragma unroll
+      for (int r = 0; r < R; ++r) cnt[r] += __popcll(__ballot(end <= row0 + r));
+    }
+    int b = cnt[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r)
+      if (lane == r) b = cnt[r];
+    if (lane < R) {
+      const int row = row0 + lane;
+      int64_t d = -2;
+      if (row < c.rows && b < c.batch) {
+        const CacheSeq s = cache_seq(c, b);
+        const int i = row - s.q0, slot = s.start + i;
+        if (i >= 0 && i < s.nq) {
+          const int e = slot >= 0 ? c.table[(int64_t)b * c.table_ld + (slot >> c.plog)] : -1;
+          d = e >= 0 && e < c.pages ? (((int64_t)e * c.kvh) << c.plog) + (slot & ((1 << c.plog) - 1)) : -1;
+        }
+      }
+      src[lane] = d;
+    }
+  }
+  __syncthreads();
+  const int per = c.kvh * TPH, first = a.k ? 0 : per, last = a.v ? 2 * per : per;
+  for (int j = first + tid + blockIdx.y * 256; j < last; j += 256 * gridDim.y) {
+    const bool key = j < per;
+    const int jj = key ? j : j - per, h = jj / TPH, e16 = 16 * (jj % TPH);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (src[r] == -2) continue;
+      uint4 u = make_uint4(0, 0, 0, 0);
+      float up = 1.f;
+      if (src[r] >= 0) {
+        const int64_t at = src[r] + ((int64_t)h << c.plog);
+        u = *(const uint4 *)((const uint8_t *)(key ? c.k : c.v) + at * HD + e16);
+        up = __uint_as_float((uint32_t)c.scale[2 * at + (key ? 0 : 1)] << 23);
+      }
+      T *out = (T *)(key ? a.k : a.v) + (int64_t)(row0 + r) * (key ? a.ldk : a.ldv) + (int64_t)h * HD + e16;
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float x[8];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[2 * i + q], up, false);
+          const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[2 * i + q], up, true);
+          x[4 * q] = lo[0];
+          x[4 * q + 1] = lo[1];
+          x[4 * q + 2] = hi[0];
+          x[4 * q + 3] = hi[1];
+        }
+        store8(out + 8 * i, x);
+      }
+    }
+  }
+}
+
+template <typename T, int HD>
+hipError_t read(const Cache8ReadArgs &a, hipStream_t s) {
+  const int chunks = a.c.kvh * (HD / 16) * ((a.k ? 1 : 0) + (a.v ? 1 : 0));
+  const int split = std::min((chunks + 255) / 256, std::max(1, 512 / a.c.rows));
+  hipLaunchKernelGGL((k_cache8_read<T, HD, 1>), dim3(a.c.rows, split), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -693,8 +801,18 @@ __global__ __launch_bounds__(256) void k_evict_move(CacheEvictArgs a) {
 
 hipError_t launch_cache_append(int dtype, const CacheAppendArgs &a, hipStream_t s) {
   if (a.c.rows <= 0) return hipSuccess;
-  if (dtype == 1) return a.c.hd == 128 ? append<bf16_t, 128>(a, s) : append<bf16_t, 64>(a, s);
-  return a.c.hd == 128 ? append<float, 128>(a, s) : append<float, 64>(a, s);
+  if (a.c.scale) {
+    if (dtype == 1) return a.c.hd == 128 ? append<bf16_t, 128, true>(a, s) : append<bf16_t, 64, true>(a, s);
+    return a.c.hd == 128 ? append<float, 128, true>(a, s) : append<float, 64, true>(a, s);
+  }
+  if (dtype == 1) return a.c.hd == 128 ? append<bf16_t, 128, false>(a, s) : append<bf16_t, 64, false>(a, s);
+  return a.c.hd == 128 ? append<float, 128, false>(a, s) : append<float, 64, false>(a, s);
+}
+
+hipError_t launch_cache8_read(int dtype, const Cache8ReadArgs &a, hipStream_t s) {
+  if (a.c.rows <= 0 || (!a.k && !a.v)) return hipSuccess;
+  if (dtype == 1) return a.c.hd == 128 ? read<bf16_t, 128>(a, s) : read<bf16_t, 64>(a, s);
+  return a.c.hd == 128 ? read<float, 128>(a, s) : read<float, 64>(a, s);
 }
 
 // Moves and parts of a launch over these bounds. One block per (sequence, kv head) for up to 8,192 slots (16 heads: 8,000

@@ -6,30 +6,14 @@
 // the slots below cache_limit(i): limits grow with i, so of the key tiles of a
 // block of rows a first part is seen by all rows whole, a second part in part, and
 // the rest by none and is left out.
-#include "common.h"
+#include "cache_tiles.h"
 
 #include <algorithm>
-#include <cfloat>
 #include <type_traits>
 
 namespace wdc {
 namespace {
 
-constexpr int RSRC_WORD3 = 0x00020000;   // raw buffer descriptor word 3
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// Buffer of `bytes` bytes from base + off: what lies outside reads as zero
-__device__ __forceinline__ u32x4_t buffer_at(const void *base, int64_t off, int bytes) {
-  const uint64_t p = (uint64_t)base + (uint64_t)off;
-  return u32x4_t{(uint32_t)uni((int)(uint32_t)p), (uint32_t)uni((int)(uint32_t)(p >> 32) & 0xffff), (uint32_t)uni(bytes),
-                 (uint32_t)RSRC_WORD3};
-}
 // Direct global -> LDS loads: lane l's 16 (4) bytes at `voff` of the buffer arrive
 // at lds + 16 l (4 l). Written as instructions because the compiler lets no transposed LDS read pass while one
 // of its own direct loads is under way (it waits for all of them); nothing is returned in
@@ -45,157 +29,6 @@ __device__ __forceinline__ void lds_load4(u32x4_t buf, uint32_t lds, int voff) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buf)
                : "memory", "m0");
 }
-// LDS address of a pointer into it, the same in every lane
-__device__ __forceinline__ uint32_t lds_addr(const void *p) {
-  return (uint32_t)uni((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p);
-}
-// waits until at most N loads are under way
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-// Four rows of 16 columns of 2 bytes, each read as 4 x 8 bytes by the lanes of a
-// group of 16 in row order, come back transposed: lane c of the group gets column c.
-__device__ __forceinline__ s16x4 lds_read_tr(const char *p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
-}
-
-__device__ __forceinline__ float quad_max(float v) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// First slots in the pool of one sequence's pages and a kv head, asked for in rising order by a whole
-// wave: 64 table entries in a register, the next 64 on their way in another. EARLY: slots are found for all 64
-// at once (long chunks over small pages: 59 -> 56 us for 2,048 rows of 16 heads of 128; single
-// tokens, which touch few entries of a page table, lose by it: 86 -> 93).
-template <bool EARLY>
-struct PageWalk {
-  const int32_t *tab;
-  int last, base, cur, next;
-  __device__ __forceinline__ int fetch(int i) const { return tab[min(i + (int)(threadIdx.x & 63), last)]; }
-  __device__ __forceinline__ static int slot(const CacheArgs &a, int h, int entry) {   // (pools hold fewer than 2^31)
-    return (cache_page(a, entry) * a.kvh + h) << a.plog;
-  }
-  __device__ __forceinline__ void init(const CacheArgs &a, int b, int h, int first) {
-    tab = a.table + (int64_t)b * a.table_ld;
-    last = a.table_ld - 1;
-    base = first;
-    cur = fetch(base);
-    next = fetch(base + 64);
-    if (EARLY) cur = slot(a, h, cur);
-  }
-  // before get(i); the entries that share i's group of 64 from the first on need no further call
-  __device__ __forceinline__ void advance(const CacheArgs &a, int h, int i) {
-    while (i - base >= 64) {
-      cur = EARLY ? slot(a, h, next) : next;
-      base += 64;
-      next = fetch(base + 64);
-    }
-  }
-  __device__ __forceinline__ int get(const CacheArgs &a, int h, int i) const {
-    const int x = __builtin_amdgcn_readlane(cur, i - base);
-    return EARLY ? x : slot(a, h, x);
-  }
-};
-
-// a sequence's lengths as wave-uniform values
-__device__ __forceinline__ CacheSeq uniform_seq(const CacheArgs &a, int b) {
-  CacheSeq s = cache_seq(a, b);
-  s.q0 = uni(s.q0);
-  s.nq = uni(s.nq);
-  s.n = uni(s.n);
-  s.start = uni(s.start);
-  return s;
-}
-
-// Ranges of keys that the rows of a block which see up to `keys` of them are cut
-// into, one block each (the first is always there: it writes zeros where nothing is seen)
-__device__ __forceinline__ int range_count(const CacheAttnArgs &a, int keys) {
-  return a.splits > 1 ? max(1, (keys + a.range - 1) / a.range) : 1;
-}
-
-// Part of range sp of packed row `row` and a head: HD unnormalised values at
-// part + slot * HD, its reference and sum at part + slots * HD + 2 slot
-__device__ __forceinline__ int64_t part_slot(const CacheAttnArgs &a, int sp, int row, int head) {
-  return ((int64_t)sp * a.c.rows + row) * a.c.heads + head;
-}
-__device__ __forceinline__ float *part_ml(const CacheAttnArgs &a, int64_t slot) {
-  return a.part + (int64_t)a.splits * a.c.rows * a.c.heads * a.c.hd + 2 * slot;
-}
-
-// What a block of an attention launch works on: query rows [m0, m0 + rpb) of
-// `count` of sequence b and kv head h, range sp of nr of the keys that they see.
-// Blocks are numbered sequence by sequence with the lengths of the device, so those that the host's bounds
-// allow for but no chunk needs come last. (2,048 single tokens over 100 keys each, 16 heads of 64: 1,432 us when every
-// block counted the sequences before its own, 515 without.) Within a sequence kv heads go fastest: with 8 (or a divisor
-// or multiple) of them the blocks of one run on one XCD (or its group) and share K and V in that L2; the last rows,
-// which see the most, come first (8,192 rows causal over themselves, 16 heads of 128: 312 us from the first, 271 so).
-struct AttnBlock {
-  CacheSeq s;
-  int b, h, m0, count, group, sp, nr;
-  int lim_lo, lim_hi;   // keys seen by the first and the last row
-  bool live;
-  __device__ __forceinline__ explicit AttnBlock(const CacheAttnArgs &a) : b(0), live(false) {
-    const CacheArgs &c = a.c;
-    const int lane = threadIdx.x & 63;
-    group = c.heads / c.kvh;
-    int li = blockIdx.x;
-    if (c.batch == 1 || (a.splits == 1 && c.max_q * group <= a.rpb)) {   // one sequence, or a block for each and kv head
-      if (c.batch > 1) {
-        b = uni(li / c.kvh);
-        li -= b * c.kvh;
-      }
-      s = uniform_seq(c, b);
-    } else {
-      bool found = false;
-      for (int e0 = 0; e0 < c.batch && !found; e0 += 64) {
-        int cnt = 0;
-        CacheSeq q{};
-        if (e0 + lane < c.batch) {
-          q = cache_seq(c, e0 + lane);
-          cnt = (q.nq * group + a.rpb - 1) / a.rpb * range_count(a, q.n) * c.kvh;
-        }
-        const int sum = wave_scan(cnt);
-        const uint64_t past = __ballot(sum > li);
-        if (past) {
-          const int k = __builtin_ctzll(past);
-          b = e0 + k;
-          li -= __builtin_amdgcn_readlane(sum - cnt, k);
-          s.q0 = __builtin_amdgcn_readlane(q.q0, k);
-          s.nq = __builtin_amdgcn_readlane(q.nq, k);
-          s.n = __builtin_amdgcn_readlane(q.n, k);
-          s.start = __builtin_amdgcn_readlane(q.start, k);
-          found = true;
-        } else {
-          li -= __builtin_amdgcn_readlane(sum, 63);
-        }
-      }
-      if (!found) return;
-    }
-    b = uni(b);
-    li = uni(li);
-    count = s.nq * group;
-    const int q = uni(li / c.kvh), nrg = range_count(a, s.n), back = uni(q / nrg), rb = (count + a.rpb - 1) / a.rpb - 1 - back;
-    h = li - q * c.kvh;
-    sp = q - back * nrg;
-    m0 = rb * a.rpb;
-    if (m0 < 0) return;
-    lim_lo = uni(cache_limit(c, s, cache_row(c, m0)));
-    lim_hi = uni(cache_limit(c, s, cache_row(c, min(m0 + a.rpb, count) - 1)));
-    nr = uni(range_count(a, lim_hi));
-    live = sp < nr;
-  }
-};
-
 // Block of a launch over (sequence, kv head) x per blocks each. With the XCD order
 // the blocks of one (sequence, kv head) share an XCD, and so its K and V in that L2.
 __device__ __forceinline__ void cache_block(const CacheArgs &c, int per, int &bh, int &li) {
@@ -223,31 +56,6 @@ __device__ __forceinline__ void cache_block(const CacheArgs &c, int per, int &bh
 // and O is scaled by the ratio of the two sums: then it is a mean of V whatever their rounding, so that a key which
 // has nearly all of the weight comes out as it is (else off by up to half a bf16 step, 1.6 times the error of a single
 // rounding over keys of which a few dominate).
-__device__ __forceinline__ float unround(float sum, float rounded) { return rounded == 0.f ? 1.f : sum / rounded; }
-
-template <int HD>
-struct Few {
-  static constexpr int ROWB = HD * 2;            // bytes of a row
-  static constexpr int RPL = 1024 / ROWB;        // rows per LDS load of a wave (4 or 8)
-  static constexpr int KT = HD == 128 ? 16 : 32; // keys per tile
-  static constexpr int NK = KT / 16;
-  static constexpr int LPH = 16 / RPL;           // LDS loads per 16 rows (4 or 2)
-  static constexpr int TILE = KT * ROWB;
-  // 16-byte chunk c of row r lies at c ^ key(r): the 16 rows of a K fragment, and
-  // the 4 rows that 16 lanes of a transposed V read take (a pair of chunks each), spread over the banks
-  static __device__ __forceinline__ int kkey(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
-  static __device__ __forceinline__ int vkey(int r) { return HD == 128 ? 2 * (r & 3) : 2 * ((r >> 1) & 1); }
-  // transposed V reads of dims 16 i ..: lane offset i % VR, the rest a constant
-  static constexpr int VR = HD == 128 ? 4 : 2;
-};
-
-// V^T fragment (16 dims, 32 keys): keys 4 lg .. of the first and the second 16 rows
-template <int HD>
-__device__ __forceinline__ bf16x8 v_frag(const char *p) {
-  const s16x4 v0 = lds_read_tr(p), v1 = lds_read_tr(p + 16 * Few<HD>::ROWB);
-  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
 // Slots of a wave's K and V tiles: one in use, the other under way. Two blocks per compute unit with two slots each do
 // more than one with four (16 heads of 64: 16 tokens over 4,000 keys 52.7 us, 57.1 with four; 2,048 over 100: 240, 479).
 constexpr int FSL = 2;
@@ -262,7 +70,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   const AttnBlock k_(a);
   if (!k_.live) return;
   const CacheSeq s = k_.s;
-  const int h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr;
+  const int h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr, part_ = k_.part;
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -301,7 +109,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
     for (int i = 0; i < F::VR; ++i) vro[i] = r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
   PageWalk<false> pw;
-  pw.init(c, k_.b, h, (KT * t0) >> c.plog);
+  pw.init(c, k_.tab, k_.tab_last, h, (KT * t0) >> c.plog);
   const int pmask = (1 << c.plog) - 1;
   // Tile t into slot j: halves of 16 rows, each on one page. Rows past the cache's
   // end lie outside the buffer range and arrive as zeros, whatever they hold; so do tiles
@@ -489,8 +297,8 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
       for (int d = 0; d < 4; ++d) x[d] += wt * y[d];
     }
     const int i = cache_row(c, mr), head = h * group + mr - i * group;
-    if (nr > 1) {
-      const int64_t at = part_slot(a, sp, s.q0 + i, head);
+    if (part_ >= 0) {
+      const int64_t at = part_slot(a, part_, s.q0 + i, head);
       *(f32x4 *)(a.part + at * HD + 4 * e) = x;
       if (e == 0) *(float2 *)part_ml(a, at) = make_float2(mx, den);
       continue;
@@ -550,12 +358,13 @@ struct TileLoads {
   };
   PageWalk<true> pw;                             // SMALL only
   int kvo_, w, h, n;                             // kvo_: the lane's byte offset in its stripe's rows of K
-  __device__ __forceinline__ void init(const CacheArgs &c, const CacheSeq &s, int b, int h_, int w_, int lane, int tile0) {
+  __device__ __forceinline__ void init(const CacheArgs &c, const CacheSeq &s, const int32_t *tab, int tab_last, int h_, int w_,
+                                       int lane, int tile0) {
     w = w_;
     h = h_;
     n = s.n;
     kvo_ = offset(lane);
-    if (SMALL) pw.init(c, b, h, (KV * tile0) >> c.plog);
+    if (SMALL) pw.init(c, tab, tab_last, h, (KV * tile0) >> c.plog);
   }
   __device__ __forceinline__ int offset(int lane) const {
     const int r = w * F::RPL + lane / (HD / 8), ch = lane % (HD / 8);
@@ -575,10 +384,10 @@ struct TileLoads {
     return kvo() ^ ((F::kkey(r) ^ F::vkey(r)) * 16);
   }
   // page of a whole tile, by a scalar load (the table does not change during a launch)
-  __device__ __forceinline__ int page(const CacheArgs &c, int b, int tile) const {
+  __device__ __forceinline__ int page(const CacheArgs &c, const int32_t *tab, int tab_last, int tile) const {
     typedef const __attribute__((address_space(4))) int32_t *scalar_ptr;
-    const int e = min((KV * tile) >> c.plog, c.table_ld - 1);
-    return cache_page(c, ((scalar_ptr)(uint64_t)(c.table + (int64_t)b * c.table_ld))[e]);
+    const int e = min((KV * tile) >> c.plog, tab_last);
+    return cache_page(c, ((scalar_ptr)(uint64_t)tab)[e]);
   }
   // where a tile lies; page: its page (unless SMALL)
   __device__ __forceinline__ void find(const CacheArgs &c, int tile, int page, Where &x) {
@@ -600,39 +409,6 @@ struct TileLoads {
   }
 };
 
-template <int HD>
-__device__ __forceinline__ float rowmax(const f32x4 (&S)[4][2], int t) {
-  float mx = S[0][t][0];
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, S[k][t][e]);
-  return quad_max(mx);
-}
-// Whether a row of the wave has a reference so large that its rounding, half a step of m = sc max S, changes what
-// fma(S, sc, -m) is for the largest S by more than 2^-4: the weights of such a row would pass float32's range or all vanish.
-__device__ __forceinline__ bool far_out(float m) { return __any(fabsf(m) > 0x1p20f); }
-
-// P of one row tile, its lane sums. Far out S sc is rounded like the reference before m is taken off (S is scaled in
-// place), so that the largest score has weight 1.
-__device__ __forceinline__ float weights(f32x4 (&S)[4][2], bf16x8 (&pf)[2], int t, float sc, float m) {
-  float ls = 0.f;
-  if (far_out(m)) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) S[k][t] *= sc;
-    sc = 1.f;
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[k][t][e], sc, -m));
-      ls += p;
-      pf[k >> 1][4 * (k & 1) + e] = (__bf16)p;
-    }
-  return ls;
-}
-
 template <int HD, bool SMALL, int W, int KG>
 __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs a) {
   using F = Few<HD>;
@@ -645,7 +421,9 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   const AttnBlock k_(a);
   if (!k_.live) return;
   const CacheSeq s = k_.s;
-  const int b = k_.b, h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr;
+  const int32_t *tab = k_.tab;
+  const int tab_last = k_.tab_last;
+  const int h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr, part_ = k_.part;
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -680,7 +458,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   const uint32_t lds0 = lds_addr(ring);
   TL tl;
   typename TL::Where wk, wv;                     // of the latest K tile asked for, and of the one before
-  auto page_of = [&](int t) { return SMALL ? 0 : tl.page(c, b, KG * (t_first + t) + kg); };
+  auto page_of = [&](int t) { return SMALL ? 0 : tl.page(c, tab, tab_last, KG * (t_first + t) + kg); };
   auto load_k = [&](int t, int page) __attribute__((always_inline)) {
     wv = wk;
     tl.find(c, KG * (t_first + t) + kg, page, wk);
@@ -690,7 +468,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
 
   int page[NB];                                  // of the K tiles that the next NB steps ask for
   if (grp_a) {                                   // K_0 .. K_3, V_0 .. V_2; the first products wait for K_0 and K_1 alone
-    tl.init(c, s, b, h, wid & 3, lane, KG * t_first + kg);
+    tl.init(c, s, tab, tab_last, h, wid & 3, lane, KG * t_first + kg);
     wk = typename TL::Where{};
     int first[NB];
 #pragma unroll
@@ -997,8 +775,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
     const int mr = m0 + 32 * wr + 16 * t + lr;
     if (mr >= count) continue;
     const int i0 = cache_row(c, mr), head = h * group + mr - i0 * group;
-    if (nr > 1) {
-      const int64_t at = part_slot(a, sp, s.q0 + i0, head);
+    if (part_ >= 0) {
+      const int64_t at = part_slot(a, part_, s.q0 + i0, head);
 #pragma unroll
       for (int i = 0; i < NI; ++i) *(f32x4 *)(a.part + at * HD + 16 * i + 4 * lg) = o[i][t];
       if (lg == 0) *(float2 *)part_ml(a, at) = make_float2(m[t], den);
@@ -1018,66 +796,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   }
 }
 
-// ---------------------------------------------------------------- parts of a split launch
-// o = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s with M the largest m_s, ranges
-// in order; thread: one row, 4 columns. 4.4 us for 384 rows, 16 heads of 64, five ranges: a launch and its latency.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
-  constexpr int TPR = HD / 4;
-  const CacheArgs &c = a.c;
-  const int group = c.heads / c.kvh, b = blockIdx.y;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int e = 4 * (int)(gid % TPR), q = (int)(gid / TPR);   // q: chunk row x heads + head
-  const CacheSeq s = cache_seq(c, b);
-  if (q >= s.nq * c.heads) return;
-  const int i = q / c.heads, head = q - i * c.heads, h = head / group, mr = i * group + head - h * group;
-  const int last = min(mr / a.rpb * a.rpb + a.rpb, s.nq * group) - 1;   // of the row's block
-  const int nr = range_count(a, cache_limit(c, s, cache_row(c, last)));
-  if (nr == 1) return;                           // finished by its block
-  const int64_t at0 = part_slot(a, 0, s.q0 + i, head), step = (int64_t)c.rows * c.heads;
-  float mx = -INFINITY, den = 0.f;
-  f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int u0 = 0; u0 < nr; u0 += 8) {           // eight ranges' loads at a time
-    float2 ml[8];
-    f32x4 y[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (u0 + u < nr) {
-        const int64_t at = at0 + (u0 + u) * step;
-        ml[u] = *(const float2 *)part_ml(a, at);
-        y[u] = *(const f32x4 *)(a.part + at * HD + e);
-      }
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (u0 + u < nr) {
-        const float mn = fmaxf(mx, ml[u].x), ref = mn == -INFINITY ? 0.f : mn;
-        const float wo = __builtin_amdgcn_exp2f(mx - ref), wn = __builtin_amdgcn_exp2f(ml[u].x - ref);
-        mx = mn;
-        den = wo * den + wn * ml[u].y;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) x[d] = wo * x[d] + wn * y[u][d];
-      }
-  }
-  T *O = (T *)a.o + (int64_t)(s.q0 + i) * a.ldo + (int64_t)head * HD + e;
-  if constexpr (sizeof(T) == 2) {
-    bf16x4 y;
-#pragma unroll
-    for (int d = 0; d < 4; ++d) y[d] = (__bf16)(den == 0.f ? 0.f : x[d] / den);
-    *(bf16x4 *)O = y;
-  } else {
-#pragma unroll
-    for (int d = 0; d < 4; ++d) O[d] = den == 0.f ? 0.f : x[d] / den;
-  }
-  if (a.lse && e == 0)
-    a.lse[(int64_t)(s.q0 + i) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
-}
-
 // ---------------------------------------------------------------- float32
-// Element offset of row `slot` of a sequence (entries tab) and kv head h in k and v
-__device__ __forceinline__ int64_t slot_row(const CacheArgs &c, const int32_t *tab, int h, int slot) {
-  return ((((int64_t)cache_page(c, tab[slot >> c.plog]) * c.kvh + h) << c.plog) + (slot & ((1 << c.plog) - 1))) * c.hd;
-}
-
 // float32 attention on v_mfma_f32_32x32x2_f32 (64 cycles each): a block's four
 // waves share 32 rows and take every fourth key tile of 32 of the block's range. S^T = K Q^T
 // leaves a lane one row and 16 keys, which O^T = V^T P^T takes one by one as its B
@@ -1094,14 +813,14 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   const AttnBlock k_(a);
   if (!k_.live) return;
   const CacheSeq s = k_.s;
-  const int b = k_.b, h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr;
+  const int32_t *tab = k_.tab;
+  const int h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr, part_ = k_.part;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lg = lane >> 5;
   const int mlast = min(m0 + 32, count) - 1, mm = min(m0 + lr, mlast), row = cache_row(c, mm);
   const int lim_lo = k_.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
   const int tiles = (k_.lim_hi + 31) / 32;
   const int t0 = nr > 1 ? sp * (a.range / 32) : 0, t1 = nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
-  const int32_t *tab = c.table + (int64_t)b * c.table_ld;
   const float *Q = (const float *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm - row * group) * HD + 4 * lg;
   const float *K = (const float *)c.k + 4 * lg, *V = (const float *)c.v + NI * lr;
   const float sc = LOG2E / sqrtf((float)HD);
@@ -1212,8 +931,8 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   }
   // wave w finishes entries e = 4 w .. 4 w + 3: NI x 4 consecutive dimensions per lane
   const int head = h * group + mm - row * group, dim0 = NI * (8 * w + 4 * lg);
-  const int64_t at = part_slot(a, sp, s.q0 + row, head);
-  float *O = nr > 1 ? a.part + at * HD + dim0
+  const int64_t at = part_slot(a, max(part_, 0), s.q0 + row, head);
+  float *O = part_ >= 0 ? a.part + at * HD + dim0
                           : (float *)a.o + (int64_t)(s.q0 + row) * a.ldo + (int64_t)head * HD + dim0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -1222,10 +941,10 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
       float y = 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u) y += wt[u] * po[u][i * 16 + 4 * w + e][lane];
-      O[NI * e + i] = nr > 1 ? y : den == 0.f ? 0.f : y / den;
+      O[NI * e + i] = part_ >= 0 ? y : den == 0.f ? 0.f : y / den;
     }
   if (w != 0 || lg != 0) return;
-  if (nr > 1) {
+  if (part_ >= 0) {
     *(float2 *)part_ml(a, at) = make_float2(mx, den);
   } else if (a.lse) {
     a.lse[(int64_t)(s.q0 + row) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
@@ -1483,14 +1202,6 @@ __global__ __launch_bounds__(256) void k_cache_mass_combine(CacheMassArgs a) {
 }
 
 // ---------------------------------------------------------------- launches
-// most blocks of one range of keys each
-int64_t attn_blocks(int rpb, const CacheArgs &c) {
-  const int64_t group = c.heads / c.kvh, per = (c.max_q * group + rpb - 1) / rpb;
-  return c.kvh * std::min<int64_t>(c.batch * per, c.rows * group / rpb + c.batch);
-}
-size_t attn_part_bytes(const CacheArgs &c, int splits) {
-  return (size_t)splits * c.rows * c.heads * (c.hd + 2) * sizeof(float);
-}
 // Rows per block and key ranges. Lengths are known on the device only; the host
 // has their bounds.
 //
@@ -1591,36 +1302,31 @@ size_t cache_attn_scratch(int dtype, const CacheArgs &c) {
   return splits > 1 ? attn_part_bytes(c, splits) : 0;
 }
 
+static hipError_t launch_pass(int dtype, const CacheAttnArgs &a, hipStream_t s) {
+  if (dtype == 1) return a.c.hd == 128 ? launch_bf16<128>(a, s) : launch_bf16<64>(a, s);
+  const dim3 grid((unsigned)(attn_blocks(a.rpb, a.c) * a.splits));
+  if (a.c.hd == 128)
+    hipLaunchKernelGGL((k_cache_attn_f32<128>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_cache_attn_f32<64>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_t s) {
   CacheAttnArgs a = in;
   attn_plan(dtype, a.c, a.part ? a.part_bytes : 0, &a.rpb, &a.range, &a.splits);
+  a.parts = a.splits;
   if (a.c.rows <= 0 || a.c.max_q <= 0) return hipSuccess;
-  hipError_t e;
-  if (dtype == 1) {
-    e = a.c.hd == 128 ? launch_bf16<128>(a, s) : launch_bf16<64>(a, s);
-  } else {
-    const dim3 grid((unsigned)(attn_blocks(a.rpb, a.c) * a.splits));
-    if (a.c.hd == 128)
-      hipLaunchKernelGGL((k_cache_attn_f32<128>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_cache_attn_f32<64>), grid, dim3(256), 0, s, a);
-    e = hipGetLastError();
-  }
-  if (e != hipSuccess || a.splits <= 1) return e;
-  const int64_t items = (int64_t)a.c.max_q * a.c.heads * (a.c.hd / 4);
-  const dim3 grid((unsigned)((items + 255) / 256), a.c.batch);
-  if (dtype == 1) {
-    if (a.c.hd == 128)
-      hipLaunchKernelGGL((k_cache_attn_combine<bf16_t, 128>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_cache_attn_combine<bf16_t, 64>), grid, dim3(256), 0, s, a);
-  } else {
-    if (a.c.hd == 128)
-      hipLaunchKernelGGL((k_cache_attn_combine<float, 128>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_cache_attn_combine<float, 64>), grid, dim3(256), 0, s, a);
-  }
-  return hipGetLastError();
+  const hipError_t e = launch_pass(dtype, a, s);
+  return e != hipSuccess || a.splits <= 1 ? e : launch_combine(dtype, a, s);
+}
+
+size_t cache_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh) {
+  return shared_part_bytes(c, shared_passes(dtype, c, sh, attn_plan));
+}
+
+hipError_t launch_cache_attention_shared(int dtype, const CacheAttnArgs &in, hipStream_t s) {
+  return launch_shared(dtype, in, attn_plan, launch_pass, s);
 }
 
 static int64_t mass_blocks(int dtype, const CacheArgs &c) {

@@ -17,6 +17,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
 
 __device__ __forceinline__ float bf2f(bf16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 
@@ -65,6 +66,16 @@ __device__ __forceinline__ float group_sum(float v) {
   v += dpp_move<0x4E>(v);   // quad_perm [2, 3, 0, 1]
   v += dpp_move<0x141>(v);  // row_half_mirror
   if (G == 16) v += dpp_move<0x140>(v);  // row_mirror
+  return v;
+}
+// Largest over each aligned group of G lanes, of values that are not NaN
+template <int G>
+__device__ __forceinline__ float group_max(float v) {
+  static_assert(G == 8 || G == 16, "group of 8 or 16 lanes");
+  v = fmaxf(v, dpp_move<0xB1>(v));
+  v = fmaxf(v, dpp_move<0x4E>(v));
+  v = fmaxf(v, dpp_move<0x141>(v));
+  if (G == 16) v = fmaxf(v, dpp_move<0x140>(v));
   return v;
 }
 // Sum over the wave, in every lane: within rows of 16 lanes by DPP moves, then
@@ -207,12 +218,14 @@ __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlan
 // clamp them to the sizes given by the host, so that no device value leads
 // outside the buffers.
 struct CacheArgs {
-  void *k, *v;              // [pages, kvh, 1 << plog, hd]
+  void *k, *v;              // [pages, kvh, 1 << plog, hd] in the model dtype, or with scale e4m3 codes
+  uint8_t *scale;           // [pages, kvh, 1 << plog, 2]: exponent bytes of k and v; null: none
   const int32_t *q_start;   // [batch + 1]
   const int32_t *kv_len;    // [batch]
   const int32_t *table;     // [batch, table_ld]
   int pages, plog, kvh;
-  int batch, rows, max_q, table_ld;
+  int batch, rows, max_q, table_ld;   // batch: entries that a launch goes through (sequences, if not said otherwise)
+  int seqs;                 // sequences
   int cap;                  // most keys of a sequence: max_kv, or what the table's pages hold
   int heads, hd, frame;
   uint32_t group_mul;       // see cache_row
@@ -260,7 +273,24 @@ struct CacheAppendArgs {
   int axis_end[3];          // pairs [axis_end[a - 1], axis_end[a]) turn by coordinate a
   double freq[64];          // turns per unit of the coordinate, per pair
 };
-hipError_t launch_cache_append(int dtype, const CacheAppendArgs &a, hipStream_t s);
+hipError_t launch_cache_append(int dtype, const CacheAppendArgs &a, hipStream_t s);   // codes if a.c.scale is set
+
+struct Cache8ReadArgs {
+  CacheArgs c;
+  void *k, *v;              // [rows, ldk / ldv] or null
+  int64_t ldk, ldv;
+};
+hipError_t launch_cache8_read(int dtype, const Cache8ReadArgs &a, hipStream_t s);
+
+// Groups of sequences that share a past (wdc_prefix); groups 0: none
+struct CacheShared {
+  const int32_t *group_start;   // [groups + 1]
+  const int32_t *prefix_len;    // [groups]
+  int groups, max_prefix, max_own;
+};
+// What a launch of an attention goes through: all keys of each sequence, the keys
+// that groups share (batch is their number), or each sequence's own keys
+enum { PASS_ALL = 0, PASS_SHARED = 1, PASS_OWN = 2 };
 
 struct CacheAttnArgs {
   CacheArgs c;
@@ -271,13 +301,24 @@ struct CacheAttnArgs {
   float *lse;               // [rows, heads] or null
   float *part;              // scratch (part_bytes) for key ranges, or null
   size_t part_bytes;
-  // set by launch_cache_attention: rows per block; keys per range (a multiple of
+  CacheShared sh;
+  // set by the launcher: rows per block; keys per range (a multiple of
   // 64) and the most ranges of a row block, 1 = not split
   int rpb, range, splits;
+  int pass, part0, parts;   // a pass's first part; parts of all passes
+  int past_range, past_splits;   // PASS_OWN: range and splits of the shared keys' pass
 };
 // scratch bytes that let a launch over these bounds split its keys as it would like to
 size_t cache_attn_scratch(int dtype, const CacheArgs &c);
 hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &a, hipStream_t s);
+// the same for sequences that share a past (a.sh), all of the scratch needed
+size_t cache_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh);
+hipError_t launch_cache_attention_shared(int dtype, const CacheAttnArgs &a, hipStream_t s);
+// and both over codes
+size_t cache8_attn_scratch(int dtype, const CacheArgs &c);
+hipError_t launch_cache8_attention(int dtype, const CacheAttnArgs &a, hipStream_t s);
+size_t cache8_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh);
+hipError_t launch_cache8_attention_shared(int dtype, const CacheAttnArgs &a, hipStream_t s);
 
 struct CacheMassArgs {
   CacheArgs c;

@@ -1718,7 +1718,7 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
   a->pages = p->pages;
   a->plog = plog;
   a->kvh = p->kv_heads;
-  a->batch = q->batch;
+  a->batch = a->seqs = q->batch;
   a->rows = (int)nrows;
   a->max_q = (int)max_q;
   a->table_ld = q->table_ld;
@@ -1727,6 +1727,42 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
   a->hd = c->hd;
   const uint32_t group = c->H / p->kv_heads;
   a->group_mul = group > 1 ? (uint32_t)(((uint64_t(1) << 32) + group - 1) / group) : 0;
+  return WDC_OK;
+}
+
+// the same of a cache of codes
+wdc_status cache8_args(wdc_ctx *c, const wdc_paged_cache8 *p, const wdc_chunks *q, CacheArgs *a) {
+  if (!c) return WDC_E_ARG;
+  const wdc_paged_cache codes = p ? wdc_paged_cache{p->d_k, p->d_v, p->pages, p->page, p->kv_heads, 0} : wdc_paged_cache{};
+  CHK(cache_args(c, p ? &codes : nullptr, q, true, true, a));
+  if (!p->d_scale) {
+    set_err(c, "cache without scales");
+    return WDC_E_ARG;
+  }
+  if (!aligned16(p->d_scale)) {
+    set_err(c, "scales not 16-byte aligned");
+    return WDC_E_ALIGN;
+  }
+  a->scale = (uint8_t *)p->d_scale;
+  return WDC_OK;
+}
+
+// Groups of sequences that share a past, after cache_args
+wdc_status shared_args(wdc_ctx *c, const wdc_prefix *p, const CacheArgs &a, CacheShared *sh) {
+  if (!p || !p->d_group_start || !p->d_prefix_len || p->groups < 1 || p->max_prefix < 0 || p->max_own < 0) {
+    set_err(c, "prefix descriptor: null pointer or size out of range");
+    return WDC_E_ARG;
+  }
+  if ((uintptr_t)p->d_group_start % 4 || (uintptr_t)p->d_prefix_len % 4) {
+    set_err(c, "prefix descriptor arrays not 4-byte aligned");
+    return WDC_E_ALIGN;
+  }
+  const int64_t heads = (int64_t)p->groups * a.kvh;
+  if (heads > 65535 || heads * std::min(a.cap, p->max_prefix) > kCacheKeys) {
+    set_err(c, "cache call too large: %d groups, %d kv heads", p->groups, a.kvh);
+    return WDC_E_SHAPE;
+  }
+  *sh = CacheShared{p->d_group_start, p->d_prefix_len, p->groups, p->max_prefix, p->max_own};
   return WDC_OK;
 }
 
@@ -1775,15 +1811,16 @@ wdc_status cache_f32(wdc_ctx *c, const char *what, const void *p, bool null_ok, 
   }
   return WDC_OK;
 }
-}  // namespace
 
-extern "C" {
+wdc_status enough_scratch(wdc_ctx *c, size_t bytes, size_t need) {
+  if (bytes >= need) return WDC_OK;
+  set_err(c, "scratch too small: %zu < %zu", bytes, need);
+  return WDC_E_WORKSPACE;
+}
 
-wdc_status wdc_cache_append(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_qkv,
-                            int64_t ld, const int32_t *d_pos, const float *d_q_weight, const float *d_k_weight,
-                            void *d_q, int64_t ldq) {
-  CacheAppendArgs a{};
-  CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
+// What the appends of both caches check and fill in
+wdc_status append_call(wdc_ctx *ctx, CacheAppendArgs &a, const void *d_qkv, int64_t ld, const int32_t *d_pos,
+                       const float *d_q_weight, const float *d_k_weight, void *d_q, int64_t ldq) {
   CHK(cache_rows(ctx, "qkv", d_qkv, ld, (int64_t)(a.c.heads + 2 * a.c.kvh) * a.c.hd, a.c.rows));
   CHK(cache_rows(ctx, "q", d_q, ldq, (int64_t)a.c.heads * a.c.hd, a.c.rows));
   CHK(cache_f32(ctx, "q_weight", d_q_weight, true, 16));
@@ -1814,17 +1851,9 @@ wdc_status wdc_cache_append(wdc_ctx *ctx, const wdc_paged_cache *cache, const wd
   return WDC_OK;
 }
 
-size_t wdc_cache_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks) {
-  CacheArgs a;
-  if (!ctx || cache_args(const_cast<wdc_ctx *>(ctx), cache, chunks, true, false, &a) != WDC_OK) return 0;
-  return cache_attn_scratch(ctx->d.dtype, a);
-}
-
-wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_q,
-                               int64_t ldq, int32_t frame, void *d_o, int64_t ldo, float *d_lse, void *d_scratch,
-                               size_t scratch_bytes) {
-  CacheAttnArgs a{};
-  CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
+// The same of the attentions, up to the launch
+wdc_status attention_rows(wdc_ctx *ctx, CacheAttnArgs &a, const void *d_q, int64_t ldq, int32_t frame, void *d_o,
+                          int64_t ldo, float *d_lse, void *d_scratch, size_t scratch_bytes) {
   const int64_t cols = (int64_t)a.c.heads * a.c.hd;
   CHK(cache_rows(ctx, "q", d_q, ldq, cols, a.c.rows));
   CHK(cache_rows(ctx, "o", d_o, ldo, cols, a.c.rows));
@@ -1842,8 +1871,107 @@ wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const
   a.lse = d_lse;
   a.part = (float *)d_scratch;
   a.part_bytes = d_scratch ? scratch_bytes : 0;
+  return WDC_OK;
+}
+}  // namespace
+
+extern "C" {
+
+wdc_status wdc_cache_append(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_qkv,
+                            int64_t ld, const int32_t *d_pos, const float *d_q_weight, const float *d_k_weight,
+                            void *d_q, int64_t ldq) {
+  CacheAppendArgs a{};
+  CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
+  return append_call(ctx, a, d_qkv, ld, d_pos, d_q_weight, d_k_weight, d_q, ldq);
+}
+
+wdc_status wdc_cache8_append(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks, const void *d_qkv,
+                             int64_t ld, const int32_t *d_pos, const float *d_q_weight, const float *d_k_weight,
+                             void *d_q, int64_t ldq) {
+  CacheAppendArgs a{};
+  CHK(cache8_args(ctx, cache, chunks, &a.c));
+  return append_call(ctx, a, d_qkv, ld, d_pos, d_q_weight, d_k_weight, d_q, ldq);
+}
+
+wdc_status wdc_cache8_read(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks, void *d_k, int64_t ldk,
+                           void *d_v, int64_t ldv) {
+  Cache8ReadArgs a{};
+  CHK(cache8_args(ctx, cache, chunks, &a.c));
+  const int64_t cols = (int64_t)a.c.kvh * a.c.hd;
+  if (!d_k && !d_v && a.c.rows > 0) {
+    set_err(ctx, "neither keys nor values asked for");
+    return WDC_E_ARG;
+  }
+  if (d_k) CHK(cache_rows(ctx, "k", d_k, ldk, cols, a.c.rows));
+  if (d_v) CHK(cache_rows(ctx, "v", d_v, ldv, cols, a.c.rows));
+  a.k = d_k;
+  a.ldk = ldk;
+  a.v = d_v;
+  a.ldv = ldv;
+  const OnStreamDevice on(ctx->stream);
+  HIPCHK(ctx, launch_cache8_read(ctx->d.dtype, a, ctx->stream));
+  return WDC_OK;
+}
+
+size_t wdc_cache_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks) {
+  CacheArgs a;
+  if (!ctx || cache_args(const_cast<wdc_ctx *>(ctx), cache, chunks, true, false, &a) != WDC_OK) return 0;
+  return cache_attn_scratch(ctx->d.dtype, a);
+}
+
+wdc_status wdc_cache_attention(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks, const void *d_q,
+                               int64_t ldq, int32_t frame, void *d_o, int64_t ldo, float *d_lse, void *d_scratch,
+                               size_t scratch_bytes) {
+  CacheAttnArgs a{};
+  CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
+  CHK(attention_rows(ctx, a, d_q, ldq, frame, d_o, ldo, d_lse, d_scratch, scratch_bytes));
   const OnStreamDevice on(ctx->stream);
   HIPCHK(ctx, launch_cache_attention(ctx->d.dtype, a, ctx->stream));
+  return WDC_OK;
+}
+
+size_t wdc_cache_attention_shared_scratch(const wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks,
+                                          const wdc_prefix *prefix) {
+  CacheArgs a;
+  CacheShared sh;
+  wdc_ctx *c = const_cast<wdc_ctx *>(ctx);
+  if (!ctx || cache_args(c, cache, chunks, true, false, &a) != WDC_OK || shared_args(c, prefix, a, &sh) != WDC_OK) return 0;
+  return cache_shared_scratch(ctx->d.dtype, a, sh);
+}
+
+wdc_status wdc_cache_attention_shared(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks,
+                                      const wdc_prefix *prefix, const void *d_q, int64_t ldq, int32_t frame, void *d_o,
+                                      int64_t ldo, float *d_lse, void *d_scratch, size_t scratch_bytes) {
+  CacheAttnArgs a{};
+  CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
+  CHK(shared_args(ctx, prefix, a.c, &a.sh));
+  CHK(attention_rows(ctx, a, d_q, ldq, frame, d_o, ldo, d_lse, d_scratch, scratch_bytes));
+  CHK(enough_scratch(ctx, d_scratch ? scratch_bytes : 0, cache_shared_scratch(ctx->d.dtype, a.c, a.sh)));
+  const OnStreamDevice on(ctx->stream);
+  HIPCHK(ctx, launch_cache_attention_shared(ctx->d.dtype, a, ctx->stream));
+  return WDC_OK;
+}
+
+size_t wdc_cache8_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks,
+                                    const wdc_prefix *prefix) {
+  CacheArgs a;
+  CacheShared sh;
+  wdc_ctx *c = const_cast<wdc_ctx *>(ctx);
+  if (!ctx || cache8_args(c, cache, chunks, &a) != WDC_OK || (prefix && shared_args(c, prefix, a, &sh) != WDC_OK)) return 0;
+  return prefix ? cache8_shared_scratch(ctx->d.dtype, a, sh) : cache8_attn_scratch(ctx->d.dtype, a);
+}
+
+wdc_status wdc_cache8_attention(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks,
+                                const wdc_prefix *prefix, const void *d_q, int64_t ldq, int32_t frame, void *d_o,
+                                int64_t ldo, float *d_lse, void *d_scratch, size_t scratch_bytes) {
+  CacheAttnArgs a{};
+  CHK(cache8_args(ctx, cache, chunks, &a.c));
+  if (prefix) CHK(shared_args(ctx, prefix, a.c, &a.sh));
+  CHK(attention_rows(ctx, a, d_q, ldq, frame, d_o, ldo, d_lse, d_scratch, scratch_bytes));
+  if (prefix) CHK(enough_scratch(ctx, d_scratch ? scratch_bytes : 0, cache8_shared_scratch(ctx->d.dtype, a.c, a.sh)));
+  const OnStreamDevice on(ctx->stream);
+  HIPCHK(ctx, prefix ? launch_cache8_attention_shared(ctx->d.dtype, a, ctx->stream)
+                     : launch_cache8_attention(ctx->d.dtype, a, ctx->stream));
   return WDC_OK;
 }
 
