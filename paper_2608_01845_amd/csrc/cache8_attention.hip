@@ -20,6 +20,18 @@ __device__ __forceinline__ void values8(uint32_t u, uint32_t v, float up, float 
     x[6 + e] = d[e];
   }
 }
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __attribute__((ext_vector_type(2))) int i32x2_t;
+typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
+// Eight rows of 16 bytes, each read as 2 x 8 bytes by the lanes of a group of 16 in row order, come back
+// transposed: lane c of the group gets byte c of each.
+__device__ __forceinline__ u32x2_t lds_read_tr8(const char *p) {
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)p));
+}
+// Buffer of `bytes` bytes from base + off (both the same in every lane): what lies outside reads as zero
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_at(const void *base, int64_t off, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((char *)base + off, 0, bytes, RSRC_WORD3);
+}
 // power of two of an exponent byte
 __device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float((byte & 255u) << 23); }
 
@@ -28,7 +40,7 @@ __device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float((
 // tile of 32 of the block's range. S^T = K Q^T leaves a lane one row and 16 keys, which O^T = V^T P^T takes one by
 // one as its B operand. Codes come straight from the cache, those of K 16 at a time (which dimension a lane
 // takes in which step is free as long as K and Q agree: lane group g has [g hd / 2, + hd / 2)).
-template <typename T, int HD>
+template <int HD>
 __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
   constexpr int NI = HD / 32, NC = HD / 2;
   typedef __attribute__((ext_vector_type(NI))) float vecn;
@@ -45,12 +57,12 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
   const int lim_lo = k_.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
   const int tiles = (k_.lim_hi + 31) / 32;
   const int t0 = nr > 1 ? sp * (a.range / 32) : 0, t1 = nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
-  const T *Q = (const T *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm - row * group) * HD + NC * lg;
+  const float *Q = (const float *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm - row * group) * HD + NC * lg;
   const uint8_t *K = (const uint8_t *)c.k + NC * lg, *V = (const uint8_t *)c.v + NI * lr;
   const float sc = LOG2E / sqrtf((float)HD);
   float qf[NC];
 #pragma unroll
-  for (int j = 0; j < NC; ++j) qf[j] = ld<T>(Q + j) * sc;
+  for (int j = 0; j < NC; ++j) qf[j] = Q[j] * sc;
   uint4 kq[NC / 16];
   float kup;
   f32x16 o[NI];
@@ -178,7 +190,7 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
   // wave w finishes entries e = 4 w .. 4 w + 3: NI x 4 consecutive dimensions per lane
   const int head = h * group + mm - row * group, dim0 = NI * (8 * w + 4 * lg);
   const int64_t at = part_slot(a, max(part_, 0), s.q0 + row, head);
-  T *O = (T *)a.o + (int64_t)(s.q0 + row) * a.ldo + (int64_t)head * HD + dim0;
+  float *O = (float *)a.o + (int64_t)(s.q0 + row) * a.ldo + (int64_t)head * HD + dim0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -189,7 +201,7 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
       if (part_ >= 0)
         a.part[at * HD + dim0 + NI * e + i] = y;
       else
-        st<T>(O + NI * e + i, den == 0.f ? 0.f : y / den);
+        O[NI * e + i] = den == 0.f ? 0.f : y / den;
     }
   if (w != 0 || lg != 0) return;
   if (part_ >= 0) {
@@ -199,32 +211,890 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
   }
 }
 
+// ---------------------------------------------------------------- bf16, few rows
+// RT tiles of 16 query rows per block of four waves; wave w takes key tiles w, w + 4, .. of 32 keys of the block's range and
+// the four partial softmaxes meet at the end. What bounds it is the stream of codes: each wave has a tile under way in registers
+// beside the one it works on.
+//
+// S^T = K Q^T (A: 16 keys, B: 16 rows): lane (lr, lg) loads hd / 4 consecutive codes of key lr, and Q in the same order of
+// dimensions, so K needs no LDS; its powers ride on the conversion to bf16. The lane is left the
+// scores of row lr and keys 4 lg + e of both halves of the tile, the B operand of O^T = V^T P^T. V goes through LDS, from which rows
+// come back transposed, 8 keys of one dimension a lane, so V's powers cannot ride on the conversion: they multiply the weights, which
+// are rounded to bf16 before that (a power of two changes no digit). The softmax is the one of the cache in bf16.
+template <int HD>
+struct Codes {
+  static constexpr int KT = 32;                  // keys per tile
+  static constexpr int NL = HD / 64;             // 16-byte loads of a lane per 16 keys
+  static constexpr int CH = HD / 16;             // 16-byte chunks of a row
+  // chunk c of row r lies at c ^ key(r): the 32 rows of a transposed read, one chunk each, spread over the banks
+  static __device__ __forceinline__ int key(int r) { return HD == 128 ? (r >> 1) & 7 : (r >> 2) & 3; }
+};
+
+// Eight codes as bf16, times a power of two. (The conversion's result is taken as a word: its second half taken as an element
+// comes out as the first.)
+__device__ __forceinline__ bf16x8 bf16_values8(uint32_t u, uint32_t v, float up) {
+  const u32x4_t w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, up, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, up, true)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, up, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, up, true))};
+  return __builtin_bit_cast(bf16x8, w);
+}
+// whether one of four codes is NaN
+__device__ __forceinline__ bool has_nan(uint32_t u) { return (((u & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }
+
+template <int HD, int RT>
+__global__ __launch_bounds__(256, 1) void k_cache8_attn_few(CacheAttnArgs a) {
+  using F = Codes<HD>;
+  constexpr int NC = HD / 32, NI = HD / 16, KT = F::KT, NL = F::NL, WAVE = 64 * RT * HD;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ float ml[4][2][16 * RT];
+  const CacheArgs &c = a.c;
+  const AttnBlock k_(a);
+  if (!k_.live) return;
+  const CacheSeq s = k_.s;
+  const int h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr, part_ = k_.part;
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int mlast = min(m0 + 16 * RT, count) - 1;
+  const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KT - 1) / KT;
+  const int t0 = nr > 1 ? sp * (a.range / KT) : 0, t1 = nr > 1 ? min(t0 + a.range / KT, tiles) : tiles;
+
+  const float sc = LOG2E / sqrtf((float)HD);
+  bf16x8 qf[RT][NC];
+  int lim[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int m = m0 + 16 * t + lr, mm = min(m, mlast), i = cache_row(c, mm);
+    lim[t] = m < count ? cache_limit(c, s, i) : 0;
+    const bf16_t *Q = (const bf16_t *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)(h * group + mm - i * group) * HD + HD / 4 * lg;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) qf[t][j] = *(const bf16x8 *)(Q + 8 * j);
+  }
+
+  char *mine = smem + w * WAVE;
+  int vwo[NL], vro[NI];                          // LDS offsets of the lane's V codes in 16 rows; of its transposed reads
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    const int r = lane / F::CH + j * (64 / F::CH);
+    vwo[j] = r * HD + ((lane % F::CH) ^ F::key(r)) * 16;   // (key(r + 16) is key(r))
+  }
+  {
+    const int i8 = lr >> 1, r = (i8 < 4 ? 0 : 12) + 4 * lg + i8;   // keys 4 lg .. of the first and the second 16 rows
+#pragma unroll
+    for (int i = 0; i < NI; ++i) vro[i] = r * HD + (i ^ F::key(r)) * 16 + 8 * (lr & 1);
+  }
+  PageWalk<false> pw;
+  pw.init(c, k_.tab, k_.tab_last, h, (KT * t0) >> c.plog);
+  const int pmask = (1 << c.plog) - 1;
+  struct Tile {
+    u32x4_t k[2][NL], v[2][NL];
+    uint32_t ks[2];                              // powers' bytes of (k, v) of key lr
+    u32x2_t es[2];                               // of keys 4 lg ..
+  } tile[2];
+  // Tile t: halves of 16 rows, each on one page. Rows past the cache's end lie outside the buffer range and arrive as
+  // zeros, whatever they hold; so do tiles past the range.
+  auto load = [&](int t, Tile &x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int key = KT * t + 16 * hf;
+      const bool live = t < t1;
+      if (live) pw.advance(c, h, key >> c.plog);
+      const int64_t slot = live ? pw.get(c, h, key >> c.plog) + (key & pmask) : 0;
+      const int rows = live ? min(max(s.n - key, 0), 16) : 0;
+      const auto kd = rsrc_at(c.k, slot * HD, rows * HD), vd = rsrc_at(c.v, slot * HD, rows * HD);
+      // (a load that starts inside a range and ends outside is none: whole groups of 4 slots, which lie on one page)
+      const auto ed = rsrc_at(c.scale, slot * 2, (rows + 3) / 4 * 8);
+      x.ks[hf] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(ed, 2 * lr, 0, 0);
+      x.es[hf] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(ed, 8 * lg, 0, 0));
+#pragma unroll
+      for (int j = 0; j < NL; ++j)
+        x.k[hf][j] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kd, lr * HD + HD / 4 * lg + 16 * j, 0, 0));
+#pragma unroll
+      for (int j = 0; j < NL; ++j)
+        x.v[hf][j] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16 + 1024 * j, 0, 0));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  f32x4 o[RT][NI];
+  float m[RT], l[RT], d[RT];                     // d: sum of the rounded weights
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = d[t] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  auto step = [&](const Tile &x, int t) __attribute__((always_inline)) {
+    f32x4 S[RT][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float up = power(x.ks[k]);
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const u32x4_t u = x.k[k][j / 2];
+        const bf16x8 kf = bf16_values8(u[2 * (j & 1)], u[2 * (j & 1) + 1], up);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          S[r][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[r][k], 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < NL; ++j) *(u32x4_t *)(mine + k * 16 * HD + vwo[j]) = x.v[k][j];
+    }
+    const bool part = KT * t + KT > lim_lo;      // some row does not see the whole tile
+    bf16x8 pf[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float y = S[r][k][e] * sc;
+          if (KT * t + 16 * k + 4 * lg + e >= lim[r]) y = -INFINITY;
+          S[r][k][e] = y;
+          mx = fmaxf(mx, y);
+        }
+      mx = quad_max(mx);
+      if (__any(mx > m[r] + 8.f)) {
+        const float mn = fmaxf(m[r], mx), al = mn == m[r] ? 1.f : __builtin_amdgcn_exp2f(m[r] - mn);
+        m[r] = mn;
+        l[r] *= al;
+        d[r] *= al;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[r][i][e] *= al;
+      }
+      const float ref = m[r] == -INFINITY ? 0.f : m[r];   // a row that has seen nothing yet
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(S[r][k][e] - ref), y = (float)(__bf16)p;
+          l[r] += p;
+          d[r] += y;
+          // (of a slot past the end, whose byte may be any, 0 stays 0: 0 times a power of infinity would not)
+          pf[r][4 * k + e] = (__bf16)__builtin_ldexpf(y, (int)(x.es[k][e >> 1] >> (16 * (e & 1) + 8) & 255u) - 127);
+        }
+    }
+    // A key that a row does not see has weight 0, but 0 times NaN is NaN in a matrix product. Tiles seen in
+    // part are looked over, and one whose V holds NaN is multiplied key by key.
+    bool odd = false;
+    if (part) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < NL; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) odd |= has_nan(x.v[k][j][q]);
+      odd = __any(odd);
+    }
+    asm volatile("" ::: "memory");
+    if (odd) {
+#pragma unroll 1
+      for (int y = 0; y < KT; ++y) {             // key 16 (q / 4) + 4 g + q % 4
+        const int q = y >> 2, g = y & 3, key = 16 * (q >> 2) + 4 * g + (q & 3);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          float p = 0.f;                         // of key and row lr, held by lane group g
+#pragma unroll
+          for (int z = 0; z < 8; ++z)
+            if (z == q) p = (float)pf[r][z];
+          p = __shfl(p, 16 * g + lr, 64);
+          if (KT * t + key < lim[r])
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+              float v[8];
+              values8(*(const uint32_t *)(mine + key * HD + (i ^ F::key(key)) * 16 + 4 * lg), 0u, 1.f, v);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[r][i][e] += p * v[e];
+            }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const u32x2_t u = lds_read_tr8(mine + vro[i]);
+        const bf16x8 vf = bf16_values8(u[0], u[1], 1.f);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][i], 0, 0, 0);
+      }
+    }
+    asm volatile("" ::: "memory");
+  };
+  if (t0 + w < t1) {
+    load(t0 + w, tile[0]);
+    for (int t = t0 + w; t < t1; t += 8) {
+      load(t + 4, tile[1]);
+      step(tile[0], t);
+      if (t + 4 >= t1) break;
+      load(t + 8, tile[0]);
+      step(tile[1], t + 4);
+    }
+  }
+
+  // the four waves' parts: each leaves its rows in its own part of LDS
+  float *po = (float *)mine;                     // [16 RT rows][HD]
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    l[t] = quad_sum(l[t]);
+    const float f = unround(l[t], quad_sum(d[t]));
+#pragma unroll
+    for (int i = 0; i < NI; ++i) *(f32x4 *)(po + (16 * t + lr) * HD + 4 * ((4 * i + lg) ^ (lr & 7))) = o[t][i] * f;
+    if (lg == 0) {
+      ml[w][0][16 * t + lr] = m[t];
+      ml[w][1][16 * t + lr] = l[t];
+    }
+  }
+  __syncthreads();
+  constexpr int TPR = HD / 4, RPI = 256 / TPR;   // threads per row, rows per turn
+  for (int r = tid / TPR; r < 16 * RT; r += RPI) {
+    const int mr = m0 + r, e = tid % TPR;
+    if (mr >= count) continue;
+    float mx = ml[0][0][r];
+#pragma unroll
+    for (int u = 1; u < 4; ++u) mx = fmaxf(mx, ml[u][0][r]);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float den = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float wt = __builtin_amdgcn_exp2f(ml[u][0][r] - ref);
+      den += wt * ml[u][1][r];
+      const f32x4 y = *(const f32x4 *)(smem + u * WAVE + (r * HD + 4 * (e ^ (r & 7))) * 4);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) x[d] += wt * y[d];
+    }
+    const int i = cache_row(c, mr), head = h * group + mr - i * group;
+    if (part_ >= 0) {
+      const int64_t at = part_slot(a, part_, s.q0 + i, head);
+      *(f32x4 *)(a.part + at * HD + 4 * e) = x;
+      if (e == 0) *(float2 *)part_ml(a, at) = make_float2(mx, den);
+      continue;
+    }
+    const float inv = 1.f / den;
+    bf16x4 y;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) y[d] = (__bf16)(den == 0.f ? 0.f : x[d] * inv);
+    *(bf16x4 *)((bf16_t *)a.o + (int64_t)(s.q0 + i) * a.ldo + (int64_t)head * HD + 4 * e) = y;
+    if (a.lse && e == 0)
+      a.lse[(int64_t)(s.q0 + i) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
+  }
+}
+
+// ---------------------------------------------------------------- bf16, many rows
+// The software pipeline of the cache in bf16 (32 query rows a wave, key tiles of 64, step t: P V of tile t, Q K of tile t + 2
+// and the exponentials of tile t + 1 in one stream), with its tiles made from codes on the way: direct buffer loads of four waves bring
+// a tile's codes and exponent bytes to LDS, and in every step all waves turn one tile of K and one of V into bf16 tiles
+// of the same layout, each code once for all rows of the block. Step t asks for the codes of K_t+5 and V_t+4, converts K_t+3
+// and V_t+2, and reads K_t+2, V_t and the first of V_t+1: two, four and three slots of K, V and codes.
+//
+// Tiles that some row sees in part, and the cache's last one, follow one at a time with their masks, tile u + 1 converted
+// while u is worked on.
+constexpr int KV = 64, KS = 2, VS = 4, RS = 3, ES = 4;   // keys a tile; slots of K, V, codes and exponent bytes
+constexpr int EB = 256;                          // bytes of a slot of exponent bytes
+constexpr float SUM_LIMIT = 0x1p8f;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+
+// Direct global -> LDS loads: lane l's 16 (4) bytes at `voff` of the buffer arrive at lds + 16 l (4 l). Instructions
+// and wait states as in the kernels over bf16 (five between a vector instruction's scalar result and its use as
+// part of a descriptor, one behind M0).
+__device__ __forceinline__ void lds_load16(u32x4_t buf, uint32_t lds, int voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uni((int)lds)), "v"(voff), "s"(buf)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void lds_load4(u32x4_t buf, uint32_t lds, int voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(uni((int)lds)), "v"(voff), "s"(buf)
+               : "memory", "m0");
+}
+
+// Loads of one wave (of four): stripe i of a tile is rows [(4 i + w) RPL, + RPL). SMALL:
+// pages of 16 or 32 slots, where every stripe has its own page; otherwise a tile lies on one page.
+template <int HD, bool SMALL>
+struct CodeLoads {
+  static constexpr int RPL = 1024 / HD;          // rows per load (8 or 16)
+  static constexpr int NS = KV / (4 * RPL);      // stripes of a wave per tile (2 or 1)
+  static constexpr int NP = SMALL ? NS : 1;
+  static constexpr int NK = NS + 1;              // loads of K, exponent bytes included
+  struct Where {
+    int64_t off[NP];                             // bytes from the pool to the stripe (SMALL), or to the tile
+    int bytes[NP];                               // what lies before the end of the cache
+  };
+  PageWalk<true> pw;                             // SMALL only
+  int w, h, n;
+  __device__ __forceinline__ void init(const CacheArgs &c, const CacheSeq &s, const int32_t *tab, int tab_last, int h_, int w_,
+                                       int tile0) {
+    w = w_;
+    h = h_;
+    n = s.n;
+    if (SMALL) pw.init(c, tab, tab_last, h, (KV * tile0) >> c.plog);
+  }
+  // page of a whole tile, by a scalar load (the table does not change during a launch)
+  __device__ __forceinline__ int page(const CacheArgs &c, const int32_t *tab, int tab_last, int tile) const {
+    typedef const __attribute__((address_space(4))) int32_t *scalar_ptr;
+    const int e = min((KV * tile) >> c.plog, tab_last);
+    return cache_page(c, ((scalar_ptr)(uint64_t)tab)[e]);
+  }
+  // where a tile lies, its page given (unless SMALL), and the load of its exponent bytes, 2 keys a lane
+  __device__ __forceinline__ void find(const CacheArgs &c, int tile, int page, Where &x, uint32_t lds) {
+    const int pmask = (1 << c.plog) - 1, key0 = KV * tile, lane = threadIdx.x & 63;
+    if (SMALL) pw.advance(c, h, key0 >> c.plog);   // a tile's pages are of one group of 64
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int at = SMALL ? (4 * i + w) * RPL : 0, key = key0 + at, rows = SMALL ? RPL : KV;
+      const int slot = SMALL ? pw.get(c, h, key >> c.plog) : ((page * c.kvh + h) << c.plog);   // (pools hold fewer than 2^31)
+      x.off[i] = (int64_t)(slot + (key & pmask)) * HD;
+      x.bytes[i] = min(max(n - key, 0), rows) * HD;
+    }
+    // lanes of keys past the end, and the upper half, ask for what is outside (pools have fewer than 2^32 of these bytes)
+    const int key = key0 + 2 * (lane & 31);
+    const int slot = SMALL ? __shfl(pw.cur, (key >> c.plog) - pw.base, 64) : (page * c.kvh + h) << c.plog;
+    const uint32_t all = (uint32_t)(((int64_t)c.pages * c.kvh << c.plog) * 2);
+    const uint32_t voff = lane < 32 && key < n ? (uint32_t)(slot + (key & pmask)) * 2 : all;
+    lds_load4(buffer_at(c.scale, 0, (int)all), lds, (int)voff);
+  }
+  __device__ __forceinline__ void load(const void *pool, const Where &x, uint32_t lds) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      lds_load16(buffer_at(pool, x.off[SMALL ? i : 0], x.bytes[SMALL ? i : 0]), lds + (4 * i + w) * 1024,
+                 16 * lane + (SMALL ? 0 : (4 * i + w) * 1024));
+  }
+};
+
+template <int HD, bool SMALL, int W, int KG>
+__global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArgs a) {
+  using F = Few<HD>;
+  using TL = CodeLoads<HD, SMALL>;
+  constexpr int NC = HD / 32, NI = HD / 16;
+  constexpr int TB = KV * F::ROWB, RB = KV * HD; // bytes of a tile in bf16, in codes
+  constexpr int V_BASE = KS * TB, RK_BASE = V_BASE + VS * TB, RV_BASE = RK_BASE + RS * RB, E_BASE = RV_BASE + RS * RB;
+  constexpr int RING = E_BASE + ES * EB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ int odd_tile[KG][4];
+  const CacheArgs &c = a.c;
+  const AttnBlock k_(a);
+  if (!k_.live) return;
+  const CacheSeq s = k_.s;
+  const int32_t *tab = k_.tab;
+  const int tab_last = k_.tab_last;
+  const int h = k_.h, m0 = k_.m0, count = k_.count, group = k_.group, sp = k_.sp, nr = k_.nr, part_ = k_.part;
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int WR = W / KG;                     // waves over the block's rows
+  const int wr = wid % WR, kg = wid / WR;
+  const bool grp_a = KG == 2 || wid < 4;         // loads tiles
+  const int mlast = min(m0 + 32 * WR, count) - 1;
+  const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KG * KV - 1) / (KG * KV);   // in steps of KG tiles
+  const int range = a.range / (KG * KV), t_first = nr > 1 ? sp * range : 0, t_end = nr > 1 ? min(t_first + range, tiles) : tiles;
+  // steps of the range, relative to t_first: `nf` that every row sees whole, then masked ones
+  const int tot = t_end - t_first, nf = min(max(lim_lo / (KG * KV) - t_first, 0), tot);
+  const int ahead = min(tot, nf + RS);           // codes that the pipeline asks for
+
+  const float sc = LOG2E / sqrtf((float)HD);
+  bf16x8 qf[2][NC];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int mm = min(m0 + 32 * wr + 16 * t + lr, mlast), i = cache_row(c, mm);
+    const bf16_t *Q = (const bf16_t *)a.q + (int64_t)(s.q0 + i) * a.ldq + (int64_t)(h * group + mm - i * group) * HD + 8 * lg;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) qf[t][j] = *(const bf16x8 *)(Q + 32 * j);
+  }
+  int kro[NC];                                   // K fragment of rows lr, dims 32 c + 8 lg
+#pragma unroll
+  for (int j = 0; j < NC; ++j) kro[j] = lr * F::ROWB + ((4 * j + lg) ^ F::kkey(lr)) * 16;
+  int vro[F::VR];                                // transposed V read of rows 4 lg .. + 3, dims 16 i ..
+  {
+    const int r = 4 * lg + (lr >> 2), j = lane & 3;
+#pragma unroll
+    for (int i = 0; i < F::VR; ++i) vro[i] = V_BASE + r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
+  }
+  char *ring = smem + kg * RING;
+  const uint32_t lds0 = lds_addr(ring);
+  TL tl;
+  typename TL::Where wk, wv;                     // of the latest K tile asked for, and of the one before
+  auto page_of = [&](int t) { return SMALL ? 0 : tl.page(c, tab, tab_last, KG * (t_first + t) + kg); };
+  // codes of K and the exponent bytes of tile t; codes of V of the tile at x
+  auto load_k = [&](int t, int slot, int page) __attribute__((always_inline)) {
+    wv = wk;
+    tl.find(c, KG * (t_first + t) + kg, page, wk, lds0 + E_BASE + (t % ES) * EB);
+    tl.load(c.k, wk, lds0 + RK_BASE + slot * RB);
+  };
+  auto load_v = [&](int slot, const typename TL::Where &x) { tl.load(c.v, x, lds0 + RV_BASE + slot * RB); };
+
+  // Conversion: 16 codes of a row a lane. NCV pieces of 1,024 codes for each wave of both K and V, or (BOTH false) one of K
+  // for the first half of the waves and one of V for the others.
+  constexpr int PIECES = RB / 1024;
+  constexpr bool BOTH = WR <= PIECES;
+  constexpr int NCV = BOTH ? PIECES / WR : 1;
+  const bool conv_k = BOTH || wr < PIECES, conv_v = BOTH || wr >= PIECES;
+  const int piece = BOTH ? wr : wr % PIECES, crow = piece * TL::RPL + lane / (HD / 16), cch = lane % (HD / 16);
+  const int kwo = crow * F::ROWB + ((2 * cch) ^ F::kkey(crow)) * 16, vwo = crow * F::ROWB + ((2 * cch) ^ F::vkey(crow)) * 16;
+  u32x4_t raw[NCV];
+  float up[NCV];
+  // (the rows of a wave's pieces differ by a multiple of 16 or of 32, which the swizzles do not see)
+  static_assert(NCV == 1 || WR * (1024 / HD) % 16 == 0, "rows of a wave's pieces");
+  auto take = [&](const char *codes, const char *bytes, int which) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NCV; ++i) {
+      raw[i] = *(const u32x4_t *)(codes + (piece + i * WR) * 1024 + 16 * lane);
+      // (past the end any byte may follow an odd key: 255 would make the zeros there NaN)
+      up[i] = power(min((uint32_t)*(const uint8_t *)(bytes + 2 * (crow + i * WR * TL::RPL) + which), 254u));
+    }
+  };
+  auto put = [&](char *to, int at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NCV; ++i) {
+      *(bf16x8 *)(to + at + i * WR * TL::RPL * F::ROWB) = bf16_values8(raw[i][0], raw[i][1], up[i]);
+      *(bf16x8 *)(to + (at ^ 16) + i * WR * TL::RPL * F::ROWB) = bf16_values8(raw[i][2], raw[i][3], up[i]);
+    }
+  };
+  auto raw_k = [&](int slot) { return ring + RK_BASE + slot * RB; };
+  auto raw_v = [&](int slot) { return ring + RV_BASE + slot * RB; };
+  auto bytes_of = [&](int t) { return ring + E_BASE + (t % ES) * EB; };
+  // both tiles t at once; whether V holds NaN
+  auto convert = [&](int t, bool k, bool v) __attribute__((always_inline)) {
+    bool odd = false;
+    if (k && conv_k) {
+      take(raw_k(t % RS), bytes_of(t), 0);
+      put(ring + (t % KS) * TB, kwo);
+    }
+    if (v && conv_v) {
+      take(raw_v(t % RS), bytes_of(t), 1);
+      put(ring + V_BASE + (t % VS) * TB, vwo);
+#pragma unroll
+      for (int i = 0; i < NCV; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) odd |= has_nan(raw[i][q]);
+    }
+    return odd;
+  };
+
+  int page[4];                                   // of the K tiles that the next four steps ask for
+  if (grp_a) {                                   // tiles 0 to 2
+    tl.init(c, s, tab, tab_last, h, wid & 3, KG * t_first + kg);
+    wk = typename TL::Where{};
+#pragma unroll
+    for (int j = 0; j < RS; ++j)
+      if (j < tot) {
+        load_k(j, j, page_of(j));
+        load_v(j, wk);
+      }
+    wait_vm<0>();
+  }
+  if (tid < 4 * KG) odd_tile[tid >> 2][tid & 3] = 0;
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+  f32x4 o[NI][2];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+  auto qk = [&](f32x4 (&S)[4][2], const char *kb) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bf16x8 kf = *(const bf16x8 *)(kb + kro[j] + k * 16 * F::ROWB);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          S[k][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][j], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[k][t], 0, 0, 0);
+      }
+  };
+  auto vfrag = [&](const char *vb, int i, int p) {   // V^T fragment: dims 16 i .., keys of the 32-key group p
+    return v_frag<HD>(vb + vro[i % F::VR] + i / F::VR * F::VR * 32 + p * 32 * F::ROWB);
+  };
+
+  if (nf > 0) {
+    f32x4 S[2][4][2];                            // S of tiles t + 1 and t + 2 (index tile & 1)
+    bf16x8 pf[2][2][2];                          // P of tiles t and t + 1 (index tile & 1), [row tile][32-key group]
+    convert(0, true, true);
+    convert(1, true, true);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (grp_a) {                                 // K_3, V_3, K_4
+      if (3 < ahead) {
+        load_k(3, 0, page_of(3));
+        load_v(0, wk);
+      }
+      if (4 < ahead) load_k(4, 1, page_of(4));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) page[j] = page_of(5 + j);
+    qk(S[0], ring);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      m[t] = fmaxf(rowmax<HD>(S[0], t) * sc, -FLT_MAX);   // (scores of -inf: weight 0)
+      l[t] = weights(S[0], pf[0][t], t, sc, m[t]);
+    }
+    // a lane's sum of weights above which a tile's weights are taken again; far out all are
+    float limit = far_out(fmaxf(fabsf(m[0]), fabsf(m[1]))) ? -1.f : SUM_LIMIT;
+    if (nf > 1) qk(S[1], ring + TB);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    convert(2, true, false);                     // into the slot of K_0
+    if (grp_a) wait_vm<0>();                     // K_3
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    constexpr int NMF = 2 * NI + 4 * NC;         // fragment reads per step, two MFMAs each
+    constexpr int NPV = NMF / 2, EPM = 32 / NMF; // P V reads; exponentials per pair of MFMAs
+    static_assert(NMF == 16 || NMF == 32, "hd 64 or 128");
+    bf16x8 fr_[NMF];
+    // One step, P = t % 4 at compile time, as in the kernel over bf16; the conversions lie in the stream: K's codes are
+    // taken at its start and put a fourth later, V's likewise in its second half. Past the last tile they run on stale slots, unused.
+    auto read = [&](int r, const char *vb, const char *kb) __attribute__((always_inline)) {
+      const int g = r >= NPV ? r - NPV : 0;
+      if (r < NPV)
+        fr_[r] = vfrag(vb, r % NI, (r < NPV ? r : 0) / NI);
+      else
+        fr_[r] = *(const bf16x8 *)(kb + kro[g / 4] + (g % 4) * 16 * F::ROWB);
+    };
+#pragma unroll
+    for (int r = 0; r < 4; ++r) read(r, ring, ring);
+    int rs = 0;                                  // t % RS
+    auto step = [&](auto pc, int t, int page) __attribute__((always_inline)) {
+      constexpr int P = decltype(pc)::value, cur = (P + 1) & 1, n = P & 1;
+      const int r1 = rs == RS - 1 ? 0 : rs + 1, r2 = rs == 0 ? RS - 1 : rs - 1;   // (t + 1) % RS, (t + 2) % RS
+      int issued = 0;
+      if (grp_a) {
+        if (t + 5 < ahead) {
+          load_k(t + 5, r2, page);
+          issued += TL::NK;
+        } else {
+          wv = wk;
+        }
+        if (t + 4 < ahead) {
+          load_v(r1, wv);
+          issued += TL::NS;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const char *vb = ring + P * TB, *kb = ring + (P % KS) * TB, *vn = ring + ((P + 1) % VS) * TB;
+      float ls[2] = {0.f, 0.f}, ex[2];
+      auto mma = [&](int q, int t_) __attribute__((always_inline)) {
+        if (q < NPV) {
+          o[q % NI][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], pf[n][t_][(q < NPV ? q : 0) / NI], o[q % NI][t_], 0, 0, 0);
+        } else {
+          const int g = q >= NPV ? q - NPV : 0;
+          S[n][g % 4][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], qf[t_][g / 4],
+                                                                    g < 4 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[n][g % 4][t_], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto expo = [&](int x) __attribute__((always_inline)) {
+        const int k = x / 8, t_ = (x / 4) % 2, e = x % 4;
+        float y = __builtin_amdgcn_exp2f(__builtin_fmaf(S[cur][k][t_][e], sc, -m[t_]));
+        asm volatile("" : "+v"(y));
+        return y;
+      };
+#pragma unroll
+      for (int q = 0; q < NMF; ++q) {
+        if constexpr (EPM == 2) {
+          ex[0] = expo(2 * q);
+          ex[1] = expo(2 * q + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mma(q, 0);
+        if constexpr (EPM == 1) {
+          ex[q & 1] = expo(q);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mma(q, 1);
+        if (q + 4 < NMF)
+          read(q + 4, vb, kb);
+        else                                     // the next step's first reads: V of tile t + 1
+          read(q + 4 - NMF, vn, kb);
+        __builtin_amdgcn_sched_barrier(0);
+        if (EPM == 2 || (q & 1)) {
+          const int x = EPM == 2 ? 2 * q : q - 1, k = x / 8, t_ = (x / 4) % 2, e = x % 4;
+          const bf16x2_t pr = {(__bf16)ex[0], (__bf16)ex[1]};
+          uint32_t u = __builtin_bit_cast(uint32_t, pr);
+          ls[t_] += ex[0] + ex[1];
+          asm volatile("" : "+v"(u), "+v"(ls[t_]));
+          u32x4_t w_ = __builtin_bit_cast(u32x4_t, pf[cur][t_][k / 2]);
+          w_[2 * (k & 1) + e / 2] = u;
+          pf[cur][t_][k / 2] = __builtin_bit_cast(bf16x8, w_);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (BOTH) {
+          if (q == 0) take(raw_k(rs), bytes_of(P + 3), 0);
+          if (q == NMF / 4) put(ring + ((P + 3) % KS) * TB, kwo);
+          if (q == NMF / 2) take(raw_v(r2), bytes_of(P + 2), 1);
+          if (q == NMF * 3 / 4) put(ring + V_BASE + ((P + 2) % VS) * TB, vwo);
+        } else {
+          if (q == 0) take(conv_k ? raw_k(rs) : raw_v(r2), conv_k ? bytes_of(P + 3) : bytes_of(P + 2), conv_k ? 0 : 1);
+          if (q == NMF / 2) put(ring + (conv_k ? ((P + 3) % KS) * TB : V_BASE + ((P + 2) % VS) * TB), conv_k ? kwo : vwo);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (t + 1 < nf) {
+        if (__any(!(fmaxf(ls[0], ls[1]) <= limit))) {
+#pragma unroll
+          for (int t_ = 0; t_ < 2; ++t_) {
+            const float mx = rowmax<HD>(S[cur], t_) * sc, mn = fmaxf(mx, m[t_]);
+            const float al = __builtin_amdgcn_exp2f(m[t_] - mn);
+            m[t_] = mn;
+            l[t_] *= al;
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][t_][e] *= al;
+            ls[t_] = weights(S[cur], pf[cur][t_], t_, sc, m[t_]);
+          }
+          limit = far_out(fmaxf(fabsf(m[0]), fabsf(m[1]))) ? -1.f : SUM_LIMIT;
+        }
+        l[0] += ls[0];
+        l[1] += ls[1];
+      }
+      rs = r1;
+      // the loads of earlier steps are done, this step's tiles are written, and all reads but the four just issued
+      if (grp_a) {
+        if (issued == TL::NK + TL::NS)
+          wait_vm<TL::NK + TL::NS>();
+        else if (issued == TL::NS)
+          wait_vm<TL::NS>();
+        else
+          wait_vm<0>();
+      }
+      asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(8) : "memory");
+    };
+    for (int t = 0; t < nf; t += 4) {
+      int next[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) next[j] = page_of(t + 9 + j);
+      step(std::integral_constant<int, 0>{}, t, page[0]);
+      if (t + 1 >= nf) break;
+      step(std::integral_constant<int, 1>{}, t + 1, page[1]);
+      if (t + 2 >= nf) break;
+      step(std::integral_constant<int, 2>{}, t + 2, page[2]);
+      if (t + 3 >= nf) break;
+      step(std::integral_constant<int, 3>{}, t + 3, page[3]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) page[j] = next[j];
+    }
+  }
+
+  // Masked tiles, one at a time: the codes of tiles nf to nf + 2 have been asked for. A key that a row does not see has weight
+  // 0, but 0 times NaN is NaN in a matrix product: a tile whose V holds NaN is multiplied key by key.
+  int lim[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int mr = m0 + 32 * wr + 16 * t + lr;
+    lim[t] = mr < count ? cache_limit(c, s, cache_row(c, mr)) : 0;
+  }
+  auto masked_convert = [&](int u) __attribute__((always_inline)) {
+    if (__any(convert(u, true, true)) && lane == 0) odd_tile[kg][u & 3] = 1;
+  };
+  if (nf < tot) {
+    if (nf > 0) {
+      if (grp_a) wait_vm<0>();
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    masked_convert(nf);
+  }
+  for (int u = nf; u < tot; ++u) {
+    if (grp_a) wait_vm<0>();                     // codes of tile u + 1 (and u + 2)
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (grp_a && u + 3 < tot) {
+      load_k(u + 3, u % RS, page_of(u + 3));
+      load_v(u % RS, wk);
+    }
+    const bool odd = odd_tile[kg][u & 3];
+    if (lane == 0 && wr == 0) odd_tile[kg][(u + 2) & 3] = 0;
+    if (u + 1 < tot) masked_convert(u + 1);
+    const char *kb = ring + (u % KS) * TB, *vb = ring + (u % VS) * TB;   // vro holds V_BASE
+    const int key0 = KV * (KG * (t_first + u) + kg);
+    f32x4 S[4][2];
+    bf16x8 pf[2][2];
+    qk(S, kb);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key0 + 16 * k + 4 * lg + e >= lim[t]) S[k][t][e] = -INFINITY;
+      const float mx = rowmax<HD>(S, t) * sc;
+      if (__any(mx > m[t])) {                    // the largest itself: its weight is 1, without rounding
+        const float mn = fmaxf(m[t], mx), al = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
+        m[t] = mn;
+        l[t] *= al;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][t][e] *= al;
+      }
+      l[t] += weights(S, pf[t], t, sc, m[t] == -INFINITY ? 0.f : m[t]);
+    }
+    if (odd) {
+      for (int k = 0; k < 4; ++k)
+        for (int e = 0; e < 4; ++e)
+          for (int g = 0; g < 4; ++g) {
+            const int key = 16 * k + 4 * g + e;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              float p = 0.f;                     // of key and row lr, held by lane group g
+#pragma unroll
+              for (int q = 0; q < 16; ++q)
+                if (q == 4 * k + e) p = (float)pf[t][q >> 3][q & 7];
+              p = __shfl(p, 16 * g + lr, 64);
+              if (key0 + key < lim[t])
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+#pragma unroll
+                  for (int d = 0; d < 4; ++d) {
+                    const int col = 16 * i + 4 * lg + d;
+                    o[i][t][d] += p * bf2f(*(const bf16_t *)(vb + V_BASE + key * F::ROWB + ((col >> 3) ^ F::vkey(key)) * 16 + (col & 7) * 2));
+                  }
+            }
+          }
+    } else {
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const bf16x8 vf = vfrag(vb, i, p);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][p], o[i][t], 0, 0, 0);
+        }
+    }
+  }
+
+  if constexpr (KG == 2) {                       // the two softmaxes of every row meet
+    f32x4 *xo = (f32x4 *)smem + (wr * 2 * NI) * 64 + lane;
+    float2 *xm = (float2 *)((f32x4 *)smem + WR * 2 * NI * 64) + wr * 128 + lane;
+    __syncthreads();
+    if (kg == 1) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) xo[(t * NI + i) * 64] = o[i][t];
+        xm[64 * t] = make_float2(m[t], l[t]);
+      }
+    }
+    __syncthreads();
+    if (kg == 1) return;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float2 y = xm[64 * t];
+      const float mn = fmaxf(m[t], y.x), ref = mn == -INFINITY ? 0.f : mn;
+      const float a0 = __builtin_amdgcn_exp2f(m[t] - ref), a1 = __builtin_amdgcn_exp2f(y.x - ref);
+      m[t] = mn;
+      l[t] = a0 * l[t] + a1 * y.y;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const f32x4 z = xo[(t * NI + i) * 64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][t][e] = a0 * o[i][t][e] + a1 * z[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const float den = quad_sum(l[t]);
+    const int mr = m0 + 32 * wr + 16 * t + lr;
+    if (mr >= count) continue;
+    const int i0 = cache_row(c, mr), head = h * group + mr - i0 * group;
+    if (part_ >= 0) {
+      const int64_t at = part_slot(a, part_, s.q0 + i0, head);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) *(f32x4 *)(a.part + at * HD + 16 * i + 4 * lg) = o[i][t];
+      if (lg == 0) *(float2 *)part_ml(a, at) = make_float2(m[t], den);
+      continue;
+    }
+    const float inv = 1.f / den;
+    bf16_t *O = (bf16_t *)a.o + (int64_t)(s.q0 + i0) * a.ldo + (int64_t)head * HD + 4 * lg;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      bf16x4 y;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) y[d] = (__bf16)(den == 0.f ? 0.f : o[i][t][d] * inv);
+      *(bf16x4 *)(O + 16 * i) = y;
+    }
+    if (a.lse && lg == 0)
+      a.lse[(int64_t)(s.q0 + i0) * c.heads + head] = den == 0.f ? -INFINITY : (m[t] + log2f(den)) * LN2;
+  }
+}
+
 // ---------------------------------------------------------------- launches
-// Blocks of 32 rows, and enough ranges to fill the compute units
 void plan8(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *range, int *splits) {
-  const int64_t slots = std::max(1, device_cus()), blocks = std::max<int64_t>(1, attn_blocks(32, c));
-  const int64_t want = std::max<int64_t>(1, slots / blocks);
-  const int64_t keys = std::max<int64_t>(256, (c.cap + want - 1) / want);
-  *rpb = 32;
-  *range = (int)((keys + 63) / 64 * 64);
-  *splits = std::max(1, (c.cap + *range - 1) / *range);
+  const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
+  // Of several sequences not all ranges that the bounds allow for are there: of few rows each two thirds; else
+  // the fewer the less the chunks fill their bound (unlike chunks going with unlike lengths)
+  const bool few = dtype == 0 || m <= 32 || (m <= 64 && (c.hd == 64 || (int64_t)c.batch * c.kvh * c.cap < 100000));
+  const int64_t cus = std::max(1, device_cus()), most = std::max<int64_t>(1, (int64_t)c.batch * c.max_q);
+  const int64_t slots = c.batch == 1 ? cus : few ? cus * 3 / 2 : cus + cus * 7 / 10 * (most - std::min<int64_t>(most, c.rows)) / most;
+  auto set = [&](int r, int64_t keys) {
+    *rpb = r;
+    const int64_t step = r == 128 && c.hd == 64 ? 128 : 64;   // keys that a block works on at a time
+    *range = (int)((std::max<int64_t>(keys, 64) + step - 1) / step * step);
+    *splits = std::max(1, (c.cap + *range - 1) / *range);
+  };
+  if (few) {
+    const int r = dtype == 1 && m <= 16 ? 16 : 32;
+    const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
+    const int64_t want = std::max<int64_t>(1, slots / blocks);
+    const int64_t least = r == 16 ? 65536 / c.hd : dtype == 1 || c.cap <= 256 ? 256 : 128;
+    set(r, std::max(least, (c.cap + want - 1) / want));
+  } else {
+    const int64_t tiles = (c.cap + 63) / 64;
+    double best = 0;
+    for (int r = 256; r >= 128; r -= 128) {
+      const double tile = c.hd == 128 ? (r == 256 ? 1.4 : 1.08) : (r == 256 ? 1.03 : 0.58);
+      const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
+      for (int64_t n = 1; n <= 32 && (n == 1 || tiles >= 4 * n); ++n) {
+        const double rounds = (double)((blocks * n + slots - 1) / slots);
+        double t = rounds * ((double)((tiles + n - 1) / n) * tile + 7.0);
+        if (n > 1) t += 5.0 + (double)attn_part_bytes(c, (int)n) * 2 / 4e6;
+        if (best == 0 || t < best) {
+          best = t;
+          set(r, (tiles + n - 1) / n * 64);
+        }
+      }
+    }
+  }
   while (*splits > 1 && attn_part_bytes(c, *splits) > scratch) {
     *range = (int)std::min<int64_t>((int64_t)*range * 2, 1 << 30);
     *splits = (c.cap + *range - 1) / *range;
   }
 }
 
-template <typename T>
-hipError_t launch_t(const CacheAttnArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)(attn_blocks(a.rpb, a.c) * a.splits));
-  if (a.c.hd == 128)
-    hipLaunchKernelGGL((k_cache8_attn_f32<T, 128>), grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((k_cache8_attn_f32<T, 64>), grid, dim3(256), 0, s, a);
+template <int HD, int RT>
+hipError_t launch_few8(const CacheAttnArgs &a, hipStream_t s) {
+  constexpr int LDS = 4 * 64 * RT * HD;
+  static DeviceOnce once;
+  const hipError_t lim = once_on_device(once, [] {
+    return hipFuncSetAttribute((const void *)k_cache8_attn_few<HD, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  });
+  if (lim != hipSuccess) return lim;
+  hipLaunchKernelGGL((k_cache8_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), LDS, s, a);
+  return hipGetLastError();
+}
+template <int HD, bool SMALL, int W, int KG>
+hipError_t launch_many8(const CacheAttnArgs &a, hipStream_t s) {
+  constexpr int LDS = KG * (KV * HD * (2 * (KS + VS) + 2 * RS) + ES * EB);
+  static DeviceOnce once;
+  const hipError_t lim = once_on_device(once, [] {
+    return hipFuncSetAttribute((const void *)k_cache8_attn_many<HD, SMALL, W, KG>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  });
+  if (lim != hipSuccess) return lim;
+  hipLaunchKernelGGL((k_cache8_attn_many<HD, SMALL, W, KG>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(64 * W), LDS, s, a);
+  return hipGetLastError();
+}
+template <int HD>
+hipError_t launch_hd(int dtype, const CacheAttnArgs &a, hipStream_t s) {
+  constexpr int W128 = HD == 64 ? 8 : 4, KG = HD == 64 ? 2 : 1;   // of blocks of 128 rows
+  const bool small = a.c.plog < 6;
+  if (dtype == 1 && a.rpb == 256) return small ? launch_many8<HD, true, 8, 1>(a, s) : launch_many8<HD, false, 8, 1>(a, s);
+  if (dtype == 1 && a.rpb == 128) return small ? launch_many8<HD, true, W128, KG>(a, s) : launch_many8<HD, false, W128, KG>(a, s);
+  if (dtype == 1) return a.rpb == 16 ? launch_few8<HD, 1>(a, s) : launch_few8<HD, 2>(a, s);
+  hipLaunchKernelGGL((k_cache8_attn_f32<HD>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 hipError_t launch_pass8(int dtype, const CacheAttnArgs &a, hipStream_t s) {
-  return dtype == 1 ? launch_t<bf16_t>(a, s) : launch_t<float>(a, s);
+  return a.c.hd == 128 ? launch_hd<128>(dtype, a, s) : launch_hd<64>(dtype, a, s);
 }
 
 }  // namespace

@@ -85,19 +85,19 @@ class Past:
 
 
 def attention64(s, frame, past=None):
-    """cache_util.attention64 over the state's k and v, the first keys of a group's sequences those of its first one and
-    seen by all of its rows."""
-    if past is None:
-        return cu.attention64(s, frame)
+    """As cache_util.attention64, over the state's k and v: o, lse, sum p |v| and the largest sum |q k| / sqrt(hd). With a
+    past the first keys of a group's sequences are those of its first one, and seen by all of its rows."""
     dev = s.k.device
     o = torch.zeros((s.rows, s.heads, s.hd), dtype=torch.float64, device=dev)
     lse = torch.full((s.rows, s.heads), -math.inf, dtype=torch.float64, device=dev)
     pv, qk = torch.zeros_like(o), torch.zeros_like(lse)
     grp, first = s.heads // s.kvh, 0
     for b, q in enumerate(s.q):
-        p = past.keys[b]
-        (lpg, lsl), (pg, sl) = cu.where(s, past.lead[b]), cu.where(s, b)
-        pg, sl = torch.cat([lpg[:p], pg[p:]]), torch.cat([lsl[:p], sl[p:]])
+        p = past.keys[b] if past else 0
+        pg, sl = cu.where(s, b)
+        if past:
+            lpg, lsl = cu.where(s, past.lead[b])
+            pg, sl = torch.cat([lpg[:p], pg[p:]]), torch.cat([lsl[:p], sl[p:]])
         lim = cu.limits(s, b, frame).clamp(min=p)
         hidden = torch.arange(len(pg), device=dev) >= lim[:, None]
         for h in range(s.heads if q and len(pg) else 0):
@@ -107,10 +107,12 @@ def attention64(s, frame, past=None):
             z = torch.logsumexp(sc, 1)
             w = torch.where(hidden, 0, torch.exp(sc - torch.where(z == -math.inf, 0, z)[:, None]))
             lse[first:first + q, h] = z
-            for r in torch.unique(lim).tolist():
-                rows = lim == r
-                o[first:first + q, h][rows] = w[rows, :r] @ v[:r]
-                pv[first:first + q, h][rows] = w[rows, :r] @ v[:r].abs()
+            # values of NaN count where they are seen, and only there
+            nan = torch.isnan(v)
+            bad = (~hidden).double() @ nan.double() > 0
+            v = torch.where(nan, 0, v)
+            o[first:first + q, h] = torch.where(bad, math.nan, w @ v)
+            pv[first:first + q, h] = w @ v.abs()
             qk[first:first + q, h] = (x.abs() @ k.abs().T / math.sqrt(s.hd)).masked_fill(hidden, 0).nan_to_num(0, 0, 0).amax(1)
         first += q
     return o, lse, pv, qk

@@ -227,7 +227,7 @@ def test_unseen_keys_have_no_influence(form, frame):
     s.k8.view(torch.uint8)[pg[-1], kvh - 1, sl[-1], 5] = 127
     c8.decode(s)
     wdc, ctx = ctx_of(s)
-    o, lse, pv, qk = cu.attention64(s, frame)
+    o, lse, pv, qk = c8.attention64(s, frame)
     bound, lse_bound = attention_bound(s, pv.nan_to_num(1e30, 1e30, 1e30), o.nan_to_num(0, 0, 0), qk, kv)
     out, z = torch.empty_like(s.x), torch.empty((s.rows, heads), device="cuda")
     ctx.cache8_attention(c8.cache8(wdc, s), cu.chunks(wdc, s), s.x, out, frame=frame, lse=z)
@@ -285,7 +285,7 @@ def test_an_odd_row_changes_no_other(form, odd):
     z = torch.empty((s.rows, heads), device="cuda")
     out = ctx.cache8_attention(c8.cache8(wdc, s), cu.chunks(wdc, s), s.x, torch.empty_like(s.x), frame=24, lse=z)
     s.x[1] = 0
-    o, lse, pv, qk = cu.attention64(s, 24)
+    o, lse, pv, qk = c8.attention64(s, 24)
     bound, lse_bound = attention_bound(s, pv, o, qk, kv)
     rest = torch.arange(s.rows, device="cuda") != 1
     within(out.reshape(o.shape)[rest], o[rest], bound[rest], "o")
@@ -387,7 +387,7 @@ def test_less_scratch_and_no_byte_behind_it(dtype, heads, kvh, hd, q, kv):
     s = c8.state8(dtype, heads, kvh, hd, 64, q, kv, seed=17)
     wdc, ctx = ctx_of(s)
     lib, cache, ch = wdc.load(), c8.cache8(wdc, s), cu.chunks(wdc, s)
-    o, lse, pv, qk = cu.attention64(s, 0)
+    o, lse, pv, qk = c8.attention64(s, 0)
     bound, _ = attention_bound(s, pv, o, qk, max(kv))
     need = lib.wdc_cache8_attention_scratch(ctx.h, cache.ref, ch.ref, None)
     assert need > 0
@@ -447,7 +447,7 @@ def test_rollout_of_chunks_append_attend_read(dtype, hd):
         at += m
         t = cu.SimpleNamespace(**vars(s))
         t.q, t.kv, t.rows, t.x = [m], [at], m, q
-        want, lse, pv, qk = cu.attention64(t, 16)
+        want, lse, pv, qk = c8.attention64(t, 16)
         bound, lse_bound = attention_bound(t, pv, want, qk, at)
         within(o.reshape(want.shape), want, bound, "o")
         within(z, lse, lse_bound + 4 * EPS32 * lse.abs(), "lse")
@@ -465,7 +465,7 @@ def test_rollout_captured_and_replayed(dtype, hd):
     want = []
     side.wait_stream(torch.cuda.current_stream())
     for x in rows:
-        want.append([[t.clone() for t in o] for o in rollout(ctx, wdc, s, x, pos, new(), sizes)])
+        want.append(rollout(ctx, wdc, s, x, pos, new(), sizes))
         side.synchronize()
     qkv, outs = s.qkv.clone(), new()
     torch.cuda.synchronize()
