@@ -510,6 +510,17 @@ __device__ __forceinline__ void lds_load4(u32x4_t buf, uint32_t lds, int voff) {
                : "memory", "m0");
 }
 
+// The lane's number, at hd 128 found anew, by instructions that are not moved out of a loop: a register kept for it, or for
+// what follows from it, would be spilled, and its reload in every step would wait for all loads under way (4,080 rows over
+// 67,320 keys: 2.03 ms, 1.92 with what the pipeline needs kept in registers and the rest found anew).
+template <int HD>
+__device__ __forceinline__ int lane_anew() {
+  if (HD == 64) return threadIdx.x & 63;
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+  return lane;
+}
+
 // Loads of one wave (of four): stripe i of a tile is rows [(4 i + w) RPL, + RPL). SMALL:
 // pages of 16 or 32 slots, where every stripe has its own page; otherwise a tile lies on one page.
 template <int HD, bool SMALL>
@@ -539,7 +550,7 @@ struct CodeLoads {
   }
   // where a tile lies, its page given (unless SMALL), and the load of its exponent bytes, 2 keys a lane
   __device__ __forceinline__ void find(const CacheArgs &c, int tile, int page, Where &x, uint32_t lds) {
-    const int pmask = (1 << c.plog) - 1, key0 = KV * tile, lane = threadIdx.x & 63;
+    const int pmask = (1 << c.plog) - 1, key0 = KV * tile, lane = lane_anew<HD>();
     if (SMALL) pw.advance(c, h, key0 >> c.plog);   // a tile's pages are of one group of 64
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
@@ -556,7 +567,7 @@ struct CodeLoads {
     lds_load4(buffer_at(c.scale, 0, (int)all), lds, (int)voff);
   }
   __device__ __forceinline__ void load(const void *pool, const Where &x, uint32_t lds) const {
-    const int lane = threadIdx.x & 63;
+    const int lane = lane_anew<HD>();
 #pragma unroll
     for (int i = 0; i < NS; ++i)
       lds_load16(buffer_at(pool, x.off[SMALL ? i : 0], x.bytes[SMALL ? i : 0]), lds + (4 * i + w) * 1024,
@@ -603,14 +614,12 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
 #pragma unroll
     for (int j = 0; j < NC; ++j) qf[t][j] = *(const bf16x8 *)(Q + 32 * j);
   }
-  int kro[NC];                                   // K fragment of rows lr, dims 32 c + 8 lg
-#pragma unroll
-  for (int j = 0; j < NC; ++j) kro[j] = lr * F::ROWB + ((4 * j + lg) ^ F::kkey(lr)) * 16;
-  int vro[F::VR];                                // transposed V read of rows 4 lg .. + 3, dims 16 i ..
+  // LDS offsets of the K fragment of rows lr, dims 8 lg .. (dims 32 j on: kro ^ 64 j), and of the transposed V read of rows
+  // 4 lg .. + 3, dims 0 .. (dims 16 i on, i < VR: vro ^ 32 i). At hd 128 the others are made where they are needed.
+  int kro = lr * F::ROWB + (lg ^ F::kkey(lr)) * 16, vro;
   {
     const int r = 4 * lg + (lr >> 2), j = lane & 3;
-#pragma unroll
-    for (int i = 0; i < F::VR; ++i) vro[i] = V_BASE + r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
+    vro = V_BASE + r * F::ROWB + ((j >> 1) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
   char *ring = smem + kg * RING;
   const uint32_t lds0 = lds_addr(ring);
@@ -631,26 +640,33 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   constexpr bool BOTH = WR <= PIECES;
   constexpr int NCV = BOTH ? PIECES / WR : 1;
   const bool conv_k = BOTH || wr < PIECES, conv_v = BOTH || wr >= PIECES;
-  const int piece = BOTH ? wr : wr % PIECES, crow = piece * TL::RPL + lane / (HD / 16), cch = lane % (HD / 16);
-  const int kwo = crow * F::ROWB + ((2 * cch) ^ F::kkey(crow)) * 16, vwo = crow * F::ROWB + ((2 * cch) ^ F::vkey(crow)) * 16;
+  const int piece = BOTH ? wr : wr % PIECES;
+  // A lane's two chunks go out one after the other, in the rows whose bit is set the upper one first: with V's swizzle
+  // (even) half of the banks would be idle in each.
+  auto upper_of = [](int row) { return HD == 128 ? row & 1 : (row >> 1) & 1; };
+  const int prow = piece * TL::RPL + lane / (HD / 16), pch = 2 * (lane % (HD / 16));
+  const int to_k = prow * F::ROWB + (pch ^ F::kkey(prow)) * 16, to_v = prow * F::ROWB + ((pch + upper_of(prow)) ^ F::vkey(prow)) * 16;
+  int to2 = to_k | to_v << 16;                   // where the first chunk goes in a tile of K, and of V
   u32x4_t raw[NCV];
   float up[NCV];
   // (the rows of a wave's pieces differ by a multiple of 16 or of 32, which the swizzles do not see)
   static_assert(NCV == 1 || WR * (1024 / HD) % 16 == 0, "rows of a wave's pieces");
   auto take = [&](const char *codes, const char *bytes, int which) __attribute__((always_inline)) {
+    const int ln = lane_anew<HD>(), row = ln / (HD / 16), up8 = which ? 8 * upper_of(row) : 0;   // (a piece starts at an even row pair)
 #pragma unroll
     for (int i = 0; i < NCV; ++i) {
-      raw[i] = *(const u32x4_t *)(codes + (piece + i * WR) * 1024 + 16 * lane);
+      const char *p = codes + (piece + i * WR) * 1024 + 16 * ln;
+      const u32x2_t x = *(const u32x2_t *)(p + up8), y = *(const u32x2_t *)(p + (up8 ^ 8));
+      raw[i] = u32x4_t{x[0], x[1], y[0], y[1]};
       // (past the end any byte may follow an odd key: 255 would make the zeros there NaN)
-      up[i] = power(min((uint32_t)*(const uint8_t *)(bytes + 2 * (crow + i * WR * TL::RPL) + which), 254u));
+      up[i] = power(min((uint32_t)*(const uint8_t *)(bytes + 2 * (row + (piece + i * WR) * TL::RPL) + which), 254u));
     }
   };
-  auto put = [&](char *to, int at) __attribute__((always_inline)) {
+  auto put = [&](char *to, int which, int half) __attribute__((always_inline)) {
+    const int at = (HD == 64 ? (which ? to_v : to_k) : which ? (uint32_t)to2 >> 16 : to2 & 0xffff) ^ (16 * half);
 #pragma unroll
-    for (int i = 0; i < NCV; ++i) {
-      *(bf16x8 *)(to + at + i * WR * TL::RPL * F::ROWB) = bf16_values8(raw[i][0], raw[i][1], up[i]);
-      *(bf16x8 *)(to + (at ^ 16) + i * WR * TL::RPL * F::ROWB) = bf16_values8(raw[i][2], raw[i][3], up[i]);
-    }
+    for (int i = 0; i < NCV; ++i)
+      *(bf16x8 *)(to + at + i * WR * TL::RPL * F::ROWB) = bf16_values8(raw[i][2 * half], raw[i][2 * half + 1], up[i]);
   };
   auto raw_k = [&](int slot) { return ring + RK_BASE + slot * RB; };
   auto raw_v = [&](int slot) { return ring + RV_BASE + slot * RB; };
@@ -660,11 +676,13 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
     bool odd = false;
     if (k && conv_k) {
       take(raw_k(t % RS), bytes_of(t), 0);
-      put(ring + (t % KS) * TB, kwo);
+      put(ring + (t % KS) * TB, 0, 0);
+      put(ring + (t % KS) * TB, 0, 1);
     }
     if (v && conv_v) {
       take(raw_v(t % RS), bytes_of(t), 1);
-      put(ring + V_BASE + (t % VS) * TB, vwo);
+      put(ring + V_BASE + (t % VS) * TB, 1, 0);
+      put(ring + V_BASE + (t % VS) * TB, 1, 1);
 #pragma unroll
       for (int i = 0; i < NCV; ++i)
 #pragma unroll
@@ -700,14 +718,14 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
     for (int j = 0; j < NC; ++j)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const bf16x8 kf = *(const bf16x8 *)(kb + kro[j] + k * 16 * F::ROWB);
+        const bf16x8 kf = *(const bf16x8 *)(kb + (kro ^ 64 * j) + k * 16 * F::ROWB);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           S[k][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][j], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[k][t], 0, 0, 0);
       }
   };
   auto vfrag = [&](const char *vb, int i, int p) {   // V^T fragment: dims 16 i .., keys of the 32-key group p
-    return v_frag<HD>(vb + vro[i % F::VR] + i / F::VR * F::VR * 32 + p * 32 * F::ROWB);
+    return v_frag<HD>(vb + (vro ^ 32 * (i % F::VR)) + i / F::VR * F::VR * 32 + p * 32 * F::ROWB);
   };
 
   if (nf > 0) {
@@ -749,7 +767,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
       if (r < NPV)
         fr_[r] = vfrag(vb, r % NI, (r < NPV ? r : 0) / NI);
       else
-        fr_[r] = *(const bf16x8 *)(kb + kro[g / 4] + (g % 4) * 16 * F::ROWB);
+        fr_[r] = *(const bf16x8 *)(kb + (kro ^ 64 * (g / 4)) + (g % 4) * 16 * F::ROWB);
     };
 #pragma unroll
     for (int r = 0; r < 4; ++r) read(r, ring, ring);
@@ -772,6 +790,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
       }
       __builtin_amdgcn_sched_barrier(0);
       const char *vb = ring + P * TB, *kb = ring + (P % KS) * TB, *vn = ring + ((P + 1) % VS) * TB;
+      if (HD == 128) asm volatile("" : "+v"(kro), "+v"(vro), "+v"(to2));
       float ls[2] = {0.f, 0.f}, ex[2];
       auto mma = [&](int q, int t_) __attribute__((always_inline)) {
         if (q < NPV) {
@@ -819,13 +838,18 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
           __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (BOTH) {
+          char *kt = ring + ((P + 3) % KS) * TB, *vt = ring + V_BASE + ((P + 2) % VS) * TB;
           if (q == 0) take(raw_k(rs), bytes_of(P + 3), 0);
-          if (q == NMF / 4) put(ring + ((P + 3) % KS) * TB, kwo);
+          if (q == NMF / 4 - 2) put(kt, 0, 0);
+          if (q == NMF / 4 + 2) put(kt, 0, 1);
           if (q == NMF / 2) take(raw_v(r2), bytes_of(P + 2), 1);
-          if (q == NMF * 3 / 4) put(ring + V_BASE + ((P + 2) % VS) * TB, vwo);
+          if (q == NMF * 3 / 4 - 2) put(vt, 1, 0);
+          if (q == NMF * 3 / 4 + 2) put(vt, 1, 1);
         } else {
+          char *to = ring + (conv_k ? ((P + 3) % KS) * TB : V_BASE + ((P + 2) % VS) * TB);
           if (q == 0) take(conv_k ? raw_k(rs) : raw_v(r2), conv_k ? bytes_of(P + 3) : bytes_of(P + 2), conv_k ? 0 : 1);
-          if (q == NMF / 2) put(ring + (conv_k ? ((P + 3) % KS) * TB : V_BASE + ((P + 2) % VS) * TB), conv_k ? kwo : vwo);
+          if (q == NMF / 2) put(to, conv_k ? 0 : 1, 0);
+          if (q == NMF / 2 + 4) put(to, conv_k ? 0 : 1, 1);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
