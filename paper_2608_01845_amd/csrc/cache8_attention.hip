@@ -575,7 +575,7 @@ struct CodeLoads {
   }
 };
 
-template <int HD, bool SMALL, int W, int KG>
+template <int HD, bool SMALL, int W, int KG, int KH>
 __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArgs a) {
   using F = Few<HD>;
   using TL = CodeLoads<HD, SMALL>;
@@ -595,8 +595,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  constexpr int WR = W / KG;                     // waves over the block's rows
-  const int wr = wid % WR, kg = wid / WR;
+  static_assert(KG == 1 || KH == 1, "keys are shared out in one way");
+  constexpr int WG = W / KG, WR = WG / KH;       // waves over a ring; over the block's rows
+  constexpr int KK = 4 / KH;                     // tiles of 16 keys of a wave
+  const int wr = wid % WR, kg = KG == 1 ? 0 : wid / WR, kh = KH == 1 ? 0 : wid / WR, cw = wid % WG;
   const bool grp_a = KG == 2 || wid < 4;         // loads tiles
   const int mlast = min(m0 + 32 * WR, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KG * KV - 1) / (KG * KV);   // in steps of KG tiles
@@ -616,10 +618,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   }
   // LDS offsets of the K fragment of rows lr, dims 8 lg .. (dims 32 j on: kro ^ 64 j), and of the transposed V read of rows
   // 4 lg .. + 3, dims 0 .. (dims 16 i on, i < VR: vro ^ 32 i). At hd 128 the others are made where they are needed.
-  int kro = lr * F::ROWB + (lg ^ F::kkey(lr)) * 16, vro;
+  int kro = kh * 16 * KK * F::ROWB + lr * F::ROWB + (lg ^ F::kkey(lr)) * 16, vro;
   {
     const int r = 4 * lg + (lr >> 2), j = lane & 3;
-    vro = V_BASE + r * F::ROWB + ((j >> 1) ^ F::vkey(r)) * 16 + 8 * (j & 1);
+    vro = V_BASE + kh * 16 * KK * F::ROWB + r * F::ROWB + ((j >> 1) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
   char *ring = smem + kg * RING;
   const uint32_t lds0 = lds_addr(ring);
@@ -637,10 +639,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   // Conversion: 16 codes of a row a lane. NCV pieces of 1,024 codes for each wave of both K and V, or (BOTH false) one of K
   // for the first half of the waves and one of V for the others.
   constexpr int PIECES = RB / 1024;
-  constexpr bool BOTH = WR <= PIECES;
-  constexpr int NCV = BOTH ? PIECES / WR : 1;
-  const bool conv_k = BOTH || wr < PIECES, conv_v = BOTH || wr >= PIECES;
-  const int piece = BOTH ? wr : wr % PIECES;
+  constexpr bool BOTH = WG <= PIECES;
+  constexpr int NCV = BOTH ? PIECES / WG : 1;
+  const bool conv_k = BOTH || cw < PIECES, conv_v = BOTH || cw >= PIECES;
+  const int piece = BOTH ? cw : cw % PIECES;
   // A lane's two chunks go out one after the other, in the rows whose bit is set the upper one first: with V's swizzle
   // (even) half of the banks would be idle in each.
   auto upper_of = [](int row) { return HD == 128 ? row & 1 : (row >> 1) & 1; };
@@ -650,23 +652,23 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   u32x4_t raw[NCV];
   float up[NCV];
   // (the rows of a wave's pieces differ by a multiple of 16 or of 32, which the swizzles do not see)
-  static_assert(NCV == 1 || WR * (1024 / HD) % 16 == 0, "rows of a wave's pieces");
+  static_assert(NCV == 1 || WG * (1024 / HD) % 16 == 0, "rows of a wave's pieces");
   auto take = [&](const char *codes, const char *bytes, int which) __attribute__((always_inline)) {
     const int ln = lane_anew<HD>(), row = ln / (HD / 16), up8 = which ? 8 * upper_of(row) : 0;   // (a piece starts at an even row pair)
 #pragma unroll
     for (int i = 0; i < NCV; ++i) {
-      const char *p = codes + (piece + i * WR) * 1024 + 16 * ln;
+      const char *p = codes + (piece + i * WG) * 1024 + 16 * ln;
       const u32x2_t x = *(const u32x2_t *)(p + up8), y = *(const u32x2_t *)(p + (up8 ^ 8));
       raw[i] = u32x4_t{x[0], x[1], y[0], y[1]};
       // (past the end any byte may follow an odd key: 255 would make the zeros there NaN)
-      up[i] = power(min((uint32_t)*(const uint8_t *)(bytes + 2 * (row + (piece + i * WR) * TL::RPL) + which), 254u));
+      up[i] = power(min((uint32_t)*(const uint8_t *)(bytes + 2 * (row + (piece + i * WG) * TL::RPL) + which), 254u));
     }
   };
   auto put = [&](char *to, int which, int half) __attribute__((always_inline)) {
     const int at = (HD == 64 ? (which ? to_v : to_k) : which ? (uint32_t)to2 >> 16 : to2 & 0xffff) ^ (16 * half);
 #pragma unroll
     for (int i = 0; i < NCV; ++i)
-      *(bf16x8 *)(to + at + i * WR * TL::RPL * F::ROWB) = bf16_values8(raw[i][2 * half], raw[i][2 * half + 1], up[i]);
+      *(bf16x8 *)(to + at + i * WG * TL::RPL * F::ROWB) = bf16_values8(raw[i][2 * half], raw[i][2 * half + 1], up[i]);
   };
   auto raw_k = [&](int slot) { return ring + RK_BASE + slot * RB; };
   auto raw_v = [&](int slot) { return ring + RV_BASE + slot * RB; };
@@ -713,11 +715,11 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
     for (int t = 0; t < 2; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
-  auto qk = [&](f32x4 (&S)[4][2], const char *kb) {
+  auto qk = [&](f32x4 (&S)[KK][2], const char *kb) {
 #pragma unroll
     for (int j = 0; j < NC; ++j)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < KK; ++k) {
         const bf16x8 kf = *(const bf16x8 *)(kb + (kro ^ 64 * j) + k * 16 * F::ROWB);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -729,8 +731,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   };
 
   if (nf > 0) {
-    f32x4 S[2][4][2];                            // S of tiles t + 1 and t + 2 (index tile & 1)
-    bf16x8 pf[2][2][2];                          // P of tiles t and t + 1 (index tile & 1), [row tile][32-key group]
+    f32x4 S[2][KK][2];                           // S of tiles t + 1 and t + 2 (index tile & 1)
+    bf16x8 pf[2][2][KK / 2];                        // P of tiles t and t + 1 (index tile & 1), [row tile][32-key group]
     convert(0, true, true);
     convert(1, true, true);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -756,8 +758,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
     convert(2, true, false);                     // into the slot of K_0
     if (grp_a) wait_vm<0>();                     // K_3
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    constexpr int NMF = 2 * NI + 4 * NC;         // fragment reads per step, two MFMAs each
-    constexpr int NPV = NMF / 2, EPM = 32 / NMF; // P V reads; exponentials per pair of MFMAs
+    constexpr int NPV = KK / 2 * NI, NMF = NPV + KK * NC;   // fragment reads of P V, and of a step; two MFMAs each
+    constexpr int EPM = 8 * KK / NMF;            // exponentials per pair of MFMAs
     static_assert(NMF == 16 || NMF == 32, "hd 64 or 128");
     bf16x8 fr_[NMF];
     // One step, P = t % 4 at compile time, as in the kernel over bf16; the conversions lie in the stream: K's codes are
@@ -767,7 +769,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
       if (r < NPV)
         fr_[r] = vfrag(vb, r % NI, (r < NPV ? r : 0) / NI);
       else
-        fr_[r] = *(const bf16x8 *)(kb + (kro ^ 64 * (g / 4)) + (g % 4) * 16 * F::ROWB);
+        fr_[r] = *(const bf16x8 *)(kb + (kro ^ 64 * (g / KK)) + (g % KK) * 16 * F::ROWB);
     };
 #pragma unroll
     for (int r = 0; r < 4; ++r) read(r, ring, ring);
@@ -797,8 +799,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
           o[q % NI][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], pf[n][t_][(q < NPV ? q : 0) / NI], o[q % NI][t_], 0, 0, 0);
         } else {
           const int g = q >= NPV ? q - NPV : 0;
-          S[n][g % 4][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], qf[t_][g / 4],
-                                                                    g < 4 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[n][g % 4][t_], 0, 0, 0);
+          S[n][g % KK][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], qf[t_][g / KK],
+                                                                     g < KK ? f32x4{0.f, 0.f, 0.f, 0.f} : S[n][g % KK][t_], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
       };
@@ -926,17 +928,17 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
       load_v(u % RS, wk);
     }
     const bool odd = odd_tile[kg][u & 3];
-    if (lane == 0 && wr == 0) odd_tile[kg][(u + 2) & 3] = 0;
+    if (lane == 0 && cw == 0) odd_tile[kg][(u + 2) & 3] = 0;
     if (u + 1 < tot) masked_convert(u + 1);
     const char *kb = ring + (u % KS) * TB, *vb = ring + (u % VS) * TB;   // vro holds V_BASE
-    const int key0 = KV * (KG * (t_first + u) + kg);
-    f32x4 S[4][2];
-    bf16x8 pf[2][2];
+    const int key0 = KV * (KG * (t_first + u) + kg) + 16 * KK * kh;
+    f32x4 S[KK][2];
+    bf16x8 pf[2][KK / 2];
     qk(S, kb);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < KK; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (key0 + 16 * k + 4 * lg + e >= lim[t]) S[k][t][e] = -INFINITY;
@@ -953,7 +955,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
       l[t] += weights(S, pf[t], t, sc, m[t] == -INFINITY ? 0.f : m[t]);
     }
     if (odd) {
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < KK; ++k)
         for (int e = 0; e < 4; ++e)
           for (int g = 0; g < 4; ++g) {
             const int key = 16 * k + 4 * g + e;
@@ -961,7 +963,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
             for (int t = 0; t < 2; ++t) {
               float p = 0.f;                     // of key and row lr, held by lane group g
 #pragma unroll
-              for (int q = 0; q < 16; ++q)
+              for (int q = 0; q < 4 * KK; ++q)
                 if (q == 4 * k + e) p = (float)pf[t][q >> 3][q & 7];
               p = __shfl(p, 16 * g + lr, 64);
               if (key0 + key < lim[t])
@@ -970,13 +972,13 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
 #pragma unroll
                   for (int d = 0; d < 4; ++d) {
                     const int col = 16 * i + 4 * lg + d;
-                    o[i][t][d] += p * bf2f(*(const bf16_t *)(vb + V_BASE + key * F::ROWB + ((col >> 3) ^ F::vkey(key)) * 16 + (col & 7) * 2));
+                    o[i][t][d] += p * bf2f(*(const bf16_t *)(vb + V_BASE + (16 * KK * kh + key) * F::ROWB + ((col >> 3) ^ F::vkey(key)) * 16 + (col & 7) * 2));
                   }
             }
           }
     } else {
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+      for (int p = 0; p < KK / 2; ++p)
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           const bf16x8 vf = vfrag(vb, i, p);
@@ -986,11 +988,11 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
     }
   }
 
-  if constexpr (KG == 2) {                       // the two softmaxes of every row meet
+  if constexpr (KG * KH == 2) {                       // the two softmaxes of every row meet
     f32x4 *xo = (f32x4 *)smem + (wr * 2 * NI) * 64 + lane;
     float2 *xm = (float2 *)((f32x4 *)smem + WR * 2 * NI * 64) + wr * 128 + lane;
     __syncthreads();
-    if (kg == 1) {
+    if (kg + kh == 1) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -999,7 +1001,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
       }
     }
     __syncthreads();
-    if (kg == 1) return;
+    if (kg + kh == 1) return;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const float2 y = xm[64 * t];
@@ -1096,23 +1098,23 @@ hipError_t launch_few8(const CacheAttnArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((k_cache8_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
-template <int HD, bool SMALL, int W, int KG>
+template <int HD, bool SMALL, int W, int KG, int KH>
 hipError_t launch_many8(const CacheAttnArgs &a, hipStream_t s) {
   constexpr int LDS = KG * (KV * HD * (2 * (KS + VS) + 2 * RS) + ES * EB);
   static DeviceOnce once;
   const hipError_t lim = once_on_device(once, [] {
-    return hipFuncSetAttribute((const void *)k_cache8_attn_many<HD, SMALL, W, KG>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    return hipFuncSetAttribute((const void *)k_cache8_attn_many<HD, SMALL, W, KG, KH>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache8_attn_many<HD, SMALL, W, KG>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(64 * W), LDS, s, a);
+  hipLaunchKernelGGL((k_cache8_attn_many<HD, SMALL, W, KG, KH>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(64 * W), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD>
 hipError_t launch_hd(int dtype, const CacheAttnArgs &a, hipStream_t s) {
-  constexpr int W128 = HD == 64 ? 8 : 4, KG = HD == 64 ? 2 : 1;   // of blocks of 128 rows
+  constexpr int KG = HD == 64 ? 2 : 1, KH = HD == 64 ? 1 : 2;   // of blocks of 128 rows
   const bool small = a.c.plog < 6;
-  if (dtype == 1 && a.rpb == 256) return small ? launch_many8<HD, true, 8, 1>(a, s) : launch_many8<HD, false, 8, 1>(a, s);
-  if (dtype == 1 && a.rpb == 128) return small ? launch_many8<HD, true, W128, KG>(a, s) : launch_many8<HD, false, W128, KG>(a, s);
+  if (dtype == 1 && a.rpb == 256) return small ? launch_many8<HD, true, 8, 1, 1>(a, s) : launch_many8<HD, false, 8, 1, 1>(a, s);
+  if (dtype == 1 && a.rpb == 128) return small ? launch_many8<HD, true, 8, KG, KH>(a, s) : launch_many8<HD, false, 8, KG, KH>(a, s);
   if (dtype == 1) return a.rpb == 16 ? launch_few8<HD, 1>(a, s) : launch_few8<HD, 2>(a, s);
   hipLaunchKernelGGL((k_cache8_attn_f32<HD>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), 0, s, a);
   return hipGetLastError();

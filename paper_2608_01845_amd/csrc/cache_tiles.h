@@ -336,12 +336,12 @@ __device__ __forceinline__ int64_t slot_row(const CacheArgs &c, const int32_t *t
   return ((((int64_t)cache_page(c, tab[slot >> c.plog]) * c.kvh + h) << c.plog) + (slot & ((1 << c.plog) - 1))) * c.hd;
 }
 
-// ---------------------------------------------------------------- weights of 32 rows over 64 keys
-template <int HD>
-__device__ __forceinline__ float rowmax(const f32x4 (&S)[4][2], int t) {
+// ---------------------------------------------------------------- weights of 32 rows over KK tiles of 16 keys
+template <int HD, int KK>
+__device__ __forceinline__ float rowmax(const f32x4 (&S)[KK][2], int t) {
   float mx = S[0][t][0];
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int k = 0; k < KK; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e) mx = fmaxf(mx, S[k][t][e]);
   return quad_max(mx);
@@ -352,15 +352,16 @@ __device__ __forceinline__ bool far_out(float m) { return __any(fabsf(m) > 0x1p2
 
 // P of one row tile, its lane sums. Far out S sc is rounded like the reference before m is taken off (S is scaled in
 // place), so that the largest score has weight 1.
-__device__ __forceinline__ float weights(f32x4 (&S)[4][2], bf16x8 (&pf)[2], int t, float sc, float m) {
+template <int KK>
+__device__ __forceinline__ float weights(f32x4 (&S)[KK][2], bf16x8 (&pf)[KK / 2], int t, float sc, float m) {
   float ls = 0.f;
   if (far_out(m)) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) S[k][t] *= sc;
+    for (int k = 0; k < KK; ++k) S[k][t] *= sc;
     sc = 1.f;
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int k = 0; k < KK; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[k][t][e], sc, -m));
