@@ -1045,38 +1045,51 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
 }
 
 // ---------------------------------------------------------------- launches
+// Rows per block and key ranges from the host's bounds, as over bf16.
+//
+// Up to 32 rows, and float32: blocks of 16 or 32 rows and enough ranges to fill the compute units, of several sequences
+// (bf16) four times over, since they may be unlike (eight tokens over 1 to 32,768 keys, 32 heads on 8 of 128: 76 us with 1.5
+// times, 54.5 with 4; of 64: 58 and 35), twice where their blocks alone do (sixteen over 4,000 each, 16 heads of 64: 41 us in
+// one range, 34 in two or four, of 128: 56.5, 57.7 and 64). No range is shorter than
+// 256 keys (one token over 4,000 keys, 32 heads on 8 of 64: 17.6 us in 4 ranges, 13.2 in 16), in float32 beyond 256 keys than 128.
+//
+// More rows: blocks of 32, 128 or 256 rows and the number of ranges by estimate: rounds of blocks on the compute units, 7 us for
+// a block's start and end, a time per 64 keys (measured alone on a compute unit), then the second launch and the scratch written and
+// read. It is within 10% of what was measured for 200 to 1,024 rows over 2,000 to 40,000 keys (32 rows of 32 heads on 8 of 128 over
+// 40,000 keys: 44 us said and 46.5 measured; 1,024 rows over 8,192, 16 heads of 128: 83 and 82).
 void plan8(int dtype, const CacheArgs &c, size_t scratch, int *rpb, int *range, int *splits) {
   const int64_t m = (int64_t)c.max_q * (c.heads / c.kvh);
-  // Of several sequences not all ranges that the bounds allow for are there: of few rows each two thirds; else
-  // the fewer the less the chunks fill their bound (unlike chunks going with unlike lengths)
-  const bool few = dtype == 0 || m <= 32 || (m <= 64 && (c.hd == 64 || (int64_t)c.batch * c.kvh * c.cap < 100000));
-  const int64_t cus = std::max(1, device_cus()), most = std::max<int64_t>(1, (int64_t)c.batch * c.max_q);
-  const int64_t slots = c.batch == 1 ? cus : few ? cus * 3 / 2 : cus + cus * 7 / 10 * (most - std::min<int64_t>(most, c.rows)) / most;
+  const int64_t cus = std::max(1, device_cus());
   auto set = [&](int r, int64_t keys) {
     *rpb = r;
     const int64_t step = r == 128 && c.hd == 64 ? 128 : 64;   // keys that a block works on at a time
     *range = (int)((std::max<int64_t>(keys, 64) + step - 1) / step * step);
     *splits = std::max(1, (c.cap + *range - 1) / *range);
   };
-  if (few) {
+  if (dtype == 0 || m <= 32) {
     const int r = dtype == 1 && m <= 16 ? 16 : 32;
     const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
+    const int64_t slots = c.batch == 1 ? cus : dtype == 0 ? cus * 3 / 2 : blocks < cus ? 4 * cus : 2 * cus;
     const int64_t want = std::max<int64_t>(1, slots / blocks);
-    const int64_t least = r == 16 ? 65536 / c.hd : dtype == 1 || c.cap <= 256 ? 256 : 128;
-    set(r, std::max(least, (c.cap + want - 1) / want));
+    set(r, std::max<int64_t>(dtype == 1 || c.cap <= 256 ? 256 : 128, (c.cap + want - 1) / want));
   } else {
-    const int64_t tiles = (c.cap + 63) / 64;
+    // of several sequences not all ranges that the bounds allow for are there, the fewer the less the chunks fill their bound
+    const int64_t most = std::max<int64_t>(1, (int64_t)c.batch * c.max_q);
+    const int64_t slots = c.batch == 1 ? cus : cus + cus * 7 / 10 * (most - std::min<int64_t>(most, c.rows)) / most;
+    const int64_t tiles = std::max(1, (c.cap + 63) / 64);
+    const double part = (double)attn_part_bytes(c, 1) * 2 / 4e6;
     double best = 0;
-    for (int r = 256; r >= 128; r -= 128) {
-      const double tile = c.hd == 128 ? (r == 256 ? 1.4 : 1.08) : (r == 256 ? 1.03 : 0.58);
+    for (int r : {256, 128, 32}) {
+      const double tile = c.hd == 128 ? (r == 256 ? 1.69 : r == 128 ? 1.15 : 0.95) : (r == 256 ? 1.09 : r == 128 ? 0.67 : 0.71);
       const int64_t blocks = std::max<int64_t>(1, attn_blocks(r, c));
-      for (int64_t n = 1; n <= 32 && (n == 1 || tiles >= 4 * n); ++n) {
-        const double rounds = (double)((blocks * n + slots - 1) / slots);
-        double t = rounds * ((double)((tiles + n - 1) / n) * tile + 7.0);
-        if (n > 1) t += 5.0 + (double)attn_part_bytes(c, (int)n) * 2 / 4e6;
+      for (int64_t rounds = 0; rounds <= 4; ++rounds) {   // 0: not split; else the most ranges that fit so many rounds
+        const int64_t most_n = std::max<int64_t>(1, std::min(rounds * slots / blocks, tiles / 4));
+        const int64_t each = (tiles + most_n - 1) / most_n, n = (tiles + each - 1) / each;
+        double t = (double)((blocks * n + slots - 1) / slots) * (each * tile + 7.0);
+        if (n > 1) t += 5.0 + part * n;
         if (best == 0 || t < best) {
           best = t;
-          set(r, (tiles + n - 1) / n * 64);
+          set(r, each * 64);
         }
       }
     }
@@ -1137,7 +1150,7 @@ hipError_t launch_cache8_attention(int dtype, const CacheAttnArgs &in, hipStream
   a.parts = a.splits;
   if (a.c.rows <= 0 || a.c.max_q <= 0) return hipSuccess;
   const hipError_t e = launch_pass8(dtype, a, s);
-  return e != hipSuccess || a.splits <= 1 ? e : launch_combine(dtype, a, s);
+  return e != hipSuccess || a.splits <= 1 ? e : launch_combine(dtype, a, few_rows_of_many_parts(a), s);
 }
 
 size_t cache8_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh) {

@@ -1318,7 +1318,7 @@ hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_
   a.parts = a.splits;
   if (a.c.rows <= 0 || a.c.max_q <= 0) return hipSuccess;
   const hipError_t e = launch_pass(dtype, a, s);
-  return e != hipSuccess || a.splits <= 1 ? e : launch_combine(dtype, a, s);
+  return e != hipSuccess || a.splits <= 1 ? e : launch_combine(dtype, a, false, s);
 }
 
 size_t cache_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh) {

@@ -305,6 +305,72 @@ __global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
     a.lse[(int64_t)(s.q0 + i) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
 }
 
+// The same for few rows of many parts: a block for each row and head, whose groups of HD / 4 threads take every
+// 1024 / HD-th part each and meet in LDS. (32 rows of 32 heads of 128, 33 parts: 9.7 us with a thread for all of them, X so.)
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_cache_attn_combine_few(CacheAttnArgs a) {
+  constexpr int TPR = HD / 4, G = 256 / TPR;
+  __shared__ f32x4 xs[G][TPR];
+  __shared__ float2 mls[G];
+  const CacheArgs &c = a.c;
+  const int group = c.heads / c.kvh, b = blockIdx.y, q = blockIdx.x;   // q: chunk row x heads + head
+  const int e = 4 * (int)(threadIdx.x % TPR), g = threadIdx.x / TPR;
+  const AttnSeq as = attn_seq(a, b);
+  const CacheSeq s = as.s;
+  if (q >= s.nq * c.heads) return;
+  const int i = q / c.heads, head = q - i * c.heads, h = head / group, mr = i * group + head - h * group;
+  const int last = min(mr / a.rpb * a.rpb + a.rpb, s.nq * group) - 1;   // of the row's block
+  const int own = range_count(a, cache_limit(c, s, cache_row(c, last)));
+  if (own == 1 && !as.joined) return;            // finished by its block
+  const int past = !as.joined ? 0 : a.past_splits > 1 ? ((as.skip << c.plog) + a.past_range - 1) / a.past_range : 1;
+  const int nr = past + own, gap = a.part0 - past;
+  const int64_t at0 = part_slot(a, 0, s.q0 + i, head), step = (int64_t)c.rows * c.heads;
+  float mx = -INFINITY, den = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  auto join = [&](float2 ml, f32x4 y) __attribute__((always_inline)) {
+    const float mn = fmaxf(mx, ml.x), ref = mn == -INFINITY ? 0.f : mn;
+    const float wo = __builtin_amdgcn_exp2f(mx - ref), wn = __builtin_amdgcn_exp2f(ml.x - ref);
+    mx = mn;
+    den = wo * den + wn * ml.y;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) x[d] = wo * x[d] + wn * y[d];
+  };
+  for (int u0 = g; u0 < nr; u0 += 4 * G) {       // four ranges' loads at a time
+    float2 ml[4];
+    f32x4 y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int p = u0 + u * G;
+      if (p < nr) {
+        const int64_t at = at0 + (p + (p < past ? 0 : gap)) * step;
+        ml[u] = *(const float2 *)part_ml(a, at);
+        y[u] = *(const f32x4 *)(a.part + at * HD + e);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (u0 + u * G < nr) join(ml[u], y[u]);
+  }
+  xs[g][e / 4] = x;
+  if (e == 0) mls[g] = make_float2(mx, den);
+  __syncthreads();
+  if (g > 0) return;
+#pragma unroll
+  for (int u = 1; u < G; ++u) join(mls[u], xs[u][e / 4]);
+  T *O = (T *)a.o + (int64_t)(s.q0 + i) * a.ldo + (int64_t)head * HD + e;
+  if constexpr (sizeof(T) == 2) {
+    bf16x4 y;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) y[d] = (__bf16)(den == 0.f ? 0.f : x[d] / den);
+    *(bf16x4 *)O = y;
+  } else {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) O[d] = den == 0.f ? 0.f : x[d] / den;
+  }
+  if (a.lse && e == 0)
+    a.lse[(int64_t)(s.q0 + i) * c.heads + head] = den == 0.f ? -INFINITY : (mx + log2f(den)) * LN2;
+}
+
 // ---------------------------------------------------------------- tiles
 __device__ __forceinline__ float unround(float sum, float rounded) { return rounded == 0.f ? 1.f : sum / rounded; }
 
@@ -381,21 +447,22 @@ inline size_t attn_part_bytes(const CacheArgs &c, int splits) {
   return (size_t)splits * c.rows * c.heads * (c.hd + 2) * sizeof(float);
 }
 
-inline hipError_t launch_combine(int dtype, const CacheAttnArgs &a, hipStream_t s) {
-  const int64_t items = (int64_t)a.c.max_q * a.c.heads * (a.c.hd / 4);
-  const dim3 grid((unsigned)((items + 255) / 256), a.c.seqs);
-  if (dtype == 1) {
-    if (a.c.hd == 128)
-      hipLaunchKernelGGL((k_cache_attn_combine<bf16_t, 128>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_cache_attn_combine<bf16_t, 64>), grid, dim3(256), 0, s, a);
-  } else {
-    if (a.c.hd == 128)
-      hipLaunchKernelGGL((k_cache_attn_combine<float, 128>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_cache_attn_combine<float, 64>), grid, dim3(256), 0, s, a);
-  }
+template <typename T, int HD>
+hipError_t launch_combine_t(const CacheAttnArgs &a, bool few, hipStream_t s) {
+  const int64_t items = (int64_t)a.c.max_q * a.c.heads;
+  if (few)
+    hipLaunchKernelGGL((k_cache_attn_combine_few<T, HD>), dim3((unsigned)items, a.c.seqs), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_cache_attn_combine<T, HD>), dim3((unsigned)((items * (HD / 4) + 255) / 256), a.c.seqs), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+// few: where parts are many and their rows do not fill the device
+inline hipError_t launch_combine(int dtype, const CacheAttnArgs &a, bool few, hipStream_t s) {
+  if (dtype == 1) return a.c.hd == 128 ? launch_combine_t<bf16_t, 128>(a, few, s) : launch_combine_t<bf16_t, 64>(a, few, s);
+  return a.c.hd == 128 ? launch_combine_t<float, 128>(a, few, s) : launch_combine_t<float, 64>(a, few, s);
+}
+inline bool few_rows_of_many_parts(const CacheAttnArgs &a) {
+  return a.parts > 8 && (int64_t)a.c.max_q * a.c.seqs * a.c.heads <= 4096;
 }
 
 // Attention over a past that groups of sequences share: a pass over the shared keys, in which the rows
@@ -443,7 +510,7 @@ hipError_t launch_shared(int dtype, const CacheAttnArgs &in, Plan &&plan, Launch
   a.range = p.range[1];
   a.splits = p.splits[1];
   e = launch(dtype, a, s);
-  return e != hipSuccess ? e : launch_combine(dtype, a, s);
+  return e != hipSuccess ? e : launch_combine(dtype, a, few_rows_of_many_parts(a), s);
 }
 
 }  // namespace
