@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
   const int mlast = min(m0 + 32, count) - 1, mm = min(m0 + lr, mlast), row = cache_row(c, mm);
   const int lim_lo = k_.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
   const int tiles = (k_.lim_hi + 31) / 32;
-  const int t0 = nr > 1 ? sp * (a.range / 32) : 0, t1 = nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
+  const int t0 = nr > 1 ? sp * (k_.range / 32) : 0, t1 = nr > 1 ? min(t0 + k_.range / 32, tiles) : tiles;
   const float *Q = (const float *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm - row * group) * HD + NC * lg;
   const uint8_t *K = (const uint8_t *)c.k + NC * lg, *V = (const uint8_t *)c.v + NI * lr;
   const float sc = LOG2E / sqrtf((float)HD);
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_few(CacheAttnArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mlast = min(m0 + 16 * RT, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KT - 1) / KT;
-  const int t0 = nr > 1 ? sp * (a.range / KT) : 0, t1 = nr > 1 ? min(t0 + a.range / KT, tiles) : tiles;
+  const int t0 = nr > 1 ? sp * (k_.range / KT) : 0, t1 = nr > 1 ? min(t0 + k_.range / KT, tiles) : tiles;
 
   const float sc = LOG2E / sqrtf((float)HD);
   bf16x8 qf[RT][NC];
@@ -602,7 +602,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   const bool grp_a = KG == 2 || wid < 4;         // loads tiles
   const int mlast = min(m0 + 32 * WR, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KG * KV - 1) / (KG * KV);   // in steps of KG tiles
-  const int range = a.range / (KG * KV), t_first = nr > 1 ? sp * range : 0, t_end = nr > 1 ? min(t_first + range, tiles) : tiles;
+  const int range = k_.range / (KG * KV), t_first = nr > 1 ? sp * range : 0, t_end = nr > 1 ? min(t_first + range, tiles) : tiles;
   // steps of the range, relative to t_first: `nf` that every row sees whole, then masked ones
   const int tot = t_end - t_first, nf = min(max(lim_lo / (KG * KV) - t_first, 0), tot);
   const int ahead = min(tot, nf + RS);           // codes that the pipeline asks for
@@ -1108,7 +1108,7 @@ hipError_t launch_few8(const CacheAttnArgs &a, hipStream_t s) {
     return hipFuncSetAttribute((const void *)k_cache8_attn_few<HD, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache8_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), LDS, s, a);
+  hipLaunchKernelGGL((k_cache8_attn_few<HD, RT>), dim3(a.blocks), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD, bool SMALL, int W, int KG, int KH>
@@ -1119,7 +1119,7 @@ hipError_t launch_many8(const CacheAttnArgs &a, hipStream_t s) {
     return hipFuncSetAttribute((const void *)k_cache8_attn_many<HD, SMALL, W, KG, KH>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache8_attn_many<HD, SMALL, W, KG, KH>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(64 * W), LDS, s, a);
+  hipLaunchKernelGGL((k_cache8_attn_many<HD, SMALL, W, KG, KH>), dim3(a.blocks), dim3(64 * W), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD>
@@ -1129,7 +1129,7 @@ hipError_t launch_hd(int dtype, const CacheAttnArgs &a, hipStream_t s) {
   if (dtype == 1 && a.rpb == 256) return small ? launch_many8<HD, true, 8, 1, 1>(a, s) : launch_many8<HD, false, 8, 1, 1>(a, s);
   if (dtype == 1 && a.rpb == 128) return small ? launch_many8<HD, true, 8, KG, KH>(a, s) : launch_many8<HD, false, 8, KG, KH>(a, s);
   if (dtype == 1) return a.rpb == 16 ? launch_few8<HD, 1>(a, s) : launch_few8<HD, 2>(a, s);
-  hipLaunchKernelGGL((k_cache8_attn_f32<HD>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_cache8_attn_f32<HD>), dim3(a.blocks), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 hipError_t launch_pass8(int dtype, const CacheAttnArgs &a, hipStream_t s) {
@@ -1147,18 +1147,25 @@ size_t cache8_attn_scratch(int dtype, const CacheArgs &c) {
 hipError_t launch_cache8_attention(int dtype, const CacheAttnArgs &in, hipStream_t s) {
   CacheAttnArgs a = in;
   plan8(dtype, a.c, a.part ? a.part_bytes : 0, &a.rpb, &a.range, &a.splits);
-  a.parts = a.splits;
+  a.blocks = attn_grid(a);
   if (a.c.rows <= 0 || a.c.max_q <= 0) return hipSuccess;
   const hipError_t e = launch_pass8(dtype, a, s);
   return e != hipSuccess || a.splits <= 1 ? e : launch_combine(dtype, a, few_rows_of_many_parts(a), s);
 }
 
+// us per 64 keys in blocks of 16, 32, 128 and 256 rows (alone on a compute unit)
+static SharedPlan shared_plan8(int dtype, const CacheArgs &c, const CacheShared &sh) {
+  static const double tile[4][4] = {{0, 1.0, 0, 0}, {0, 2.0, 0, 0}, {0.55, 0.71, 0.67, 1.09}, {0.72, 0.95, 1.15, 1.69}};
+  return plan_shared(dtype, c, sh, tile[2 * dtype + (c.hd == 128)]);
+}
+
 size_t cache8_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh) {
-  return shared_part_bytes(c, shared_passes(dtype, c, sh, plan8));
+  const SharedPlan p = shared_plan8(dtype, c, sh);
+  return attn_part_bytes(c, p.splits[0] + p.splits[1]);
 }
 
 hipError_t launch_cache8_attention_shared(int dtype, const CacheAttnArgs &in, hipStream_t s) {
-  return launch_shared(dtype, in, plan8, launch_pass8, s);
+  return launch_shared(dtype, in, shared_plan8(dtype, in.c, in.sh), launch_pass8, s);
 }
 
 }  // namespace wdc

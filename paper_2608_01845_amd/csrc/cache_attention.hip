@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mlast = min(m0 + 16 * RT, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KT - 1) / KT;
-  const int t0 = nr > 1 ? sp * (a.range / KT) : 0, t1 = nr > 1 ? min(t0 + a.range / KT, tiles) : tiles;
+  const int t0 = nr > 1 ? sp * (k_.range / KT) : 0, t1 = nr > 1 ? min(t0 + k_.range / KT, tiles) : tiles;
 
   const float sc = LOG2E / sqrtf((float)HD);
   bf16x8 qf[RT][NC];
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   const bool grp_a = KG == 2 || wid < 4;         // loads tiles
   const int mlast = min(m0 + 32 * WR, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KG * KV - 1) / (KG * KV);   // in steps of KG tiles
-  const int range = a.range / (KG * KV), t_first = nr > 1 ? sp * range : 0, t_end = nr > 1 ? min(t_first + range, tiles) : tiles;
+  const int range = k_.range / (KG * KV), t_first = nr > 1 ? sp * range : 0, t_end = nr > 1 ? min(t_first + range, tiles) : tiles;
   // steps of the range, relative to t_first: `nf` that every row sees whole, then masked ones
   const int tot = t_end - t_first, nf = min(max(lim_lo / (KG * KV) - t_first, 0), tot);
 
@@ -820,7 +820,7 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_f32(CacheAttnArgs a) {
   const int mlast = min(m0 + 32, count) - 1, mm = min(m0 + lr, mlast), row = cache_row(c, mm);
   const int lim_lo = k_.lim_lo, lim = m0 + lr < count ? cache_limit(c, s, row) : 0;
   const int tiles = (k_.lim_hi + 31) / 32;
-  const int t0 = nr > 1 ? sp * (a.range / 32) : 0, t1 = nr > 1 ? min(t0 + a.range / 32, tiles) : tiles;
+  const int t0 = nr > 1 ? sp * (k_.range / 32) : 0, t1 = nr > 1 ? min(t0 + k_.range / 32, tiles) : tiles;
   const float *Q = (const float *)a.q + (int64_t)(s.q0 + row) * a.ldq + (int64_t)(h * group + mm - row * group) * HD + 4 * lg;
   const float *K = (const float *)c.k + 4 * lg, *V = (const float *)c.v + NI * lr;
   const float sc = LOG2E / sqrtf((float)HD);
@@ -1271,7 +1271,7 @@ hipError_t launch_few(const CacheAttnArgs &a, hipStream_t s) {
     return hipFuncSetAttribute((const void *)k_cache_attn_few<HD, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache_attn_few<HD, RT>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(256), LDS, s, a);
+  hipLaunchKernelGGL((k_cache_attn_few<HD, RT>), dim3(a.blocks), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD, bool SMALL, int W, int KG>
@@ -1282,7 +1282,7 @@ hipError_t launch_many(const CacheAttnArgs &a, hipStream_t s) {
     return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL, W, KG>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL, W, KG>), dim3((unsigned)(attn_blocks(a.rpb, a.c) * a.splits)), dim3(64 * W), LDS, s, a);
+  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL, W, KG>), dim3(a.blocks), dim3(64 * W), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD>
@@ -1304,7 +1304,7 @@ size_t cache_attn_scratch(int dtype, const CacheArgs &c) {
 
 static hipError_t launch_pass(int dtype, const CacheAttnArgs &a, hipStream_t s) {
   if (dtype == 1) return a.c.hd == 128 ? launch_bf16<128>(a, s) : launch_bf16<64>(a, s);
-  const dim3 grid((unsigned)(attn_blocks(a.rpb, a.c) * a.splits));
+  const dim3 grid(a.blocks);
   if (a.c.hd == 128)
     hipLaunchKernelGGL((k_cache_attn_f32<128>), grid, dim3(256), 0, s, a);
   else
@@ -1315,18 +1315,25 @@ static hipError_t launch_pass(int dtype, const CacheAttnArgs &a, hipStream_t s) 
 hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_t s) {
   CacheAttnArgs a = in;
   attn_plan(dtype, a.c, a.part ? a.part_bytes : 0, &a.rpb, &a.range, &a.splits);
-  a.parts = a.splits;
+  a.blocks = attn_grid(a);
   if (a.c.rows <= 0 || a.c.max_q <= 0) return hipSuccess;
   const hipError_t e = launch_pass(dtype, a, s);
   return e != hipSuccess || a.splits <= 1 ? e : launch_combine(dtype, a, false, s);
 }
 
+// us per 64 keys in blocks of 16, 32, 128 and 256 rows (alone on a compute unit)
+static SharedPlan shared_plan(int dtype, const CacheArgs &c, const CacheShared &sh) {
+  static const double tile[4][4] = {{0, 1.0, 0, 0}, {0, 2.0, 0, 0}, {0.55, 0.71, 0.58, 1.03}, {0.72, 0.95, 1.08, 1.4}};
+  return plan_shared(dtype, c, sh, tile[2 * dtype + (c.hd == 128)]);
+}
+
 size_t cache_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh) {
-  return shared_part_bytes(c, shared_passes(dtype, c, sh, attn_plan));
+  const SharedPlan p = shared_plan(dtype, c, sh);
+  return attn_part_bytes(c, p.splits[0] + p.splits[1]);
 }
 
 hipError_t launch_cache_attention_shared(int dtype, const CacheAttnArgs &in, hipStream_t s) {
-  return launch_shared(dtype, in, attn_plan, launch_pass, s);
+  return launch_shared(dtype, in, shared_plan(dtype, in.c, in.sh), launch_pass, s);
 }
 
 static int64_t mass_blocks(int dtype, const CacheArgs &c) {

@@ -100,7 +100,7 @@ __device__ __forceinline__ CacheSeq uniform_seq(const CacheArgs &a, int b) {
 
 // Keys that the rows of group g share: whole pages of its first sequence (*lead)
 __device__ __forceinline__ int shared_keys(const CacheArgs &c, const CacheShared &sh, int g, int *lead) {
-  *lead = min(max(sh.group_start[g], 0), c.seqs - 1);
+  *lead = min(max(sh.group_start[g], 0), c.batch - 1);
   const int n = min(max(c.kv_len[*lead], 0), c.cap);
   return min(min(max(sh.prefix_len[g], 0), sh.max_prefix), n) >> c.plog << c.plog;
 }
@@ -117,54 +117,57 @@ __device__ __forceinline__ int shared_group(const CacheShared &sh, int b) {
   return lo < sh.groups && sh.group_start[lo] <= b ? lo : -1;
 }
 
-// Entry b of a launch's list of sequences, its row of the page table and what is left out at that row's
-// start. Passes over a shared past (CacheAttnArgs::pass): the groups' rows over the keys that they share, which all of them see,
-// then each sequence's rows over its own keys, slots counted from the first of them.
+// Entry of a launch's list: rows and keys, the row of the page table and the pages left out at its start. Where groups
+// share a past, their rows over the shared keys come first, all of them seen, then each sequence's rows over its own
+// keys, slots counted from the first of them.
 struct AttnSeq {
   CacheSeq s;
   int row, skip;   // table row, pages
-  bool joined;     // the rows have other parts as well
+  int shared;      // 0: all of the rows' keys, 1: those that their group shares, 2: the others
 };
-__device__ __forceinline__ AttnSeq attn_seq(const CacheAttnArgs &a, int b) {
+__device__ __forceinline__ AttnSeq shared_entry(const CacheAttnArgs &a, int g) {
   const CacheArgs &c = a.c;
   AttnSeq x;
-  x.row = b;
+  x.s.n = shared_keys(c, a.sh, g, &x.row);
+  const int b0 = min(max(a.sh.group_start[g], 0), c.batch), b1 = min(max(a.sh.group_start[g + 1], b0), c.batch);
+  x.s.q0 = min(max(c.q_start[b0], 0), c.rows);
+  x.s.nq = x.s.n > 0 ? min(max(c.q_start[b1], x.s.q0), c.rows) - x.s.q0 : 0;
+  x.s.start = x.s.n;                             // (cache_limit: every row sees all)
   x.skip = 0;
-  x.joined = a.pass == PASS_SHARED;
-  if (a.pass == PASS_SHARED) {
-    x.s.n = shared_keys(c, a.sh, b, &x.row);
-    const int b0 = min(max(a.sh.group_start[b], 0), c.seqs), b1 = min(max(a.sh.group_start[b + 1], b0), c.seqs);
-    x.s.q0 = min(max(c.q_start[b0], 0), c.rows);
-    x.s.nq = x.s.n > 0 ? min(max(c.q_start[b1], x.s.q0), c.rows) - x.s.q0 : 0;
-    x.s.start = 0;
-    return x;
-  }
-  x.s = cache_seq(c, b);
-  if (a.pass == PASS_OWN) {
+  x.shared = 1;
+  return x;
+}
+__device__ __forceinline__ AttnSeq own_entry(const CacheAttnArgs &a, int b) {
+  AttnSeq x;
+  x.s = cache_seq(a.c, b);
+  x.row = b;
+  x.skip = x.shared = 0;
+  if (a.sh.groups > 0) {
     const int g = shared_group(a.sh, b);
     int lead;
-    const int p = g < 0 ? 0 : shared_keys(c, a.sh, g, &lead), q = x.s.n - x.s.start;
+    const int p = g < 0 ? 0 : shared_keys(a.c, a.sh, g, &lead), q = x.s.n - x.s.start;
     x.s.n = min(max(x.s.n - p, 0), a.sh.max_own);
     x.s.start = x.s.n - q;
-    x.skip = p >> c.plog;
-    x.joined = p > 0;
+    x.skip = p >> a.c.plog;
+    x.shared = p > 0 ? 2 : 0;
   }
   return x;
 }
 
 // Ranges of keys that the rows of a block which see up to `keys` of them are cut
 // into, one block each (the first is always there: it writes zeros where nothing is seen)
-__device__ __forceinline__ int range_count(const CacheAttnArgs &a, int keys) {
-  return a.splits > 1 ? max(1, (keys + a.range - 1) / a.range) : 1;
+__device__ __forceinline__ int range_count(const CacheAttnArgs &a, int keys, bool past = false) {
+  const int range = past ? a.past_range : a.range;
+  return (past ? a.past_splits : a.splits) > 1 ? max(1, (keys + range - 1) / range) : 1;
 }
 
-// Part of range sp of packed row `row` and a head: HD unnormalised values at
+// Part sp (ranges of shared keys come first) of packed row `row` and a head: HD unnormalised values at
 // part + slot * HD, its reference and sum at part + slots * HD + 2 slot
 __device__ __forceinline__ int64_t part_slot(const CacheAttnArgs &a, int sp, int row, int head) {
   return ((int64_t)sp * a.c.rows + row) * a.c.heads + head;
 }
 __device__ __forceinline__ float *part_ml(const CacheAttnArgs &a, int64_t slot) {
-  return a.part + (int64_t)a.parts * a.c.rows * a.c.heads * a.c.hd + 2 * slot;
+  return a.part + (int64_t)(a.past_splits + a.splits) * a.c.rows * a.c.heads * a.c.hd + 2 * slot;
 }
 
 // What a block of an attention launch works on: query rows [m0, m0 + rpb) of
@@ -179,37 +182,36 @@ struct AttnBlock {
   const int32_t *tab;   // its pages, and the last one's number
   int tab_last;
   int h, m0, count, group, sp, nr;
+  int range;            // keys of a range
   int lim_lo, lim_hi;   // keys seen by the first and the last row
   int part;             // the range's number among the parts of its rows, -1: what the block computes is the result
   bool live;
   __device__ __forceinline__ explicit AttnBlock(const CacheAttnArgs &a) : live(false) {
     const CacheArgs &c = a.c;
-    int b = 0, skip = 0, row;
-    bool joined;
+    int row, skip = 0, shared = 0;
     const int lane = threadIdx.x & 63;
     group = c.heads / c.kvh;
     int li = blockIdx.x;
-    if (c.batch == 1 || (a.splits == 1 && c.max_q * group <= a.rpb)) {   // one sequence, or a block for each and kv head
+    if (a.sh.groups == 0 && (c.batch == 1 || (a.splits == 1 && c.max_q * group <= a.rpb))) {   // one sequence, or a block for each and kv head
+      row = 0;
       if (c.batch > 1) {
-        b = uni(li / c.kvh);
-        li -= b * c.kvh;
+        row = uni(li / c.kvh);
+        li -= row * c.kvh;
       }
-      const AttnSeq x = attn_seq(a, b);
-      s.q0 = uni(x.s.q0);
-      s.nq = uni(x.s.nq);
-      s.n = uni(x.s.n);
-      s.start = uni(x.s.start);
-      row = uni(x.row);
-      skip = uni(x.skip);
-      joined = uni(x.joined);
+      s = uniform_seq(c, row);
     } else {
       bool found = false;
-      for (int e0 = 0; e0 < c.batch && !found; e0 += 64) {
+      const int entries = a.sh.groups + c.batch;
+      for (int e0 = 0; e0 < entries && !found; e0 += 64) {
         int cnt = 0;
         AttnSeq x{};
-        if (e0 + lane < c.batch) {
-          x = attn_seq(a, e0 + lane);
-          cnt = (x.s.nq * group + a.rpb - 1) / a.rpb * range_count(a, x.s.n) * c.kvh;
+        const int e = e0 + lane;
+        if (e < entries) {
+          if (e < a.sh.groups)
+            x = shared_entry(a, e);
+          else
+            x = own_entry(a, e - a.sh.groups);
+          cnt = (x.s.nq * group + a.rpb - 1) / a.rpb * range_count(a, x.s.n, x.shared == 1) * c.kvh;
         }
         const int sum = wave_scan(cnt);
         const uint64_t past = __ballot(sum > li);
@@ -222,7 +224,7 @@ struct AttnBlock {
           s.start = __builtin_amdgcn_readlane(x.s.start, k);
           row = __builtin_amdgcn_readlane(x.row, k);
           skip = __builtin_amdgcn_readlane(x.skip, k);
-          joined = __builtin_amdgcn_readlane(x.joined, k);
+          shared = __builtin_amdgcn_readlane(x.shared, k);
           found = true;
         } else {
           li -= __builtin_amdgcn_readlane(sum, 63);
@@ -234,16 +236,18 @@ struct AttnBlock {
     skip = min(skip, c.table_ld - 1);            // (pages beyond the table hold no keys)
     tab = c.table + (int64_t)row * c.table_ld + skip;
     tab_last = c.table_ld - 1 - skip;
+    range = shared == 1 ? a.past_range : a.range;
     count = s.nq * group;
-    const int q = uni(li / c.kvh), nrg = range_count(a, s.n), back = uni(q / nrg), rb = (count + a.rpb - 1) / a.rpb - 1 - back;
+    const int q = uni(li / c.kvh), nrg = range_count(a, s.n, shared == 1), back = uni(q / nrg);
+    const int rb = (count + a.rpb - 1) / a.rpb - 1 - back;
     h = li - q * c.kvh;
     sp = q - back * nrg;
     m0 = rb * a.rpb;
     if (m0 < 0) return;
     lim_lo = uni(cache_limit(c, s, cache_row(c, m0)));
     lim_hi = uni(cache_limit(c, s, cache_row(c, min(m0 + a.rpb, count) - 1)));
-    nr = uni(range_count(a, lim_hi));
-    part = nr > 1 || joined ? a.part0 + sp : -1;
+    nr = uni(range_count(a, lim_hi, shared == 1));
+    part = nr > 1 || shared ? (shared == 1 ? sp : a.past_splits + sp) : -1;
     live = sp < nr;
   }
 };
@@ -258,15 +262,15 @@ __global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
   const int group = c.heads / c.kvh, b = blockIdx.y;
   const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int e = 4 * (int)(gid % TPR), q = (int)(gid / TPR);   // q: chunk row x heads + head
-  const AttnSeq as = attn_seq(a, b);
+  const AttnSeq as = own_entry(a, b);
   const CacheSeq s = as.s;
   if (q >= s.nq * c.heads) return;
   const int i = q / c.heads, head = q - i * c.heads, h = head / group, mr = i * group + head - h * group;
   const int last = min(mr / a.rpb * a.rpb + a.rpb, s.nq * group) - 1;   // of the row's block
   const int own = range_count(a, cache_limit(c, s, cache_row(c, last)));
-  if (own == 1 && !as.joined) return;            // finished by its block
-  const int past = !as.joined ? 0 : a.past_splits > 1 ? ((as.skip << c.plog) + a.past_range - 1) / a.past_range : 1;
-  const int nr = past + own, gap = a.part0 - past;   // part of range u: u, or u + gap of the own ones
+  if (own == 1 && !as.shared) return;            // finished by its block
+  const int past = as.shared ? range_count(a, as.skip << c.plog, true) : 0;
+  const int nr = past + own, gap = a.past_splits - past;   // part of range u: u, or u + gap of the own ones
   const int64_t at0 = part_slot(a, 0, s.q0 + i, head), step = (int64_t)c.rows * c.heads;
   float mx = -INFINITY, den = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -315,15 +319,15 @@ __global__ __launch_bounds__(256) void k_cache_attn_combine_few(CacheAttnArgs a)
   const CacheArgs &c = a.c;
   const int group = c.heads / c.kvh, b = blockIdx.y, q = blockIdx.x;   // q: chunk row x heads + head
   const int e = 4 * (int)(threadIdx.x % TPR), g = threadIdx.x / TPR;
-  const AttnSeq as = attn_seq(a, b);
+  const AttnSeq as = own_entry(a, b);
   const CacheSeq s = as.s;
   if (q >= s.nq * c.heads) return;
   const int i = q / c.heads, head = q - i * c.heads, h = head / group, mr = i * group + head - h * group;
   const int last = min(mr / a.rpb * a.rpb + a.rpb, s.nq * group) - 1;   // of the row's block
   const int own = range_count(a, cache_limit(c, s, cache_row(c, last)));
-  if (own == 1 && !as.joined) return;            // finished by its block
-  const int past = !as.joined ? 0 : a.past_splits > 1 ? ((as.skip << c.plog) + a.past_range - 1) / a.past_range : 1;
-  const int nr = past + own, gap = a.part0 - past;
+  if (own == 1 && !as.shared) return;            // finished by its block
+  const int past = as.shared ? range_count(a, as.skip << c.plog, true) : 0;
+  const int nr = past + own, gap = a.past_splits - past;
   const int64_t at0 = part_slot(a, 0, s.q0 + i, head), step = (int64_t)c.rows * c.heads;
   float mx = -INFINITY, den = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -451,9 +455,9 @@ template <typename T, int HD>
 hipError_t launch_combine_t(const CacheAttnArgs &a, bool few, hipStream_t s) {
   const int64_t items = (int64_t)a.c.max_q * a.c.heads;
   if (few)
-    hipLaunchKernelGGL((k_cache_attn_combine_few<T, HD>), dim3((unsigned)items, a.c.seqs), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_cache_attn_combine_few<T, HD>), dim3((unsigned)items, a.c.batch), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_cache_attn_combine<T, HD>), dim3((unsigned)((items * (HD / 4) + 255) / 256), a.c.seqs), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_cache_attn_combine<T, HD>), dim3((unsigned)((items * (HD / 4) + 255) / 256), a.c.batch), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 // few: where parts are many and their rows do not fill the device
@@ -462,56 +466,77 @@ inline hipError_t launch_combine(int dtype, const CacheAttnArgs &a, bool few, hi
   return a.c.hd == 128 ? launch_combine_t<float, 128>(a, few, s) : launch_combine_t<float, 64>(a, few, s);
 }
 inline bool few_rows_of_many_parts(const CacheAttnArgs &a) {
-  return a.parts > 8 && (int64_t)a.c.max_q * a.c.seqs * a.c.heads <= 4096;
+  return a.past_splits + a.splits > 8 && (int64_t)a.c.max_q * a.c.batch * a.c.heads <= 4096;
 }
 
-// Attention over a past that groups of sequences share: a pass over the shared keys, in which the rows
-// of a whole group are one axis of query rows, a pass of every sequence over its own keys, and
-// the parts of both joined. plan(dtype, bounds, scratch, rpb, range, splits) as of a launch over all keys.
-struct SharedPasses {
-  CacheArgs past, own;   // bounds of the two passes
-  int rpb[2], range[2], splits[2];
+// Ranges and rows per block of a launch over groups that share a past and their sequences' own keys. Both kinds of blocks are in one
+// launch, so that the compute units that one leaves idle do the other. By estimate: all blocks' times over the
+// compute units and half of the longest one's, 7 us for a start and end and tile[] us per 64 keys in blocks of 16, 32, 128
+// and 256 rows, and the parts written and read.
+struct SharedPlan {
+  int64_t blocks;
+  int rpb, range[2], splits[2];   // of the shared keys, of the own ones
 };
-template <class Plan>
-SharedPasses shared_passes(int dtype, const CacheArgs &c, const CacheShared &sh, Plan &&plan) {
-  SharedPasses p;
-  p.past = p.own = c;
-  p.past.batch = sh.groups;
-  p.past.max_q = c.rows;
-  p.past.cap = std::min(c.cap, sh.max_prefix);
-  p.own.cap = std::min(c.cap, sh.max_own);
-  plan(dtype, p.past, ~(size_t)0, &p.rpb[0], &p.range[0], &p.splits[0]);
-  plan(dtype, p.own, ~(size_t)0, &p.rpb[1], &p.range[1], &p.splits[1]);
+inline SharedPlan plan_shared(int dtype, const CacheArgs &c, const CacheShared &sh, const double (&tile)[4]) {
+  CacheArgs of[2] = {c, c};
+  of[0].batch = sh.groups;
+  of[0].max_q = c.rows;
+  of[0].cap = std::min(c.cap, sh.max_prefix);
+  of[1].cap = std::min(c.cap, sh.max_own);
+  const int64_t m = (int64_t)c.rows * (c.heads / c.kvh), cus = std::max(1, device_cus());
+  const double part = (double)attn_part_bytes(c, 1) * 2 / 4e6;
+  constexpr int ROWS[4] = {16, 32, 128, 256};
+  SharedPlan p{};
+  double best = 0;
+  const int r0 = dtype == 1 && m <= 16 ? 0 : 1, r1 = dtype == 0 || m <= 32 ? r0 : 3;
+  for (int r = r0; r <= r1; ++r) {
+    const int rpb = ROWS[r], step = rpb == 128 && c.hd == 64 ? 128 : 64;
+    int64_t tiles[2], blocks[2];
+    for (int k = 0; k < 2; ++k) {
+      tiles[k] = (std::max(of[k].cap, 1) + step - 1) / step * (step / 64);
+      blocks[k] = std::max<int64_t>(1, attn_blocks(rpb, of[k]));
+    }
+    for (int64_t i = 0; i < 9; ++i) {            // shared keys in 1, 2, 4, .. ranges, and as many as fill the compute units
+      const int64_t n0 = i < 8 ? int64_t(1) << i : cus / blocks[0];
+      if (n0 < 1 || (n0 > 1 && tiles[0] < 4 * n0)) continue;
+      for (int64_t n1 = 1; n1 <= 4; n1 *= 2) {
+        if (n1 > 1 && tiles[1] < 4 * n1) continue;
+        double sum = 0, top = 0;
+        int64_t range[2], n[2], all = 0;
+        for (int k = 0; k < 2; ++k) {
+          const int64_t per = step / 64, w = (tiles[k] + (k ? n1 : n0) - 1) / (k ? n1 : n0);
+          range[k] = (w + per - 1) / per * step;
+          n[k] = std::max<int64_t>(1, (of[k].cap + range[k] - 1) / range[k]);
+          const double t = (double)range[k] / 64 * tile[r] + 7.0;
+          sum += t * (double)(blocks[k] * n[k]);
+          top = std::max(top, t);
+          all += blocks[k] * n[k];
+        }
+        const double t = (all <= cus ? top : sum / cus + 0.5 * top) + part * (double)(n[0] + n[1]);
+        if (best == 0 || t < best) {
+          best = t;
+          p = SharedPlan{all, rpb, {(int)range[0], (int)range[1]}, {(int)n[0], (int)n[1]}};
+        }
+      }
+    }
+  }
   return p;
 }
-inline size_t shared_part_bytes(const CacheArgs &c, const SharedPasses &p) {
-  return attn_part_bytes(c, p.splits[0] + p.splits[1]);
-}
-template <class Plan, class Launch>
-hipError_t launch_shared(int dtype, const CacheAttnArgs &in, Plan &&plan, Launch &&launch, hipStream_t s) {
+template <class Launch>
+hipError_t launch_shared(int dtype, const CacheAttnArgs &in, const SharedPlan &p, Launch &&launch, hipStream_t s) {
   if (in.c.rows <= 0 || in.c.max_q <= 0) return hipSuccess;
-  const SharedPasses p = shared_passes(dtype, in.c, in.sh, plan);
   CacheAttnArgs a = in;
-  a.parts = p.splits[0] + p.splits[1];
-  a.pass = PASS_SHARED;
-  a.c.batch = in.sh.groups;
-  a.c.max_q = in.c.rows;
-  a.c.frame = 0;                                 // all rows see the shared keys
-  a.rpb = p.rpb[0];
-  a.range = p.range[0];
-  a.splits = p.splits[0];
-  hipError_t e = launch(dtype, a, s);
-  if (e != hipSuccess) return e;
-  a.pass = PASS_OWN;
-  a.c = in.c;
-  a.part0 = a.past_splits = p.splits[0];
+  a.blocks = (unsigned)p.blocks;
+  a.rpb = p.rpb;
   a.past_range = p.range[0];
-  a.rpb = p.rpb[1];
+  a.past_splits = p.splits[0];
   a.range = p.range[1];
   a.splits = p.splits[1];
-  e = launch(dtype, a, s);
+  const hipError_t e = launch(dtype, a, s);
   return e != hipSuccess ? e : launch_combine(dtype, a, few_rows_of_many_parts(a), s);
 }
+// a launch over all keys of every sequence
+inline unsigned attn_grid(const CacheAttnArgs &a) { return (unsigned)(attn_blocks(a.rpb, a.c) * a.splits); }
 
 }  // namespace
 }  // namespace wdc

@@ -224,8 +224,7 @@ struct CacheArgs {
   const int32_t *kv_len;    // [batch]
   const int32_t *table;     // [batch, table_ld]
   int pages, plog, kvh;
-  int batch, rows, max_q, table_ld;   // batch: entries that a launch goes through (sequences, if not said otherwise)
-  int seqs;                 // sequences
+  int batch, rows, max_q, table_ld;
   int cap;                  // most keys of a sequence: max_kv, or what the table's pages hold
   int heads, hd, frame;
   uint32_t group_mul;       // see cache_row
@@ -282,16 +281,13 @@ struct Cache8ReadArgs {
 };
 hipError_t launch_cache8_read(int dtype, const Cache8ReadArgs &a, hipStream_t s);
 
-// Groups of sequences that share a past (wdc_prefix); groups 0: none
+// Groups of sequences that share a past (wdc_prefix); groups 0: none. A launch then goes through the
+// groups, whose rows attend over the keys that they share, and through the sequences, over their own keys.
 struct CacheShared {
   const int32_t *group_start;   // [groups + 1]
   const int32_t *prefix_len;    // [groups]
   int groups, max_prefix, max_own;
 };
-// What a launch of an attention goes through: all keys of each sequence, the keys
-// that groups share (batch is their number), or each sequence's own keys
-enum { PASS_ALL = 0, PASS_SHARED = 1, PASS_OWN = 2 };
-
 struct CacheAttnArgs {
   CacheArgs c;
   const void *q;
@@ -302,11 +298,11 @@ struct CacheAttnArgs {
   float *part;              // scratch (part_bytes) for key ranges, or null
   size_t part_bytes;
   CacheShared sh;
-  // set by the launcher: rows per block; keys per range (a multiple of
-  // 64) and the most ranges of a row block, 1 = not split
+  // set by the launcher: blocks of the launch; rows of each; keys per range (a multiple of
+  // 64) and the most ranges of a row block, 1 = not split; the same of the keys that groups share
+  unsigned blocks;
   int rpb, range, splits;
-  int pass, part0, parts;   // a pass's first part; parts of all passes
-  int past_range, past_splits;   // PASS_OWN: range and splits of the shared keys' pass
+  int past_range, past_splits;
 };
 // scratch bytes that let a launch over these bounds split its keys as it would like to
 size_t cache_attn_scratch(int dtype, const CacheArgs &c);

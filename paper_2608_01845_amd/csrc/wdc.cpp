@@ -1718,7 +1718,7 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
   a->pages = p->pages;
   a->plog = plog;
   a->kvh = p->kv_heads;
-  a->batch = a->seqs = q->batch;
+  a->batch = q->batch;
   a->rows = (int)nrows;
   a->max_q = (int)max_q;
   a->table_ld = q->table_ld;
