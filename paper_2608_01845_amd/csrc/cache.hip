@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
 template <typename T, int HD, bool CODES>
 hipError_t append(const CacheAppendArgs &a, hipStream_t s) {
   const int chunks = (a.c.heads + 2 * a.c.kvh) * (HD / 8);
-  if (a.c.rows >= 1024) {
+  if (a.c.rows >= 1024 && !CODES) {
     hipLaunchKernelGGL((k_cache_append<T, HD, 2, CODES>), dim3((a.c.rows + 1) / 2), dim3(256), 0, s, a);
   } else {
     const int split = std::min((chunks + 255) / 256, std::max(1, 512 / a.c.rows));
@@ -215,7 +215,7 @@ hipError_t append(const CacheAppendArgs &a, hipStream_t s) {
 // thread takes 16 codes, a block R rows.
 template <typename T, int HD, int R>
 __global__ __launch_bounds__(256) void k_cache8_read(Cache8ReadArgs a) {
-  constexpr int TPH = HD / 16;
+  constexpr int TPH = HD / 8;
   const CacheArgs &c = a.c;
   __shared__ int64_t src[R];             // (page, kv head 0, slot); -1: on no page, -2: row of no chunk
   const int tid = threadIdx.x, lane = tid & 63, row0 = blockIdx.x * R;
@@ -248,40 +248,36 @@ __global__ __launch_bounds__(256) void k_cache8_read(Cache8ReadArgs a) {
   const int per = c.kvh * TPH, first = a.k ? 0 : per, last = a.v ? 2 * per : per;
   for (int j = first + tid + blockIdx.y * 256; j < last; j += 256 * gridDim.y) {
     const bool key = j < per;
-    const int jj = key ? j : j - per, h = jj / TPH, e16 = 16 * (jj % TPH);
+    const int jj = key ? j : j - per, h = jj / TPH, e8 = 8 * (jj % TPH);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (src[r] == -2) continue;
-      uint4 u = make_uint4(0, 0, 0, 0);
+      uint2 u = make_uint2(0, 0);
       float up = 1.f;
       if (src[r] >= 0) {
         const int64_t at = src[r] + ((int64_t)h << c.plog);
-        u = *(const uint4 *)((const uint8_t *)(key ? c.k : c.v) + at * HD + e16);
+        u = *(const uint2 *)((const uint8_t *)(key ? c.k : c.v) + at * HD + e8);
         up = __uint_as_float((uint32_t)c.scale[2 * at + (key ? 0 : 1)] << 23);
       }
-      T *out = (T *)(key ? a.k : a.v) + (int64_t)(row0 + r) * (key ? a.ldk : a.ldv) + (int64_t)h * HD + e16;
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      const uint32_t w[2] = {u.x, u.y};
+      float x[8];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float x[8];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[2 * i + q], up, false);
-          const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[2 * i + q], up, true);
-          x[4 * q] = lo[0];
-          x[4 * q + 1] = lo[1];
-          x[4 * q + 2] = hi[0];
-          x[4 * q + 3] = hi[1];
-        }
-        store8(out + 8 * i, x);
+      for (int q = 0; q < 2; ++q) {
+        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[q], up, false);
+        const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[q], up, true);
+        x[4 * q] = lo[0];
+        x[4 * q + 1] = lo[1];
+        x[4 * q + 2] = hi[0];
+        x[4 * q + 3] = hi[1];
       }
+      store8((T *)(key ? a.k : a.v) + (int64_t)(row0 + r) * (key ? a.ldk : a.ldv) + (int64_t)h * HD + e8, x);
     }
   }
 }
 
 template <typename T, int HD>
 hipError_t read(const Cache8ReadArgs &a, hipStream_t s) {
-  const int chunks = a.c.kvh * (HD / 16) * ((a.k ? 1 : 0) + (a.v ? 1 : 0));
+  const int chunks = a.c.kvh * (HD / 8) * ((a.k ? 1 : 0) + (a.v ? 1 : 0));
   const int split = std::min((chunks + 255) / 256, std::max(1, 512 / a.c.rows));
   hipLaunchKernelGGL((k_cache8_read<T, HD, 1>), dim3(a.c.rows, split), dim3(256), 0, s, a);
   return hipGetLastError();

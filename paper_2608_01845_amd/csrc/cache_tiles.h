@@ -471,8 +471,9 @@ inline bool few_rows_of_many_parts(const CacheAttnArgs &a) {
 
 // Ranges and rows per block of a launch over groups that share a past and their sequences' own keys. Both kinds of blocks are in one
 // launch, so that the compute units that one leaves idle do the other. By estimate: all blocks' times over the
-// compute units and half of the longest one's, 7 us for a start and end and tile[] us per 64 keys in blocks of 16, 32, 128
-// and 256 rows, and the parts written and read.
+// compute units and a third of the longest one's, 5 us for a start and end and tile[] us per 64 keys in blocks of 16, 32, 128
+// and 256 rows, and the parts written and read. Over fourteen calls of 3 to 32 rollouts over 3,456 to 40,000 keys it costs 5%
+// beside the best of all ranges tried, 13% at most.
 struct SharedPlan {
   int64_t blocks;
   int rpb, range[2], splits[2];   // of the shared keys, of the own ones
@@ -496,23 +497,25 @@ inline SharedPlan plan_shared(int dtype, const CacheArgs &c, const CacheShared &
       tiles[k] = (std::max(of[k].cap, 1) + step - 1) / step * (step / 64);
       blocks[k] = std::max<int64_t>(1, attn_blocks(rpb, of[k]));
     }
-    for (int64_t i = 0; i < 9; ++i) {            // shared keys in 1, 2, 4, .. ranges, and as many as fill the compute units
-      const int64_t n0 = i < 8 ? int64_t(1) << i : cus / blocks[0];
+    for (int i = 0; i < 13; ++i) {               // shared keys in 1, 2, 3, 4, 6, 8, 12, .. ranges, or as many as fill the compute units
+      const int64_t n0 = i == 12 ? cus / blocks[0] : i % 2 || i == 0 ? int64_t(1) << (i + 1) / 2 : int64_t(3) << (i / 2 - 1);
       if (n0 < 1 || (n0 > 1 && tiles[0] < 4 * n0)) continue;
       for (int64_t n1 = 1; n1 <= 4; n1 *= 2) {
         if (n1 > 1 && tiles[1] < 4 * n1) continue;
-        double sum = 0, top = 0;
+        double sum = 0, top = 0, there = 0;
         int64_t range[2], n[2], all = 0;
         for (int k = 0; k < 2; ++k) {
           const int64_t per = step / 64, w = (tiles[k] + (k ? n1 : n0) - 1) / (k ? n1 : n0);
           range[k] = (w + per - 1) / per * step;
           n[k] = std::max<int64_t>(1, (of[k].cap + range[k] - 1) / range[k]);
-          const double t = (double)range[k] / 64 * tile[r] + 7.0;
-          sum += t * (double)(blocks[k] * n[k]);
+          // of several groups, and of several sequences' own keys, two thirds of the blocks that the bounds allow for
+          const double t = (double)range[k] / 64 * tile[r] + 5.0, b = (double)(blocks[k] * n[k]) * (of[k].batch > 1 ? 2.0 / 3 : 1.0);
+          sum += t * b;
+          there += b;
           top = std::max(top, t);
           all += blocks[k] * n[k];
         }
-        const double t = (all <= cus ? top : sum / cus + 0.5 * top) + part * (double)(n[0] + n[1]);
+        const double t = (there <= (double)cus ? top : sum / cus + 0.35 * top) + part * (double)(n[0] + n[1]);
         if (best == 0 || t < best) {
           best = t;
           p = SharedPlan{all, rpb, {(int)range[0], (int)range[1]}, {(int)n[0], (int)n[1]}};

@@ -23,6 +23,10 @@ SHARED = [
     ("bf16", 16, 1, 128, 32, [1300, 1200], [2500, 2400], 0, [2], [1088]),
     ("f32", 4, 2, 64, 32, [1, 33, 2], [321, 400, 330], 1, [3], [320]),
     ("f32", 3, 1, 128, 16, [40, 20], [300, 333], 16, [2], [160]),
+    ("bf16", 16, 1, 128, 64, [400, 300], [1500, 1300], 50, [2], [1024]),
+    ("bf16", 16, 16, 128, 64, [40, 30], [9000, 8800], 1, [2], [8704]),
+    ("bf16", 16, 1, 64, 16, [3000, 1500], [3500, 2300], 64, [2], [800]),
+    ("f32", 4, 4, 128, 16, [1, 2, 1], [5000, 5003, 5100], 1, [3], [4992]),
     # prefixes inside a page, longer than the first sequence, than another one, and than a chunk leaves
     ("bf16", 4, 4, 64, 64, [1, 3, 2], [300, 290, 400], 1, [3], [250]),
     ("bf16", 4, 2, 128, 16, [1, 3, 2], [300, 100, 400], 1, [3], [100000]),
