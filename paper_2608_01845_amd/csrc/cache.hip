@@ -76,7 +76,8 @@ __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint2 &codes)
 // Bound by memory: 4,080 rows of 16 + 2 x 16 heads of 128 (100 MB) 21.9 us, 4.6 TB/s, where a large copy
 // reaches 4.9 (four inputs in turn, more than the last-level cache holds: 25.5 us); blocks of 1 row 22.7 us, of 4
 // rows 24.4. Fewer than 1,024 rows take a row a block and split its heads over blocks: one launch of 4 us, most of
-// it latency.
+// it latency. Codes (84 MB) go a row a block always: 20.8 us, 4.0 TB/s, of two rows 22.4, of which the single bytes of the powers
+// cost 0.5.
 template <typename T, int HD, int R, bool CODES>
 __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
   constexpr int TPH = HD / 8, HALF = HD / 2;
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
   __shared__ int64_t dst[R];             // element offset of (page, kv head 0, slot) in k and v; -1: not stored
   __shared__ int live[R];
   const int tid = threadIdx.x, lane = tid & 63;
-  const int row0 = blockIdx.x * R;
+  const int row0 = a.first + blockIdx.x * R;
   const int nqk = c.heads + c.kvh, chunks = (nqk + c.kvh) * TPH;
   // chunk j of the rows, asked for one turn ahead, the first before the rows' places are looked up
   float next[R][8];
@@ -198,40 +199,51 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheAppendArgs a) {
   }
 }
 
-template <typename T, int HD, bool CODES>
-hipError_t append(const CacheAppendArgs &a, hipStream_t s) {
-  const int chunks = (a.c.heads + 2 * a.c.kvh) * (HD / 8);
-  if (a.c.rows >= 1024 && !CODES) {
-    hipLaunchKernelGGL((k_cache_append<T, HD, 2, CODES>), dim3((a.c.rows + 1) / 2), dim3(256), 0, s, a);
-  } else {
-    const int split = std::min((chunks + 255) / 256, std::max(1, 512 / a.c.rows));
-    hipLaunchKernelGGL((k_cache_append<T, HD, 1, CODES>), dim3(a.c.rows, split), dim3(256), 0, s, a);
+// Rows [a.first, rows) in launches of at most 2^23 blocks (a launch has fewer than 2^32 threads); f(first row, rows)
+template <class F>
+hipError_t row_launches(int rows, int per_block, F &&f) {
+  constexpr int64_t MOST = int64_t(1) << 23;
+  for (int64_t first = 0; first < rows; first += MOST * per_block) {
+    f((int)first, (int)std::min<int64_t>(rows - first, MOST * per_block));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
+}
+
+template <typename T, int HD, bool CODES>
+hipError_t append(const CacheAppendArgs &in, hipStream_t s) {
+  CacheAppendArgs a = in;
+  const int chunks = (a.c.heads + 2 * a.c.kvh) * (HD / 8);
+  if (a.c.rows >= 1024 && !CODES)
+    return row_launches(a.c.rows, 2, [&](int first, int rows) {
+      a.first = first;
+      hipLaunchKernelGGL((k_cache_append<T, HD, 2, CODES>), dim3((rows + 1) / 2), dim3(256), 0, s, a);
+    });
+  const int split = std::min((chunks + 255) / 256, std::max(1, 512 / a.c.rows));
+  return row_launches(a.c.rows, 1, [&](int first, int rows) {
+    a.first = first;
+    hipLaunchKernelGGL((k_cache_append<T, HD, 1, CODES>), dim3(rows, split), dim3(256), 0, s, a);
+  });
 }
 
 // ---------------------------------------------------------------- read
-// Stored rows back in the model dtype: row i of a chunk of q rows over n keys is slot n - q + i. A
-// thread takes 16 codes, a block R rows.
-template <typename T, int HD, int R>
+// Stored rows back in the model dtype: row i of a chunk of q rows over n keys is slot n - q + i. A block takes a row, a thread
+// 8 codes at a time. Bound by memory, more so by its writes: 33,660 rows of 2 x 16 heads of 128 (415 MB, two thirds of it
+// written) 92.5 us, 4.5 TB/s, where a large copy reaches 4.9; two rows a block 95 to 99 us, four 103, stores past the caches 123.
+template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_cache8_read(Cache8ReadArgs a) {
   constexpr int TPH = HD / 8;
   const CacheArgs &c = a.c;
-  __shared__ int64_t src[R];             // (page, kv head 0, slot); -1: on no page, -2: row of no chunk
-  const int tid = threadIdx.x, lane = tid & 63, row0 = blockIdx.x * R;
+  __shared__ int64_t src;                // (page, kv head 0, slot); -1: on no page, -2: row of no chunk
+  const int tid = threadIdx.x, lane = tid & 63, row = a.first + blockIdx.x;
   if (tid < 64) {
-    int cnt[R] = {};
+    int b = 0;                           // the count of chunk ends <= row
     for (int e0 = 0; e0 < c.batch; e0 += 64) {
       const int end = e0 + lane < c.batch ? c.q_start[e0 + lane + 1] : 0x7fffffff;
-#pragma unroll
-      for (int r = 0; r < R; ++r) cnt[r] += __popcll(__ballot(end <= row0 + r));
+      b += __popcll(__ballot(end <= row));
     }
-    int b = cnt[0];
-#pragma unroll
-    for (int r = 1; r < R; ++r)
-      if (lane == r) b = cnt[r];
-    if (lane < R) {
-      const int row = row0 + lane;
+    if (lane == 0) {
       int64_t d = -2;
       if (row < c.rows && b < c.batch) {
         const CacheSeq s = cache_seq(c, b);
@@ -241,46 +253,47 @@ __global__ __launch_bounds__(256) void k_cache8_read(Cache8ReadArgs a) {
           d = e >= 0 && e < c.pages ? (((int64_t)e * c.kvh) << c.plog) + (slot & ((1 << c.plog) - 1)) : -1;
         }
       }
-      src[lane] = d;
+      src = d;
     }
   }
   __syncthreads();
+  const int64_t from = src;
+  if (from == -2) return;
   const int per = c.kvh * TPH, first = a.k ? 0 : per, last = a.v ? 2 * per : per;
   for (int j = first + tid + blockIdx.y * 256; j < last; j += 256 * gridDim.y) {
     const bool key = j < per;
     const int jj = key ? j : j - per, h = jj / TPH, e8 = 8 * (jj % TPH);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (src[r] == -2) continue;
-      uint2 u = make_uint2(0, 0);
-      float up = 1.f;
-      if (src[r] >= 0) {
-        const int64_t at = src[r] + ((int64_t)h << c.plog);
-        u = *(const uint2 *)((const uint8_t *)(key ? c.k : c.v) + at * HD + e8);
-        up = __uint_as_float((uint32_t)c.scale[2 * at + (key ? 0 : 1)] << 23);
-      }
-      const uint32_t w[2] = {u.x, u.y};
-      float x[8];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[q], up, false);
-        const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[q], up, true);
-        x[4 * q] = lo[0];
-        x[4 * q + 1] = lo[1];
-        x[4 * q + 2] = hi[0];
-        x[4 * q + 3] = hi[1];
-      }
-      store8((T *)(key ? a.k : a.v) + (int64_t)(row0 + r) * (key ? a.ldk : a.ldv) + (int64_t)h * HD + e8, x);
+    uint2 u = make_uint2(0, 0);
+    float up = 1.f;
+    if (from >= 0) {
+      const int64_t at = from + ((int64_t)h << c.plog);
+      u = *(const uint2 *)((const uint8_t *)(key ? c.k : c.v) + at * HD + e8);
+      up = __uint_as_float((uint32_t)c.scale[2 * at + (key ? 0 : 1)] << 23);
     }
+    const uint32_t w[2] = {u.x, u.y};
+    float x[8];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[q], up, false);
+      const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[q], up, true);
+      x[4 * q] = lo[0];
+      x[4 * q + 1] = lo[1];
+      x[4 * q + 2] = hi[0];
+      x[4 * q + 3] = hi[1];
+    }
+    store8((T *)(key ? a.k : a.v) + (int64_t)row * (key ? a.ldk : a.ldv) + (int64_t)h * HD + e8, x);
   }
 }
 
 template <typename T, int HD>
-hipError_t read(const Cache8ReadArgs &a, hipStream_t s) {
+hipError_t read(const Cache8ReadArgs &in, hipStream_t s) {
+  Cache8ReadArgs a = in;
   const int chunks = a.c.kvh * (HD / 8) * ((a.k ? 1 : 0) + (a.v ? 1 : 0));
   const int split = std::min((chunks + 255) / 256, std::max(1, 512 / a.c.rows));
-  hipLaunchKernelGGL((k_cache8_read<T, HD, 1>), dim3(a.c.rows, split), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return row_launches(a.c.rows, 1, [&](int first, int rows) {
+    a.first = first;
+    hipLaunchKernelGGL((k_cache8_read<T, HD>), dim3(rows, split), dim3(256), 0, s, a);
+  });
 }
 
 // ---------------------------------------------------------------- evict

@@ -269,6 +269,7 @@ struct CacheAppendArgs {
   void *q;
   int64_t ldq;
   int norm;
+  int first;                // first row of the launch, set by the launcher
   int axis_end[3];          // pairs [axis_end[a - 1], axis_end[a]) turn by coordinate a
   double freq[64];          // turns per unit of the coordinate, per pair
 };
@@ -278,6 +279,7 @@ struct Cache8ReadArgs {
   CacheArgs c;
   void *k, *v;              // [rows, ldk / ldv] or null
   int64_t ldk, ldv;
+  int first;                // first row of the launch, set by the launcher
 };
 hipError_t launch_cache8_read(int dtype, const Cache8ReadArgs &a, hipStream_t s);
 

@@ -6,6 +6,7 @@ import torch
 
 from tests import cache8_util as c8
 from tests import cache_util as cu
+from tests.gpu_util import torch_cuda
 from tests.test_gpu_cache import (APPEND, ATTENTION, ATTENTION_WIDE, EPS, EPS32, append64, attention_bound, ctx_of, few, ids,
                                   within)
 
@@ -379,6 +380,28 @@ def test_pool_beyond_32_bit_offsets(dtype, hd):
     for a, b in zip(*res):
         assert torch.equal(a, b)
     del k, v, at
+
+
+def test_more_rows_than_one_launch_has():
+    """Rows on both sides of 2^23 (and of 2^24 in the read) are stored and read back like others."""
+    n, hd, page = (1 << 24) + 77, 64, 256
+    torch_cuda()
+    import paper_2608_01845_amd as wdc
+    ctx = wdc.Context(cu.config("bf16", 1, hd, qk_norm=False, rope=(0, 0, 0)), allocate_weights=False)
+    pages = -(-n // page)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").flip(0).reshape(1, -1).contiguous()
+    k8, v8 = (torch.zeros((pages, 1, page, hd), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2))
+    scale = torch.zeros((pages, 1, page, 2), dtype=torch.uint8, device="cuda")
+    cache, ch = wdc.PagedCache8(k8, v8, scale), wdc.Chunks(i32(0, n), i32(n), table, rows=n)
+    qkv = torch.randn((n, 3 * hd), dtype=torch.bfloat16, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    q = ctx.cache8_append(cache, ch, qkv, torch.zeros((n, hd), dtype=torch.bfloat16, device="cuda"))
+    v = ctx.cache8_read(cache, ch, v=torch.zeros((n, hd), dtype=torch.bfloat16, device="cuda"))[1]
+    for at in (0, (1 << 23) - 50, (1 << 24) - 50, n - 100):
+        rows = slice(at, at + 100)
+        assert torch.equal(q[rows], qkv[rows, :hd])
+        code, byte = c8.quantised64(qkv[rows, 2 * hd:].double())
+        assert torch.equal(v[rows].double(), c8.values64(code, byte))
 
 
 @pytest.mark.parametrize("dtype,heads,kvh,hd,q,kv", [("bf16", 4, 4, 128, [1, 1], [9000, 5000]), ("bf16", 4, 4, 64, [300], [9000]),

@@ -237,3 +237,20 @@ def test_shared_is_the_unshared_attention():
     bound, _ = attention_bound(s, pv, o, qk, 1200)
     within(a.reshape(o.shape), o, bound, "o")
     within(b.reshape(o.shape), o, bound, "o")
+
+
+@pytest.mark.parametrize("codes", [False, True])
+def test_no_rows(codes):
+    s = c8.state8("bf16", 4, 2, 64, 16, [0, 0], [40, 30], seed=59)
+    wdc, ctx = ctx_of(s)
+    past = c8.Past(s, [2], [32])
+    for ch in (cu.chunks(wdc, s), cu.chunks(wdc, s, max_kv=0)):
+        if codes:
+            ctx.cache8_attention(c8.cache8(wdc, s), ch, s.x, torch.empty_like(s.x), prefix=past.desc(wdc, s))
+        else:
+            ctx.cache_attention_shared(wdc.PagedCache(s.k, s.v), ch, past.desc(wdc, s), s.x, torch.empty_like(s.x))
+    s = c8.state8("bf16", 4, 2, 64, 16, [2, 1], [40, 30], seed=59)
+    past = c8.Past(s, [2], [32])
+    out = torch.full_like(s.x, 7.0)
+    ctx.cache8_attention(c8.cache8(wdc, s), cu.chunks(wdc, s, max_kv=0), s.x, out, prefix=past.desc(wdc, s))
+    assert (out == 0).all()
