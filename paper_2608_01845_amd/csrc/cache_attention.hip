@@ -409,7 +409,7 @@ struct TileLoads {
   }
 };
 
-template <int HD, bool SMALL, int W, int KG>
+template <int HD, bool SMALL, int W, int KG, int KH>
 __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs a) {
   using F = Few<HD>;
   using TL = TileLoads<HD, SMALL>;
@@ -427,8 +427,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  constexpr int WR = W / KG;                     // waves over the block's rows
-  const int wr = wid % WR, kg = wid / WR;
+  static_assert(KG == 1 || KH == 1, "keys are shared out in one way");
+  constexpr int WR = W / (KG * KH);              // waves over the block's rows
+  constexpr int KK = 4 / KH;                     // tiles of 16 keys of a wave
+  const int wr = wid % WR, kg = KG == 1 ? 0 : wid / WR, kh = KH == 1 ? 0 : wid / WR;
   const bool grp_a = KG == 2 || wid < 4;         // loads tiles
   const int mlast = min(m0 + 32 * WR, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KG * KV - 1) / (KG * KV);   // in steps of KG tiles
@@ -447,12 +449,12 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   }
   int kro[NC];                                   // K fragment of rows lr, dims 32 c + 8 lg
 #pragma unroll
-  for (int j = 0; j < NC; ++j) kro[j] = lr * F::ROWB + ((4 * j + lg) ^ F::kkey(lr)) * 16;
+  for (int j = 0; j < NC; ++j) kro[j] = (16 * KK * kh + lr) * F::ROWB + ((4 * j + lg) ^ F::kkey(lr)) * 16;
   int vro[F::VR];                                // transposed V read of rows 4 lg .. + 3, dims 16 i ..
   {
     const int r = 4 * lg + (lr >> 2), j = lane & 3;
 #pragma unroll
-    for (int i = 0; i < F::VR; ++i) vro[i] = V_BASE + r * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
+    for (int i = 0; i < F::VR; ++i) vro[i] = V_BASE + (16 * KK * kh + r) * F::ROWB + ((2 * i + (j >> 1)) ^ F::vkey(r)) * 16 + 8 * (j & 1);
   }
   char *ring = smem + kg * 2 * NB * TB;
   const uint32_t lds0 = lds_addr(ring);
@@ -496,11 +498,11 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
     for (int t = 0; t < 2; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
-  auto qk = [&](f32x4 (&S)[4][2], const char *kb) {
+  auto qk = [&](f32x4 (&S)[KK][2], const char *kb) {
 #pragma unroll
     for (int j = 0; j < NC; ++j)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < KK; ++k) {
         const bf16x8 kf = *(const bf16x8 *)(kb + kro[j] + k * 16 * F::ROWB);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -512,8 +514,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   };
 
   if (nf > 0) {
-    f32x4 S[2][4][2];                            // S of tiles t + 1 and t + 2 (index tile & 1)
-    bf16x8 pf[2][2][2];                          // P of tiles t and t + 1 (index tile & 1), [row tile][32-key group]
+    f32x4 S[2][KK][2];                           // S of tiles t + 1 and t + 2 (index tile & 1)
+    bf16x8 pf[2][2][KK / 2];                          // P of tiles t and t + 1 (index tile & 1), [row tile][32-key group]
     qk(S[0], ring);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -530,8 +532,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
         wait_vm<0>();
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // step 0 refills the slot of K_0
-    constexpr int NMF = 2 * NI + 4 * NC;         // fragment reads per step, two MFMAs each
-    constexpr int NPV = NMF / 2, EPM = 32 / NMF; // P V reads; exponentials per pair of MFMAs
+    constexpr int NPV = KK / 2 * NI, NMF = NPV + KK * NC;   // fragment reads of P V, and of a step; two MFMAs each
+    constexpr int EPM = 8 * KK / NMF;            // exponentials per pair of MFMAs
     static_assert(NMF == 16 || NMF == 32, "hd 64 or 128");
     bf16x8 fr_[NMF];
     // One step, P = t % NB at compile time. c indexes S of tile t + 1 and the P it becomes, n S of tile t
@@ -544,7 +546,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
       if (r < NPV)
         fr_[r] = vfrag(vb, r % NI, (r < NPV ? r : 0) / NI);
       else
-        fr_[r] = *(const bf16x8 *)(kb + kro[g / 4] + (g % 4) * 16 * F::ROWB);
+        fr_[r] = *(const bf16x8 *)(kb + kro[g / KK] + (g % KK) * 16 * F::ROWB);
     };
 #pragma unroll
     for (int r = 0; r < 4; ++r) read(r, ring, ring);
@@ -571,8 +573,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
           o[q % NI][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], pf[n][t_][(q < NPV ? q : 0) / NI], o[q % NI][t_], 0, 0, 0);
         } else {
           const int g = q >= NPV ? q - NPV : 0;
-          S[n][g % 4][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], qf[t_][g / 4],
-                                                                    g < 4 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[n][g % 4][t_], 0, 0, 0);
+          S[n][g % KK][t_] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr_[q], qf[t_][g / KK],
+                                                                     g < KK ? f32x4{0.f, 0.f, 0.f, 0.f} : S[n][g % KK][t_], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
       };
@@ -677,20 +679,20 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
     // its V is NaN in a matrix product: a tile that holds one is multiplied key by key.
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < TB / (1024 * WR); ++i) {
+    for (int i = 0; i < TB / (1024 * WR); ++i) {   // (with KH of 2 both waves of a row part look over all of it)
       const u32x4_t y = *(const u32x4_t *)(vb + V_BASE + (i * 64 * WR + 64 * wr + lane) * 16);
 #pragma unroll
       for (int q = 0; q < 4; ++q) odd |= (y[q] & 0x7f80u) == 0x7f80u || (y[q] & 0x7f800000u) == 0x7f800000u;
     }
     odd = __syncthreads_or(odd);
-    const int key0 = KV * (KG * (t_first + u) + kg);
-    f32x4 S[4][2];
-    bf16x8 pf[2][2];
+    const int key0 = KV * (KG * (t_first + u) + kg) + 16 * KK * kh;
+    f32x4 S[KK][2];
+    bf16x8 pf[2][KK / 2];
     qk(S, kb);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < KK; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (key0 + 16 * k + 4 * lg + e >= lim[t]) S[k][t][e] = -INFINITY;
@@ -707,7 +709,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
       l[t] += weights(S, pf[t], t, sc, m[t] == -INFINITY ? 0.f : m[t]);
     }
     if (odd) {
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < KK; ++k)
         for (int e = 0; e < 4; ++e)
           for (int g = 0; g < 4; ++g) {
             const int key = 16 * k + 4 * g + e;
@@ -715,7 +717,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
             for (int t = 0; t < 2; ++t) {
               float p = 0.f;                     // of key and row lr, held by lane group g
 #pragma unroll
-              for (int q = 0; q < 16; ++q)
+              for (int q = 0; q < 4 * KK; ++q)
                 if (q == 4 * k + e) p = (float)pf[t][q >> 3][q & 7];
               p = __shfl(p, 16 * g + lr, 64);
               if (key0 + key < lim[t])
@@ -724,13 +726,13 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
 #pragma unroll
                   for (int d = 0; d < 4; ++d) {
                     const int col = 16 * i + 4 * lg + d;
-                    o[i][t][d] += p * bf2f(*(const bf16_t *)(vb + V_BASE + key * F::ROWB + ((col >> 3) ^ F::vkey(key)) * 16 + (col & 7) * 2));
+                    o[i][t][d] += p * bf2f(*(const bf16_t *)(vb + V_BASE + (16 * KK * kh + key) * F::ROWB + ((col >> 3) ^ F::vkey(key)) * 16 + (col & 7) * 2));
                   }
             }
           }
     } else {
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+      for (int p = 0; p < KK / 2; ++p)
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           const bf16x8 vf = vfrag(vb, i, p);
@@ -740,11 +742,11 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
     }
   }
 
-  if constexpr (KG == 2) {                       // the two softmaxes of every row meet
+  if constexpr (KG * KH == 2) {                       // the two softmaxes of every row meet
     f32x4 *xo = (f32x4 *)smem + (wr * 2 * NI) * 64 + lane;
     float2 *xm = (float2 *)((f32x4 *)smem + WR * 2 * NI * 64) + wr * 128 + lane;
     __syncthreads();
-    if (kg == 1) {
+    if (kg + kh == 1) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -753,7 +755,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
       }
     }
     __syncthreads();
-    if (kg == 1) return;
+    if (kg + kh == 1) return;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const float2 y = xm[64 * t];
@@ -1274,23 +1276,26 @@ hipError_t launch_few(const CacheAttnArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((k_cache_attn_few<HD, RT>), dim3(a.blocks), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
-template <int HD, bool SMALL, int W, int KG>
+template <int HD, bool SMALL, int W, int KG, int KH>
 hipError_t launch_many(const CacheAttnArgs &a, hipStream_t s) {
   constexpr int LDS = KG * 2 * NB * KV * Few<HD>::ROWB;
   static DeviceOnce once;
   const hipError_t lim = once_on_device(once, [] {
-    return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL, W, KG>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    return hipFuncSetAttribute((const void *)k_cache_attn_many<HD, SMALL, W, KG, KH>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   });
   if (lim != hipSuccess) return lim;
-  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL, W, KG>), dim3(a.blocks), dim3(64 * W), LDS, s, a);
+  hipLaunchKernelGGL((k_cache_attn_many<HD, SMALL, W, KG, KH>), dim3(a.blocks), dim3(64 * W), LDS, s, a);
   return hipGetLastError();
 }
 template <int HD>
 hipError_t launch_bf16(const CacheAttnArgs &a, hipStream_t s) {
   constexpr int W128 = HD == 64 ? 8 : 4, KG = HD == 64 ? 2 : 1;   // of blocks of 128 rows
   const int rpb = a.rpb;
-  if (rpb == 256) return a.c.plog < 6 ? launch_many<HD, true, 8, 1>(a, s) : launch_many<HD, false, 8, 1>(a, s);
-  if (rpb == 128) return a.c.plog < 6 ? launch_many<HD, true, W128, KG>(a, s) : launch_many<HD, false, W128, KG>(a, s);
+  const bool small = a.c.plog < 6;
+  if (rpb == 256) return small ? launch_many<HD, true, 8, 1, 1>(a, s) : launch_many<HD, false, 8, 1, 1>(a, s);
+  if constexpr (HD == 128)
+    if (rpb == 128 && a.sh.groups > 0) return small ? launch_many<HD, true, 8, 1, 2>(a, s) : launch_many<HD, false, 8, 1, 2>(a, s);
+  if (rpb == 128) return small ? launch_many<HD, true, W128, KG, 1>(a, s) : launch_many<HD, false, W128, KG, 1>(a, s);
   return rpb == 16 ? launch_few<HD, 1>(a, s) : launch_few<HD, 2>(a, s);
 }
 
