@@ -442,7 +442,7 @@ typedef struct {
 
 /* wdc_cache_append into such a cache. Keys (normalised and turned) and values of a row and kv head get the smallest power of two,
  * from 2^-117 on, that keeps their finite elements within 448 times it, and are rounded once, to nearest even; infinities and
- * NaN are stored as NaN, and finite values that round to 2^128 read back as infinity. */
+ * NaN are stored as NaN, and elements beyond 240 * 2^120 (the largest finite value of this form) as that. */
 wdc_status wdc_cache8_append(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks, const void *d_qkv,
                              int64_t ld, const int32_t *d_pos, const float *d_q_weight, const float *d_k_weight,
                              void *d_q, int64_t ldq);
@@ -454,7 +454,7 @@ wdc_status wdc_cache8_read(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wd
                            void *d_v, int64_t ldv);
 
 /* wdc_cache_attention over such a cache, on the values that its codes stand for, or with a prefix (may be NULL)
- * wdc_cache_attention_shared, whose scratch is required. */
+ * wdc_cache_attention_shared, whose scratch is required. Sums stay finite while |v| is below 2^120 / (keys). */
 size_t wdc_cache8_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks,
                                     const wdc_prefix *prefix);
 wdc_status wdc_cache8_attention(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks,

@@ -42,7 +42,8 @@ __device__ __forceinline__ void store8(T *p, const float (&x)[8]) {
 // Eight elements of a head over HD / 8 lanes as e4m3 codes of x 2^-E, with E the smallest exponent, from -117 on, that keeps
 // the head's finite elements within 448 2^E (448: the largest code). Returns E + 127. A power of two changes no
 // digit of a floating-point code, and from 2^-117 on every value code 2^E is a normal number in bf16 as in float32: what
-// reads the cache has the values exactly. The one rounding is to nearest even; infinities and NaN become NaN.
+// reads the cache has the values exactly. The one rounding is to nearest even; infinities and NaN become NaN, and elements
+// beyond 240 * 2^120, the largest value of these that is finite, become it.
 template <int HD>
 __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint2 &codes) {
   float big = 0.f;
@@ -51,9 +52,10 @@ __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint2 &codes)
   const uint32_t u = __float_as_uint(group_max<HD / 8>(big));
   const int byte = max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), 10);
   const float down = __uint_as_float((uint32_t)(254 - byte) << 23);
+  const float most = byte == 247 ? 240.f : 448.f;   // 256 * 2^120 would be an infinity
   float y[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = fabsf(x[e]) < INFINITY ? x[e] * down : NAN;
+  for (int e = 0; e < 8; ++e) y[e] = fabsf(x[e]) < INFINITY ? fminf(fmaxf(x[e] * down, -most), most) : NAN;
   int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
   lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
   hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);

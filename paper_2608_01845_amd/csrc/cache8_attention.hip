@@ -39,7 +39,9 @@ __device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float((
 // As over a cache in float32: v_mfma_f32_32x32x2_f32, four waves share 32 rows and take every fourth key
 // tile of 32 of the block's range. S^T = K Q^T leaves a lane one row and 16 keys, which O^T = V^T P^T takes one by
 // one as its B operand. Codes come straight from the cache, those of K 16 at a time (which dimension a lane
-// takes in which step is free as long as K and Q agree: lane group g has [g hd / 2, + hd / 2)).
+// takes in which step is free as long as K and Q agree: lane group g has [g hd / 2, + hd / 2)). Keys past the
+// cache's end are read as its last key and get weight 0. Bound by the matrix instructions: chunks of 256 and 100 rows over
+// 1,500 and 777 keys, 4 heads of 64, 14.7 us and 4 of the parts' launch, as over float32 (14.2), most of it latency.
 template <int HD>
 __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
   constexpr int NI = HD / 32, NC = HD / 2;
@@ -81,7 +83,7 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
   for (int t = t0 + w; t < t1; t += 4) {
     vecn v[16];
 #pragma unroll
-    for (int e4 = 0; e4 < 4; ++e4) {             // four keys of one page, as a rule
+    for (int e4 = 0; e4 < 4; ++e4) {             // four keys of one page
       const int key = 32 * t + 8 * e4 + 4 * lg, k0 = min(key, s.n - 1);
       const int64_t at = slot_row(c, tab, h, k0);
 #pragma unroll
@@ -221,6 +223,10 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
 // scores of row lr and keys 4 lg + e of both halves of the tile, the B operand of O^T = V^T P^T. V goes through LDS, from which rows
 // come back transposed, 8 keys of one dimension a lane, so V's powers cannot ride on the conversion: they multiply the weights, which
 // are rounded to bf16 before that (a power of two changes no digit). The softmax is the one of the cache in bf16.
+//
+// Eight tokens over 1 to 32,768 keys, 32 heads on 8 of 128 (235 MB): 48.6 us and 4.7 of the parts' launch, 4.8 TB/s, where
+// the cache in bf16 takes 80 for twice the bytes (5.4 TB/s; a large copy, which writes too, 4.9). 232 registers allow two blocks
+// per compute unit; forced to three, 13 of them spill (76.9 us with two blocks per unit's ranges, 57.5 unforced).
 template <int HD>
 struct Codes {
   static constexpr int KT = 32;                  // keys per tile
@@ -493,6 +499,15 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_few(CacheAttnArgs a) {
 //
 // Tiles that some row sees in part, and the cache's last one, follow one at a time with their masks, tile u + 1 converted
 // while u is worked on.
+//
+// Bound like the kernel over bf16 by the matrix cores, the exponentials and their power: 4,080 rows over 67,320 keys, 16 heads of
+// 128, 1,906 to 1,940 us by device, 1,140 to 1,160 TFLOP/s, where that one takes 1,780 to 1,850; the conversion adds 8% to
+// a step's vector instructions and half of its LDS traffic again. Blocks of 128 rows: at hd 64 KG = 2 groups of four waves take every
+// second tile each; at hd 128 two such rings do not fit into LDS, and KH = 2 groups of four take half of every tile's keys
+// (32 rows of 32 heads on 8 over 40,000 keys: 50 us with four waves over all of them, 45 so).
+//
+// References move when a lane's sum of weights over a tile passes 2^8 (2^16 over bf16), to the row's largest score: sums of weights
+// times v are finite while |v| is below 2^120 over the number of keys.
 constexpr int KV = 64, KS = 2, VS = 4, RS = 3, ES = 4;   // keys a tile; slots of K, V, codes and exponent bytes
 constexpr int EB = 256;                          // bytes of a slot of exponent bytes
 constexpr float SUM_LIMIT = 0x1p8f;

@@ -325,7 +325,9 @@ __global__ __launch_bounds__(256, 1) void k_cache_attn_few(CacheAttnArgs a) {
 // wave alone on a SIMD waits for its own results (1,720 cycles, of which 960 issue). At hd 64 two
 // tiles fit into LDS at a time: KG = 2 groups of 4 waves take every second one each, 0.58 us a
 // tile (0.77 with 4 waves), and their softmaxes meet at the end (2,048 rows causal over themselves, 16 heads: 26.7 us,
-// 38.4 with 256 rows; 4,096 over 4,096 in full: 88.6, 77.4 with 256).
+// 38.4 with 256 rows; 4,096 over 4,096 in full: 88.6, 77.4 with 256). Over a shared past the 128 rows at hd 128 have KH = 2
+// groups of 4 waves, which take half of every tile's keys each and meet the same way (32 rollouts of a token, 32 heads on 8, off
+// 24,448 shared keys: 56.7 us with 4 waves, 49 so).
 //
 // Tiles that all rows see whole run through a software pipeline: step t holds the P V
 // products of tile t, the Q K products of tile t + 2 and, in the same instruction
@@ -1328,7 +1330,7 @@ hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_
 
 // us per 64 keys in blocks of 16, 32, 128 and 256 rows (alone on a compute unit)
 static SharedPlan shared_plan(int dtype, const CacheArgs &c, const CacheShared &sh) {
-  static const double tile[4][4] = {{0, 1.0, 0, 0}, {0, 2.0, 0, 0}, {0.55, 0.71, 0.58, 1.03}, {0.72, 0.95, 1.08, 1.4}};
+  static const double tile[4][4] = {{0, 1.0, 0, 0}, {0, 2.0, 0, 0}, {0.55, 0.71, 0.58, 1.03}, {0.72, 0.95, 0.95, 1.4}};
   return plan_shared(dtype, c, sh, tile[2 * dtype + (c.hd == 128)]);
 }
 

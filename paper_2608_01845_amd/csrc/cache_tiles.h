@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
 }
 
 // The same for few rows of many parts: a block for each row and head, whose groups of HD / 4 threads take every
-// 1024 / HD-th part each and meet in LDS. (32 rows of 32 heads of 128, 33 parts: 9.7 us with a thread for all of them, X so.)
+// 1024 / HD-th part each and meet in LDS. (32 rows of 32 heads of 128, 33 parts: 9.7 us with a thread for all of them, 7.6 so.)
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_cache_attn_combine_few(CacheAttnArgs a) {
   constexpr int TPR = HD / 4, G = 256 / TPR;

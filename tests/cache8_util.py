@@ -13,12 +13,14 @@ CODES = [(8 + c % 8) * 2.0 ** (c // 8 - 10) if c >= 8 else c * 2.0 ** -9 for c i
 
 def quantised64(x):
     """Codes [..., hd] and exponent bytes [...] of heads x float64: the smallest exponent from -117 on that keeps the finite
-    elements within 448, the nearest code (the even one of two)."""
+    elements within 448, the nearest code (the even one of two); beyond 240 * 2^120 that value."""
     size = torch.where(torch.isfinite(x), x.abs(), 0).amax(-1)
     e = torch.full_like(size, -117)
     for step in range(-117, 121):
         e = torch.where(size > 448.0 * 2.0 ** step, step + 1.0, e)
     y = x * torch.exp2(-e)[..., None]
+    top = torch.where(e == 120, 240.0, 448.0)[..., None]
+    y = torch.where(torch.isfinite(x), torch.minimum(torch.maximum(y, -top), top), y)
     table = torch.tensor(CODES, dtype=torch.float64, device=x.device)
     mid = (table[1:] + table[:-1]) / 2
     at = torch.searchsorted(mid, y.abs().contiguous())           # midpoints below |y|

@@ -88,6 +88,9 @@ def test_append_of_extreme_values(dtype, hd):
     mid = [(a + b) / 2 for a, b in zip(c8.CODES, c8.CODES[1:])]
     x[11] = torch.tensor((mid * 8)[:6 * hd])          # every tie
     x[10, ::hd] = x[11, ::hd] = 448
+    x[12] = torch.linspace(-3.38e38, 3.38e38, 6 * hd)  # (the step is infinite: NaN and infinities)
+    x[13] = 3.38e38                                   # the end of bf16's range
+    x[14] = torch.linspace(-1, 1, 6 * hd) * 3.38e38
     s.qkv = x.to(s.td).cuda()
     ctx.cache8_append(c8.cache8(wdc, s), cu.chunks(wdc, s), s.qkv, torch.empty_like(s.x))
     pg, sl = cu.where(s, 0)
@@ -97,6 +100,7 @@ def test_append_of_extreme_values(dtype, hd):
         got = pool.view(torch.uint8)[pg, :, sl]
         assert torch.equal(s.scale[pg, :, sl, which], byte)
         nan = (code & 127) == 127
+        assert torch.equal(torch.isfinite(c8.values64(got, s.scale[pg, :, sl, which]).to(s.td)), torch.isfinite(part))
         assert torch.equal(nan, (got & 127) == 127) and torch.equal(got[~nan], code[~nan])
 
 
