@@ -192,31 +192,19 @@ struct AttnBlock {
     const int lane = threadIdx.x & 63;
     group = c.heads / c.kvh;
     int li = blockIdx.x;
-    if (a.sh.groups == 0 && (c.batch == 1 || (a.splits == 1 && c.max_q * group <= a.rpb))) {   // one sequence, or a block for each and kv head
-      row = 0;
-      if (c.batch > 1) {
-        row = uni(li / c.kvh);
-        li -= row * c.kvh;
-      }
-      s = uniform_seq(c, row);
-    } else {
-      bool found = false;
-      const int entries = a.sh.groups + c.batch;
-      for (int e0 = 0; e0 < entries && !found; e0 += 64) {
+    // the entry whose blocks have this one among them; li counts within it, or past all of them
+    auto among = [&](int entries, bool past) {
+      for (int e0 = 0; e0 < entries; e0 += 64) {
         int cnt = 0;
         AttnSeq x{};
-        const int e = e0 + lane;
-        if (e < entries) {
-          if (e < a.sh.groups)
-            x = shared_entry(a, e);
-          else
-            x = own_entry(a, e - a.sh.groups);
-          cnt = (x.s.nq * group + a.rpb - 1) / a.rpb * range_count(a, x.s.n, x.shared == 1) * c.kvh;
+        if (e0 + lane < entries) {
+          x = past ? shared_entry(a, e0 + lane) : own_entry(a, e0 + lane);
+          cnt = (x.s.nq * group + a.rpb - 1) / a.rpb * range_count(a, x.s.n, past) * c.kvh;
         }
         const int sum = wave_scan(cnt);
-        const uint64_t past = __ballot(sum > li);
-        if (past) {
-          const int k = __builtin_ctzll(past);
+        const uint64_t found = __ballot(sum > li);
+        if (found) {
+          const int k = __builtin_ctzll(found);
           li -= __builtin_amdgcn_readlane(sum - cnt, k);
           s.q0 = __builtin_amdgcn_readlane(x.s.q0, k);
           s.nq = __builtin_amdgcn_readlane(x.s.nq, k);
@@ -225,12 +213,32 @@ struct AttnBlock {
           row = __builtin_amdgcn_readlane(x.row, k);
           skip = __builtin_amdgcn_readlane(x.skip, k);
           shared = __builtin_amdgcn_readlane(x.shared, k);
-          found = true;
-        } else {
-          li -= __builtin_amdgcn_readlane(sum, 63);
+          return true;
         }
+        li -= __builtin_amdgcn_readlane(sum, 63);
       }
-      if (!found) return;
+      return false;
+    };
+    if (a.sh.groups == 0 || a.only == 2 || !among(a.sh.groups, true)) {
+      if (a.only == 1) return;
+      if (c.batch == 1 || (a.splits == 1 && c.max_q * group <= a.rpb)) {   // one sequence, or a block for each and kv head
+        int b = 0;
+        if (c.batch > 1) {
+          b = uni(li / c.kvh);
+          if (b >= c.batch) return;
+          li -= b * c.kvh;
+        }
+        const AttnSeq x = own_entry(a, b);
+        s.q0 = uni(x.s.q0);
+        s.nq = uni(x.s.nq);
+        s.n = uni(x.s.n);
+        s.start = uni(x.s.start);
+        row = b;
+        skip = uni(x.skip);
+        shared = uni(x.shared);
+      } else if (!among(c.batch, false)) {
+        return;
+      }
     }
     li = uni(li);
     skip = min(skip, c.table_ld - 1);            // (pages beyond the table hold no keys)
@@ -254,7 +262,8 @@ struct AttnBlock {
 
 // ---------------------------------------------------------------- parts of a split launch
 // o = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s with M the largest m_s, ranges
-// in order (of shared keys first); thread: one row, 4 columns. 4.4 us for 384 rows, 16 heads of 64, five ranges: a launch and its latency.
+// in order (of shared keys first); thread: one row, 4 columns. 4.4 us for 384 rows, 16 heads of 64, five ranges: a launch and its
+// latency.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_cache_attn_combine(CacheAttnArgs a) {
   constexpr int TPR = HD / 4;
@@ -469,14 +478,21 @@ inline bool few_rows_of_many_parts(const CacheAttnArgs &a) {
   return a.past_splits + a.splits > 8 && (int64_t)a.c.max_q * a.c.batch * a.c.heads <= 4096;
 }
 
-// Ranges and rows per block of a launch over groups that share a past and their sequences' own keys. Both kinds of blocks are in one
-// launch, so that the compute units that one leaves idle do the other. By estimate: all blocks' times over the
-// compute units and a third of the longest one's, 5 us for a start and end and tile[] us per 64 keys in blocks of 16, 32, 128
-// and 256 rows, and the parts written and read. Over fourteen calls of 3 to 32 rollouts over 3,456 to 40,000 keys it costs 5%
-// beside the best of all ranges tried, 13% at most.
+// Rows per block and ranges over the keys that groups share [0] and over their sequences' own keys [1].
+// Both kinds of blocks go out in one launch, so that the compute units that one leaves idle do the other, or
+// in two, each with blocks of its own height: many sequences with few own keys want low ones (1,024 tokens of 32 heads on 8
+// of 128 off 8,128 shared keys, 65 own ones each: 542 us in one launch, 230 in two; 64 of 16 heads of 64 off 16,000, up to 442 own
+// ones: 65 and 45; 32 of 32 heads on 8 off 24,448, up to 900 own ones: 48 and 53).
+//
+// By estimate: all blocks' times over the places for them (two a compute unit for blocks of 16 rows), of several
+// groups or sequences two thirds of the blocks that the bounds allow for, and a third of the longest one's; 5 us for a start and
+// end and tile[] us per 64 keys in blocks of 16, 32, 128 and 256 rows; the parts written and read; 8 us for a further launch.
+// Over fourteen calls of 3 to 32 rollouts over 3,456 to 40,000 keys one launch so planned costs 5% beside the best of all
+// ranges tried, 13% at most.
 struct SharedPlan {
-  int64_t blocks;
-  int rpb, range[2], splits[2];   // of the shared keys, of the own ones
+  bool together;
+  int64_t blocks[2];
+  int rpb[2], range[2], splits[2];
 };
 inline SharedPlan plan_shared(int dtype, const CacheArgs &c, const CacheShared &sh, const double (&tile)[4]) {
   CacheArgs of[2] = {c, c};
@@ -484,58 +500,98 @@ inline SharedPlan plan_shared(int dtype, const CacheArgs &c, const CacheShared &
   of[0].max_q = c.rows;
   of[0].cap = std::min(c.cap, sh.max_prefix);
   of[1].cap = std::min(c.cap, sh.max_own);
-  const int64_t m = (int64_t)c.rows * (c.heads / c.kvh), cus = std::max(1, device_cus());
-  const double part = (double)attn_part_bytes(c, 1) * 2 / 4e6;
+  const double cus = std::max(1, device_cus()), part = (double)attn_part_bytes(c, 1) * 2 / 4e6;
   constexpr int ROWS[4] = {16, 32, 128, 256};
-  SharedPlan p{};
-  double best = 0;
-  const int r0 = dtype == 1 && m <= 16 ? 0 : 1, r1 = dtype == 0 || m <= 32 ? r0 : 3;
-  for (int r = r0; r <= r1; ++r) {
-    const int rpb = ROWS[r], step = rpb == 128 && c.hd == 64 ? 128 : 64;
-    int64_t tiles[2], blocks[2];
-    for (int k = 0; k < 2; ++k) {
-      tiles[k] = (std::max(of[k].cap, 1) + step - 1) / step * (step / 64);
-      blocks[k] = std::max<int64_t>(1, attn_blocks(rpb, of[k]));
-    }
-    for (int i = 0; i < 13; ++i) {               // shared keys in 1, 2, 3, 4, 6, 8, 12, .. ranges, or as many as fill the compute units
-      const int64_t n0 = i == 12 ? cus / blocks[0] : i % 2 || i == 0 ? int64_t(1) << (i + 1) / 2 : int64_t(3) << (i / 2 - 1);
-      if (n0 < 1 || (n0 > 1 && tiles[0] < 4 * n0)) continue;
+  // one kind of blocks at ROWS[r] and n ranges: their number, the ranges, and for the estimate the sum of the
+  // times and the longest
+  struct Kind {
+    int64_t blocks, range, splits;
+    double sum, there, top;
+  };
+  auto kind = [&](int k, int r, int64_t n) {
+    const int64_t step = ROWS[r] == 128 && c.hd == 64 ? 128 : 64, cap = std::max(of[k].cap, 1);
+    Kind x;
+    x.range = ((cap + n - 1) / n + step - 1) / step * step;
+    x.splits = std::max<int64_t>(1, (cap + x.range - 1) / x.range);
+    x.blocks = std::max<int64_t>(1, attn_blocks(ROWS[r], of[k])) * x.splits;
+    x.there = (double)x.blocks * (of[k].batch > 1 ? 2.0 / 3 : 1.0);
+    x.top = (double)x.range / 64 * tile[r] + 5.0;
+    x.sum = x.top * x.there;
+    return x;
+  };
+  auto time = [&](double sum, double there, double top, int r) {
+    const double places = r == 0 ? 2 * cus : cus;
+    return there <= places ? top : sum / places + 0.35 * top;
+  };
+  // heights for so many rows of a (group or sequence, kv head)
+  auto first = [&](int64_t m) { return dtype == 0 || (m > 16 && m <= 32) ? 1 : 0; };
+  auto last = [&](int64_t m) { return dtype == 0 || (m > 16 && m <= 32) ? 1 : m <= 16 ? 0 : 3; };
+  // 1, 2, 3, 4, 6, 8, 12, .. 64 ranges, or as many as fill the compute units
+  auto ranges = [&](int k, int r, int i) -> int64_t {
+    const int64_t n = i == 12           ? (int64_t)cus / std::max<int64_t>(1, attn_blocks(ROWS[r], of[k]))
+                      : i % 2 || i == 0 ? int64_t(1) << (i + 1) / 2
+                                        : int64_t(3) << (i / 2 - 1);
+    return n == 1 || (n > 1 && of[k].cap >= 256 * n) ? n : 0;
+  };
+  const int64_t group = c.heads / c.kvh, m[2] = {c.rows * group, c.max_q * group};
+  SharedPlan best{}, apart{};
+  double t_best = 0, t_apart = 8.0;
+  for (int r = first(m[0]); r <= last(m[0]); ++r)
+    for (int i = 0; i < 13; ++i) {
+      const int64_t n0 = ranges(0, r, i);
+      if (n0 == 0) continue;
+      const Kind x = kind(0, r, n0);
       for (int64_t n1 = 1; n1 <= 4; n1 *= 2) {
-        if (n1 > 1 && tiles[1] < 4 * n1) continue;
-        double sum = 0, top = 0, there = 0;
-        int64_t range[2], n[2], all = 0;
-        for (int k = 0; k < 2; ++k) {
-          const int64_t per = step / 64, w = (tiles[k] + (k ? n1 : n0) - 1) / (k ? n1 : n0);
-          range[k] = (w + per - 1) / per * step;
-          n[k] = std::max<int64_t>(1, (of[k].cap + range[k] - 1) / range[k]);
-          // of several groups, and of several sequences' own keys, two thirds of the blocks that the bounds allow for
-          const double t = (double)range[k] / 64 * tile[r] + 5.0, b = (double)(blocks[k] * n[k]) * (of[k].batch > 1 ? 2.0 / 3 : 1.0);
-          sum += t * b;
-          there += b;
-          top = std::max(top, t);
-          all += blocks[k] * n[k];
-        }
-        const double t = (there <= (double)cus ? top : sum / cus + 0.35 * top) + part * (double)(n[0] + n[1]);
-        if (best == 0 || t < best) {
-          best = t;
-          p = SharedPlan{all, rpb, {(int)range[0], (int)range[1]}, {(int)n[0], (int)n[1]}};
+        if (n1 > 1 && of[1].cap < 256 * n1) continue;
+        const Kind y = kind(1, r, n1);
+        const double t = time(x.sum + y.sum, x.there + y.there, std::max(x.top, y.top), r) + part * (double)(x.splits + y.splits);
+        if (t_best == 0 || t < t_best) {
+          t_best = t;
+          best = SharedPlan{true, {x.blocks, y.blocks}, {ROWS[r], ROWS[r]}, {(int)x.range, (int)y.range},
+                            {(int)x.splits, (int)y.splits}};
         }
       }
     }
+  for (int k = 0; k < 2; ++k) {
+    double t_kind = 0;
+    for (int r = first(m[k]); r <= last(m[k]); ++r)
+      for (int i = 0; i < 13; ++i) {
+        const int64_t n = ranges(k, r, i);
+        if (n == 0) continue;
+        const Kind x = kind(k, r, n);
+        const double t = time(x.sum, x.there, x.top, r) + part * (double)x.splits;
+        if (t_kind == 0 || t < t_kind) {
+          t_kind = t;
+          apart.blocks[k] = x.blocks;
+          apart.rpb[k] = ROWS[r];
+          apart.range[k] = (int)x.range;
+          apart.splits[k] = (int)x.splits;
+        }
+      }
+    t_apart += t_kind;
   }
-  return p;
+  return t_apart < t_best ? apart : best;
 }
 template <class Launch>
 hipError_t launch_shared(int dtype, const CacheAttnArgs &in, const SharedPlan &p, Launch &&launch, hipStream_t s) {
   if (in.c.rows <= 0 || in.c.max_q <= 0) return hipSuccess;
   CacheAttnArgs a = in;
-  a.blocks = (unsigned)p.blocks;
-  a.rpb = p.rpb;
   a.past_range = p.range[0];
   a.past_splits = p.splits[0];
   a.range = p.range[1];
   a.splits = p.splits[1];
-  const hipError_t e = launch(dtype, a, s);
+  hipError_t e = hipSuccess;
+  if (!p.together) {
+    a.only = 1;
+    a.blocks = (unsigned)p.blocks[0];
+    a.rpb = p.rpb[0];
+    e = launch(dtype, a, s);
+    if (e != hipSuccess) return e;
+    a.only = 2;
+  }
+  a.blocks = (unsigned)(p.blocks[1] + (p.together ? p.blocks[0] : 0));
+  a.rpb = p.rpb[1];
+  e = launch(dtype, a, s);
   return e != hipSuccess ? e : launch_combine(dtype, a, few_rows_of_many_parts(a), s);
 }
 // a launch over all keys of every sequence

@@ -305,6 +305,7 @@ struct CacheAttnArgs {
   unsigned blocks;
   int rpb, range, splits;
   int past_range, past_splits;
+  int only;                 // 1: the keys that groups share, 2: the others (0: both, or no groups)
 };
 // scratch bytes that let a launch over these bounds split its keys as it would like to
 size_t cache_attn_scratch(int dtype, const CacheArgs &c);

@@ -27,6 +27,8 @@ SHARED = [
     ("bf16", 16, 16, 128, 64, [40, 30], [9000, 8800], 1, [2], [8704]),
     ("bf16", 16, 1, 64, 16, [3000, 1500], [3500, 2300], 64, [2], [800]),
     ("f32", 4, 4, 128, 16, [1, 2, 1], [5000, 5003, 5100], 1, [3], [4992]),
+    ("bf16", 4, 1, 128, 16, [i % 3 for i in range(300)], [40 + i % 3 + i % 17 for i in range(300)], 1, [3] * 100, [32] * 100),
+    ("bf16", 4, 4, 64, 64, [1] * 200, [900 + i % 70 for i in range(200)], 0, [200], [896]),
     # prefixes inside a page, longer than the first sequence, than another one, and than a chunk leaves
     ("bf16", 4, 4, 64, 64, [1, 3, 2], [300, 290, 400], 1, [3], [250]),
     ("bf16", 4, 2, 128, 16, [1, 3, 2], [300, 100, 400], 1, [3], [100000]),
