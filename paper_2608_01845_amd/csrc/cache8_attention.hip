@@ -249,7 +249,7 @@ __device__ __forceinline__ bf16x8 bf16_values8(uint32_t u, uint32_t v, float up)
 __device__ __forceinline__ bool has_nan(uint32_t u) { return (((u & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }
 
 template <int HD, int RT>
-__global__ __launch_bounds__(256, 1) void k_cache8_attn_few(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few(CacheAttnArgs a) {
   using F = Codes<HD>;
   constexpr int NC = HD / 32, NI = HD / 16, KT = F::KT, NL = F::NL, WAVE = 64 * RT * HD;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -776,6 +776,10 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
     constexpr int NPV = KK / 2 * NI, NMF = NPV + KK * NC;   // fragment reads of P V, and of a step; two MFMAs each
     constexpr int EPM = 8 * KK / NMF;            // exponentials per pair of MFMAs
     static_assert(NMF == 16 || NMF == 32, "hd 64 or 128");
+    // Where V's codes are taken and put. Behind the last of them come the reads of four V fragments, two instructions
+    // each, which are all that the step's last wait leaves under way: what was put is there when the barrier opens.
+    constexpr int TAKE_V = NMF == 32 ? 16 : 7, PUT_V = NMF == 32 ? 22 : 9, LAST_PUT = NMF == 32 ? 26 : 11;
+    static_assert(LAST_PUT <= NMF - 5 && NPV >= 4, "tiles put before the last eight reads");
     bf16x8 fr_[NMF];
     // One step, P = t % 4 at compile time, as in the kernel over bf16; the conversions lie in the stream: K's codes are
     // taken at its start and put a fourth later, V's likewise in its second half. Past the last tile they run on stale slots, unused.
@@ -859,14 +863,14 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
           if (q == 0) take(raw_k(rs), bytes_of(P + 3), 0);
           if (q == NMF / 4 - 2) put(kt, 0, 0);
           if (q == NMF / 4 + 2) put(kt, 0, 1);
-          if (q == NMF / 2) take(raw_v(r2), bytes_of(P + 2), 1);
-          if (q == NMF * 3 / 4 - 2) put(vt, 1, 0);
-          if (q == NMF * 3 / 4 + 2) put(vt, 1, 1);
+          if (q == TAKE_V) take(raw_v(r2), bytes_of(P + 2), 1);
+          if (q == PUT_V) put(vt, 1, 0);
+          if (q == LAST_PUT) put(vt, 1, 1);
         } else {
           char *to = ring + (conv_k ? ((P + 3) % KS) * TB : V_BASE + ((P + 2) % VS) * TB);
           if (q == 0) take(conv_k ? raw_k(rs) : raw_v(r2), conv_k ? bytes_of(P + 3) : bytes_of(P + 2), conv_k ? 0 : 1);
           if (q == NMF / 2) put(to, conv_k ? 0 : 1, 0);
-          if (q == NMF / 2 + 4) put(to, conv_k ? 0 : 1, 1);
+          if (q == LAST_PUT) put(to, conv_k ? 0 : 1, 1);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
