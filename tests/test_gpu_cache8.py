@@ -213,7 +213,8 @@ def test_attention_matches_definition(case):
 
 
 FORMS = [("bf16", 4, 4, 64, 64, 3, 700), ("bf16", 4, 4, 128, 16, 20, 700), ("f32", 4, 2, 64, 32, 40, 700),
-         ("f32", 2, 2, 128, 64, 40, 700), ("bf16", 4, 4, 128, 64, 1024, 2100)]
+         ("f32", 2, 2, 128, 64, 40, 700), ("bf16", 4, 4, 128, 64, 1024, 2100), ("bf16", 4, 4, 128, 16, 1024, 2100),
+         ("bf16", 4, 4, 64, 32, 20, 700)]
 FORMS += [("bf16", heads, kvh, hd, page, q, q + 500) for heads, kvh, q in ((4, 4, 200), (16, 1, 4096)) for hd in (64, 128)
           for page in (16, 64)]
 forms = pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(str(x) for x in f))

@@ -209,17 +209,18 @@ def test_two_graphs_in_flight():
             assert torch.equal(a, b)
 
 
-def test_unseen_own_keys_have_no_influence():
-    s = cu.state("bf16", 4, 2, 64, 32, [40, 30], [200, 190], seed=57)
+@pytest.mark.parametrize("hd, page, q", [(64, 32, [40, 30]), (128, 32, [400, 300]), (128, 64, [400, 300])])
+def test_unseen_own_keys_have_no_influence(hd, page, q):
+    s = cu.state("bf16", 4, 2, hd, page, q, [160 + n for n in q], seed=57)
     for b in range(2):
         pg, sl = cu.where(s, b)
         j = s.kv[b] - s.q[b] // 2
         s.v[pg[j], 0, sl[j], 3] = math.nan
         s.k[pg[-1], 1, sl[-1], 5] = math.nan
-    past = c8.Past(s, [2], [96])
+    past = c8.Past(s, [2], [128])
     wdc, ctx = ctx_of(s)
     o, _, pv, qk = c8.attention64(s, 8, past)
-    bound, _ = attention_bound(s, pv.nan_to_num(1e30), o.nan_to_num(0), qk, 200)
+    bound, _ = attention_bound(s, pv.nan_to_num(1e30), o.nan_to_num(0), qk, max(s.kv))
     out = ctx.cache_attention_shared(wdc.PagedCache(s.k, s.v), cu.chunks(wdc, s), past.desc(wdc, s), s.x, torch.empty_like(s.x), frame=8)
     got, fine = out.reshape(o.shape).double(), torch.isfinite(o)
     assert not fine.all() and fine.any() and torch.equal(fine, torch.isfinite(got))
