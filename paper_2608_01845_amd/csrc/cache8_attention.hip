@@ -506,6 +506,9 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
 // second tile each; at hd 128 two such rings do not fit into LDS, and KH = 2 groups of four take half of every tile's keys
 // (32 rows of 32 heads on 8 over 40,000 keys: 50 us with four waves over all of them, 45 so).
 //
+// A wave whose 32 rows are all past the last one only loads and converts, which leaves LDS and the matrix cores to the
+// others: 60 rows of a kv head over 40,000 keys, 39.7 us with every wave at work and 35.6 so, at hd 64 43.1 and 37.8.
+//
 // References move when a lane's sum of weights over a tile passes 2^8 (2^16 over bf16), to the row's largest score: sums of weights
 // times v are finite while |v| is below 2^120 over the number of keys.
 constexpr int KV = 64, KS = 2, VS = 4, RS = 3, ES = 4;   // keys a tile; slots of K, V, codes and exponent bytes
@@ -613,7 +616,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   static_assert(KG == 1 || KH == 1, "keys are shared out in one way");
   constexpr int WG = W / KG, WR = WG / KH;       // waves over a ring; over the block's rows
   constexpr int KK = 4 / KH;                     // tiles of 16 keys of a wave
-  const int wr = wid % WR, kg = KG == 1 ? 0 : wid / WR, kh = KH == 1 ? 0 : wid / WR, cw = wid % WG;
+  // (rows of few waves lie on different SIMDs: waves w and w + 4 share one)
+  const int kg = KG == 1 ? 0 : wid / WR, kh = KH == 1 ? 0 : wid / WR, wr = (wid + (kg + kh) * (WR / 2)) % WR, cw = wid % WG;
   const bool grp_a = KG == 2 || wid < 4;         // loads tiles
   const int mlast = min(m0 + 32 * WR, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KG * KV - 1) / (KG * KV);   // in steps of KG tiles
@@ -621,6 +625,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   // steps of the range, relative to t_first: `nf` that every row sees whole, then masked ones
   const int tot = t_end - t_first, nf = min(max(lim_lo / (KG * KV) - t_first, 0), tot);
   const int ahead = min(tot, nf + RS);           // codes that the pipeline asks for
+  const bool none = m0 + 32 * wr >= count;       // the wave has no rows: it loads and converts, and works on nothing
 
   const float sc = LOG2E / sqrtf((float)HD);
   bf16x8 qf[2][NC];
@@ -905,6 +910,48 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
       }
       asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(8) : "memory");
     };
+    // A step of a wave without rows: its share of the loads and the conversion.
+    auto serve = [&](int t) __attribute__((always_inline)) {
+      const int r1 = rs == RS - 1 ? 0 : rs + 1, r2 = rs == 0 ? RS - 1 : rs - 1;
+      int issued = 0;
+      if (grp_a) {
+        if (t + 5 < ahead) {
+          load_k(t + 5, r2, page_of(t + 5));
+          issued += TL::NK;
+        } else {
+          wv = wk;
+        }
+        if (t + 4 < ahead) {
+          load_v(r1, wv);
+          issued += TL::NS;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (conv_k) {
+        take(raw_k(rs), bytes_of(t + 3), 0);
+        put(ring + ((t + 3) % KS) * TB, 0, 0);
+        put(ring + ((t + 3) % KS) * TB, 0, 1);
+      }
+      if (conv_v) {
+        take(raw_v(r2), bytes_of(t + 2), 1);
+        put(ring + V_BASE + ((t + 2) % VS) * TB, 1, 0);
+        put(ring + V_BASE + ((t + 2) % VS) * TB, 1, 1);
+      }
+      rs = r1;
+      if (grp_a) {
+        if (issued == TL::NK + TL::NS)
+          wait_vm<TL::NK + TL::NS>();
+        else if (issued == TL::NS)
+          wait_vm<TL::NS>();
+        else
+          wait_vm<0>();
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    if (none) {
+#pragma unroll 1
+      for (int t = 0; t < nf; ++t) serve(t);
+    } else
     for (int t = 0; t < nf; t += 4) {
       int next[4];
 #pragma unroll
@@ -949,6 +996,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
     const bool odd = odd_tile[kg][u & 3];
     if (lane == 0 && cw == 0) odd_tile[kg][(u + 2) & 3] = 0;
     if (u + 1 < tot) masked_convert(u + 1);
+    if (none) continue;
     const char *kb = ring + (u % KS) * TB, *vb = ring + (u % VS) * TB;   // vro holds V_BASE
     const int key0 = KV * (KG * (t_first + u) + kg) + 16 * KK * kh;
     f32x4 S[KK][2];

@@ -217,6 +217,8 @@ FORMS = [("bf16", 4, 4, 64, 64, 3, 700), ("bf16", 4, 4, 128, 16, 20, 700), ("f32
          ("bf16", 4, 4, 64, 32, 20, 700)]
 FORMS += [("bf16", heads, kvh, hd, page, q, q + 500) for heads, kvh, q in ((4, 4, 200), (16, 1, 4096)) for hd in (64, 128)
           for page in (16, 64)]
+# (blocks of 128 rows with 40)
+FORMS += [form for page in (16, 64) for form in (("bf16", 32, 8, 128, page, 10, 9100), ("bf16", 16, 4, 64, page, 10, 4100))]
 forms = pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(str(x) for x in f))
 
 
