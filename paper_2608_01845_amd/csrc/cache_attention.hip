@@ -432,13 +432,19 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
   static_assert(KG == 1 || KH == 1, "keys are shared out in one way");
   constexpr int WR = W / (KG * KH);              // waves over the block's rows
   constexpr int KK = 4 / KH;                     // tiles of 16 keys of a wave
-  const int wr = wid % WR, kg = KG == 1 ? 0 : wid / WR, kh = KH == 1 ? 0 : wid / WR;
+  // (rows of few waves lie on different SIMDs: waves w and w + 4 share one)
+  const int kg = KG == 1 ? 0 : wid / WR, kh = KH == 1 ? 0 : wid / WR, wr = (wid + (kg + kh) * (WR / 2)) % WR;
   const bool grp_a = KG == 2 || wid < 4;         // loads tiles
   const int mlast = min(m0 + 32 * WR, count) - 1;
   const int lim_lo = k_.lim_lo, tiles = (k_.lim_hi + KG * KV - 1) / (KG * KV);   // in steps of KG tiles
   const int range = k_.range / (KG * KV), t_first = nr > 1 ? sp * range : 0, t_end = nr > 1 ? min(t_first + range, tiles) : tiles;
   // steps of the range, relative to t_first: `nf` that every row sees whole, then masked ones
   const int tot = t_end - t_first, nf = min(max(lim_lo / (KG * KV) - t_first, 0), tot);
+  // The wave has no rows: it loads, and works on nothing (60 rows of a kv head over 40,000 keys, hd 64: 47.4 us with every wave
+  // at work and 42.2 so; 32 of 32 heads on 8 off 24,448 shared keys: 49 and 45.7). In the other forms the
+  // second loop costs registers: 4,080 rows over 67,320 keys 1,760 us without it, 1,860 with. Short ranges lose by the code
+  // that they fetch (six causal chunks, hd 64, pages of 16: 28.3 us, 29.3 where the rule was for all lengths).
+  const bool none = KG * KH == 2 && nf >= 8 && m0 + 32 * wr >= count;
 
   const float sc = LOG2E / sqrtf((float)HD);
   bf16x8 qf[2][NC];
@@ -646,6 +652,31 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
       }
       asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(8) : "memory");
     };
+    if (none) {
+#pragma unroll 1
+      for (int t = 0; t < nf; ++t) {
+        int issued = 0;
+        if (grp_a) {
+          if (t + 4 < tot) {
+            load_k(t + 4, page_of(t + 4));
+            issued += TL::NS;
+          } else {
+            wv = wk;
+          }
+          if (t + 3 < tot) {
+            load_v(t + 3, wv);
+            issued += TL::NS;
+          }
+          if (issued == 2 * TL::NS)
+            wait_vm<2 * TL::NS>();
+          else if (issued == TL::NS)
+            wait_vm<TL::NS>();
+          else
+            wait_vm<0>();
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      }
+    } else
     for (int t = 0; t < nf; t += NB) {
       int next[NB];
 #pragma unroll
@@ -687,6 +718,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache_attn_many(CacheAttnArgs
       for (int q = 0; q < 4; ++q) odd |= (y[q] & 0x7f80u) == 0x7f80u || (y[q] & 0x7f800000u) == 0x7f800000u;
     }
     odd = __syncthreads_or(odd);
+    if (none) continue;
     const int key0 = KV * (KG * (t_first + u) + kg) + 16 * KK * kh;
     f32x4 S[KK][2];
     bf16x8 pf[2][KK / 2];

@@ -39,6 +39,8 @@ SHARED = [
     ("bf16", 4, 2, 64, 16, [1 + i % 3 for i in range(150)], [96 + 3 + 7 * i % 50 for i in range(150)], 1, [70, 1, 79], [96, 16, 80]),
     ("bf16", 4, 2, 128, 16, [1] * 150, [130 + 5 * i for i in range(150)], 1, [1] * 75 + [75], [16 * (i % 7) for i in range(75)] + [112]),
 ]
+# blocks of 128 rows with 40, many tiles each
+SHARED += [("bf16", 32, 8, hd, page, [4, 6], [n + 30, n + 100], 1, [2], [n]) for hd, n in ((128, 20032), (64, 40000)) for page in (16, 64)]
 ids = lambda c: f"{c[0]}-{c[1]}x{c[2]}x{c[3]}-p{c[4]}-{few(c[5])}-{few(c[6])}-f{c[7]}-{few(c[8])}-{few(c[9])}"  # noqa: E731
 
 
