@@ -501,7 +501,7 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
 // while u is worked on.
 //
 // Bound like the kernel over bf16 by the matrix cores, the exponentials and their power: 4,080 rows over 67,320 keys, 16 heads of
-// 128, 1,906 to 1,940 us by device, 1,140 to 1,160 TFLOP/s, where that one takes 1,780 to 1,850; the conversion adds 8% to
+// 128, 1,906 to 2,005 us by device, 1,100 to 1,160 TFLOP/s, where that one takes 1,760 to 1,850; the conversion adds 8% to
 // a step's vector instructions and half of its LDS traffic again. Blocks of 128 rows: at hd 64 KG = 2 groups of four waves take every
 // second tile each; at hd 128 two such rings do not fit into LDS, and KH = 2 groups of four take half of every tile's keys
 // (32 rows of 32 heads on 8 over 40,000 keys: 50 us with four waves over all of them, 45 so).

@@ -482,7 +482,8 @@ inline bool few_rows_of_many_parts(const CacheAttnArgs &a) {
 // Both kinds of blocks go out in one launch, so that the compute units that one leaves idle do the other, or
 // in two, each with blocks of its own height: many sequences with few own keys want low ones (1,024 tokens of 32 heads on 8
 // of 128 off 8,128 shared keys, 65 own ones each: 542 us in one launch, 230 in two; 64 of 16 heads of 64 off 16,000, up to 442 own
-// ones: 65 and 45; 32 of 32 heads on 8 off 24,448, up to 900 own ones: 48 and 53).
+// ones: 65 and 45; 32 of 32 heads on 8 off 24,448, up to 900 own ones: 48 and 53,
+// both before waves without rows were spared the work).
 //
 // By estimate: all blocks' times over the places for them (two a compute unit for blocks of 16 rows), of several
 // groups or sequences two thirds of the blocks that the bounds allow for, and a third of the longest one's; 5 us for a start and
