@@ -693,7 +693,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   auto raw_k = [&](int slot) { return ring + RK_BASE + slot * RB; };
   auto raw_v = [&](int slot) { return ring + RV_BASE + slot * RB; };
   auto bytes_of = [&](int t) { return ring + E_BASE + (t % ES) * EB; };
-  // both tiles t at once; whether V holds NaN
+  // both tiles t at once; whether V holds NaN, or a power that makes codes infinite (256 * 2^120 on; one of zeros makes none)
   auto convert = [&](int t, bool k, bool v) __attribute__((always_inline)) {
     bool odd = false;
     if (k && conv_k) {
@@ -708,7 +708,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
 #pragma unroll
       for (int i = 0; i < NCV; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) odd |= has_nan(raw[i][q]);
+        for (int q = 0; q < 4; ++q) odd |= has_nan(raw[i][q]) || (up[i] >= 0x1p120f && (raw[i][q] & 0x7f7f7f7fu) != 0);
     }
     return odd;
   };
@@ -969,7 +969,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   }
 
   // Masked tiles, one at a time: the codes of tiles nf to nf + 2 have been asked for. A key that a row does not see has weight
-  // 0, but 0 times NaN is NaN in a matrix product: a tile whose V holds NaN is multiplied key by key.
+  // 0, but 0 times an infinity or NaN is NaN in a matrix product: a tile whose V may hold one is multiplied key by key.
   int lim[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
