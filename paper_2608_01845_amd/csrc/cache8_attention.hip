@@ -21,13 +21,6 @@ __device__ __forceinline__ void values8(uint32_t u, uint32_t v, float up, float 
   }
 }
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-typedef __attribute__((ext_vector_type(2))) int i32x2_t;
-typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
-// Eight rows of 16 bytes, each read as 2 x 8 bytes by the lanes of a group of 16 in row order, come back
-// transposed: lane c of the group gets byte c of each.
-__device__ __forceinline__ u32x2_t lds_read_tr8(const char *p) {
-  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)p));
-}
 // Buffer of `bytes` bytes from base + off (both the same in every lane): what lies outside reads as zero
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_at(const void *base, int64_t off, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc((char *)base + off, 0, bytes, RSRC_WORD3);
@@ -221,8 +214,9 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
 // S^T = K Q^T (A: 16 keys, B: 16 rows): lane (lr, lg) loads hd / 4 consecutive codes of key lr, and Q in the same order of
 // dimensions, so K needs no LDS; its powers ride on the conversion to bf16. The lane is left the
 // scores of row lr and keys 4 lg + e of both halves of the tile, the B operand of O^T = V^T P^T. V goes through LDS, from which rows
-// come back transposed, 8 keys of one dimension a lane, so V's powers cannot ride on the conversion: they multiply the weights, which
-// are rounded to bf16 before that (a power of two changes no digit). The softmax is the one of the cache in bf16.
+// come back transposed, 8 keys of one dimension a lane. It goes there in bf16, converted while a lane's codes are of one key, its
+// power with them: powers multiplied into the weights would take weights of 2^-9 and below out of bf16's normal numbers at the smallest
+// power. The softmax is the one of the cache in bf16.
 //
 // Eight tokens over 1 to 32,768 keys, 32 heads on 8 of 128 (235 MB): 48.6 us and 4.7 of the parts' launch, 4.8 TB/s, where
 // the cache in bf16 takes 80 for twice the bytes (5.4 TB/s; a large copy, which writes too, 4.9). 232 registers allow two blocks
@@ -232,8 +226,6 @@ struct Codes {
   static constexpr int KT = 32;                  // keys per tile
   static constexpr int NL = HD / 64;             // 16-byte loads of a lane per 16 keys
   static constexpr int CH = HD / 16;             // 16-byte chunks of a row
-  // chunk c of row r lies at c ^ key(r): the 32 rows of a transposed read, one chunk each, spread over the banks
-  static __device__ __forceinline__ int key(int r) { return HD == 128 ? (r >> 1) & 7 : (r >> 2) & 3; }
 };
 
 // Eight codes as bf16, times a power of two. (The conversion's result is taken as a word: its second half taken as an element
@@ -245,13 +237,24 @@ __device__ __forceinline__ bf16x8 bf16_values8(uint32_t u, uint32_t v, float up)
                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, up, true))};
   return __builtin_bit_cast(bf16x8, w);
 }
-// whether one of four codes is NaN
-__device__ __forceinline__ bool has_nan(uint32_t u) { return (((u & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }
+// Whether one of sixteen codes may be no finite number: one is NaN, or not all are zeros and the power makes the largest codes
+// infinite (256 * 2^120 on)
+__device__ __forceinline__ bool not_finite(u32x4_t u, float up) {
+  uint32_t nan = 0, some = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    nan |= (u[q] & 0x7f7f7f7fu) + 0x01010101u;
+    some |= u[q];
+  }
+  return (nan & 0x80808080u) != 0 || (up >= 0x1p120f && (some & 0x7f7f7f7fu) != 0);
+}
 
 template <int HD, int RT>
 __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few(CacheAttnArgs a) {
   using F = Codes<HD>;
+  using L = Few<HD>;                             // layout of V in LDS
   constexpr int NC = HD / 32, NI = HD / 16, KT = F::KT, NL = F::NL, WAVE = 64 * RT * HD;
+  static_assert(WAVE >= KT * L::ROWB, "a tile of V in bf16");
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ float ml[4][2][16 * RT];
   const CacheArgs &c = a.c;
@@ -279,16 +282,19 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
   }
 
   char *mine = smem + w * WAVE;
-  int vwo[NL], vro[NI];                          // LDS offsets of the lane's V codes in 16 rows; of its transposed reads
+  // LDS offsets in 16 rows of V in bf16: of the first half of the lane's 16 codes (the second: ^ 16), and of the transposed
+  // read of rows 4 lg .. + 3, dims 16 i ..
+  const int vrow = lane / F::CH;                 // row of the lane's codes, of load j: + 64 / CH j
+  int vwo[NL], vro[L::VR];
 #pragma unroll
   for (int j = 0; j < NL; ++j) {
-    const int r = lane / F::CH + j * (64 / F::CH);
-    vwo[j] = r * HD + ((lane % F::CH) ^ F::key(r)) * 16;   // (key(r + 16) is key(r))
+    const int r = vrow + j * (64 / F::CH);
+    vwo[j] = r * L::ROWB + ((2 * (lane % F::CH)) ^ L::vkey(r)) * 16;
   }
   {
-    const int i8 = lr >> 1, r = (i8 < 4 ? 0 : 12) + 4 * lg + i8;   // keys 4 lg .. of the first and the second 16 rows
+    const int r = 4 * lg + (lr >> 2), j = lane & 3;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) vro[i] = r * HD + (i ^ F::key(r)) * 16 + 8 * (lr & 1);
+    for (int i = 0; i < L::VR; ++i) vro[i] = r * L::ROWB + ((2 * i + (j >> 1)) ^ L::vkey(r)) * 16 + 8 * (j & 1);
   }
   PageWalk<false> pw;
   pw.init(c, k_.tab, k_.tab_last, h, (KT * t0) >> c.plog);
@@ -296,7 +302,6 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
   struct Tile {
     u32x4_t k[2][NL], v[2][NL];
     uint32_t ks[2];                              // powers' bytes of (k, v) of key lr
-    u32x2_t es[2];                               // of keys 4 lg ..
   } tile[2];
   // Tile t: halves of 16 rows, each on one page. Rows past the cache's end lie outside the buffer range and arrive as
   // zeros, whatever they hold; so do tiles past the range.
@@ -309,10 +314,8 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
       const int64_t slot = live ? pw.get(c, h, key >> c.plog) + (key & pmask) : 0;
       const int rows = live ? min(max(s.n - key, 0), 16) : 0;
       const auto kd = rsrc_at(c.k, slot * HD, rows * HD), vd = rsrc_at(c.v, slot * HD, rows * HD);
-      // (a load that starts inside a range and ends outside is none: whole groups of 4 slots, which lie on one page)
-      const auto ed = rsrc_at(c.scale, slot * 2, (rows + 3) / 4 * 8);
+      const auto ed = rsrc_at(c.scale, slot * 2, rows * 2);
       x.ks[hf] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(ed, 2 * lr, 0, 0);
-      x.es[hf] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(ed, 8 * lg, 0, 0));
 #pragma unroll
       for (int j = 0; j < NL; ++j)
         x.k[hf][j] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kd, lr * HD + HD / 4 * lg + 16 * j, 0, 0));
@@ -334,6 +337,7 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
   }
   auto step = [&](const Tile &x, int t) __attribute__((always_inline)) {
     f32x4 S[RT][2];
+    float vup[2][NL];                            // powers of the lane's rows of V
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const float up = power(x.ks[k]);
@@ -346,7 +350,14 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
           S[r][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : S[r][k], 0, 0, 0);
       }
 #pragma unroll
-      for (int j = 0; j < NL; ++j) *(u32x4_t *)(mine + k * 16 * HD + vwo[j]) = x.v[k][j];
+      for (int j = 0; j < NL; ++j) {
+        // (255, which no append writes, would make codes of 0 NaN)
+        vup[k][j] = power(min((uint32_t)__shfl((int)x.ks[k], vrow + j * (64 / F::CH), 64) >> 8, 254u));
+        char *to = mine + k * 16 * L::ROWB;
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          *(bf16x8 *)(to + (vwo[j] ^ 16 * q)) = bf16_values8(x.v[k][j][2 * q], x.v[k][j][2 * q + 1], vup[k][j]);
+      }
     }
     const bool part = KT * t + KT > lim_lo;      // some row does not see the whole tile
     bf16x8 pf[RT];
@@ -378,23 +389,20 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(S[r][k][e] - ref), y = (float)(__bf16)p;
+          const float p = __builtin_amdgcn_exp2f(S[r][k][e] - ref);
           l[r] += p;
-          d[r] += y;
-          // (of a slot past the end, whose byte may be any, 0 stays 0: 0 times a power of infinity would not)
-          pf[r][4 * k + e] = (__bf16)__builtin_ldexpf(y, (int)(x.es[k][e >> 1] >> (16 * (e & 1) + 8) & 255u) - 127);
+          pf[r][4 * k + e] = (__bf16)p;
+          d[r] += (float)pf[r][4 * k + e];
         }
     }
-    // A key that a row does not see has weight 0, but 0 times NaN is NaN in a matrix product. Tiles seen in
-    // part are looked over, and one whose V holds NaN is multiplied key by key.
+    // A key that a row does not see has weight 0, but 0 times an infinity or NaN of its V is NaN in a matrix product.
+    // Tiles seen in part are looked over, and one that may hold such a value is multiplied key by key.
     bool odd = false;
     if (part) {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int j = 0; j < NL; ++j)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) odd |= has_nan(x.v[k][j][q]);
+        for (int j = 0; j < NL; ++j) odd |= not_finite(x.v[k][j], vup[k][j]);
       odd = __any(odd);
     }
     asm volatile("" ::: "memory");
@@ -411,19 +419,18 @@ __global__ __launch_bounds__(256, HD * RT == 256 ? 1 : 2) void k_cache8_attn_few
           p = __shfl(p, 16 * g + lr, 64);
           if (KT * t + key < lim[r])
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-              float v[8];
-              values8(*(const uint32_t *)(mine + key * HD + (i ^ F::key(key)) * 16 + 4 * lg), 0u, 1.f, v);
+            for (int i = 0; i < NI; ++i)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[r][i][e] += p * v[e];
-            }
+              for (int e = 0; e < 4; ++e) {
+                const int col = 16 * i + 4 * lg + e;
+                o[r][i][e] += p * bf2f(*(const bf16_t *)(mine + key * L::ROWB + ((col >> 3) ^ L::vkey(key)) * 16 + (col & 7) * 2));
+              }
         }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const u32x2_t u = lds_read_tr8(mine + vro[i]);
-        const bf16x8 vf = bf16_values8(u[0], u[1], 1.f);
+        const bf16x8 vf = v_frag<HD>(mine + vro[i % L::VR] + i / L::VR * L::VR * 32);
 #pragma unroll
         for (int r = 0; r < RT; ++r) o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][i], 0, 0, 0);
       }
@@ -693,7 +700,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
   auto raw_k = [&](int slot) { return ring + RK_BASE + slot * RB; };
   auto raw_v = [&](int slot) { return ring + RV_BASE + slot * RB; };
   auto bytes_of = [&](int t) { return ring + E_BASE + (t % ES) * EB; };
-  // both tiles t at once; whether V holds NaN, or a power that makes codes infinite (256 * 2^120 on; one of zeros makes none)
+  // both tiles t at once; whether V may hold an infinity or NaN
   auto convert = [&](int t, bool k, bool v) __attribute__((always_inline)) {
     bool odd = false;
     if (k && conv_k) {
@@ -706,9 +713,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void k_cache8_attn_many(CacheAttnArg
       put(ring + V_BASE + (t % VS) * TB, 1, 0);
       put(ring + V_BASE + (t % VS) * TB, 1, 1);
 #pragma unroll
-      for (int i = 0; i < NCV; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) odd |= has_nan(raw[i][q]) || (up[i] >= 0x1p120f && (raw[i][q] & 0x7f7f7f7fu) != 0);
+      for (int i = 0; i < NCV; ++i) odd |= not_finite(raw[i], up[i]);
     }
     return odd;
   };
