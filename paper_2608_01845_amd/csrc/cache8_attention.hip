@@ -1226,18 +1226,13 @@ hipError_t launch_cache8_attention(int dtype, const CacheAttnArgs &in, hipStream
 }
 
 // us per 64 keys in blocks of 16, 32, 128 and 256 rows (alone on a compute unit)
-static SharedPlan shared_plan8(int dtype, const CacheArgs &c, const CacheShared &sh) {
+SharedPlan cache8_shared_plan(int dtype, const CacheArgs &c, const CacheShared &sh) {
   static const double tile[4][4] = {{0, 1.0, 0, 0}, {0, 2.0, 0, 0}, {0.55, 0.71, 0.67, 1.09}, {0.72, 0.95, 1.15, 1.69}};
   return plan_shared(dtype, c, sh, tile[2 * dtype + (c.hd == 128)]);
 }
 
-size_t cache8_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh) {
-  const SharedPlan p = shared_plan8(dtype, c, sh);
-  return attn_part_bytes(c, p.splits[0] + p.splits[1]);
-}
-
-hipError_t launch_cache8_attention_shared(int dtype, const CacheAttnArgs &in, hipStream_t s) {
-  return launch_shared(dtype, in, shared_plan8(dtype, in.c, in.sh), launch_pass8, s);
+hipError_t launch_cache8_attention_shared(int dtype, const CacheAttnArgs &in, const SharedPlan &p, hipStream_t s) {
+  return launch_shared(dtype, in, p, launch_pass8, s);
 }
 
 }  // namespace wdc

@@ -1361,18 +1361,13 @@ hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &in, hipStream_
 }
 
 // us per 64 keys in blocks of 16, 32, 128 and 256 rows (alone on a compute unit)
-static SharedPlan shared_plan(int dtype, const CacheArgs &c, const CacheShared &sh) {
+SharedPlan cache_shared_plan(int dtype, const CacheArgs &c, const CacheShared &sh) {
   static const double tile[4][4] = {{0, 1.0, 0, 0}, {0, 2.0, 0, 0}, {0.55, 0.71, 0.58, 1.03}, {0.72, 0.95, 0.95, 1.4}};
   return plan_shared(dtype, c, sh, tile[2 * dtype + (c.hd == 128)]);
 }
 
-size_t cache_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh) {
-  const SharedPlan p = shared_plan(dtype, c, sh);
-  return attn_part_bytes(c, p.splits[0] + p.splits[1]);
-}
-
-hipError_t launch_cache_attention_shared(int dtype, const CacheAttnArgs &in, hipStream_t s) {
-  return launch_shared(dtype, in, shared_plan(dtype, in.c, in.sh), launch_pass, s);
+hipError_t launch_cache_attention_shared(int dtype, const CacheAttnArgs &in, const SharedPlan &p, hipStream_t s) {
+  return launch_shared(dtype, in, p, launch_pass, s);
 }
 
 static int64_t mass_blocks(int dtype, const CacheArgs &c) {

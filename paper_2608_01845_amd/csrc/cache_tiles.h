@@ -490,11 +490,6 @@ inline bool few_rows_of_many_parts(const CacheAttnArgs &a) {
 // end and tile[] us per 64 keys in blocks of 16, 32, 128 and 256 rows; the parts written and read; 8 us for a further launch.
 // Over fourteen calls of 3 to 32 rollouts over 3,456 to 40,000 keys one launch so planned costs 5% beside the best of all
 // ranges tried, 13% at most.
-struct SharedPlan {
-  bool together;
-  int64_t blocks[2];
-  int rpb[2], range[2], splits[2];
-};
 inline SharedPlan plan_shared(int dtype, const CacheArgs &c, const CacheShared &sh, const double (&tile)[4]) {
   CacheArgs of[2] = {c, c};
   of[0].batch = sh.groups;
@@ -549,7 +544,7 @@ inline SharedPlan plan_shared(int dtype, const CacheArgs &c, const CacheShared &
         if (t_best == 0 || t < t_best) {
           t_best = t;
           best = SharedPlan{true, {x.blocks, y.blocks}, {ROWS[r], ROWS[r]}, {(int)x.range, (int)y.range},
-                            {(int)x.splits, (int)y.splits}};
+                            {(int)x.splits, (int)y.splits}, 0};
         }
       }
     }
@@ -571,7 +566,9 @@ inline SharedPlan plan_shared(int dtype, const CacheArgs &c, const CacheShared &
       }
     t_apart += t_kind;
   }
-  return t_apart < t_best ? apart : best;
+  SharedPlan &p = t_apart < t_best ? apart : best;
+  p.scratch = attn_part_bytes(c, p.splits[0] + p.splits[1]);
+  return p;
 }
 template <class Launch>
 hipError_t launch_shared(int dtype, const CacheAttnArgs &in, const SharedPlan &p, Launch &&launch, hipStream_t s) {

@@ -310,14 +310,22 @@ struct CacheAttnArgs {
 // scratch bytes that let a launch over these bounds split its keys as it would like to
 size_t cache_attn_scratch(int dtype, const CacheArgs &c);
 hipError_t launch_cache_attention(int dtype, const CacheAttnArgs &a, hipStream_t s);
-// the same for sequences that share a past (a.sh), all of the scratch needed
-size_t cache_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh);
-hipError_t launch_cache_attention_shared(int dtype, const CacheAttnArgs &a, hipStream_t s);
+// Blocks over the keys that groups share [0] and over their sequences' own keys [1], in one launch or in two. Made for the
+// current device, once a call: the scratch is checked and the launches go out by the same plan.
+struct SharedPlan {
+  bool together;
+  int64_t blocks[2];
+  int rpb[2], range[2], splits[2];
+  size_t scratch;           // bytes, all of them needed
+};
+// the same for sequences that share a past (a.sh)
+SharedPlan cache_shared_plan(int dtype, const CacheArgs &c, const CacheShared &sh);
+hipError_t launch_cache_attention_shared(int dtype, const CacheAttnArgs &a, const SharedPlan &p, hipStream_t s);
 // and both over codes
 size_t cache8_attn_scratch(int dtype, const CacheArgs &c);
 hipError_t launch_cache8_attention(int dtype, const CacheAttnArgs &a, hipStream_t s);
-size_t cache8_shared_scratch(int dtype, const CacheArgs &c, const CacheShared &sh);
-hipError_t launch_cache8_attention_shared(int dtype, const CacheAttnArgs &a, hipStream_t s);
+SharedPlan cache8_shared_plan(int dtype, const CacheArgs &c, const CacheShared &sh);
+hipError_t launch_cache8_attention_shared(int dtype, const CacheAttnArgs &a, const SharedPlan &p, hipStream_t s);
 
 struct CacheMassArgs {
   CacheArgs c;

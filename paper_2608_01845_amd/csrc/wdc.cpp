@@ -1936,7 +1936,8 @@ size_t wdc_cache_attention_shared_scratch(const wdc_ctx *ctx, const wdc_paged_ca
   CacheShared sh;
   wdc_ctx *c = const_cast<wdc_ctx *>(ctx);
   if (!ctx || cache_args(c, cache, chunks, true, false, &a) != WDC_OK || shared_args(c, prefix, a, &sh) != WDC_OK) return 0;
-  return cache_shared_scratch(ctx->d.dtype, a, sh);
+  const OnStreamDevice on(ctx->stream);
+  return cache_shared_plan(ctx->d.dtype, a, sh).scratch;
 }
 
 wdc_status wdc_cache_attention_shared(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc_chunks *chunks,
@@ -1946,9 +1947,10 @@ wdc_status wdc_cache_attention_shared(wdc_ctx *ctx, const wdc_paged_cache *cache
   CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
   CHK(shared_args(ctx, prefix, a.c, &a.sh));
   CHK(attention_rows(ctx, a, d_q, ldq, frame, d_o, ldo, d_lse, d_scratch, scratch_bytes));
-  CHK(enough_scratch(ctx, d_scratch ? scratch_bytes : 0, cache_shared_scratch(ctx->d.dtype, a.c, a.sh)));
   const OnStreamDevice on(ctx->stream);
-  HIPCHK(ctx, launch_cache_attention_shared(ctx->d.dtype, a, ctx->stream));
+  const SharedPlan plan = cache_shared_plan(ctx->d.dtype, a.c, a.sh);
+  CHK(enough_scratch(ctx, a.part_bytes, plan.scratch));
+  HIPCHK(ctx, launch_cache_attention_shared(ctx->d.dtype, a, plan, ctx->stream));
   return WDC_OK;
 }
 
@@ -1958,7 +1960,8 @@ size_t wdc_cache8_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache8 *
   CacheShared sh;
   wdc_ctx *c = const_cast<wdc_ctx *>(ctx);
   if (!ctx || cache8_args(c, cache, chunks, &a) != WDC_OK || (prefix && shared_args(c, prefix, a, &sh) != WDC_OK)) return 0;
-  return prefix ? cache8_shared_scratch(ctx->d.dtype, a, sh) : cache8_attn_scratch(ctx->d.dtype, a);
+  const OnStreamDevice on(ctx->stream);
+  return prefix ? cache8_shared_plan(ctx->d.dtype, a, sh).scratch : cache8_attn_scratch(ctx->d.dtype, a);
 }
 
 wdc_status wdc_cache8_attention(wdc_ctx *ctx, const wdc_paged_cache8 *cache, const wdc_chunks *chunks,
@@ -1968,10 +1971,14 @@ wdc_status wdc_cache8_attention(wdc_ctx *ctx, const wdc_paged_cache8 *cache, con
   CHK(cache8_args(ctx, cache, chunks, &a.c));
   if (prefix) CHK(shared_args(ctx, prefix, a.c, &a.sh));
   CHK(attention_rows(ctx, a, d_q, ldq, frame, d_o, ldo, d_lse, d_scratch, scratch_bytes));
-  if (prefix) CHK(enough_scratch(ctx, d_scratch ? scratch_bytes : 0, cache8_shared_scratch(ctx->d.dtype, a.c, a.sh)));
   const OnStreamDevice on(ctx->stream);
-  HIPCHK(ctx, prefix ? launch_cache8_attention_shared(ctx->d.dtype, a, ctx->stream)
-                     : launch_cache8_attention(ctx->d.dtype, a, ctx->stream));
+  if (!prefix) {
+    HIPCHK(ctx, launch_cache8_attention(ctx->d.dtype, a, ctx->stream));
+    return WDC_OK;
+  }
+  const SharedPlan plan = cache8_shared_plan(ctx->d.dtype, a.c, a.sh);
+  CHK(enough_scratch(ctx, a.part_bytes, plan.scratch));
+  HIPCHK(ctx, launch_cache8_attention_shared(ctx->d.dtype, a, plan, ctx->stream));
   return WDC_OK;
 }
 

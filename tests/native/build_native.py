@@ -5,7 +5,7 @@ kernels) with AddressSanitizer and UndefinedBehaviorSanitizer on the host side
 only (each -fsanitize= after -Xarch_host: the GPU code is built as usual), and
 linked as tests/native/_out/libwdc_hostsan.so. The C99 driver abi_driver.c is
 compiled with the same sanitizers (its runtime serves the library too) into
-tests/native/_out/abi_driver. Outputs are rebuilt on every call.
+tests/native/_out/abi_driver, and so is two_devices.c. Outputs are rebuilt on every call.
 
 Usage: python tests/native/build_native.py  (also run by __graft_entry__.build()).
 """
@@ -23,6 +23,7 @@ OUT = os.path.join(HERE, "_out")
 LIB = os.path.join(OUT, "libwdc_hostsan.so")
 DRIVER = os.path.join(OUT, "abi_driver")
 ONCE = os.path.join(OUT, "once_test")
+DEVICES = os.path.join(OUT, "two_devices")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 CLANG = os.path.join(ROCM, "llvm", "bin", "clang")
 
@@ -58,6 +59,14 @@ def build(verbose: bool = False) -> str:
           f"-L{OUT}", "-lwdc_hostsan", f"-L{ROCM}/lib", "-lamdhip64", "-lm",
           "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{ROCM}/lib"])
     os.replace(DRIVER + ".tmp", DRIVER)
+    # the same library over HIP calls that the program itself defines (two devices, no GPU)
+    _run([clang, "-std=c99", "-g", "-O1", "-Wall", "-Wextra", "-Werror", "-D__HIP_PLATFORM_AMD__",
+          f"-I{ROCM}/include", f"-I{os.path.join(ROOT, 'include')}",
+          "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-fno-omit-frame-pointer",
+          os.path.join(HERE, "two_devices.c"), "-o", DEVICES + ".tmp", "-Wl,--export-dynamic",
+          f"-L{OUT}", "-lwdc_hostsan", f"-L{ROCM}/lib", "-lamdhip64", "-lm",
+          "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{ROCM}/lib"])
+    os.replace(DEVICES + ".tmp", DEVICES)
     # host code alone: one-time work under several threads
     _run([clang, "-x", "c++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-Werror", "-pthread",
           os.path.join(HERE, "once_test.cpp"), "-o", ONCE + ".tmp", "-lstdc++"])
