@@ -415,7 +415,8 @@ wdc_status wdc_cache_evict(wdc_ctx *ctx, const wdc_paged_cache *cache, const wdc
  * those of the group's first sequence: every row of the group sees all of them, whatever its own table's
  * entries there. From there on a sequence has its own slots, seen as in wdc_cache_attention. The host
  * gives bounds: the longest prefix and the most own keys of a sequence; device values beyond them are cut to them.
- * groups * kv_heads <= 65535 and groups * kv_heads * (prefix keys) <= 2^28, else WDC_E_SHAPE. */
+ * Of the limit on keys above remain, with the keys that these bounds allow for: kv_heads * (keys of one sequence), groups * kv_heads *
+ * (prefix keys) and batch * kv_heads * (own keys) <= 2^28; groups * kv_heads <= 65535; else WDC_E_SHAPE. */
 typedef struct {
   const int32_t *d_group_start, *d_prefix_len;
   int32_t groups, max_prefix, max_own;

@@ -1667,8 +1667,10 @@ wdc_status wdc_linear(wdc_ctx *ctx, const void *d_a, int64_t lda, const void *d_
 namespace {
 constexpr int64_t kCacheRows = int64_t(1) << 26, kCacheKeys = int64_t(1) << 28;   // (launches stay below 2^32 threads)
 
-// Descriptor checks shared by the cache operators; fills *a. `rows`: the call takes chunk rows.
-wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q, bool rows, bool values, CacheArgs *a) {
+// Descriptor checks shared by the cache operators; fills *a. `rows`: the call takes chunk rows. With a prefix
+// (checked by shared_args) the keys that a group shares count once, there, and here the own ones.
+wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q, bool rows, bool values, CacheArgs *a,
+                      const wdc_prefix *prefix = nullptr) {
   if (!c) return WDC_E_ARG;
   if (!p || !q || !p->d_k || (values && !p->d_v) || !q->d_kv_len || !q->d_table || (rows && !q->d_q_start) ||
       p->pages < 1 || q->batch < 1 || q->table_ld < 1 || q->max_kv < 0 || (rows && (q->rows < 0 || q->max_q < 0))) {
@@ -1703,7 +1705,9 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
   while ((1 << plog) < p->page) ++plog;
   const int64_t cap = std::min<int64_t>(q->max_kv, (int64_t)q->table_ld << plog);
   const int64_t nrows = rows ? q->rows : 0, max_q = rows ? std::min(q->max_q, q->rows) : 0, heads = (int64_t)q->batch * p->kv_heads;
-  if (heads > 65535 || nrows * c->H > kCacheRows || max_q * q->batch * c->H > kCacheRows || heads * cap > kCacheKeys ||
+  const int64_t own = prefix ? std::min<int64_t>(cap, std::max(prefix->max_own, 0)) : cap;
+  if (heads > 65535 || nrows * c->H > kCacheRows || max_q * q->batch * c->H > kCacheRows || heads * own > kCacheKeys ||
+      p->kv_heads * cap > kCacheKeys ||
       ((int64_t)p->pages * p->kv_heads << plog) > 0x7fffffff) {
     set_err(c, "cache call too large: %d sequences, %d kv heads, %lld rows, %lld keys", q->batch, p->kv_heads,
             (long long)nrows, (long long)cap);
@@ -1731,10 +1735,10 @@ wdc_status cache_args(wdc_ctx *c, const wdc_paged_cache *p, const wdc_chunks *q,
 }
 
 // the same of a cache of codes
-wdc_status cache8_args(wdc_ctx *c, const wdc_paged_cache8 *p, const wdc_chunks *q, CacheArgs *a) {
+wdc_status cache8_args(wdc_ctx *c, const wdc_paged_cache8 *p, const wdc_chunks *q, CacheArgs *a, const wdc_prefix *prefix = nullptr) {
   if (!c) return WDC_E_ARG;
   const wdc_paged_cache codes = p ? wdc_paged_cache{p->d_k, p->d_v, p->pages, p->page, p->kv_heads, 0} : wdc_paged_cache{};
-  CHK(cache_args(c, p ? &codes : nullptr, q, true, true, a));
+  CHK(cache_args(c, p ? &codes : nullptr, q, true, true, a, prefix));
   if (!p->d_scale) {
     set_err(c, "cache without scales");
     return WDC_E_ARG;
@@ -1935,7 +1939,7 @@ size_t wdc_cache_attention_shared_scratch(const wdc_ctx *ctx, const wdc_paged_ca
   CacheArgs a;
   CacheShared sh;
   wdc_ctx *c = const_cast<wdc_ctx *>(ctx);
-  if (!ctx || cache_args(c, cache, chunks, true, false, &a) != WDC_OK || shared_args(c, prefix, a, &sh) != WDC_OK) return 0;
+  if (!ctx || cache_args(c, cache, chunks, true, false, &a, prefix) != WDC_OK || shared_args(c, prefix, a, &sh) != WDC_OK) return 0;
   const OnStreamDevice on(ctx->stream);
   return cache_shared_plan(ctx->d.dtype, a, sh).scratch;
 }
@@ -1944,7 +1948,7 @@ wdc_status wdc_cache_attention_shared(wdc_ctx *ctx, const wdc_paged_cache *cache
                                       const wdc_prefix *prefix, const void *d_q, int64_t ldq, int32_t frame, void *d_o,
                                       int64_t ldo, float *d_lse, void *d_scratch, size_t scratch_bytes) {
   CacheAttnArgs a{};
-  CHK(cache_args(ctx, cache, chunks, true, true, &a.c));
+  CHK(cache_args(ctx, cache, chunks, true, true, &a.c, prefix));
   CHK(shared_args(ctx, prefix, a.c, &a.sh));
   CHK(attention_rows(ctx, a, d_q, ldq, frame, d_o, ldo, d_lse, d_scratch, scratch_bytes));
   const OnStreamDevice on(ctx->stream);
@@ -1959,7 +1963,7 @@ size_t wdc_cache8_attention_scratch(const wdc_ctx *ctx, const wdc_paged_cache8 *
   CacheArgs a;
   CacheShared sh;
   wdc_ctx *c = const_cast<wdc_ctx *>(ctx);
-  if (!ctx || cache8_args(c, cache, chunks, &a) != WDC_OK || (prefix && shared_args(c, prefix, a, &sh) != WDC_OK)) return 0;
+  if (!ctx || cache8_args(c, cache, chunks, &a, prefix) != WDC_OK || (prefix && shared_args(c, prefix, a, &sh) != WDC_OK)) return 0;
   const OnStreamDevice on(ctx->stream);
   return prefix ? cache8_shared_plan(ctx->d.dtype, a, sh).scratch : cache8_attn_scratch(ctx->d.dtype, a);
 }
@@ -1968,7 +1972,7 @@ wdc_status wdc_cache8_attention(wdc_ctx *ctx, const wdc_paged_cache8 *cache, con
                                 const wdc_prefix *prefix, const void *d_q, int64_t ldq, int32_t frame, void *d_o,
                                 int64_t ldo, float *d_lse, void *d_scratch, size_t scratch_bytes) {
   CacheAttnArgs a{};
-  CHK(cache8_args(ctx, cache, chunks, &a.c));
+  CHK(cache8_args(ctx, cache, chunks, &a.c, prefix));
   if (prefix) CHK(shared_args(ctx, prefix, a.c, &a.sh));
   CHK(attention_rows(ctx, a, d_q, ldq, frame, d_o, ldo, d_lse, d_scratch, scratch_bytes));
   const OnStreamDevice on(ctx->stream);
