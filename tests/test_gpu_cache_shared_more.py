@@ -1,10 +1,10 @@
-"""Attention over a shared past: bounds beyond what unshared calls allow."""
+"""Attention over a shared past: bounds beyond what unshared calls allow, the unshared result."""
 import pytest
 import torch
 
 from tests import cache8_util as c8
 from tests import cache_util as cu
-from tests.test_gpu_cache import EPS32, attention_bound, ctx_of, within
+from tests.test_gpu_cache import EPS, EPS32, attention_bound, ctx_of, few, within
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,41 @@ def test_bounds_that_only_sharing_allows(dtype, hd):
     for out, z in both(ctx, wdc, s, ch, past.desc(wdc, s, max_prefix=69888, max_own=40), 1):
         within(out, o, bound, "o")
         within(z, lse, lse_bound + 4 * EPS32 * lse.abs(), "lse")
+
+
+SAME = [
+    # dtype, heads, kvh, hd, page, q, kv, frame, groups, prefix
+    ("f32", 4, 2, 64, 32, [1, 33, 2], [321, 400, 330], 1, [3], [320]),
+    ("f32", 3, 1, 128, 16, [1, 1, 1, 1], [3000 + 40 * i for i in range(4)], 1, [2, 2], [2992, 1600]),
+    ("bf16", 8, 2, 128, 64, [1] * 8, [1000 + 20 * i for i in range(8)], 1, [8], [960]),      # few rows apart, many together
+    ("bf16", 32, 8, 64, 16, [1] * 24, [5000 + 20 * i for i in range(24)], 1, [24], [4992]),
+    ("bf16", 4, 4, 128, 16, [333, 200], [1500, 1300], 64, [2], [960]),                        # many apart too
+    ("bf16", 16, 1, 64, 128, [600, 700], [1500, 1400], 100, [2], [640]),
+]
+ids = lambda c: f"{c[0]}-{c[1]}x{c[2]}x{c[3]}-p{c[4]}-{few(c[5])}"  # noqa: E731
+
+
+@pytest.mark.parametrize("scale", [1.0, 3.0])
+@pytest.mark.parametrize("case", SAME, ids=ids)
+def test_tables_that_name_the_same_pages(case, scale):
+    """Shared and unshared calls compared with each other. float32: two orders of the same sums, each off by float32's arithmetic.
+    bf16: both round weights to bf16; divided by the sum of the weights that is off by 2^-8 sum p|v|, by the sum of the rounded ones
+    by 2^-8 sum p|v - o| <= 2^-8 (sum p|v| + |o|); each result is rounded once. scale: of q and k; at 3 a few keys have most of the weight."""
+    dtype, heads, kvh, hd, page, q, kv, frame, groups, prefix = case
+    s = c8.state8(dtype, heads, kvh, hd, page, q, kv, seed=71, spread=0.3, scale=scale)
+    wdc, ctx = ctx_of(s)
+    past, ch = c8.Past(s, groups, prefix), cu.chunks(wdc, s)
+    for b, lead in enumerate(past.lead):
+        s.table[b, :past.keys[b] // page] = s.table[lead, :past.keys[b] // page]
+    o, lse, pv, qk = c8.attention64(s, frame, past)
+    arithmetic, lse_bound = attention_bound(s, pv, o, qk, max(kv))
+    arithmetic = arithmetic - (EPS[dtype] * o.abs() + (EPS["bf16"] * pv if dtype == "bf16" else 0))
+    bound = 2 * arithmetic + 2 * EPS[dtype] * o.abs() + (EPS["bf16"] * (2 * pv + o.abs()) if dtype == "bf16" else 0)
+    for codes, (out, z) in enumerate(both(ctx, wdc, s, ch, past.desc(wdc, s), frame)):
+        ref, y = torch.empty_like(s.x), torch.empty_like(z)
+        if codes:
+            ctx.cache8_attention(c8.cache8(wdc, s), ch, s.x, ref, frame=frame, lse=y)
+        else:
+            ctx.cache_attention(wdc.PagedCache(s.k, s.v), ch, s.x, ref, frame=frame, lse=y)
+        within(out, ref.reshape(out.shape).double(), bound, "o")
+        within(z, y.double(), 2 * (lse_bound + 4 * EPS32 * lse.abs()), "lse")
