@@ -1,4 +1,5 @@
-"""Attention over a shared past: bounds beyond what unshared calls allow, the unshared result."""
+"""Attention over a shared past: bounds beyond what unshared calls allow, the unshared result, sequences in no group,
+prefixes that change between replays."""
 import pytest
 import torch
 
@@ -72,3 +73,56 @@ def test_tables_that_name_the_same_pages(case, scale):
             ctx.cache_attention(wdc.PagedCache(s.k, s.v), ch, s.x, ref, frame=frame, lse=y)
         within(out, ref.reshape(out.shape).double(), bound, "o")
         within(z, y.double(), 2 * (lse_bound + 4 * EPS32 * lse.abs()), "lse")
+
+
+@pytest.mark.parametrize("dtype,hd,q", [("bf16", 64, 1), ("bf16", 128, 50), ("f32", 64, 9)])
+@pytest.mark.parametrize("tight", [False, True])
+def test_sequences_in_no_group(dtype, hd, q, tight):
+    """Before the first group and behind the last one: each on its own keys, to the bound of these keys."""
+    s = c8.state8(dtype, 4, 2, hd, 16, [q] * 5, [400, 410, 420, 430, 440], seed=72)
+    wdc, ctx = ctx_of(s)
+    some = c8.Past(s, [2, 1, 2], [0, 320, 0])
+    pre = wdc.Prefix(some.group_start[1:3].contiguous(), some.prefix_len[1:2].contiguous(),
+                     **(dict(max_prefix=320, max_own=440) if tight else {}))
+    for frame in (0, 1):
+        o, lse, pv, qk = c8.attention64(s, frame, some)
+        bound, lse_bound = attention_bound(s, pv, o, qk, 440)
+        for out, z in both(ctx, wdc, s, cu.chunks(wdc, s), pre, frame):
+            within(out, o, bound, "o")
+            within(z, lse, lse_bound + 4 * EPS32 * lse.abs(), "lse")
+
+
+@pytest.mark.parametrize("dtype,hd,q,kv,prefix", [("bf16", 128, [1, 1, 1], [900, 800, 1000], 640), ("bf16", 64, [200, 150], [900, 800], 576),
+                                                  ("f32", 64, [9, 4], [300, 250], 128)])
+@pytest.mark.parametrize("codes", [False, True])
+def test_replays_follow_the_prefix(dtype, hd, q, kv, prefix, codes):
+    """One captured call, replayed with other prefix lengths, against the definition with each of them."""
+    s = c8.state8(dtype, 4, 2, hd, 16, q, kv, seed=73)
+    past = c8.Past(s, [len(q)], [prefix])
+    import paper_2608_01845_amd as wdc
+    side = torch.cuda.Stream()
+    ctx = wdc.Context(cu.config(dtype, 4, hd), allocate_weights=False, stream=side)
+    pre, ch = past.desc(wdc, s, max_own=max(kv)), cu.chunks(wdc, s)
+    cache = c8.cache8(wdc, s) if codes else wdc.PagedCache(s.k, s.v)
+    out, z = torch.empty_like(s.x), torch.empty((s.rows, 4), device="cuda")
+    lens, want = (prefix, 0, prefix - 64), []
+    for n in lens:
+        o, lse, pv, qk = c8.attention64(s, 1, c8.Past(s, [len(q)], [n]))
+        want.append((o, lse, *attention_bound(s, pv, o, qk, max(kv))))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        if codes:
+            ctx.cache8_attention(cache, ch, s.x, out, frame=1, lse=z, prefix=pre)
+        else:
+            ctx.cache_attention_shared(cache, ch, pre, s.x, out, frame=1, lse=z)
+    for i in (0, 2, 1, 0):
+        past.prefix_len.fill_(lens[i])
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            g.replay()
+        side.synchronize()
+        o, lse, bound, lse_bound = want[i]
+        within(out.reshape(o.shape), o, bound, "o")
+        within(z, lse, lse_bound + 4 * EPS32 * lse.abs(), "lse")
