@@ -218,9 +218,9 @@ __global__ __launch_bounds__(256, 1) void k_cache8_attn_f32(CacheAttnArgs a) {
 // power with them: powers multiplied into the weights would take weights of 2^-9 and below out of bf16's normal numbers at the smallest
 // power. The softmax is the one of the cache in bf16.
 //
-// Eight tokens over 1 to 32,768 keys, 32 heads on 8 of 128 (235 MB): 48.6 us and 4.7 of the parts' launch, 4.8 TB/s, where
-// the cache in bf16 takes 80 for twice the bytes (5.4 TB/s; a large copy, which writes too, 4.9). 232 registers allow two blocks
-// per compute unit; forced to three, 13 of them spill (76.9 us with two blocks per unit's ranges, 57.5 unforced).
+// Eight tokens over 1 to 32,768 keys, 32 heads on 8 of 128 (235 MB): 47.4 us and 4.8 of the parts' launch, 5.0 TB/s, where
+// the cache in bf16 takes 80 for twice the bytes (5.4 TB/s; a large copy, which writes too, 4.9). 182 registers allow two blocks
+// per compute unit (at hd 64 112 do four; with 32 rows 172 do two, and 364 at hd 128 one).
 template <int HD>
 struct Codes {
   static constexpr int KT = 32;                  // keys per tile
@@ -537,7 +537,8 @@ __device__ __forceinline__ void lds_load4(u32x4_t buf, uint32_t lds, int voff) {
 
 // The lane's number, at hd 128 found anew, by instructions that are not moved out of a loop: a register kept for it, or for
 // what follows from it, would be spilled, and its reload in every step would wait for all loads under way (4,080 rows over
-// 67,320 keys: 2.03 ms, 1.92 with what the pipeline needs kept in registers and the rest found anew).
+// 67,320 keys: 2.03 ms, 1.92 with what the pipeline needs kept in registers and the rest found anew). Blocks of 256 rows over pages
+// of 16 or 32 slots still have one such reload a step, of four registers.
 template <int HD>
 __device__ __forceinline__ int lane_anew() {
   if (HD == 64) return threadIdx.x & 63;
